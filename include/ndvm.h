@@ -27,6 +27,8 @@
  *     capture).
  *   - Non-finite lane results are data, not errors.
  *   - dtype NDVM_F64 means every buffer holds double; NDVM_F32 means float.
+ *   - The network operators at the end take no tape; their element types and layouts
+ *     are stated there.
  */
 #ifndef NDVM_H
 #define NDVM_H
@@ -50,7 +52,8 @@ typedef enum {
 } ndvm_status;
 
 typedef enum { NDVM_FE_SCHEME = 0, NDVM_FE_BYTECODE = 1 } ndvm_frontend;
-typedef enum { NDVM_F64 = 0, NDVM_F32 = 1 } ndvm_dtype;
+/* NDVM_F16 and NDVM_BF16 are element types of the network operators alone; the replays take F64 and F32. */
+typedef enum { NDVM_F64 = 0, NDVM_F32 = 1, NDVM_F16 = 2, NDVM_BF16 = 3 } ndvm_dtype;
 
 typedef struct ndvm_tape ndvm_tape; /* opaque; immutable once built */
 
@@ -255,6 +258,97 @@ enum {
  * roofline.  Synchronous; NDVM_E_INVALID_ARG for an unknown fn or iters < 1.
  */
 ndvm_status ndvm_measure_op_cost(int fn, int iters, double* ns_per_call, void* stream);
+
+/*
+ * Network operators: the parts of a residual block whose output is the lanes' parameters (the
+ * paper's section 2 makes the evaluator an operator that gradients pass through, so what proposes
+ * theta can be trained through a replay; the paper names no operator of that network).
+ *   - A matrix argument is `rows` rows of contiguous elements, `*_stride` elements from one row to
+ *     the next (at least a row's length, or 0 for an input whose rows are all the same memory).
+ *     Pointers are aligned to their element type; other alignments only cost speed.
+ *   - Everything is computed in binary32 and rounded to the output's type once, except where said.
+ *   - Sums are added up in an order that depends on the sizes alone: the same call gives the same
+ *     bits again.
+ *   - Errors: NDVM_E_INVALID_ARG for null pointers, sizes, strides, alignment or a workspace that
+ *     is too small; NDVM_E_UNSUPPORTED for a type the operator does not take.  Outputs may not
+ *     overlap inputs, except ndvm_dropout's y, which may be x or residual.
+ */
+
+/*
+ * ndvm_layer_norm_forward -- y = (x - mean) * rstd * weight + bias over each row of `cols` elements,
+ * mean and variance (of the differences, not of the squares) over the row, rstd = 1 / sqrt(variance + eps).
+ *   dtype  : x and y (F32, F16, BF16);  wtype : weight and bias, dtype or F32
+ *   rows   : 0 is allowed and does nothing;  cols : at least 1
+ *   weight, bias : device, cols values, or NULL for 1 and 0
+ *   eps    : not negative, finite
+ *   stats  : device, 2 x rows floats for the backward pass (all means, then all rstd), or NULL
+ */
+ndvm_status ndvm_layer_norm_forward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* x,
+                                    int64_t x_stride, const void* weight, const void* bias, double eps, void* y,
+                                    int64_t y_stride, float* stats, void* stream);
+
+/* ndvm_layer_norm_workspace_bytes -- device workspace that ndvm_layer_norm_backward needs for dweight or dbias. */
+size_t ndvm_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * ndvm_layer_norm_backward -- gradients of ndvm_layer_norm_forward under the cotangent dy.
+ *   x, weight, stats : as the forward pass had and wrote them
+ *   dx, dweight, dbias : outputs (dweight and dbias of wtype, cols values), each NULL if not wanted;
+ *                        rows = 0 sets dweight and dbias to 0
+ *   workspace : device, 16-byte aligned; may be NULL when dweight and dbias are
+ */
+ndvm_status ndvm_layer_norm_backward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* dy,
+                                     int64_t dy_stride, const void* x, int64_t x_stride, const void* weight,
+                                     const float* stats, void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                                     void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * ndvm_dropout -- y = residual + (kept ? x / (1 - p) : 0); element i (row-major index, whatever the
+ * strides) is kept if word offset + i of the generator's sequence is at least round(p 2^32), so nothing
+ * is stored for the backward pass: that is the same call on the cotangent with the same p, seed and
+ * offset and no residual.  The sequence: Philox4x32, 10 rounds (Salmon, Moraes, Dror, Shaw, 2011), word
+ * w being word w % 4 of the block of counter (w / 4 as 64 bits, 0, 0) under the key `seed`.
+ *   dtype    : x, residual and y (F32, F16, BF16)
+ *   residual : device, or NULL for none (a dropped x contributes an exact 0, also where it is not finite)
+ *   p        : 0 <= p <= 1 - 2^-32
+ *   offset   : a multiple of 4; calls of one seed draw apart where their [offset, offset + rows * cols) are
+ */
+ndvm_status ndvm_dropout(ndvm_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,
+                         const void* residual, int64_t r_stride, double p, uint64_t seed, uint64_t offset, void* y,
+                         int64_t y_stride, void* stream);
+
+typedef enum { NDVM_ACT_SILU = 0, NDVM_ACT_GELU = 1, NDVM_ACT_RELU = 2, NDVM_ACT_SIGMOID = 3 } ndvm_activation;
+
+/*
+ * ndvm_gated_forward -- h = act(x Wg^T) * (x Wu^T), both products, the activation and the product in
+ * one kernel: x is rows x k, w_gate and w_up are n x k, h is rows x n.
+ *   dtype : every matrix (F16, BF16; sums in binary32)
+ *   act   : silu g / (1 + e^-g), gelu g (1 + erf(g / sqrt 2)) / 2, relu, or sigmoid
+ *   rows  : 0 is allowed and does nothing;  k, n : at least 1; rows, k and n below 2^31
+ *   workspace : device, 256-byte aligned, ndvm_gated_workspace_bytes(..., 0, ...) bytes (NULL if that is 0)
+ */
+ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,
+                               int64_t x_stride, const void* w_gate, int64_t g_stride, const void* w_up,
+                               int64_t u_stride, void* h, int64_t h_stride, void* workspace, size_t ws_bytes,
+                               void* stream);
+
+/*
+ * ndvm_gated_workspace_bytes -- device workspace of a forward (backward = 0) or backward (1) call whose
+ * row strides, base addresses and sizes are multiples of 16 bytes (aligned = 1) or not (0: room for
+ * aligned copies).  0 on invalid sizes.
+ */
+size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backward, int aligned);
+
+/*
+ * ndvm_gated_backward -- gradients of ndvm_gated_forward under the cotangent dh (rows x n).  The two
+ * products are computed again; dG and dU are rounded to dtype before the products that make dx (rows x k)
+ * and dw_gate, dw_up (n x k, contiguous).  Each output may be NULL if not wanted; rows = 0 sets dw_gate
+ * and dw_up to 0.
+ */
+ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                const void* dh, int64_t dh_stride, const void* x, int64_t x_stride, const void* w_gate,
+                                int64_t g_stride, const void* w_up, int64_t u_stride, void* dx, int64_t dx_stride,
+                                void* dw_gate, void* dw_up, void* workspace, size_t ws_bytes, void* stream);
 
 /* ndvm_launch_count -- replay kernels launched by this process so far. */
 unsigned long long ndvm_launch_count(void);

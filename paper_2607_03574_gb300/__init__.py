@@ -7,6 +7,7 @@ memory and streams.  The names follow the C ABI in ``include/ndvm.h``:
     tape = trace_build(program_text, frontend=FE_SCHEME)
     loss, grad = value_and_grad(tape, params, obs)     # params (B, P) CUDA tensor
     loss = loss_op(tape)(params, obs)                  # differentiable in params
+    y = layer_norm(x, w, b), gated(...), dropout(...)  # a parameter-proposing network's parts (network.py)
 
 There is no CPU fallback: if the library is missing or the device is not a CUDA
 GPU, the calls raise.
@@ -69,6 +70,17 @@ def load(build_if_missing: bool = True):
             "ndvm_value_and_grad_host_async": (ctypes.c_int, [P, ctypes.c_int, I64, P, P, I64, P, P, P]),
             "ndvm_tape_shared_work": (ctypes.c_int, [P, ctypes.POINTER(ctypes.c_double)]),
             "ndvm_check_device": (ctypes.c_int, [P]),
+            "ndvm_layer_norm_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, P, ctypes.c_double, P,
+                                                       I64, P, P]),
+            "ndvm_layer_norm_workspace_bytes": (SZ, [I64, I64]),
+            "ndvm_layer_norm_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, I64, P, P, P, I64, P,
+                                                        P, P, SZ, P]),
+            "ndvm_dropout": (ctypes.c_int, [ctypes.c_int, I64, I64, P, I64, P, I64, ctypes.c_double, U64, U64, P, I64, P]),
+            "ndvm_gated_workspace_bytes": (SZ, [I64, I64, I64, ctypes.c_int, ctypes.c_int]),
+            "ndvm_gated_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, I64, P, I64, P, I64, P, I64, P, I64, P,
+                                                  SZ, P]),
+            "ndvm_gated_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, I64, P, I64, P, I64, P, I64, P, I64,
+                                                   P, I64, P, P, P, SZ, P]),
             "ndvm_launch_count": (ctypes.c_ulonglong, []),
             "ndvm_measure_fp64_peak": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double), P]),
             "ndvm_measure_op_cost": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_double), P]),
@@ -416,3 +428,7 @@ def loss_op(tape: Tape):
 
 def check_device(tape: Tape):
     _check(load().ndvm_check_device(tape.handle))
+
+
+from .network import (ACTIVATIONS, dropout, dropout_backward, dropout_forward, gated, gated_backward,  # noqa: E402,F401
+                      gated_forward, layer_norm, layer_norm_backward, layer_norm_forward)

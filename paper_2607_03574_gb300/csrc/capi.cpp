@@ -58,6 +58,8 @@ struct DevCache {
 
 }  // namespace
 
+ndvm_status ndvm::set_error(ndvm_status s, const char* message) { return fail(s, message); }
+
 struct ndvm_tape {
   Tape tape;
   Plan grad_plan, value_plan;
