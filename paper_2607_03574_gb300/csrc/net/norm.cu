@@ -1,140 +1,426 @@
 // Layer norm over a row of C elements, and its backward pass:
 //   m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), xh = (x - m) r, y = xh w + b
 //   g = dy w, dx = r (g - mean(g) - xh mean(g xh)), dw = sum over rows of dy xh, db = sum over rows of dy
+//
+// Both passes are bound by memory: forward reads x and writes y, backward reads x and dy and writes dx.
+// So a row is read once and held in registers (in its own type) by the threads that share it, a warp or a
+// block; the backward pass keeps each thread's column sums in registers over all rows that its block
+// takes, and a second kernel adds up the blocks' sums (in a fixed order: the same bits every time).
 #include "net.h"
 #include "types.cuh"
 
 namespace ndvm {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kColumnBlocks = 64;  // row ranges whose column sums are added up apart
-
-__device__ __forceinline__ float2 block_sum2(float a, float b) {
-  __shared__ float2 part[kThreads / 32];
-  for (int o = 16; o; o >>= 1) {
-    a += __shfl_xor_sync(~0u, a, o);
-    b += __shfl_xor_sync(~0u, b, o);
-  }
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = make_float2(a, b);
-  __syncthreads();
-  float2 s = part[0];
-  for (int w = 1; w < kThreads / 32; w++) s.x += part[w].x, s.y += part[w].y;
-  return s;
-}
-
-// a block a row
-template <typename T, typename W>
-__global__ void k_forward(NormArgs a) {
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-    float s = 0.0f;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kThreads) s += to_f32(x[c]);
-    const float mean = block_sum2(s, 0.0f).x / (float)a.cols;
-    s = 0.0f;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kThreads) {
-      const float d = to_f32(x[c]) - mean;
-      s += d * d;
+// weights are of the activations' type or binary32
+template <typename T, int V>
+__device__ __forceinline__ void load_weight(float (&w)[V], const void* p, int f32, int64_t c, float none) {
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < V; e++) w[e] = none;
+  } else if (f32) {
+    constexpr int Q = V >= 4 ? 4 : 1;
+#pragma unroll
+    for (int q = 0; q < V; q += Q) {
+      const Pack<float, Q> v = load_pack<float, Q>(static_cast<const float*>(p) + c + q);
+#pragma unroll
+      for (int e = 0; e < Q; e++) w[q + e] = v.v[e];
     }
-    const float rstd = 1.0f / sqrtf(block_sum2(s, 0.0f).x / (float)a.cols + a.eps);
-    T* y = static_cast<T*>(a.y) + row * a.y_stride;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kThreads) {
-      float v = (to_f32(x[c]) - mean) * rstd;
-      if (a.weight) v *= to_f32(static_cast<const W*>(a.weight)[c]);
-      if (a.bias) v += to_f32(static_cast<const W*>(a.bias)[c]);
-      y[c] = from_f32<T>(v);
-    }
-    if (threadIdx.x == 0 && a.stats) {
-      a.stats[row] = mean;
-      a.stats[a.rows + row] = rstd;
-    }
+  } else {
+    const Pack<T, V> v = load_pack<T, V>(static_cast<const T*>(p) + c);
+#pragma unroll
+    for (int e = 0; e < V; e++) w[e] = to_f32(v.v[e]);
   }
 }
 
-template <typename T, typename W>
-__global__ void k_backward_x(NormArgs a) {
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
-    const float mean = a.stats[row], rstd = a.stats[a.rows + row];
-    float sg = 0.0f, sgx = 0.0f;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kThreads) {
-      const float g = to_f32(dy[c]) * (a.weight ? to_f32(static_cast<const W*>(a.weight)[c]) : 1.0f);
-      sg += g;
-      sgx += g * ((to_f32(x[c]) - mean) * rstd);
-    }
-    const float2 s = block_sum2(sg, sgx);
-    const float mg = s.x / (float)a.cols, mgx = s.y / (float)a.cols;
-    T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kThreads) {
-      const float g = to_f32(dy[c]) * (a.weight ? to_f32(static_cast<const W*>(a.weight)[c]) : 1.0f);
-      dx[c] = from_f32<T>(rstd * (g - mg - (to_f32(x[c]) - mean) * rstd * mgx));
-    }
+// Sums over the kRow threads that share a row: a warp's shuffles, then the warps' sums in shared memory
+// (`part` is the caller's, another one for each sum of a row, so one barrier a sum is enough).
+template <int kRow>
+__device__ __forceinline__ float row_sum(float v, float* part) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+  if constexpr (kRow > 32) {
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < kRow / 32; w++) v += part[w];
+  }
+  return v;
+}
+
+template <int kRow> constexpr int kBlock = kRow > 32 ? kRow : 128;  // threads a block
+
+// A row in the registers of kRow threads, N packs of V elements each: pack j of thread t holds the
+// columns (j kRow + t) V ...
+template <typename T, int V, int N, int kRow>
+__global__ void __launch_bounds__(kBlock<kRow>) k_forward(NormArgs a, int w_f32) {
+  __shared__ float part[2][32];
+  const int t = threadIdx.x % kRow;
+  const int64_t row = (int64_t)blockIdx.x * (kBlock<kRow> / kRow) + threadIdx.x / kRow;
+  if (row >= a.rows) return;  // (whole warps; with a block a row, no block)
+  const int cols = (int)a.cols;
+  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  Pack<T, V> px[N];
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < N; j++) {
+    const int c = (j * kRow + t) * V;
+    if (c < cols) px[j] = load_pack<T, V>(x + c);
+  }
+#pragma unroll
+  for (int j = 0; j < N; j++)
+    if ((j * kRow + t) * V < cols)
+#pragma unroll
+      for (int e = 0; e < V; e++) sum += to_f32(px[j].v[e]);
+  const float mean = row_sum<kRow>(sum, part[0]) / (float)cols;
+  sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < N; j++)
+    if ((j * kRow + t) * V < cols)
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        const float d = to_f32(px[j].v[e]) - mean;
+        sum += d * d;
+      }
+  const float rstd = 1.0f / sqrtf(row_sum<kRow>(sum, part[1]) / (float)cols + a.eps);
+  T* y = static_cast<T*>(a.y) + row * a.y_stride;
+#pragma unroll
+  for (int j = 0; j < N; j++) {
+    const int c = (j * kRow + t) * V;
+    if (c >= cols) continue;
+    float w[V], b[V];
+    load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
+    load_weight<T, V>(b, a.bias, w_f32, c, 0.0f);
+#pragma unroll
+    for (int e = 0; e < V; e++) px[j].v[e] = from_f32<T>((to_f32(px[j].v[e]) - mean) * rstd * w[e] + b[e]);
+    store_pack(y + c, px[j]);
+  }
+  if (t == 0 && a.stats) {
+    a.stats[row] = mean;
+    a.stats[a.rows + row] = rstd;
   }
 }
 
-// column sums over a range of rows: partial[0][range][c] = sum dy xh, partial[1][range][c] = sum dy
+// Rows longer than the registers of a block hold: three passes over the row, the later ones from L2.
+constexpr int kLong = 512;
 template <typename T>
-__global__ void k_columns(NormArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+__global__ void __launch_bounds__(kLong) k_forward_long(NormArgs a, int w_f32) {
+  __shared__ float part[2][32];
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  float s = 0.0f;
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLong) s += to_f32(x[c]);
+  const float mean = row_sum<kLong>(s, part[0]) / (float)a.cols;
+  s = 0.0f;
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLong) {
+    const float d = to_f32(x[c]) - mean;
+    s += d * d;
+  }
+  const float rstd = 1.0f / sqrtf(row_sum<kLong>(s, part[1]) / (float)a.cols + a.eps);
+  T* y = static_cast<T*>(a.y) + row * a.y_stride;
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLong) {
+    float w[1], b[1];
+    load_weight<T, 1>(w, a.weight, w_f32, c, 1.0f);
+    load_weight<T, 1>(b, a.bias, w_f32, c, 0.0f);
+    y[c] = from_f32<T>((to_f32(x[c]) - mean) * rstd * w[0] + b[0]);
+  }
+  if (threadIdx.x == 0 && a.stats) {
+    a.stats[row] = mean;
+    a.stats[a.rows + row] = rstd;
+  }
+}
+
+// Backward: a block takes every gridDim.x-th group of rows; the next row's loads are in flight while the
+// present one is worked on.  partial[block][0][c] = the block's sum of dy xh, [1][c] = of dy.
+template <typename T, int V, int N, int kRow>
+__global__ void __launch_bounds__(kBlock<kRow>) k_backward(NormArgs a, int w_f32) {
+  constexpr int kRows = kBlock<kRow> / kRow;
+  __shared__ float part[4][32];
+  const int t = threadIdx.x % kRow, cols = (int)a.cols;
+  const bool sums = a.partial != nullptr;
+  const float inv = 1.0f / (float)cols;
+  float dw[N][V], db[N][V];
+#pragma unroll
+  for (int j = 0; j < N; j++)
+#pragma unroll
+    for (int e = 0; e < V; e++) dw[j][e] = db[j][e] = 0.0f;
+  Pack<T, V> nx[N], nd[N];
+  float nmean = 0.0f, nrstd = 0.0f;
+  const auto fetch = [&](int64_t row) {
+    if (row >= a.rows) return;
+    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+    const T* d = static_cast<const T*>(a.dy) + row * a.dy_stride;
+    nmean = a.stats[row];
+    nrstd = a.stats[a.rows + row];
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const int c = (j * kRow + t) * V;
+      if (c < cols) {
+        nx[j] = load_pack<T, V>(x + c);
+        nd[j] = load_pack<T, V>(d + c);
+      }
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kRow;
+  fetch(row);
+  for (int turn = 0; row < a.rows; row += step, turn ^= 2) {
+    Pack<T, V> px[N], pd[N];
+    const float mean = nmean, rstd = nrstd;
+#pragma unroll
+    for (int j = 0; j < N; j++) px[j] = nx[j], pd[j] = nd[j];
+    fetch(row + step);
+    float sg = 0.0f, sgx = 0.0f;
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const int c = (j * kRow + t) * V;
+      if (c >= cols) continue;
+      float w[V];
+      load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        const float d = to_f32(pd[j].v[e]), xh = (to_f32(px[j].v[e]) - mean) * rstd, g = d * w[e];
+        sg += g;
+        sgx += g * xh;
+        dw[j][e] += d * xh;
+        db[j][e] += d;
+      }
+    }
+    if (!a.dx) continue;
+    const float mg = row_sum<kRow>(sg, part[turn]) * inv, mgx = row_sum<kRow>(sgx, part[turn + 1]) * inv;
+    T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const int c = (j * kRow + t) * V;
+      if (c >= cols) continue;
+      float w[V];
+      load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        const float xh = (to_f32(px[j].v[e]) - mean) * rstd;
+        px[j].v[e] = from_f32<T>(rstd * (to_f32(pd[j].v[e]) * w[e] - mg - xh * mgx));
+      }
+      store_pack(dx + c, px[j]);
+    }
+  }
+  if (!sums) return;
+  float* out = a.partial + (int64_t)blockIdx.x * 2 * cols;
+  if constexpr (kRows == 1) {
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const int c = (j * kRow + t) * V;
+      if (c >= cols) continue;
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        out[c + e] = dw[j][e];
+        out[cols + c + e] = db[j][e];
+      }
+    }
+  } else {
+    __shared__ float all[kRows][2][N * V * kRow];
+#pragma unroll
+    for (int j = 0; j < N; j++)
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        const int c = (j * kRow + t) * V + e;
+        all[threadIdx.x / kRow][0][c] = dw[j][e];
+        all[threadIdx.x / kRow][1][c] = db[j][e];
+      }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * cols; i += kBlock<kRow>) {
+      const int k = i >= cols, c = i - k * cols;
+      float s = all[0][k][c];
+#pragma unroll
+      for (int q = 1; q < kRows; q++) s += all[q][k][c];
+      out[i] = s;
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLong) k_backward_long(NormArgs a, int w_f32) {
+  __shared__ float part[2][32];
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+  const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
+  const float mean = a.stats[row], rstd = a.stats[a.rows + row];
+  float sg = 0.0f, sgx = 0.0f, w[1];
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLong) {
+    load_weight<T, 1>(w, a.weight, w_f32, c, 1.0f);
+    const float g = to_f32(dy[c]) * w[0];
+    sg += g;
+    sgx += g * ((to_f32(x[c]) - mean) * rstd);
+  }
+  const float mg = row_sum<kLong>(sg, part[0]) / (float)a.cols, mgx = row_sum<kLong>(sgx, part[1]) / (float)a.cols;
+  T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
+  for (int64_t c = threadIdx.x; c < a.cols; c += kLong) {
+    load_weight<T, 1>(w, a.weight, w_f32, c, 1.0f);
+    dx[c] = from_f32<T>(rstd * (to_f32(dy[c]) * w[0] - mg - (to_f32(x[c]) - mean) * rstd * mgx));
+  }
+}
+
+// column sums of every gridDim.y-th row, for rows that k_backward does not hold
+template <typename T>
+__global__ void k_columns_long(NormArgs a) {
+  const int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (c >= a.cols) return;
   float sw = 0.0f, sb = 0.0f;
-  for (int64_t row = blockIdx.y; row < a.rows; row += kColumnBlocks) {
+  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
     const float dy = to_f32(static_cast<const T*>(a.dy)[row * a.dy_stride + c]);
     sw += dy * ((to_f32(static_cast<const T*>(a.x)[row * a.x_stride + c]) - a.stats[row]) * a.stats[a.rows + row]);
     sb += dy;
   }
-  a.partial[(int64_t)blockIdx.y * a.cols + c] = sw;
-  a.partial[((int64_t)kColumnBlocks + blockIdx.y) * a.cols + c] = sb;
+  a.partial[(int64_t)blockIdx.y * 2 * a.cols + c] = sw;
+  a.partial[((int64_t)blockIdx.y * 2 + 1) * a.cols + c] = sb;
 }
 
+// adds up the blocks' column sums: 32 columns a block, 32 chains each, joined in shared memory
 template <typename W>
-__global__ void k_columns_join(NormArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (c >= a.cols) return;
-  float sw = 0.0f, sb = 0.0f;
-  for (int p = 0; p < kColumnBlocks; p++) {
-    sw += a.partial[(int64_t)p * a.cols + c];
-    sb += a.partial[((int64_t)kColumnBlocks + p) * a.cols + c];
+__global__ void __launch_bounds__(1024) k_columns_join(const float* partial, int blocks, int64_t cols, W* dweight, W* dbias) {
+  __shared__ float part[32][33];
+  const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  W* out = blockIdx.y ? dbias : dweight;
+  if (!out) return;
+  float s = 0.0f;
+  if (c < cols) {
+    const float* p = partial + (int64_t)blockIdx.y * cols + c;
+#pragma unroll 8
+    for (int b = threadIdx.y; b < blocks; b += 32) s += p[(int64_t)b * 2 * cols];
   }
-  if (a.dweight) static_cast<W*>(a.dweight)[c] = from_f32<W>(sw);
-  if (a.dbias) static_cast<W*>(a.dbias)[c] = from_f32<W>(sb);
+  part[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  s = part[threadIdx.x][threadIdx.y];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+  const int64_t d = (int64_t)blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x == 0 && d < cols) out[d] = from_f32<W>(s);
 }
 
-template <typename T, typename W>
-cudaError_t forward(const NormArgs& a, cudaStream_t s) {
+constexpr int kSms = 152;
+constexpr int kMostBlocks = kSms * 6;  // of k_backward: their column sums are what the workspace holds
+constexpr int kLongBlocks = 64;        // row ranges of k_columns_long
+
+bool on16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool on16(const void* p, int64_t stride, int64_t rows, size_t elem) {
+  return on16(p) && (rows <= 1 || (stride * (int64_t)elem) % 16 == 0);
+}
+
+// The kernel variant for rows of `cols` elements: V elements a load (16 bytes where every row starts and
+// ends on 16 bytes, else 1), N loads a thread, kRow threads a row.  `f` is called with the three as
+// integral constants; false: the row is longer than any variant holds.
+template <int K> using Int = std::integral_constant<int, K>;
+
+template <typename T, typename F>
+bool forward_variant(bool vectors, int64_t cols, F&& f) {
+  constexpr int V = 16 / sizeof(T);
+  if (vectors) {
+    const int64_t packs = cols / V;  // a warp a row up to 8 loads a thread (no barriers), then blocks
+    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>());
+    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>());
+    else if (packs <= 128) f(Int<V>(), Int<4>(), Int<32>());
+    else if (packs <= 256) f(Int<V>(), Int<8>(), Int<32>());
+    else if (packs <= 512) f(Int<V>(), Int<4>(), Int<128>());
+    else if (packs <= 1024) f(Int<V>(), Int<4>(), Int<256>());
+    else if (packs <= 2048) f(Int<V>(), Int<4>(), Int<512>());
+    else return false;
+  } else {
+    if (cols <= 128) f(Int<1>(), Int<4>(), Int<32>());
+    else if (cols <= 512) f(Int<1>(), Int<16>(), Int<32>());
+    else if (cols <= 2048) f(Int<1>(), Int<16>(), Int<128>());
+    else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>());
+    else return false;
+  }
+  return true;
+}
+
+template <typename T, typename F>
+bool backward_variant(bool vectors, int64_t cols, F&& f) {
+  constexpr int V = 16 / sizeof(T);
+  if (vectors) {
+    const int64_t packs = cols / V;
+    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>());
+    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>());
+    else if (packs <= 128) f(Int<V>(), Int<1>(), Int<128>());
+    else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>());
+    else if (packs <= 512) f(Int<V>(), Int<2>(), Int<256>());
+    else if (packs <= 1024) f(Int<V>(), Int<2>(), Int<512>());
+    else if (packs <= 2048 && sizeof(T) == 4) f(Int<4>(), Int<4>(), Int<512>());  // (16-bit rows would not fit in 128 registers)
+    else return false;
+  } else {
+    if (cols <= 256) f(Int<1>(), Int<8>(), Int<32>());
+    else if (cols <= 1024) f(Int<1>(), Int<8>(), Int<128>());
+    else if (cols <= 2048) f(Int<1>(), Int<8>(), Int<256>());
+    else if (cols <= 4096) f(Int<1>(), Int<8>(), Int<512>());
+    else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>());
+    else return false;
+  }
+  return true;
+}
+
+template <typename T>
+cudaError_t forward(const NormArgs& a, int w_f32, cudaStream_t s) {
   if (a.rows == 0) return cudaSuccess;
-  k_forward<T, W><<<(unsigned)(a.rows < 65536 ? a.rows : 65536), kThreads, 0, s>>>(a);
+  if (a.rows > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  const bool vectors = a.cols % (16 / sizeof(T)) == 0 && on16(a.x, a.x_stride, a.rows, sizeof(T)) &&
+                       on16(a.y, a.y_stride, a.rows, sizeof(T)) && on16(a.weight) && on16(a.bias);
+  const bool held = forward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r) {
+    constexpr int kRow = decltype(r)::value, kRows = kBlock<kRow> / kRow;
+    k_forward<T, decltype(v)::value, decltype(n)::value, kRow>
+        <<<(unsigned)((a.rows + kRows - 1) / kRows), kBlock<kRow>, 0, s>>>(a, w_f32);
+  });
+  if (!held) k_forward_long<T><<<(unsigned)a.rows, kLong, 0, s>>>(a, w_f32);
   return cudaGetLastError();
 }
 
-template <typename T, typename W>
-cudaError_t backward(const NormArgs& a, cudaStream_t s) {
-  if (a.dx && a.rows > 0) k_backward_x<T, W><<<(unsigned)(a.rows < 65536 ? a.rows : 65536), kThreads, 0, s>>>(a);
-  if (a.dweight || a.dbias) {
-    const unsigned g = (unsigned)((a.cols + kThreads - 1) / kThreads);
-    k_columns<T><<<dim3(g, kColumnBlocks), kThreads, 0, s>>>(a);
-    k_columns_join<W><<<g, kThreads, 0, s>>>(a);
+template <typename T>
+cudaError_t backward(NormArgs a, int w_f32, cudaStream_t s) {
+  if (a.rows > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  const bool sums = a.dweight || a.dbias;
+  if (!sums) a.partial = nullptr;
+  int blocks = 0;
+  if (a.rows > 0 && (a.dx || sums)) {
+    const bool vectors = a.cols % (16 / sizeof(T)) == 0 && on16(a.x, a.x_stride, a.rows, sizeof(T)) &&
+                         on16(a.dy, a.dy_stride, a.rows, sizeof(T)) && on16(a.weight) &&
+                         (!a.dx || on16(a.dx, a.dx_stride, a.rows, sizeof(T)));
+    const bool held = backward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r) {
+      constexpr int kRow = decltype(r)::value, kRows = kBlock<kRow> / kRow;
+      // as many blocks as stay resident, or a block a group of rows where there are fewer
+      static const int resident = [] {
+        int b = 0;
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&b, k_backward<T, decltype(v)::value, decltype(n)::value, kRow>,
+                                                      kBlock<kRow>, 0);
+        return std::clamp(b * kSms, kSms, kMostBlocks);
+      }();
+      blocks = (int)std::min<int64_t>(resident, (a.rows + kRows - 1) / kRows);
+      k_backward<T, decltype(v)::value, decltype(n)::value, kRow><<<blocks, kBlock<kRow>, 0, s>>>(a, w_f32);
+    });
+    if (!held) {
+      if (a.dx) k_backward_long<T><<<(unsigned)a.rows, kLong, 0, s>>>(a, w_f32);
+      blocks = (int)std::min<int64_t>(kLongBlocks, a.rows);
+      if (sums) k_columns_long<T><<<dim3((unsigned)((a.cols + 255) / 256), blocks), 256, 0, s>>>(a);
+    }
+  }
+  if (sums) {
+    const dim3 grid((unsigned)((a.cols + 31) / 32), 2), block(32, 32);
+    if (w_f32) k_columns_join<<<grid, block, 0, s>>>(a.partial, blocks, a.cols, static_cast<float*>(a.dweight), static_cast<float*>(a.dbias));
+    else k_columns_join<<<grid, block, 0, s>>>(a.partial, blocks, a.cols, static_cast<T*>(a.dweight), static_cast<T*>(a.dbias));
   }
   return cudaGetLastError();
-}
-
-template <typename F>
-cudaError_t by_type(ndvm_dtype t, ndvm_dtype wt, F&& f) {
-  if (t == NDVM_F32) return f(float(), float());
-  if (t == NDVM_F16) return wt == NDVM_F32 ? f(__half(), float()) : f(__half(), __half());
-  return wt == NDVM_F32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
 }
 
 }  // namespace
 
 cudaError_t launch_norm_forward(const NormArgs& a, ndvm_dtype t, ndvm_dtype wt, cudaStream_t s) {
-  return by_type(t, wt, [&](auto x, auto w) { return forward<decltype(x), decltype(w)>(a, s); });
+  const int f = wt == NDVM_F32;
+  return t == NDVM_F32 ? forward<float>(a, f, s) : t == NDVM_F16 ? forward<__half>(a, f, s) : forward<__nv_bfloat16>(a, f, s);
 }
 cudaError_t launch_norm_backward(const NormArgs& a, ndvm_dtype t, ndvm_dtype wt, cudaStream_t s) {
-  return by_type(t, wt, [&](auto x, auto w) { return backward<decltype(x), decltype(w)>(a, s); });
+  const int f = wt == NDVM_F32;
+  return t == NDVM_F32 ? backward<float>(a, f, s) : t == NDVM_F16 ? backward<__half>(a, f, s) : backward<__nv_bfloat16>(a, f, s);
 }
-size_t norm_workspace(int64_t, int64_t cols) { return (size_t)cols * 2 * kColumnBlocks * sizeof(float); }
+size_t norm_workspace(int64_t rows, int64_t cols) {
+  return (size_t)std::clamp<int64_t>(rows, 1, kMostBlocks) * (size_t)cols * 2 * sizeof(float);
+}
 
 }  // namespace ndvm
