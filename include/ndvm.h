@@ -333,9 +333,9 @@ ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t ro
                                void* stream);
 
 /*
- * ndvm_gated_workspace_bytes -- device workspace of a forward (backward = 0) or backward (1) call whose
- * row strides, base addresses and sizes are multiples of 16 bytes (aligned = 1) or not (0: room for
- * aligned copies).  0 on invalid sizes.
+ * ndvm_gated_workspace_bytes -- device workspace of a forward (backward = 0) or backward (1) call.
+ * aligned = 1: x, w_gate and w_up start on 16 bytes and their row strides are multiples of 8 elements and
+ * not 0; otherwise 0, which adds room for copies that are.  0 on invalid sizes.
  */
 size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backward, int aligned);
 
@@ -349,6 +349,12 @@ ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t r
                                 const void* dh, int64_t dh_stride, const void* x, int64_t x_stride, const void* w_gate,
                                 int64_t g_stride, const void* w_up, int64_t u_stride, void* dx, int64_t dx_stride,
                                 void* dw_gate, void* dw_up, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * ndvm_check_operators -- synchronize and report whether a kernel of the network operators gave up a wait on
+ * the current device since the last check (NDVM_E_DEVICE_CHECK: its outputs are not valid); clears the flag.
+ */
+ndvm_status ndvm_check_operators(void);
 
 /* ndvm_launch_count -- replay kernels launched by this process so far. */
 unsigned long long ndvm_launch_count(void);

@@ -1,14 +1,23 @@
 // Gated projection h = act(G) U with G = x Wg^T, U = x Wu^T, and its backward pass:
 //   dU = dh act(G), dG = dh U act'(G), dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.
-// G and U are computed again in the backward pass rather than kept: they stay in binary32 until dG and
-// dU are rounded, once, to the operands' type.
+// G and U are computed again in the backward pass rather than kept (8 bytes an element in binary32): they stay in
+// binary32 until dG and dU are rounded, once, to the operands' type, which the next products need.
+//
+// All products run in one kernel frame (k_product): D[m, n] = sum over c of A[m, c] B[n, c], 128 rows a tile,
+// operands by TMA, sums in tensor memory.
+//   forward   A = x, B = a tile's rows of Wg and then of Wu: G and U land in the two halves of a tile's columns
+//   gradient  the same products; the epilogue reads dh and writes dG and dU to the workspace
+//   dx        A = dG, B = Wg^T, then A = dU, B = Wu^T into the same sums
+//   dW        A = dG^T (or dU^T), B = x^T
+// Transposes are read as they lie: the operand's rows are contiguous instead of its contraction.
 #include "net.h"
+#include "tc.cuh"
 #include "types.cuh"
 
 namespace ndvm {
 namespace {
 
-constexpr int kTile = 64, kStep = 16;
+__device__ int g_stopped;  // a wait in k_product ran out (ndvm_check_operators)
 
 __device__ __forceinline__ void activate(int act, float g, float* a, float* da) {
   if (act == NDVM_ACT_RELU) {
@@ -17,109 +26,559 @@ __device__ __forceinline__ void activate(int act, float g, float* a, float* da) 
   } else if (act == NDVM_ACT_GELU) {
     const float cdf = 0.5f * (1.0f + erff(g * 0.70710678f));
     *a = g * cdf;
-    *da = cdf + g * expf(-0.5f * g * g) * 0.39894228f;
+    *da = cdf + g * __expf(-0.5f * g * g) * 0.39894228f;
   } else {
-    const float s = 1.0f / (1.0f + expf(-g));
+    const float s = __fdividef(1.0f, 1.0f + __expf(-g));
     *a = act == NDVM_ACT_SILU ? g * s : s;
     *da = act == NDVM_ACT_SILU ? s * (1.0f + g * (1.0f - s)) : s * (1.0f - s);
   }
 }
 
-// A view of a matrix operand: element (i, j) at p[i * si + j * sj].
-template <typename T>
-struct View {
-  const T* p;
-  int64_t si, sj;
+// ------------------------------------------------------------------ products on the tensor cores
+enum Mode { kForward, kGradient, kInput, kWeight };
+
+constexpr int kM = 128, kC = 64;  // rows of a tile, contraction of a step (128 bytes)
+constexpr int kThreads = 192;     // a warp that loads, one that multiplies, four that read the sums
+
+__host__ __device__ constexpr bool a_rows(Mode m) { return m == kWeight; }
+__host__ __device__ constexpr bool b_rows(Mode m) { return m == kInput || m == kWeight; }
+__host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == kGradient; }
+
+template <int kN> constexpr int kStageBytes = (kM + kN) * kC * 2;
+template <int kN> constexpr int kStages = 196608 / kStageBytes<kN> < 8 ? 196608 / kStageBytes<kN> : 8;
+template <int kN> constexpr int kSmem = kStages<kN> * kStageBytes<kN> + 1024 /* alignment */ + 256 /* barriers */;
+
+struct ProductArgs {
+  CUtensorMap a[2], b[2];
+  int m, n, c;                   // rows and columns of the result, contraction of one segment
+  int tiles_m, tiles_n, matrices;  // matrices: results of one shape, by the a's (kWeight: 1 or 2), else 1
+  int steps, splits;             // contraction steps of a result, and how many parts they are cut into
+  int act;
+  void* out[2]; int64_t stride;  // kWeight: both matrices'; kGradient: dG and dU; else out[0]
+  const void* dh; int64_t dh_stride;
+  float* partial;                // splits > 1: [split][matrix][m][n]
 };
 
-// acc += A[m0.., 0..k) B[n0.., 0..k)^T for a 64 x 64 tile, 4 x 4 elements a thread
+// 32 values to 32 elements of a row: 16 bytes a store where the row allows, else one by one
 template <typename T>
-__device__ void tile_product(View<T> A, View<T> B, int64_t m0, int64_t n0, int64_t m, int64_t n, int64_t k,
-                             float (&sa)[kStep][kTile + 1], float (&sb)[kStep][kTile + 1], float (&acc)[4][4]) {
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int64_t k0 = 0; k0 < k; k0 += kStep) {
-    for (int e = threadIdx.x; e < kTile * kStep; e += 256) {
-      const int i = e / kStep, j = e % kStep;
-      const bool in = k0 + j < k;
-      sa[j][i] = in && m0 + i < m ? to_f32(A.p[(m0 + i) * A.si + (k0 + j) * A.sj]) : 0.0f;
-      sb[j][i] = in && n0 + i < n ? to_f32(B.p[(n0 + i) * B.si + (k0 + j) * B.sj]) : 0.0f;
+__device__ __forceinline__ void store_row32(T* p, const float (&v)[32], int count, bool vectors) {
+  if (vectors && count >= 32) {
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+      Pack<T, 8> o;
+#pragma unroll
+      for (int e = 0; e < 8; e++) o.v[e] = from_f32<T>(v[q * 8 + e]);
+      store_pack(p + q * 8, o);
     }
-    __syncthreads();
-    for (int j = 0; j < kStep; j++)
-      for (int p = 0; p < 4; p++)
-        for (int q = 0; q < 4; q++) acc[p][q] += sa[j][ty + 16 * p] * sb[j][tx + 16 * q];
-    __syncthreads();
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; e++)
+      if (e < count) p[e] = from_f32<T>(v[e]);
   }
 }
 
-// the two products and, forward: h; backward: dG and dU (rows x n each, in the workspace)
-template <typename T, bool kBackward>
-__global__ void __launch_bounds__(256) k_products(GatedArgs a) {
-  __shared__ float sa[kStep][kTile + 1], sb[kStep][kTile + 1];
-  float g[4][4] = {}, u[4][4] = {};
-  const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
-  const View<T> x{static_cast<const T*>(a.x), a.x_stride, 1};
-  tile_product(x, View<T>{static_cast<const T*>(a.w_gate), a.g_stride, 1}, m0, n0, a.rows, a.n, a.k, sa, sb, g);
-  tile_product(x, View<T>{static_cast<const T*>(a.w_up), a.u_stride, 1}, m0, n0, a.rows, a.n, a.k, sa, sb, u);
-  for (int p = 0; p < 4; p++)
-    for (int q = 0; q < 4; q++) {
-      const int64_t i = m0 + threadIdx.x / 16 + 16 * p, j = n0 + threadIdx.x % 16 + 16 * q;
-      if (i >= a.rows || j >= a.n) continue;
-      float act, da;
-      activate(a.act, g[p][q], &act, &da);
-      if (kBackward) {
-        const float dh = to_f32(static_cast<const T*>(a.dh)[i * a.dh_stride + j]);
-        T* d = static_cast<T*>(a.workspace);
-        d[i * a.n + j] = from_f32<T>(dh * u[p][q] * da);
-        d[(a.rows + i) * a.n + j] = from_f32<T>(dh * act);
-      } else {
-        static_cast<T*>(a.h)[i * a.h_stride + j] = from_f32<T>(act * u[p][q]);
+template <typename T, Mode kMode, int kN>
+__global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ ProductArgs p) {
+  extern __shared__ char raw[];
+  constexpr int S = kStages<kN>;
+  constexpr uint32_t kABytes = kM * kC * 2;
+  constexpr int kColumns = 2 * kN;  // of tensor memory: two tiles' sums
+  constexpr int kOutN = dual(kMode) ? kN / 2 : kN;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_stop;
+  const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
+  const uint32_t bars = base + S * kStageBytes<kN>;
+  const auto full = [&](int i) { return bars + i * 8; };
+  const auto empty = [&](int i) { return bars + (S + i) * 8; };
+  const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
+  const auto taken = [&](int i) { return bars + (2 * S + 2 + i) * 8; };  // and have been read
+  const uint32_t drain = bars + (2 * S + 4) * 8;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  volatile int* stop = &s_stop;
+
+  if (threadIdx.x == 0) {
+    s_stop = 0;
+    for (int i = 0; i < S; i++) tc::barrier_init(full(i), 1), tc::barrier_init(empty(i), 1);
+    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), 4);
+    tc::barrier_init(drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tc::tmem_alloc<kColumns>(tc::smem(&s_tmem));
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = s_tmem;
+
+  const int tiles = p.tiles_m * p.tiles_n, items = tiles * p.matrices * p.splits;
+  const int segment = (p.c + kC - 1) / kC;  // steps of one segment
+  struct Item { int m0, n0, matrix, split, from, to; };
+  // tiles in bands of 16 rows of tiles, down a band first: blocks that run together share operands in L2
+  const auto item = [&](int i) {
+    Item it;
+    it.split = i / (tiles * p.matrices);
+    i -= it.split * (tiles * p.matrices);
+    it.matrix = i / tiles;
+    i -= it.matrix * tiles;
+    const int band = i / (16 * p.tiles_n), first = band * 16, height = min(16, p.tiles_m - first);
+    i -= band * 16 * p.tiles_n;
+    it.m0 = (first + i % height) * kM;
+    it.n0 = i / height * kOutN;
+    it.from = (int)((int64_t)p.steps * it.split / p.splits);
+    it.to = (int)((int64_t)p.steps * (it.split + 1) / p.splits);
+    return it;
+  };
+
+  if (warp == 0 && lane == 0) {
+    // ---- loads
+    int stage = 0;
+    uint32_t phase = 0;
+    int issued = 0;
+    bool ok = true;
+    for (int i = blockIdx.x; ok && i < items; i += gridDim.x) {
+      const Item it = item(i);
+      for (int s = it.from; s < it.to; s++) {
+        if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, stop))) break;
+        const uint32_t a = base + stage * kStageBytes<kN>, b = a + kABytes, bar = full(stage);
+        tc::barrier_expect(bar, kStageBytes<kN>);
+        const int seg = kMode == kInput ? s / segment : kMode == kWeight ? it.matrix : 0;
+        const int c = (kMode == kInput ? s - seg * segment : s) * kC;
+        if (a_rows(kMode)) {
+          for (int q = 0; q < kM / 64; q++) tc::load_box(a + q * 8192, &p.a[seg], it.m0 + q * 64, c, bar);
+        } else {
+          tc::load_box(a, &p.a[seg], c, it.m0, bar);
+        }
+        if (dual(kMode)) {
+          tc::load_box(b, &p.b[0], c, it.n0, bar);
+          tc::load_box(b + kN / 2 * kC * 2, &p.b[1], c, it.n0, bar);
+        } else {
+          for (int q = 0; q < kN / 64; q++) tc::load_box(b + q * 8192, &p.b[kMode == kInput ? seg : 0], it.n0 + q * 64, c, bar);
+        }
+        issued++;
+        if (++stage == S) stage = 0, phase ^= 1;
       }
     }
-}
-
-// out[m x n] = A1 B1^T + A2 B2^T (A2 null: the first alone)
-template <typename T>
-__global__ void __launch_bounds__(256) k_product(View<T> A1, View<T> B1, View<T> A2, View<T> B2, int64_t m, int64_t n,
-                                                 int64_t k, T* out, int64_t stride) {
-  __shared__ float sa[kStep][kTile + 1], sb[kStep][kTile + 1];
-  float acc[4][4] = {};
-  const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
-  tile_product(A1, B1, m0, n0, m, n, k, sa, sb, acc);
-  if (A2.p) tile_product(A2, B2, m0, n0, m, n, k, sa, sb, acc);
-  for (int p = 0; p < 4; p++)
-    for (int q = 0; q < 4; q++) {
-      const int64_t i = m0 + threadIdx.x / 16 + 16 * p, j = n0 + threadIdx.x % 16 + 16 * q;
-      if (i < m && j < n) out[i * stride + j] = from_f32<T>(acc[p][q]);
+    if (!ok)  // the copies in flight end before the block does
+      for (int k = 1; k <= min(issued, S); k++) {
+        const int at = (issued - k) % S, turn = (issued - k) / S;
+        tc::barrier_drain(full(at), turn & 1);
+      }
+  } else if (warp == 1 && lane == 0) {
+    // ---- products
+    constexpr uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, a_rows(kMode), b_rows(kMode), kM, kN);
+    int stage = 0, slot = 0;
+    uint32_t phase = 0, slot_phase = 0;
+    bool ok = true;
+    for (int i = blockIdx.x; ok && i < items; i += gridDim.x) {
+      const Item it = item(i);
+      if (!(ok = tc::barrier_wait(taken(slot), slot_phase ^ 1, stop))) break;
+      tc::fence_after();
+      for (int s = it.from; s < it.to; s++) {
+        if (!(ok = tc::barrier_wait(full(stage), phase, stop))) break;
+        tc::fence_after();
+        const uint32_t at = base + stage * kStageBytes<kN>;
+        const uint64_t a = tc::operand(at, a_rows(kMode)), b = tc::operand(at + kABytes, b_rows(kMode));
+#pragma unroll
+        for (int q = 0; q < kC / 16; q++)  // 16 of the contraction: 32 bytes along a line, or 16 lines
+          tc::mma(tmem + slot * kN, a + q * (a_rows(kMode) ? 2048 >> 4 : 32 >> 4), b + q * (b_rows(kMode) ? 2048 >> 4 : 32 >> 4),
+                  desc, s > it.from || q > 0);
+        tc::commit(empty(stage));
+        if (++stage == S) stage = 0, phase ^= 1;
+      }
+      tc::commit(done(slot));
+      if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
+    if (!ok) {  // the products in flight end before tensor memory is freed
+      tc::commit(drain);
+      tc::barrier_drain(drain, 0);
+    }
+  } else if (warp >= 2) {
+    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own
+    const int lanes = (warp % 4) * 32;
+    int slot = 0;
+    uint32_t slot_phase = 0;
+    const bool vec_out = reinterpret_cast<uintptr_t>(p.out[0]) % 16 == 0 && reinterpret_cast<uintptr_t>(p.out[1]) % 16 == 0 &&
+                         p.stride % 8 == 0;
+    const bool vec_dh = kMode == kGradient && reinterpret_cast<uintptr_t>(p.dh) % 16 == 0 && p.dh_stride % 8 == 0;
+    for (int i = blockIdx.x; i < items; i += gridDim.x) {
+      const Item it = item(i);
+      const int row = it.m0 + lanes + lane;
+      // (the whole warp goes on or gives up: reading tensor memory is a warp's instruction)
+      if (!__all_sync(~0u, tc::barrier_wait(done(slot), slot_phase, stop))) break;
+      tc::fence_after();
+      const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
+#pragma unroll 1
+      for (int j = 0; j < kOutN; j += 32) {
+        const int col = it.n0 + j, count = min(32, p.n - col);
+        if (count <= 0) break;
+        float v[32];
+        tc::tmem_load32(v, at + j);
+        if (dual(kMode)) {
+          float u[32];
+          tc::tmem_load32(u, at + kN / 2 + j);
+          if (kMode == kForward) {
+            tc::tmem_loaded();
+            if (row < p.m) {
+#pragma unroll
+              for (int e = 0; e < 32; e++) {
+                float a, da;
+                activate(p.act, v[e], &a, &da);
+                v[e] = a * u[e];
+              }
+              store_row32(static_cast<T*>(p.out[0]) + row * p.stride + col, v, count, vec_out);
+            }
+          } else {
+            Pack<T, 8> d[4];
+            if (row < p.m) {
+              const T* dh = static_cast<const T*>(p.dh) + row * p.dh_stride + col;
+              if (vec_dh && count == 32) {
+#pragma unroll
+                for (int q = 0; q < 4; q++) d[q] = load_pack<T, 8>(dh + q * 8);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 32; e++) d[e / 8].v[e % 8] = e < count ? dh[e] : from_f32<T>(0.0f);
+              }
+            }
+            tc::tmem_loaded();
+            if (row < p.m) {
+#pragma unroll
+              for (int e = 0; e < 32; e++) {
+                float a, da;
+                activate(p.act, v[e], &a, &da);
+                const float f = to_f32(d[e / 8].v[e % 8]);
+                v[e] = f * u[e] * da;
+                u[e] = f * a;
+              }
+              store_row32(static_cast<T*>(p.out[0]) + row * p.stride + col, v, count, vec_out);
+              store_row32(static_cast<T*>(p.out[1]) + row * p.stride + col, u, count, vec_out);
+            }
+          }
+        } else {
+          tc::tmem_loaded();
+          if (row < p.m) {
+            if (p.splits > 1) {
+              float* o = p.partial + (((int64_t)it.split * p.matrices + it.matrix) * p.m + row) * p.n + col;
+#pragma unroll
+              for (int e = 0; e < 32; e++)
+                if (e < count) o[e] = v[e];
+            } else {
+              store_row32(static_cast<T*>(p.out[it.matrix]) + row * p.stride + col, v, count, vec_out);
+            }
+          }
+        }
+      }
+      tc::fence_before();
+      __syncwarp();
+      if (lane == 0) tc::barrier_arrive(taken(slot));
+      if (++slot == 2) slot = 0, slot_phase ^= 1;
+    }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (threadIdx.x == 0 && s_stop) g_stopped = 1;
+  tc::fence_after();
+  if (warp == 1) tc::tmem_free<kColumns>(tmem);
 }
 
-dim3 tiles(int64_t m, int64_t n) { return dim3((unsigned)((n + kTile - 1) / kTile), (unsigned)((m + kTile - 1) / kTile)); }
+// the parts of split sums added up in order, and rounded
+template <typename T>
+__global__ void __launch_bounds__(256) k_join(const float* partial, int splits, int matrices, int64_t m, int64_t n, T* out0,
+                                              T* out1, int64_t stride) {
+  const int64_t total = matrices * m * n;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    float s = 0.0f;
+    for (int k = 0; k < splits; k++) s += partial[k * total + i];
+    const int64_t row = i / n, r = row % m;
+    (row >= m ? out1 : out0)[r * stride + (i - row * n)] = from_f32<T>(s);
+  }
+}
+
+// rows of `cols` elements to rows that start on 16 bytes (TMA reads no others)
+template <typename T>
+__global__ void __launch_bounds__(256) k_pack(const T* from, int64_t stride, int64_t rows, int64_t cols, T* to, int64_t pitch) {
+  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < cols; c += (int64_t)gridDim.x * 256)
+      to[r * pitch + c] = from[r * stride + c];
+}
+
+// --------------------------------------------------------------------------- few rows: vectors
+// Up to 8 rows: the weights are read once and are nearly all the traffic, so a warp takes one row of each
+// weight, 16 bytes a lane and load, against every row of x (from L1), sums in registers.
+constexpr int kFewRows = 8;
+
+template <typename T, int R, int V, bool kBackward>
+__global__ void __launch_bounds__(256) k_few(GatedArgs a, T* dg, T* du, int64_t pitch) {
+  const int lane = threadIdx.x % 32;
+  const int64_t j = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  if (j >= a.n) return;
+  const T* wg = static_cast<const T*>(a.w_gate) + j * a.g_stride;
+  const T* wu = static_cast<const T*>(a.w_up) + j * a.u_stride;
+  const T* x = static_cast<const T*>(a.x);
+  float g[R] = {}, u[R] = {};
+  constexpr int kUnroll = R > 2 ? 2 : 4;
+#pragma unroll kUnroll
+  for (int64_t c = lane * V; c < a.k; c += 32 * V) {
+    const Pack<T, V> pg = load_pack<T, V>(wg + c), pu = load_pack<T, V>(wu + c);
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+      if (R > 1 && r >= a.rows) break;
+      const Pack<T, V> px = load_pack<T, V>(x + r * a.x_stride + c);
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        g[r] += to_f32(px.v[e]) * to_f32(pg.v[e]);
+        u[r] += to_f32(px.v[e]) * to_f32(pu.v[e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; r++) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      g[r] += __shfl_xor_sync(~0u, g[r], o);
+      u[r] += __shfl_xor_sync(~0u, u[r], o);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; r++) {
+    if (lane != r || r >= a.rows) continue;
+    float act, da;
+    activate(a.act, g[r], &act, &da);
+    if (kBackward) {
+      const float dh = to_f32(static_cast<const T*>(a.dh)[r * a.dh_stride + j]);
+      dg[r * pitch + j] = from_f32<T>(dh * u[r] * da);
+      du[r * pitch + j] = from_f32<T>(dh * act);
+    } else {
+      static_cast<T*>(a.h)[r * a.h_stride + j] = from_f32<T>(act * u[r]);
+    }
+  }
+}
+
+template <typename T, bool kBackward>
+void few(const GatedArgs& a, bool vectors, T* dg, T* du, int64_t pitch, cudaStream_t s) {
+  const unsigned grid = (unsigned)((a.n + 7) / 8);
+  const auto go = [&](auto r) {
+    constexpr int R = decltype(r)::value;
+    if (vectors) k_few<T, R, 8, kBackward><<<grid, 256, 0, s>>>(a, dg, du, pitch);
+    else k_few<T, R, 1, kBackward><<<grid, 256, 0, s>>>(a, dg, du, pitch);
+  };
+  if (a.rows == 1) go(std::integral_constant<int, 1>());
+  else if (a.rows == 2) go(std::integral_constant<int, 2>());
+  else if (a.rows <= 4) go(std::integral_constant<int, 4>());
+  else go(std::integral_constant<int, 8>());
+}
+
+// ------------------------------------------------------------------------------------ launches
+constexpr int kSms = 152;
+
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+bool tma_ready(const void* p, int64_t stride, int64_t rows, int64_t cols) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows == 1 || (stride % 8 == 0 && stride >= cols));
+}
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {
+  static const Encode e = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<Encode>(f);
+  }();
+  return e;
+}
+
+// a matrix of `rows` rows of `cols` contiguous elements, read in boxes of 64 columns and `box` rows
+template <typename T>
+bool map_matrix(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box) {
+  if (!encoder()) return false;
+  if (rows == 1) stride = up(cols, 8);  // (never taken)
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
+  const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, ones[2] = {1, 1};
+  const CUtensorMapDataType type = std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return encoder()(map, type, 2, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Columns of a tile's sums: 256 (the fewest bytes an operation), or fewer where that would leave SMs idle.
+int tile_width(int64_t m, int64_t n, bool two) {
+  for (int w : {256, 128})
+    if (ceil_div(m, kM) * ceil_div(n, two ? w / 2 : w) >= kSms) return w;
+  return 64;
+}
+// Parts that a result's contraction is cut into: enough for every SM to have one, none shorter than 8 steps.
+int split_count(int64_t tiles, int64_t steps) {
+  if (tiles >= kSms) return 1;
+  return (int)std::clamp<int64_t>(kSms / tiles, 1, std::max<int64_t>(steps / 8, 1));
+}
+
+template <typename T, Mode kMode, int kN>
+cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
+  static const cudaError_t set =
+      cudaFuncSetAttribute(k_product<T, kMode, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kN>);
+  if (set != cudaSuccess) return set;
+  const int items = p.tiles_m * p.tiles_n * p.matrices * p.splits;
+  k_product<T, kMode, kN><<<std::min(items, kSms), kThreads, kSmem<kN>, s>>>(p);
+  return cudaGetLastError();
+}
+
+// how a product of the given size is cut up (the weights' gradients as if both were wanted: one of them
+// alone has the same bits)
+struct Cut { int width, splits; };
+Cut cut(Mode mode, int64_t m, int64_t n, int64_t c) {
+  Cut k;
+  const int matrices = mode == kWeight ? 2 : 1;
+  k.width = tile_width(m * matrices, n, dual(mode));
+  const int64_t tiles = matrices * ceil_div(m, kM) * ceil_div(n, dual(mode) ? k.width / 2 : k.width);
+  k.splits = dual(mode) ? 1 : split_count(tiles, ceil_div(c, kC) * (mode == kInput ? 2 : 1));
+  return k;
+}
+
+template <typename T, Mode kMode>
+cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s) {
+  const int out = dual(kMode) ? k.width / 2 : k.width;
+  p.tiles_m = (int)ceil_div(p.m, kM);
+  p.tiles_n = (int)ceil_div(p.n, out);
+  p.steps = (int)ceil_div(p.c, kC) * (kMode == kInput ? 2 : 1);
+  p.splits = k.splits;
+  if ((int64_t)p.tiles_m * p.tiles_n * p.matrices * p.splits > 0x40000000) return cudaErrorInvalidConfiguration;
+  const cudaError_t e = k.width == 256   ? launch_width<T, kMode, 256>(p, s)
+                        : k.width == 128 ? launch_width<T, kMode, 128>(p, s)
+                                         : launch_width<T, kMode, 64>(p, s);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  const int64_t total = (int64_t)p.matrices * p.m * p.n;
+  k_join<T><<<(unsigned)std::min<int64_t>(ceil_div(total, 256), kSms * 8), 256, 0, s>>>(
+      p.partial, p.splits, p.matrices, p.m, p.n, static_cast<T*>(p.out[0]), static_cast<T*>(p.out[1]), p.stride);
+  return cudaGetLastError();
+}
+
+// The workspace: aligned copies of what TMA cannot read, dG and dU, and split sums (dx's and the weights'
+// take turns).
+struct Layout {
+  int64_t k_pitch, n_pitch;
+  size_t x, gate, up, grad, partial, total;
+  Layout(int64_t rows, int64_t k, int64_t n, bool backward, bool copies) {
+    k_pitch = ndvm::up(k, 8);
+    n_pitch = ndvm::up(n, 8);
+    total = 0;
+    const auto take = [&](int64_t bytes) {
+      const size_t at = total;
+      total += (size_t)ndvm::up(bytes, 256);
+      return at;
+    };
+    x = take(copies ? rows * k_pitch * 2 : 0);
+    gate = take(copies ? n * k_pitch * 2 : 0);
+    up = take(copies ? n * k_pitch * 2 : 0);
+    grad = take(backward ? 2 * rows * n_pitch * 2 : 0);
+    int64_t parts = 0;
+    if (backward && rows > 0) {
+      const Cut i = cut(kInput, rows, k, n), w = cut(kWeight, n, k, rows);
+      if (i.splits > 1) parts = i.splits * rows * k;
+      if (w.splits > 1) parts = std::max(parts, 2 * w.splits * n * k);
+    }
+    partial = take(parts * 4);
+  }
+};
 
 template <typename T>
-cudaError_t forward(const GatedArgs& a, cudaStream_t s) {
+void pack(const void*& p, int64_t& stride, int64_t rows, int64_t cols, void* to, int64_t pitch, cudaStream_t s) {
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(cols, 256), 1024), (unsigned)std::min<int64_t>(rows, 16384));
+  k_pack<T><<<grid, 256, 0, s>>>(static_cast<const T*>(p), stride, rows, cols, static_cast<T*>(to), pitch);
+  p = to;
+  stride = pitch;
+}
+
+bool all_ready(const GatedArgs& a) {
+  return tma_ready(a.x, a.x_stride, a.rows, a.k) && tma_ready(a.w_gate, a.g_stride, a.n, a.k) &&
+         tma_ready(a.w_up, a.u_stride, a.n, a.k);
+}
+
+template <typename T>
+void make_ready(GatedArgs& a, const Layout& l, bool x, bool weights, cudaStream_t s) {
+  char* ws = static_cast<char*>(a.workspace);
+  if (x && !tma_ready(a.x, a.x_stride, a.rows, a.k)) pack<T>(a.x, a.x_stride, a.rows, a.k, ws + l.x, l.k_pitch, s);
+  if (!weights) return;
+  if (!tma_ready(a.w_gate, a.g_stride, a.n, a.k)) pack<T>(a.w_gate, a.g_stride, a.n, a.k, ws + l.gate, l.k_pitch, s);
+  if (!tma_ready(a.w_up, a.u_stride, a.n, a.k)) pack<T>(a.w_up, a.u_stride, a.n, a.k, ws + l.up, l.k_pitch, s);
+}
+
+// G and U, and h or dG and dU of them
+template <typename T, Mode kMode>
+cudaError_t products(const GatedArgs& a, void* out0, void* out1, int64_t stride, cudaStream_t s) {
+  const Cut k = cut(kMode, a.rows, a.n, a.k);
+  ProductArgs p{};
+  if (!map_matrix<T>(&p.a[0], a.x, a.rows, a.k, a.x_stride, kM) || !map_matrix<T>(&p.b[0], a.w_gate, a.n, a.k, a.g_stride, k.width / 2) ||
+      !map_matrix<T>(&p.b[1], a.w_up, a.n, a.k, a.u_stride, k.width / 2))
+    return cudaErrorInvalidValue;
+  p.m = (int)a.rows; p.n = (int)a.n; p.c = (int)a.k;
+  p.matrices = 1;
+  p.act = a.act; p.out[0] = out0; p.out[1] = out1; p.stride = stride; p.dh = a.dh; p.dh_stride = a.dh_stride;
+  return launch_product<T, kMode>(p, k, s);
+}
+
+template <typename T>
+cudaError_t forward(GatedArgs a, cudaStream_t s) {
   if (a.rows == 0) return cudaSuccess;
-  k_products<T, false><<<tiles(a.rows, a.n), 256, 0, s>>>(a);
-  return cudaGetLastError();
+  if (a.rows <= kFewRows) {
+    few<T, false>(a, all_ready(a) && a.k % 8 == 0, nullptr, nullptr, 0, s);
+    return cudaGetLastError();
+  }
+  const Layout l(a.rows, a.k, a.n, false, !all_ready(a));
+  make_ready<T>(a, l, true, true, s);
+  return products<T, kForward>(a, a.h, nullptr, a.h_stride, s);
 }
 
 template <typename T>
-cudaError_t backward(const GatedArgs& a, cudaStream_t s) {
-  if (a.rows > 0) k_products<T, true><<<tiles(a.rows, a.n), 256, 0, s>>>(a);
-  const T* dg = static_cast<const T*>(a.workspace);
-  const T* du = dg + a.rows * a.n;
-  const T *x = static_cast<const T*>(a.x), *wg = static_cast<const T*>(a.w_gate), *wu = static_cast<const T*>(a.w_up);
-  const View<T> none{nullptr, 0, 0};
-  if (a.dx && a.rows > 0)
-    k_product<T><<<tiles(a.rows, a.k), 256, 0, s>>>(View<T>{dg, a.n, 1}, View<T>{wg, 1, a.g_stride}, View<T>{du, a.n, 1},
-                                                    View<T>{wu, 1, a.u_stride}, a.rows, a.k, a.n, static_cast<T*>(a.dx), a.dx_stride);
-  if (a.dw_gate)
-    k_product<T><<<tiles(a.n, a.k), 256, 0, s>>>(View<T>{dg, 1, a.n}, View<T>{x, 1, a.x_stride}, none, none, a.n, a.k, a.rows,
-                                                 static_cast<T*>(a.dw_gate), a.k);
-  if (a.dw_up)
-    k_product<T><<<tiles(a.n, a.k), 256, 0, s>>>(View<T>{du, 1, a.n}, View<T>{x, 1, a.x_stride}, none, none, a.n, a.k, a.rows,
-                                                 static_cast<T*>(a.dw_up), a.k);
-  return cudaGetLastError();
+cudaError_t backward(GatedArgs a, cudaStream_t s) {
+  if (a.rows == 0) {
+    cudaError_t e = cudaSuccess;
+    if (a.dw_gate) e = cudaMemsetAsync(a.dw_gate, 0, (size_t)(a.n * a.k) * 2, s);
+    if (a.dw_up && e == cudaSuccess) e = cudaMemsetAsync(a.dw_up, 0, (size_t)(a.n * a.k) * 2, s);
+    return e;
+  }
+  const bool weights = a.dw_gate || a.dw_up;
+  if (!a.dx && !weights) return cudaSuccess;
+  const Layout l(a.rows, a.k, a.n, true, !all_ready(a));
+  char* ws = static_cast<char*>(a.workspace);
+  T* dg = reinterpret_cast<T*>(ws + l.grad);
+  T* du = dg + a.rows * l.n_pitch;
+  cudaError_t e;
+  if (a.rows <= kFewRows) {
+    few<T, true>(a, all_ready(a) && a.k % 8 == 0, dg, du, l.n_pitch, s);
+    make_ready<T>(a, l, weights, a.dx != nullptr, s);
+  } else {
+    make_ready<T>(a, l, true, true, s);
+    if ((e = products<T, kGradient>(a, dg, du, l.n_pitch, s)) != cudaSuccess) return e;
+  }
+  ProductArgs p{};
+  p.partial = reinterpret_cast<float*>(ws + l.partial);
+  if (a.dx) {
+    const Cut k = cut(kInput, a.rows, a.k, a.n);
+    if (!map_matrix<T>(&p.a[0], dg, a.rows, a.n, l.n_pitch, kM) || !map_matrix<T>(&p.a[1], du, a.rows, a.n, l.n_pitch, kM) ||
+        !map_matrix<T>(&p.b[0], a.w_gate, a.n, a.k, a.g_stride, 64) || !map_matrix<T>(&p.b[1], a.w_up, a.n, a.k, a.u_stride, 64))
+      return cudaErrorInvalidValue;
+    p.m = (int)a.rows; p.n = (int)a.k; p.c = (int)a.n; p.matrices = 1;
+    p.out[0] = a.dx; p.out[1] = nullptr; p.stride = a.dx_stride;
+    if ((e = launch_product<T, kInput>(p, k, s)) != cudaSuccess) return e;
+  }
+  if (weights) {
+    const Cut k = cut(kWeight, a.n, a.k, a.rows);
+    p.matrices = 0;
+    for (int w = 0; w < 2; w++) {
+      void* out = w ? a.dw_up : a.dw_gate;
+      if (!out) continue;
+      if (!map_matrix<T>(&p.a[p.matrices], w ? du : dg, a.rows, a.n, l.n_pitch, 64)) return cudaErrorInvalidValue;
+      p.out[p.matrices++] = out;
+    }
+    if (!map_matrix<T>(&p.b[0], a.x, a.rows, a.k, a.x_stride, 64)) return cudaErrorInvalidValue;
+    p.m = (int)a.n; p.n = (int)a.k; p.c = (int)a.rows; p.stride = a.k;
+    if (p.matrices == 1) p.out[1] = nullptr;
+    if ((e = launch_product<T, kWeight>(p, k, s)) != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -130,6 +589,16 @@ cudaError_t launch_gated_forward(const GatedArgs& a, ndvm_dtype t, cudaStream_t 
 cudaError_t launch_gated_backward(const GatedArgs& a, ndvm_dtype t, cudaStream_t s) {
   return t == NDVM_F16 ? backward<__half>(a, s) : backward<__nv_bfloat16>(a, s);
 }
-size_t gated_workspace(int64_t rows, int64_t, int64_t n) { return (size_t)rows * (size_t)n * 4; }
+size_t gated_workspace(int64_t rows, int64_t k, int64_t n, bool backward, bool copies) {
+  if (rows == 0 || (!backward && rows <= kFewRows)) return 0;
+  return Layout(rows, k, n, backward, copies).total;
+}
+size_t gated_workspace(const GatedArgs& a, bool backward) { return gated_workspace(a.rows, a.k, a.n, backward, !all_ready(a)); }
+cudaError_t gated_stopped(int* flag) {
+  cudaError_t e = cudaMemcpyFromSymbol(flag, g_stopped, sizeof *flag);
+  const int none = 0;
+  if (e == cudaSuccess && *flag) e = cudaMemcpyToSymbol(g_stopped, &none, sizeof none);
+  return e;
+}
 
 }  // namespace ndvm

@@ -48,6 +48,8 @@ struct GatedArgs {
 };
 cudaError_t launch_gated_forward(const GatedArgs& a, ndvm_dtype t, cudaStream_t s);
 cudaError_t launch_gated_backward(const GatedArgs& a, ndvm_dtype t, cudaStream_t s);
-size_t gated_workspace(int64_t rows, int64_t k, int64_t n);
+size_t gated_workspace(int64_t rows, int64_t k, int64_t n, bool backward, bool copies);
+size_t gated_workspace(const GatedArgs& a, bool backward);  // of this call
+cudaError_t gated_stopped(int* flag);                       // reads and clears: a kernel gave up waiting
 
 }  // namespace ndvm

@@ -130,21 +130,29 @@ static ndvm_status gated_check(ndvm_dtype dtype, ndvm_activation act, int64_t ro
   return NDVM_OK;
 }
 
-size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backward, int) {
+static const char* gated_room(const GatedArgs& a, bool backward, const void* workspace, size_t ws_bytes) {
+  const size_t need = gated_workspace(a, backward);
+  return need && (!workspace || !aligned(workspace, 256) || ws_bytes < need)
+             ? "the workspace is null, not 256-byte aligned or smaller than ndvm_gated_workspace_bytes" : nullptr;
+}
+
+size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backward, int aligned) {
   constexpr int64_t most = ((int64_t)1 << 31) - 1;
   if (rows < 0 || k < 1 || n < 1 || rows > most || k > most || n > most) return 0;
-  return backward ? gated_workspace(rows, k, n) : 0;
+  return gated_workspace(rows, k, n, backward != 0, !aligned);
 }
 
 ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,
                                int64_t x_stride, const void* w_gate, int64_t g_stride, const void* w_up,
-                               int64_t u_stride, void* h, int64_t h_stride, void*, size_t, void* stream) {
+                               int64_t u_stride, void* h, int64_t h_stride, void* workspace, size_t ws_bytes,
+                               void* stream) {
   if (ndvm_status s = gated_check(dtype, act, rows, k, n, x, x_stride, w_gate, g_stride, w_up, u_stride)) return s;
   if (rows == 0) return NDVM_OK;
   REFUSE(matrix_out(h, rows, n, h_stride, dtype));
   GatedArgs a{};
   a.rows = rows; a.k = k; a.n = n; a.x = x; a.x_stride = x_stride; a.w_gate = w_gate; a.w_up = w_up;
-  a.g_stride = g_stride; a.u_stride = u_stride; a.act = act; a.h = h; a.h_stride = h_stride;
+  a.g_stride = g_stride; a.u_stride = u_stride; a.act = act; a.h = h; a.h_stride = h_stride; a.workspace = workspace;
+  REFUSE(gated_room(a, false, workspace, ws_bytes));
   return done(launch_gated_forward(a, dtype, (cudaStream_t)stream), "gated projection launch");
 }
 
@@ -156,8 +164,6 @@ ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t r
   if (rows > 0) {
     REFUSE(matrix_in(dh, rows, n, dh_stride, dtype));
     if (dx) REFUSE(matrix_out(dx, rows, k, dx_stride, dtype));
-    if (!workspace || !aligned(workspace, 256) || ws_bytes < gated_workspace(rows, k, n))
-      return bad("the workspace is null, not 256-byte aligned or smaller than ndvm_gated_workspace_bytes");
   }
   REFUSE(vector_in(dw_gate, dtype));
   REFUSE(vector_in(dw_up, dtype));
@@ -165,7 +171,16 @@ ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t r
   a.rows = rows; a.k = k; a.n = n; a.x = x; a.x_stride = x_stride; a.w_gate = w_gate; a.w_up = w_up;
   a.g_stride = g_stride; a.u_stride = u_stride; a.act = act; a.dh = dh; a.dh_stride = dh_stride; a.dx = dx;
   a.dx_stride = dx_stride; a.dw_gate = dw_gate; a.dw_up = dw_up; a.workspace = workspace;
+  REFUSE(gated_room(a, true, workspace, ws_bytes));
   return done(launch_gated_backward(a, dtype, (cudaStream_t)stream), "gated projection launch");
+}
+
+ndvm_status ndvm_check_operators(void) {
+  int flag = 0;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = gated_stopped(&flag);
+  if (e != cudaSuccess) return done(e, "read flag");
+  return flag ? set_error(NDVM_E_DEVICE_CHECK, "a kernel of the gated projection gave up waiting for its operands") : NDVM_OK;
 }
 
 }  // extern "C"

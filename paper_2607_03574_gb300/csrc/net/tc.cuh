@@ -1,0 +1,117 @@
+// Tensor-core building blocks for sm_103a: tiles that the tensor memory accelerator (TMA) copies into shared
+// memory in the 128-byte swizzle, products of them that accumulate in tensor memory (tcgen05), and the
+// mbarriers between the two.  Every wait has a limit, after which the caller gives up.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace ndvm {
+namespace tc {
+
+__device__ __forceinline__ uint32_t smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+// Waits for the phase of `parity` to end; false once `*stop` is set, or after kWaitNs, which sets it: the
+// longest wait of a sound launch, for one tile's whole sum, is some milliseconds.
+constexpr uint64_t kWaitNs = 4000000000ull;
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
+  if (barrier_try(bar, parity)) return true;
+  const uint64_t start = now_ns();
+  while (!barrier_try(bar, parity)) {
+    if (*stop) return false;
+    if (now_ns() - start > kWaitNs) {
+      *stop = 1;
+      return false;
+    }
+  }
+  return true;
+}
+// the same for what is in flight when a launch gives up
+__device__ __forceinline__ void barrier_drain(uint32_t bar, uint32_t parity) {
+  const uint64_t start = now_ns();
+  while (!barrier_try(bar, parity) && now_ns() - start <= kWaitNs) {}
+}
+
+// a box of the tensor at (x, y) to shared memory; its bytes count on the barrier
+__device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+
+template <int kColumns>
+__device__ __forceinline__ void tmem_alloc(uint32_t to) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "n"(kColumns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+template <int kColumns>
+__device__ __forceinline__ void tmem_free(uint32_t addr) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "n"(kColumns));
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// D (+)= A B^T for 16 of the contraction: 16-bit operands in shared memory, binary32 sums in tensor memory
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+      ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+}
+// arrives on the barrier when the products issued so far are done
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// 32 columns of this thread's lane of tensor memory
+__device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t addr) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+#pragma unroll
+  for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Shared-memory descriptor of an operand in the 128-byte swizzle.  Contraction contiguous: a line of 128
+// bytes is 64 of the contraction, groups of 8 lines (rows or columns of the product) are 1024 bytes apart.
+// Rows contiguous: a line is 64 rows, groups of 8 lines (of the contraction) are 1024 bytes apart, the next
+// 64 rows start 8192 bytes on.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, bool rows_contiguous) {
+  const uint64_t leading = rows_contiguous ? 8192 >> 4 : 1, stride = 1024 >> 4;
+  return ((uint64_t)(addr >> 4) & 0x3fff) | leading << 16 | stride << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Instruction descriptor: binary32 sums, both operands half or both bfloat16, which of them have rows contiguous
+__host__ __device__ constexpr uint32_t instruction(bool bf16, bool a_rows, bool b_rows, int m, int n) {
+  return 1u << 4 | (uint32_t)bf16 << 7 | (uint32_t)bf16 << 10 | (uint32_t)a_rows << 15 | (uint32_t)b_rows << 16 |
+         (uint32_t)(n / 8) << 17 | (uint32_t)(m / 16) << 24;
+}
+
+}  // namespace tc
+}  // namespace ndvm

@@ -220,12 +220,9 @@ def _gated_shapes(x, w_gate, w_up):
     return rows, k, w_gate.shape[0], xs, _rows(w_gate, "w_gate")[2], _rows(w_up, "w_up")[2]
 
 
-def _all16(*pairs):
-    """Whether every (address, row stride in bytes) is a multiple of 16."""
-    bits = 0
-    for p, s in pairs:
-        bits |= p | s
-    return int(bits % 16 == 0)
+def _aligned(px, xs, pg, gs, pu, us):
+    """Whether the products can read every operand where it lies (addresses, row strides in elements)."""
+    return int((px | pg | pu) % 16 == 0 and (xs | gs | us) % 8 == 0 and xs != 0 and gs != 0 and us != 0)
 
 
 def gated_forward(x, w_gate, w_up, activation="silu", h=None, workspace=None, stream=None):
@@ -243,7 +240,7 @@ def gated_forward(x, w_gate, w_up, activation="silu", h=None, workspace=None, st
             h = torch.empty(shape, dtype=x.dtype, device=x.device)
     _like(h, "h", shape, x.dtype)
     px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
-    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 0, _all16((px, 2 * xs), (pg, 2 * gs), (pu, 2 * us)))
+    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 0, _aligned(px, xs, pg, gs, pu, us))
     ws, wp, nbytes = _workspace(workspace, need, x.device, stream)
     _check(lib.ndvm_gated_forward(code, act, rows, k, n, px, xs, pg, gs, pu, us, h.data_ptr(), _rows(h, "h")[2], wp, nbytes,
                                   _stream_ptr(stream)))
@@ -275,7 +272,7 @@ def gated_backward(dh, x, w_gate, w_up, activation="silu", wants=(True, True, Tr
             if not t.is_contiguous():
                 raise NdvmError(1, f"{name} must be contiguous")
     px, pg, pu, ph, hs = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), dh.data_ptr(), _rows(dh, "dh")[2]
-    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 1, _all16((px, 2 * xs), (pg, 2 * gs), (pu, 2 * us), (ph, 2 * hs)))
+    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 1, _aligned(px, xs, pg, gs, pu, us))
     ws, wp, nbytes = _workspace(workspace, need, x.device, stream)
     _check(lib.ndvm_gated_backward(code, act, rows, k, n, ph, hs, px, xs, pg, gs, pu, us,
                                    None if dx is None else dx.data_ptr(), 0 if dx is None else _rows(dx, "dx")[2],
@@ -373,3 +370,8 @@ def gated(x, w_gate, w_up, activation="silu"):
     if not _recorded(x, w_gate, w_up):
         return gated_forward(x, w_gate, w_up, activation)
     return (_ops or _make_ops())[2].apply(x, w_gate, w_up, activation)
+
+
+def check_operators():
+    """Synchronize and raise if a kernel of the operators gave up waiting since the last check."""
+    _check(load().ndvm_check_operators())
