@@ -46,35 +46,40 @@ __host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == k
 
 template <int kN> constexpr int kStageBytes = (kM + kN) * kC * 2;
 template <int kN> constexpr int kStages = 196608 / kStageBytes<kN> < 8 ? 196608 / kStageBytes<kN> : 8;
-template <int kN> constexpr int kSmem = kStages<kN> * kStageBytes<kN> + 1024 /* alignment */ + 256 /* barriers */;
+constexpr int kStaging = 8192;  // of each warp that reads sums: what its stores are made from
+template <int kN> constexpr int kSmem = kStages<kN> * kStageBytes<kN> + 4 * kStaging + 1024 /* alignment */ + 256 /* barriers */;
 
 struct ProductArgs {
   CUtensorMap a[2], b[2];
+  CUtensorMap o[2];              // the results (kGradient: dG and dU), or o[0] the split sums
   int m, n, c;                   // rows and columns of the result, contraction of one segment
   int tiles_m, tiles_n, matrices;  // matrices: results of one shape, by the a's (kWeight: 1 or 2), else 1
   int steps, splits;             // contraction steps of a result, and how many parts they are cut into
   int act;
+  int a_box;                     // rows of A that a tile loads (fewer than 128 where the result has fewer)
+  int copies;                    // results are stored by copies (their rows start on 16 bytes)
   void* out[2]; int64_t stride;  // kWeight: both matrices'; kGradient: dG and dU; else out[0]
   const void* dh; int64_t dh_stride;
-  float* partial;                // splits > 1: [split][matrix][m][n]
+  float* partial; int64_t partial_pitch;  // splits > 1: [split][matrix][m][pitch]
 };
 
-// 32 values to 32 elements of a row: 16 bytes a store where the row allows, else one by one
+// 32 values of a row to the staging buffer, in the 64-byte swizzle (a line of 64 bytes a row: the 16-byte
+// pieces of two lines that share banks are spread over all of them)
 template <typename T>
-__device__ __forceinline__ void store_row32(T* p, const float (&v)[32], int count, bool vectors) {
-  if (vectors && count >= 32) {
+__device__ __forceinline__ void stage_row(uint32_t buffer, int lane, const float (&v)[32]) {
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
-      Pack<T, 8> o;
+  for (int q = 0; q < 4; q++) {
+    union { uint4 u; T t[8]; } o;
 #pragma unroll
-      for (int e = 0; e < 8; e++) o.v[e] = from_f32<T>(v[q * 8 + e]);
-      store_pack(p + q * 8, o);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; e++)
-      if (e < count) p[e] = from_f32<T>(v[e]);
+    for (int e = 0; e < 8; e++) o.t[e] = from_f32<T>(v[q * 8 + e]);
+    tc::store16(buffer + lane * 64 + ((q ^ (lane >> 1 & 3)) << 4), o.u);
   }
+}
+// the buffer's rows to rows that start anywhere, a row at a time
+template <typename T>
+__device__ __forceinline__ void unstage(const char* buffer, int lane, T* out, int64_t stride, int rows, int cols) {
+  for (int r = 0; r < rows; r++)
+    if (lane < cols) out[r * stride + lane] = *reinterpret_cast<const T*>(buffer + r * 64 + ((lane / 8 ^ (r >> 1 & 3)) << 4) + lane % 8 * 2);
 }
 
 template <typename T, Mode kMode, int kN>
@@ -87,7 +92,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   __shared__ uint32_t s_tmem;
   __shared__ int s_stop;
   const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
-  const uint32_t bars = base + S * kStageBytes<kN>;
+  const uint32_t staging = base + S * kStageBytes<kN>, bars = staging + 4 * kStaging;
   const auto full = [&](int i) { return bars + i * 8; };
   const auto empty = [&](int i) { return bars + (S + i) * 8; };
   const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
@@ -139,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
       for (int s = it.from; s < it.to; s++) {
         if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, stop))) break;
         const uint32_t a = base + stage * kStageBytes<kN>, b = a + kABytes, bar = full(stage);
-        tc::barrier_expect(bar, kStageBytes<kN>);
+        tc::barrier_expect(bar, a_rows(kMode) ? kStageBytes<kN> : kStageBytes<kN> - kABytes + p.a_box * kC * 2);
         const int seg = kMode == kInput ? s / segment : kMode == kWeight ? it.matrix : 0;
         const int c = (kMode == kInput ? s - seg * segment : s) * kC;
         if (a_rows(kMode)) {
@@ -192,85 +197,95 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
       tc::barrier_drain(drain, 0);
     }
   } else if (warp >= 2) {
-    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own
+    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, 32 columns at a
+    // time, by way of two staging buffers that asynchronous copies empty
     const int lanes = (warp % 4) * 32;
-    int slot = 0;
+    const uint32_t mine = staging + (warp - 2) * kStaging;
+    const char* const mine_ptr = raw + (mine - tc::smem(raw));
+    constexpr int kBuffer = kStaging / 2;
+    int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
-    const bool vec_out = reinterpret_cast<uintptr_t>(p.out[0]) % 16 == 0 && reinterpret_cast<uintptr_t>(p.out[1]) % 16 == 0 &&
-                         p.stride % 8 == 0;
     const bool vec_dh = kMode == kGradient && reinterpret_cast<uintptr_t>(p.dh) % 16 == 0 && p.dh_stride % 8 == 0;
     for (int i = blockIdx.x; i < items; i += gridDim.x) {
       const Item it = item(i);
-      const int row = it.m0 + lanes + lane;
+      const int row0 = it.m0 + lanes, row = row0 + lane;
+      Pack<T, 8> dh[kMode == kGradient ? kOutN / 8 : 1];
+      if (kMode == kGradient && row < p.m) {  // asked for before the wait for the sums
+        const T* from = static_cast<const T*>(p.dh) + row * p.dh_stride + it.n0;
+        const int count = p.n - it.n0;
+#pragma unroll
+        for (int q = 0; q < kOutN / 8; q++) {
+          if (vec_dh && q * 8 + 8 <= count) {
+            dh[q] = load_pack<T, 8>(from + q * 8);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) dh[q].v[e] = q * 8 + e < count ? from[q * 8 + e] : from_f32<T>(0.0f);
+          }
+        }
+      }
       // (the whole warp goes on or gives up: reading tensor memory is a warp's instruction)
       if (!__all_sync(~0u, tc::barrier_wait(done(slot), slot_phase, stop))) break;
       tc::fence_after();
       const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
-#pragma unroll 1
+#pragma unroll (kMode == kGradient ? kOutN / 32 : 1)
       for (int j = 0; j < kOutN; j += 32) {
         const int col = it.n0 + j, count = min(32, p.n - col);
         if (count <= 0) break;
-        float v[32];
+        float v[32], u[32];
         tc::tmem_load32(v, at + j);
+        if (dual(kMode)) tc::tmem_load32(u, at + kN / 2 + j);
+        tc::tmem_loaded();
         if (dual(kMode)) {
-          float u[32];
-          tc::tmem_load32(u, at + kN / 2 + j);
-          if (kMode == kForward) {
-            tc::tmem_loaded();
-            if (row < p.m) {
 #pragma unroll
-              for (int e = 0; e < 32; e++) {
-                float a, da;
-                activate(p.act, v[e], &a, &da);
-                v[e] = a * u[e];
-              }
-              store_row32(static_cast<T*>(p.out[0]) + row * p.stride + col, v, count, vec_out);
-            }
-          } else {
-            Pack<T, 8> d[4];
-            if (row < p.m) {
-              const T* dh = static_cast<const T*>(p.dh) + row * p.dh_stride + col;
-              if (vec_dh && count == 32) {
-#pragma unroll
-                for (int q = 0; q < 4; q++) d[q] = load_pack<T, 8>(dh + q * 8);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 32; e++) d[e / 8].v[e % 8] = e < count ? dh[e] : from_f32<T>(0.0f);
-              }
-            }
-            tc::tmem_loaded();
-            if (row < p.m) {
-#pragma unroll
-              for (int e = 0; e < 32; e++) {
-                float a, da;
-                activate(p.act, v[e], &a, &da);
-                const float f = to_f32(d[e / 8].v[e % 8]);
-                v[e] = f * u[e] * da;
-                u[e] = f * a;
-              }
-              store_row32(static_cast<T*>(p.out[0]) + row * p.stride + col, v, count, vec_out);
-              store_row32(static_cast<T*>(p.out[1]) + row * p.stride + col, u, count, vec_out);
-            }
-          }
-        } else {
-          tc::tmem_loaded();
-          if (row < p.m) {
-            if (p.splits > 1) {
-              float* o = p.partial + (((int64_t)it.split * p.matrices + it.matrix) * p.m + row) * p.n + col;
-#pragma unroll
-              for (int e = 0; e < 32; e++)
-                if (e < count) o[e] = v[e];
+          for (int e = 0; e < 32; e++) {
+            float a, da;
+            activate(p.act, v[e], &a, &da);
+            if (kMode == kForward) {
+              v[e] = a * u[e];
             } else {
-              store_row32(static_cast<T*>(p.out[it.matrix]) + row * p.stride + col, v, count, vec_out);
+              const float d = to_f32(dh[(j + e) / 8].v[e % 8]);
+              v[e] = d * u[e] * da;
+              u[e] = d * a;
             }
           }
         }
+        const uint32_t to = mine + buffer * kBuffer;
+        if (lane == 0) tc::stores_read<1>();  // the buffer's last stores have left it
+        __syncwarp();
+        if (!dual(kMode) && p.splits > 1) {
+#pragma unroll
+          for (int q = 0; q < 8; q++)  // binary32: a line of 128 bytes a row, in the 128-byte swizzle
+            tc::store16(to + lane * 128 + ((q ^ (lane & 7)) << 4),
+                        make_uint4(__float_as_uint(v[q * 4]), __float_as_uint(v[q * 4 + 1]), __float_as_uint(v[q * 4 + 2]),
+                                   __float_as_uint(v[q * 4 + 3])));
+          tc::fence_async();
+          __syncwarp();
+          if (lane == 0 && row0 < p.m) tc::store_box(&p.o[0], col, row0, it.split * p.matrices + it.matrix, to);
+        } else {
+          stage_row<T>(to, lane, v);
+          if (kMode == kGradient) stage_row<T>(to + 2048, lane, u);
+          if (p.copies) {
+            tc::fence_async();
+            __syncwarp();
+            if (lane == 0 && row0 < p.m) {
+              tc::store_box(&p.o[kMode == kWeight ? it.matrix : 0], col, row0, to);
+              if (kMode == kGradient) tc::store_box(&p.o[1], col, row0, to + 2048);
+            }
+          } else {
+            __syncwarp();
+            T* out = static_cast<T*>(p.out[kMode == kWeight ? it.matrix : 0]) + row0 * p.stride + col;
+            unstage<T>(mine_ptr + buffer * kBuffer, lane, out, p.stride, min(32, p.m - row0), count);
+          }
+        }
+        if (lane == 0) tc::stores_commit();
+        buffer ^= 1;
       }
       tc::fence_before();
       __syncwarp();
       if (lane == 0) tc::barrier_arrive(taken(slot));
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
+    if (lane == 0) tc::stores_done();
   }
   __syncwarp();
   __syncthreads();
@@ -279,16 +294,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   if (warp == 1) tc::tmem_free<kColumns>(tmem);
 }
 
-// the parts of split sums added up in order, and rounded
+// the parts of split sums added up in order, and rounded: 4 columns a thread
 template <typename T>
-__global__ void __launch_bounds__(256) k_join(const float* partial, int splits, int matrices, int64_t m, int64_t n, T* out0,
-                                              T* out1, int64_t stride) {
-  const int64_t total = matrices * m * n;
+__global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitch, int splits, int matrices, int64_t m, int64_t n,
+                                              T* out0, T* out1, int64_t stride) {
+  const int64_t quads = pitch / 4, total = matrices * m * quads;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    float s = 0.0f;
-    for (int k = 0; k < splits; k++) s += partial[k * total + i];
-    const int64_t row = i / n, r = row % m;
-    (row >= m ? out1 : out0)[r * stride + (i - row * n)] = from_f32<T>(s);
+    const float* p = partial + i * 4;
+    float4 s = *reinterpret_cast<const float4*>(p);
+#pragma unroll 4
+    for (int k = 1; k < splits; k++) {
+      const float4 v = *reinterpret_cast<const float4*>(p + k * total * 4);
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    const int64_t row = i / quads, c = (i - row * quads) * 4;
+    T* out = row >= m ? out1 + (row - m) * stride + c : out0 + row * stride + c;
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+      if (c + e < n) out[e] = from_f32<T>(v[e]);
   }
 }
 
@@ -303,7 +327,7 @@ __global__ void __launch_bounds__(256) k_pack(const T* from, int64_t stride, int
 // --------------------------------------------------------------------------- few rows: vectors
 // Up to 8 rows: the weights are read once and are nearly all the traffic, so a warp takes one row of each
 // weight, 16 bytes a lane and load, against every row of x (from L1), sums in registers.
-constexpr int kFewRows = 8;
+constexpr int kFewRows = 1;
 
 template <typename T, int R, int V, bool kBackward>
 __global__ void __launch_bounds__(256) k_few(GatedArgs a, T* dg, T* du, int64_t pitch) {
@@ -391,23 +415,40 @@ Encode encoder() {
   return e;
 }
 
-// a matrix of `rows` rows of `cols` contiguous elements, read in boxes of 64 columns and `box` rows
+// A matrix of `rows` rows of `cols` contiguous elements, read in boxes of 64 columns and `box` rows in the
+// 128-byte swizzle; or written in boxes of 32 by 32 (of 64 bytes a row: the 64-byte swizzle).
 template <typename T>
-bool map_matrix(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box) {
+bool map_matrix(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box, bool written = false) {
   if (!encoder()) return false;
   if (rows == 1) stride = up(cols, 8);  // (never taken)
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, ones[2] = {1, 1};
+  const cuuint32_t boxes[2] = {written ? 32u : 64u, (cuuint32_t)box}, ones[2] = {1, 1};
   const CUtensorMapDataType type = std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   return encoder()(map, type, 2, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   written ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// split sums: `parts` matrices of m rows, written in boxes of 32 by 32
+bool map_partial(CUtensorMap* map, float* p, int64_t parts, int64_t m, int64_t n, int64_t pitch) {
+  if (!encoder()) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)n, (cuuint64_t)m, (cuuint64_t)parts};
+  const cuuint64_t strides[2] = {(cuuint64_t)pitch * 4, (cuuint64_t)(pitch * m) * 4};
+  const cuuint32_t boxes[3] = {32, 32, 1}, ones[3] = {1, 1, 1};
+  return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, p, dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns of a tile's sums: 256 (the fewest bytes an operation), or fewer where that would leave SMs idle.
+// Columns of a tile's sums.  A round of tiles over the SMs takes about as long as its columns, narrower ones a
+// little longer (more bytes an operation: measured TODO).
 int tile_width(int64_t m, int64_t n, bool two) {
-  for (int w : {256, 128})
-    if (ceil_div(m, kM) * ceil_div(n, two ? w / 2 : w) >= kSms) return w;
-  return 64;
+  int best = 256;
+  double least = 1e300;
+  for (int w : {256, 128, 64}) {
+    const double rounds = (double)ceil_div(ceil_div(m, kM) * ceil_div(n, two ? w / 2 : w), kSms);
+    const double cost = rounds * (w == 256 ? 1.0 : w == 128 ? 0.6 : 0.4);
+    if (cost < least) least = cost, best = w;
+  }
+  return best;
 }
 // Parts that a result's contraction is cut into: enough for every SM to have one, none shorter than 8 steps.
 int split_count(int64_t tiles, int64_t steps) {
@@ -424,6 +465,8 @@ cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
   k_product<T, kMode, kN><<<std::min(items, kSms), kThreads, kSmem<kN>, s>>>(p);
   return cudaGetLastError();
 }
+
+int a_box(int64_t m) { return (int)std::min<int64_t>(up(m, 8), kM); }
 
 // how a product of the given size is cut up (the weights' gradients as if both were wanted: one of them
 // alone has the same bits)
@@ -444,14 +487,26 @@ cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s) {
   p.tiles_n = (int)ceil_div(p.n, out);
   p.steps = (int)ceil_div(p.c, kC) * (kMode == kInput ? 2 : 1);
   p.splits = k.splits;
+  p.a_box = a_rows(kMode) ? kM : a_box(p.m);
+  p.copies = 1;
+  if (p.splits > 1) {
+    p.partial_pitch = up(p.n, 4);
+    if (!map_partial(&p.o[0], p.partial, (int64_t)p.splits * p.matrices, p.m, p.n, p.partial_pitch)) return cudaErrorInvalidValue;
+  } else {
+    for (int w = 0; w < 2; w++) {
+      if (!p.out[w]) continue;
+      p.copies &= tma_ready(p.out[w], p.stride, p.m, p.n);
+      if (p.copies && !map_matrix<T>(&p.o[w], p.out[w], p.m, p.n, p.stride, 32, true)) return cudaErrorInvalidValue;
+    }
+  }
   if ((int64_t)p.tiles_m * p.tiles_n * p.matrices * p.splits > 0x40000000) return cudaErrorInvalidConfiguration;
   const cudaError_t e = k.width == 256   ? launch_width<T, kMode, 256>(p, s)
                         : k.width == 128 ? launch_width<T, kMode, 128>(p, s)
                                          : launch_width<T, kMode, 64>(p, s);
   if (e != cudaSuccess || p.splits == 1) return e;
-  const int64_t total = (int64_t)p.matrices * p.m * p.n;
+  const int64_t total = (int64_t)p.matrices * p.m * p.partial_pitch / 4;
   k_join<T><<<(unsigned)std::min<int64_t>(ceil_div(total, 256), kSms * 8), 256, 0, s>>>(
-      p.partial, p.splits, p.matrices, p.m, p.n, static_cast<T*>(p.out[0]), static_cast<T*>(p.out[1]), p.stride);
+      p.partial, p.partial_pitch, p.splits, p.matrices, p.m, p.n, static_cast<T*>(p.out[0]), static_cast<T*>(p.out[1]), p.stride);
   return cudaGetLastError();
 }
 
@@ -476,8 +531,8 @@ struct Layout {
     int64_t parts = 0;
     if (backward && rows > 0) {
       const Cut i = cut(kInput, rows, k, n), w = cut(kWeight, n, k, rows);
-      if (i.splits > 1) parts = i.splits * rows * k;
-      if (w.splits > 1) parts = std::max(parts, 2 * w.splits * n * k);
+      if (i.splits > 1) parts = i.splits * rows * ndvm::up(k, 4);
+      if (w.splits > 1) parts = std::max(parts, 2 * w.splits * n * ndvm::up(k, 4));
     }
     partial = take(parts * 4);
   }
@@ -510,7 +565,7 @@ template <typename T, Mode kMode>
 cudaError_t products(const GatedArgs& a, void* out0, void* out1, int64_t stride, cudaStream_t s) {
   const Cut k = cut(kMode, a.rows, a.n, a.k);
   ProductArgs p{};
-  if (!map_matrix<T>(&p.a[0], a.x, a.rows, a.k, a.x_stride, kM) || !map_matrix<T>(&p.b[0], a.w_gate, a.n, a.k, a.g_stride, k.width / 2) ||
+  if (!map_matrix<T>(&p.a[0], a.x, a.rows, a.k, a.x_stride, a_box(a.rows)) || !map_matrix<T>(&p.b[0], a.w_gate, a.n, a.k, a.g_stride, k.width / 2) ||
       !map_matrix<T>(&p.b[1], a.w_up, a.n, a.k, a.u_stride, k.width / 2))
     return cudaErrorInvalidValue;
   p.m = (int)a.rows; p.n = (int)a.n; p.c = (int)a.k;
@@ -557,7 +612,8 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
   p.partial = reinterpret_cast<float*>(ws + l.partial);
   if (a.dx) {
     const Cut k = cut(kInput, a.rows, a.k, a.n);
-    if (!map_matrix<T>(&p.a[0], dg, a.rows, a.n, l.n_pitch, kM) || !map_matrix<T>(&p.a[1], du, a.rows, a.n, l.n_pitch, kM) ||
+    const int box = a_box(a.rows);
+    if (!map_matrix<T>(&p.a[0], dg, a.rows, a.n, l.n_pitch, box) || !map_matrix<T>(&p.a[1], du, a.rows, a.n, l.n_pitch, box) ||
         !map_matrix<T>(&p.b[0], a.w_gate, a.n, a.k, a.g_stride, 64) || !map_matrix<T>(&p.b[1], a.w_up, a.n, a.k, a.u_stride, 64))
       return cudaErrorInvalidValue;
     p.m = (int)a.rows; p.n = (int)a.k; p.c = (int)a.n; p.matrices = 1;
