@@ -19,26 +19,36 @@ namespace {
 
 __device__ int g_stopped;  // a wait in k_product ran out (ndvm_check_operators)
 
-__device__ __forceinline__ void activate(int act, float g, float* a, float* da) {
-  if (act == NDVM_ACT_RELU) {
+template <int kAct>
+__device__ __forceinline__ void activate(float g, float* a, float* da) {
+  if constexpr (kAct == NDVM_ACT_RELU) {
     *a = g > 0.0f ? g : (g != g ? g : 0.0f);
     *da = g > 0.0f ? 1.0f : 0.0f;
-  } else if (act == NDVM_ACT_GELU) {
+  } else if constexpr (kAct == NDVM_ACT_GELU) {
     const float cdf = 0.5f * (1.0f + erff(g * 0.70710678f));
     *a = g * cdf;
     *da = cdf + g * __expf(-0.5f * g * g) * 0.39894228f;
   } else {
     const float s = __fdividef(1.0f, 1.0f + __expf(-g));
-    *a = act == NDVM_ACT_SILU ? g * s : s;
-    *da = act == NDVM_ACT_SILU ? s * (1.0f + g * (1.0f - s)) : s * (1.0f - s);
+    *a = kAct == NDVM_ACT_SILU ? g * s : s;
+    *da = kAct == NDVM_ACT_SILU ? s * (1.0f + g * (1.0f - s)) : s * (1.0f - s);
   }
+}
+// f(activation as a constant): one branch around a loop over many elements, not one in each
+template <typename F>
+__device__ __forceinline__ void by_activation(int act, F&& f) {
+  if (act == NDVM_ACT_SILU) f(std::integral_constant<int, NDVM_ACT_SILU>());
+  else if (act == NDVM_ACT_GELU) f(std::integral_constant<int, NDVM_ACT_GELU>());
+  else if (act == NDVM_ACT_RELU) f(std::integral_constant<int, NDVM_ACT_RELU>());
+  else f(std::integral_constant<int, NDVM_ACT_SIGMOID>());
 }
 
 // ------------------------------------------------------------------ products on the tensor cores
 enum Mode { kForward, kGradient, kInput, kWeight };
 
 constexpr int kM = 128, kC = 64;  // rows of a tile, contraction of a step (128 bytes)
-constexpr int kThreads = 192;     // a warp that loads, one that multiplies, four that read the sums
+constexpr int kReaders = 8;       // warps that read the sums: two for each quarter of a tile's rows
+constexpr int kThreads = 64 + 32 * kReaders;  // and one that loads, one that multiplies
 
 __host__ __device__ constexpr bool a_rows(Mode m) { return m == kWeight; }
 __host__ __device__ constexpr bool b_rows(Mode m) { return m == kInput || m == kWeight; }
@@ -46,8 +56,8 @@ __host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == k
 
 template <int kN> constexpr int kStageBytes = (kM + kN) * kC * 2;
 template <int kN> constexpr int kStages = 196608 / kStageBytes<kN> < 8 ? 196608 / kStageBytes<kN> : 8;
-constexpr int kStaging = 8192;  // of each warp that reads sums: what its stores are made from
-template <int kN> constexpr int kSmem = kStages<kN> * kStageBytes<kN> + 4 * kStaging + 1024 /* alignment */ + 256 /* barriers */;
+constexpr int kStaging = 4096;  // of each warp that reads sums: what its stores are made from
+template <int kN> constexpr int kSmem = kStages<kN> * kStageBytes<kN> + kReaders * kStaging + 1024 /* alignment */ + 256 /* barriers */;
 
 struct ProductArgs {
   CUtensorMap a[2], b[2];
@@ -92,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   __shared__ uint32_t s_tmem;
   __shared__ int s_stop;
   const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
-  const uint32_t staging = base + S * kStageBytes<kN>, bars = staging + 4 * kStaging;
+  const uint32_t staging = base + S * kStageBytes<kN>, bars = staging + kReaders * kStaging;
   const auto full = [&](int i) { return bars + i * 8; };
   const auto empty = [&](int i) { return bars + (S + i) * 8; };
   const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
@@ -104,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   if (threadIdx.x == 0) {
     s_stop = 0;
     for (int i = 0; i < S; i++) tc::barrier_init(full(i), 1), tc::barrier_init(empty(i), 1);
-    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), 4);
+    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), kReaders);
     tc::barrier_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -197,60 +207,76 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
       tc::barrier_drain(drain, 0);
     }
   } else if (warp >= 2) {
-    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, 32 columns at a
-    // time, by way of two staging buffers that asynchronous copies empty
+    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, every other 32
+    // columns, by way of staging that asynchronous copies empty.  (Two warps a scheduler: one alone left the
+    // latencies of the reads, the copies and dh in the open.  4096 rows, 1024 -> 4096: TODO)
     const int lanes = (warp % 4) * 32;
     const uint32_t mine = staging + (warp - 2) * kStaging;
     const char* const mine_ptr = raw + (mine - tc::smem(raw));
-    constexpr int kBuffer = kStaging / 2;
+    const int first = (warp - 2) / 4 * 32;
     int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
     const bool vec_dh = kMode == kGradient && reinterpret_cast<uintptr_t>(p.dh) % 16 == 0 && p.dh_stride % 8 == 0;
     for (int i = blockIdx.x; i < items; i += gridDim.x) {
       const Item it = item(i);
       const int row0 = it.m0 + lanes, row = row0 + lane;
-      Pack<T, 8> dh[kMode == kGradient ? kOutN / 8 : 1];
-      if (kMode == kGradient && row < p.m) {  // asked for before the wait for the sums
-        const T* from = static_cast<const T*>(p.dh) + row * p.dh_stride + it.n0;
-        const int count = p.n - it.n0;
+      Pack<T, 8> next[4];  // dh of the columns to come: asked for a piece ahead, the first before the wait for the sums
+      const auto fetch = [&](int j) {
+        if (kMode != kGradient || row >= p.m || j >= kOutN) return;
+        const T* from = static_cast<const T*>(p.dh) + row * p.dh_stride + it.n0 + j;
+        const int count = p.n - it.n0 - j;
 #pragma unroll
-        for (int q = 0; q < kOutN / 8; q++) {
+        for (int q = 0; q < 4; q++) {
           if (vec_dh && q * 8 + 8 <= count) {
-            dh[q] = load_pack<T, 8>(from + q * 8);
+            next[q] = load_pack<T, 8>(from + q * 8);
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) dh[q].v[e] = q * 8 + e < count ? from[q * 8 + e] : from_f32<T>(0.0f);
+            for (int e = 0; e < 8; e++) next[q].v[e] = q * 8 + e < count ? from[q * 8 + e] : from_f32<T>(0.0f);
           }
         }
-      }
+      };
+      fetch(first);
       // (the whole warp goes on or gives up: reading tensor memory is a warp's instruction)
       if (!__all_sync(~0u, tc::barrier_wait(done(slot), slot_phase, stop))) break;
       tc::fence_after();
       const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
-#pragma unroll (kMode == kGradient ? kOutN / 32 : 1)
-      for (int j = 0; j < kOutN; j += 32) {
+#pragma unroll 1
+      for (int j = first; j < kOutN; j += 64) {
         const int col = it.n0 + j, count = min(32, p.n - col);
         if (count <= 0) break;
         float v[32], u[32];
+        Pack<T, 8> dh[4];
         tc::tmem_load32(v, at + j);
         if (dual(kMode)) tc::tmem_load32(u, at + kN / 2 + j);
-        tc::tmem_loaded();
-        if (dual(kMode)) {
+        if (kMode == kGradient) {
 #pragma unroll
-          for (int e = 0; e < 32; e++) {
-            float a, da;
-            activate(p.act, v[e], &a, &da);
-            if (kMode == kForward) {
-              v[e] = a * u[e];
-            } else {
-              const float d = to_f32(dh[(j + e) / 8].v[e % 8]);
-              v[e] = d * u[e] * da;
-              u[e] = d * a;
-            }
-          }
+          for (int q = 0; q < 4; q++) dh[q] = next[q];
+          fetch(j + 64);
         }
-        const uint32_t to = mine + buffer * kBuffer;
-        if (lane == 0) tc::stores_read<1>();  // the buffer's last stores have left it
+        tc::tmem_loaded();
+        if (dual(kMode))
+          by_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 32; e++) {
+              float a, da;
+              activate<decltype(act)::value>(v[e], &a, &da);
+              if (kMode == kForward) {
+                v[e] = a * u[e];
+              } else {
+                const float d = to_f32(dh[e / 8].v[e % 8]);
+                v[e] = d * u[e] * da;
+                u[e] = d * a;
+              }
+            }
+          });
+        // 4096 bytes hold two pieces of one result (then the other's copy may still be under way), or one
+        // of dG and dU or of binary32 sums
+        const bool whole = kMode == kGradient || (!dual(kMode) && p.splits > 1);
+        const uint32_t to = mine + (whole ? 0 : buffer * 2048);
+        if (lane == 0) {
+          if (whole) tc::stores_read<0>();
+          else tc::stores_read<1>();
+        }
         __syncwarp();
         if (!dual(kMode) && p.splits > 1) {
 #pragma unroll
@@ -274,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           } else {
             __syncwarp();
             T* out = static_cast<T*>(p.out[kMode == kWeight ? it.matrix : 0]) + row0 * p.stride + col;
-            unstage<T>(mine_ptr + buffer * kBuffer, lane, out, p.stride, min(32, p.m - row0), count);
+            unstage<T>(mine_ptr + (to - mine), lane, out, p.stride, min(32, p.m - row0), count);
           }
         }
         if (lane == 0) tc::stores_commit();
@@ -365,7 +391,7 @@ __global__ void __launch_bounds__(256) k_few(GatedArgs a, T* dg, T* du, int64_t 
   for (int r = 0; r < R; r++) {
     if (lane != r || r >= a.rows) continue;
     float act, da;
-    activate(a.act, g[r], &act, &da);
+    by_activation(a.act, [&](auto k) { activate<decltype(k)::value>(g[r], &act, &da); });
     if (kBackward) {
       const float dh = to_f32(static_cast<const T*>(a.dh)[r * a.dh_stride + j]);
       dg[r * pitch + j] = from_f32<T>(dh * u[r] * da);
