@@ -16,17 +16,26 @@ from __future__ import annotations
 
 import ctypes
 
-from . import NdvmError, _check, _on_stream, _stream_ptr, _torch, load
+import paper_2607_03574_gb300 as _nd
+
+from . import NdvmError, _check, _on_stream, _torch, load
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 
+_torch_module = None
 _types = {}
 
 
+def _start():
+    """torch and the library, looked up once (the calls below are short beside an import's lookups)."""
+    global _torch_module
+    torch = _torch()
+    _types.update({torch.float32: 1, torch.float16: 2, torch.bfloat16: 3})
+    _torch_module = torch
+    return torch
+
+
 def _type(t, name):
-    if not _types:
-        torch = _torch()
-        _types.update({torch.float32: 1, torch.float16: 2, torch.bfloat16: 3})
     code = _types.get(t.dtype)
     if code is None:
         raise NdvmError(3, f"{name}: unsupported dtype {t.dtype}")
@@ -35,11 +44,13 @@ def _type(t, name):
 
 def _rows(t, name):
     """(rows, cols, row stride) of a tensor whose last dimension is contiguous."""
-    shape, dim = t.shape, t.dim()
-    if dim == 0:
+    shape = t.shape
+    if not shape:
         raise NdvmError(1, f"{name} must have at least one dimension")
     cols = shape[-1]
     if t.is_contiguous():
+        if len(shape) == 2:
+            return shape[0], cols, cols
         rows = 1
         for n in shape[:-1]:
             rows *= n
@@ -61,79 +72,105 @@ def _rows(t, name):
     return rows, cols, step
 
 
-def _on_device(x, named):
-    """Every tensor on x's device, which is the current one (the kernels launch there)."""
-    if not x.is_cuda:
+def _device(torch, x):
+    """The index of x's device, which has to be the current one (the kernels launch there)."""
+    device = x.get_device()
+    if device < 0:
         raise NdvmError(1, "x must be a CUDA tensor (the network operators have no CPU path)")
-    device = x.device
-    if device.index != _torch().cuda.current_device():
-        raise NdvmError(1, f"x is on {device}, which is not the current device")
-    for name, t in named:
-        if t is not None and t.device != device:
-            raise NdvmError(1, f"{name} is on {t.device}, x on {device}")
+    if device != torch._C._cuda_getDevice():
+        raise NdvmError(1, f"x is on cuda:{device}, which is not the current device")
+    return device
 
 
-def _like(t, name, shape, dtype):
+def _same_device(device, t, name):
+    if t.get_device() != device:
+        raise NdvmError(1, f"{name} is on {t.device}, x on cuda:{device}")
+
+
+def _stream(torch, stream, device):
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+def _given(t, name, shape, dtype, device):
+    """Checks an output (or a tensor of a known shape) that the caller gave."""
     if t.shape != shape or t.dtype != dtype:
         raise NdvmError(1, f"{name} must have shape {tuple(shape)} and dtype {dtype}")
+    _same_device(device, t, name)
 
 
-def _vector(t, name, cols):
+def _vector(t, name, cols, device):
+    """The address of a vector of `cols` elements, or None."""
     if t is None:
         return None
-    if t.dim() != 1 or t.shape[0] != cols or not t.is_contiguous():
+    if t.shape != (cols,) or not t.is_contiguous():
         raise NdvmError(1, f"{name} must be a contiguous vector of {cols} elements")
+    _same_device(device, t, name)
     return t.data_ptr()
 
 
-def _weight_type(x_type, weight, bias):
-    ref = weight if weight is not None else bias
-    if ref is None:
-        return x_type
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise NdvmError(1, "weight and bias must have the same dtype")
-    return _type(ref, "weight")
+def _stats(stats, rows, device):
+    _given(stats, "stats", (2, rows), _torch_module.float32, device)
+    if not stats.is_contiguous():
+        raise NdvmError(1, "stats must be contiguous")
+    return stats.data_ptr()
 
 
-def _workspace(given, nbytes, device, stream):
+def _new(torch, shape, dtype, device, stream):
+    """An uninitialised tensor that belongs to `stream` (torch's allocator; None: the current one)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on_stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(torch, given, nbytes, device, stream):
     """(tensor, its address, its bytes): the caller's workspace or one that belongs to `stream`."""
     if given is not None:
-        if not given.is_cuda or given.device != device or not given.is_contiguous():
-            raise NdvmError(1, f"workspace must be a contiguous tensor on {device}")
+        _same_device(device, given, "workspace")
+        if not given.is_contiguous():
+            raise NdvmError(1, "workspace must be contiguous")
         return given, given.data_ptr(), given.numel() * given.element_size()
     if not nbytes:
         return None, None, 0
-    torch = _torch()
-    with _on_stream(stream):
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    ws = _new(torch, nbytes, torch.uint8, device, stream)
     return ws, ws.data_ptr(), nbytes
 
 
 # ------------------------------------------------------------------------------- layer norm
+def _weight_type(x_code, weight, bias):
+    if weight is None:
+        return x_code if bias is None else _type(bias, "bias")
+    if bias is not None and weight.dtype != bias.dtype:
+        raise NdvmError(1, "weight and bias must have the same dtype")
+    return _type(weight, "weight")
+
+
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, y=None, stats=None, want_stats=True, stream=None):
     """(y, stats): layer norm over the last dimension.  weight and bias: vectors of x's type or float32.
     stats: float32 [2, rows], means and reciprocal deviations for the backward pass (None with
     want_stats=False).  Outputs this call allocates belong to `stream`."""
-    torch = _torch()
-    lib = load()
-    _on_device(x, (("weight", weight), ("bias", bias), ("y", y), ("stats", stats)))
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
     code = _type(x, "x")
-    wcode = _weight_type(code, weight, bias)
     rows, cols, xs = _rows(x, "x")
-    if y is None or (stats is None and want_stats):
-        with _on_stream(stream):
-            if y is None:
-                y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            if stats is None and want_stats:
-                stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    _like(y, "y", x.shape, x.dtype)
+    if y is None:
+        y, ys = _new(torch, x.shape, x.dtype, device, stream), cols
+    else:
+        _given(y, "y", x.shape, x.dtype, device)
+        ys = _rows(y, "y")[2]
     if stats is not None:
-        _like(stats, "stats", (2, rows), torch.float32)
-        if not stats.is_contiguous():
-            raise NdvmError(1, "stats must be contiguous")
-    _check(lib.ndvm_layer_norm_forward(code, wcode, rows, cols, x.data_ptr(), xs, _vector(weight, "weight", cols),
-                                       _vector(bias, "bias", cols), eps, y.data_ptr(), _rows(y, "y")[2],
-                                       None if stats is None else stats.data_ptr(), _stream_ptr(stream)))
+        sp = _stats(stats, rows, device)
+    elif want_stats:
+        stats = _new(torch, (2, rows), torch.float32, device, stream)
+        sp = stats.data_ptr()
+    else:
+        sp = None
+    status = lib.ndvm_layer_norm_forward(code, _weight_type(code, weight, bias), rows, cols, x.data_ptr(), xs,
+                                         _vector(weight, "weight", cols, device), _vector(bias, "bias", cols, device), eps,
+                                         y.data_ptr(), ys, sp, _stream(torch, stream, device))
+    if status:
+        _check(status)
     return y, stats
 
 
@@ -141,36 +178,41 @@ def layer_norm_backward(dy, x, weight, stats, wants=(True, True, True), dx=None,
                         wtype=None, workspace=None, stream=None):
     """(dx, dweight, dbias) of layer_norm_forward; `wants` says which (the others are None).  dweight and
     dbias have weight's type (`wtype` where there is no weight; x's by default)."""
-    torch = _torch()
-    lib = load()
-    _on_device(x, (("dy", dy), ("weight", weight), ("stats", stats), ("dx", dx), ("dweight", dweight), ("dbias", dbias)))
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
     code = _type(x, "x")
     rows, cols, xs = _rows(x, "x")
-    _like(dy, "dy", x.shape, x.dtype)
-    _like(stats, "stats", (2, rows), torch.float32)
-    if not stats.is_contiguous():
-        raise NdvmError(1, "stats must be contiguous")
+    _given(dy, "dy", x.shape, x.dtype, device)
+    sp = _stats(stats, rows, device)
     wdtype = weight.dtype if weight is not None else (wtype or x.dtype)
-    with _on_stream(stream):
-        if dx is None and wants[0]:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if dweight is None and wants[1]:
-            dweight = torch.empty(cols, dtype=wdtype, device=x.device)
-        if dbias is None and wants[2]:
-            dbias = torch.empty(cols, dtype=wdtype, device=x.device)
+    xp = dxs = dwp = dbp = None
     if dx is not None:
-        _like(dx, "dx", x.shape, x.dtype)
-    for name, t in (("dweight", dweight), ("dbias", dbias)):
-        if t is not None:
-            _like(t, name, (cols,), wdtype)
-    need = lib.ndvm_layer_norm_workspace_bytes(rows, cols) if dweight is not None or dbias is not None else 0
-    ws, wp, nbytes = _workspace(workspace, need, x.device, stream)
-    wcode = _weight_type(code, dweight if weight is None else weight, dbias)
-    _check(lib.ndvm_layer_norm_backward(code, wcode, rows, cols, dy.data_ptr(), _rows(dy, "dy")[2], x.data_ptr(), xs,
-                                        _vector(weight, "weight", cols), stats.data_ptr(),
-                                        None if dx is None else dx.data_ptr(), 0 if dx is None else _rows(dx, "dx")[2],
-                                        _vector(dweight, "dweight", cols), _vector(dbias, "dbias", cols), wp, nbytes,
-                                        _stream_ptr(stream)))
+        _given(dx, "dx", x.shape, x.dtype, device)
+        xp, dxs = dx.data_ptr(), _rows(dx, "dx")[2]
+    elif wants[0]:
+        dx = _new(torch, x.shape, x.dtype, device, stream)
+        xp, dxs = dx.data_ptr(), cols
+    if dweight is not None:
+        _given(dweight, "dweight", (cols,), wdtype, device)
+        dwp = _vector(dweight, "dweight", cols, device)
+    elif wants[1]:
+        dweight = _new(torch, cols, wdtype, device, stream)
+        dwp = dweight.data_ptr()
+    if dbias is not None:
+        _given(dbias, "dbias", (cols,), wdtype, device)
+        dbp = _vector(dbias, "dbias", cols, device)
+    elif wants[2]:
+        dbias = _new(torch, cols, wdtype, device, stream)
+        dbp = dbias.data_ptr()
+    need = lib.ndvm_layer_norm_workspace_bytes(rows, cols) if dwp is not None or dbp is not None else 0
+    ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
+    status = lib.ndvm_layer_norm_backward(code, _weight_type(code, dweight if weight is None else weight, dbias), rows, cols,
+                                          dy.data_ptr(), _rows(dy, "dy")[2], x.data_ptr(), xs,
+                                          _vector(weight, "weight", cols, device), sp, xp, dxs or 0, dwp, dbp, wp, nbytes,
+                                          _stream(torch, stream, device))
+    if status:
+        _check(status)
     return dx, dweight, dbias
 
 
@@ -178,23 +220,26 @@ def layer_norm_backward(dy, x, weight, stats, wants=(True, True, True), dx=None,
 def dropout_forward(x, p, seed, offset=0, residual=None, y=None, stream=None):
     """residual + (kept ? x / (1 - p) : 0): element i (row-major) takes word offset + i of the sequence that
     `seed` names (0 <= seed, offset < 2^64; offset a multiple of 4).  y may be x or residual."""
-    torch = _torch()
-    lib = load()
-    _on_device(x, (("residual", residual), ("y", y)))
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
     code = _type(x, "x")
     rows, cols, xs = _rows(x, "x")
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise NdvmError(1, "seed and offset must be in [0, 2^64)")
+    rp, rs = None, 0
     if residual is not None:
-        _like(residual, "residual", x.shape, x.dtype)
+        _given(residual, "residual", x.shape, x.dtype, device)
+        rp, rs = residual.data_ptr(), _rows(residual, "residual")[2]
     if y is None:
-        with _on_stream(stream):
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _like(y, "y", x.shape, x.dtype)
-    if x.numel():
-        _check(lib.ndvm_dropout(code, rows, cols, x.data_ptr(), xs, None if residual is None else residual.data_ptr(),
-                                0 if residual is None else _rows(residual, "residual")[2], p, seed, offset, y.data_ptr(),
-                                _rows(y, "y")[2], _stream_ptr(stream)))
+        y, ys = _new(torch, x.shape, x.dtype, device, stream), cols
+    else:
+        _given(y, "y", x.shape, x.dtype, device)
+        ys = _rows(y, "y")[2]
+    status = lib.ndvm_dropout(code, rows, cols, x.data_ptr(), xs, rp, rs, p, seed, offset, y.data_ptr(), ys,
+                              _stream(torch, stream, device))
+    if status:
+        _check(status)
     return y
 
 
@@ -204,80 +249,84 @@ def dropout_backward(dy, p, seed, offset=0, dx=None, stream=None):
 
 
 # ------------------------------------------------------------------------- gated projection
-def _activation(name):
-    code = ACTIVATIONS.get(name)
-    if code is None:
-        raise NdvmError(1, f"unknown activation {name!r}: one of {', '.join(ACTIVATIONS)}")
-    return code
-
-
-def _gated_shapes(x, w_gate, w_up):
+def _gated_operands(x, w_gate, w_up, activation, device):
+    """(activation, rows, k, n, addresses and row strides of x, w_gate and w_up, whether the products can read
+    every one of them where it lies)."""
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise NdvmError(1, f"unknown activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
     rows, k, xs = _rows(x, "x")
     if w_gate.dim() != 2 or w_gate.shape != w_up.shape or w_gate.shape[1] != k:
         raise NdvmError(1, f"w_gate and w_up must both be (n, {k}) matrices")
     if w_gate.dtype != x.dtype or w_up.dtype != x.dtype:
         raise NdvmError(1, "x, w_gate and w_up must have the same dtype")
-    return rows, k, w_gate.shape[0], xs, _rows(w_gate, "w_gate")[2], _rows(w_up, "w_up")[2]
-
-
-def _aligned(px, xs, pg, gs, pu, us):
-    """Whether the products can read every operand where it lies (addresses, row strides in elements)."""
-    return int((px | pg | pu) % 16 == 0 and (xs | gs | us) % 8 == 0 and xs != 0 and gs != 0 and us != 0)
+    _same_device(device, w_gate, "w_gate")
+    _same_device(device, w_up, "w_up")
+    gs, us = _rows(w_gate, "w_gate")[2], _rows(w_up, "w_up")[2]
+    px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+    ready = int((px | pg | pu) % 16 == 0 and (xs | gs | us) % 8 == 0 and xs != 0 and gs != 0 and us != 0)
+    return act, rows, k, w_gate.shape[0], (px, xs, pg, gs, pu, us), ready
 
 
 def gated_forward(x, w_gate, w_up, activation="silu", h=None, workspace=None, stream=None):
     """h = act(x w_gate^T) * (x w_up^T): x (..., k), both weights (n, k), h (..., n); 16-bit types.  Outputs
     and the workspace that this call allocates belong to `stream`."""
-    torch = _torch()
-    lib = load()
-    act = _activation(activation)
-    _on_device(x, (("w_gate", w_gate), ("w_up", w_up), ("h", h)))
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
     code = _type(x, "x")
-    rows, k, n, xs, gs, us = _gated_shapes(x, w_gate, w_up)
+    act, rows, k, n, operands, ready = _gated_operands(x, w_gate, w_up, activation, device)
     shape = x.shape[:-1] + (n,)
     if h is None:
-        with _on_stream(stream):
-            h = torch.empty(shape, dtype=x.dtype, device=x.device)
-    _like(h, "h", shape, x.dtype)
-    px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
-    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 0, _aligned(px, xs, pg, gs, pu, us))
-    ws, wp, nbytes = _workspace(workspace, need, x.device, stream)
-    _check(lib.ndvm_gated_forward(code, act, rows, k, n, px, xs, pg, gs, pu, us, h.data_ptr(), _rows(h, "h")[2], wp, nbytes,
-                                  _stream_ptr(stream)))
+        h, hs = _new(torch, shape, x.dtype, device, stream), n
+    else:
+        _given(h, "h", shape, x.dtype, device)
+        hs = _rows(h, "h")[2]
+    need = 0 if ready else lib.ndvm_gated_workspace_bytes(rows, k, n, 0, 0)
+    ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
+    status = lib.ndvm_gated_forward(code, act, rows, k, n, *operands, h.data_ptr(), hs, wp, nbytes,
+                                    _stream(torch, stream, device))
+    if status:
+        _check(status)
     return h
 
 
 def gated_backward(dh, x, w_gate, w_up, activation="silu", wants=(True, True, True), dx=None, dw_gate=None, dw_up=None,
                    workspace=None, stream=None):
     """(dx, dw_gate, dw_up) of gated_forward; `wants` says which (the others are None)."""
-    torch = _torch()
-    lib = load()
-    act = _activation(activation)
-    _on_device(x, (("dh", dh), ("w_gate", w_gate), ("w_up", w_up), ("dx", dx), ("dw_gate", dw_gate), ("dw_up", dw_up)))
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
     code = _type(x, "x")
-    rows, k, n, xs, gs, us = _gated_shapes(x, w_gate, w_up)
-    _like(dh, "dh", x.shape[:-1] + (n,), x.dtype)
-    with _on_stream(stream):
-        if dx is None and wants[0]:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if dw_gate is None and wants[1]:
-            dw_gate = torch.empty((n, k), dtype=x.dtype, device=x.device)
-        if dw_up is None and wants[2]:
-            dw_up = torch.empty((n, k), dtype=x.dtype, device=x.device)
+    act, rows, k, n, operands, ready = _gated_operands(x, w_gate, w_up, activation, device)
+    _given(dh, "dh", x.shape[:-1] + (n,), x.dtype, device)
+    xp = gp = up = None
+    dxs = 0
     if dx is not None:
-        _like(dx, "dx", x.shape, x.dtype)
+        _given(dx, "dx", x.shape, x.dtype, device)
+        xp, dxs = dx.data_ptr(), _rows(dx, "dx")[2]
+    elif wants[0]:
+        dx = _new(torch, x.shape, x.dtype, device, stream)
+        xp, dxs = dx.data_ptr(), k
     for name, t in (("dw_gate", dw_gate), ("dw_up", dw_up)):
         if t is not None:
-            _like(t, name, (n, k), x.dtype)
+            _given(t, name, (n, k), x.dtype, device)
             if not t.is_contiguous():
                 raise NdvmError(1, f"{name} must be contiguous")
-    px, pg, pu, ph, hs = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), dh.data_ptr(), _rows(dh, "dh")[2]
-    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 1, _aligned(px, xs, pg, gs, pu, us))
-    ws, wp, nbytes = _workspace(workspace, need, x.device, stream)
-    _check(lib.ndvm_gated_backward(code, act, rows, k, n, ph, hs, px, xs, pg, gs, pu, us,
-                                   None if dx is None else dx.data_ptr(), 0 if dx is None else _rows(dx, "dx")[2],
-                                   None if dw_gate is None else dw_gate.data_ptr(),
-                                   None if dw_up is None else dw_up.data_ptr(), wp, nbytes, _stream_ptr(stream)))
+    if dw_gate is None and wants[1]:
+        dw_gate = _new(torch, (n, k), x.dtype, device, stream)
+    if dw_up is None and wants[2]:
+        dw_up = _new(torch, (n, k), x.dtype, device, stream)
+    if dw_gate is not None:
+        gp = dw_gate.data_ptr()
+    if dw_up is not None:
+        up = dw_up.data_ptr()
+    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 1, ready)
+    ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
+    status = lib.ndvm_gated_backward(code, act, rows, k, n, dh.data_ptr(), _rows(dh, "dh")[2], *operands, xp, dxs, gp, up, wp,
+                                     nbytes, _stream(torch, stream, device))
+    if status:
+        _check(status)
     return dx, dw_gate, dw_up
 
 
@@ -296,10 +345,15 @@ def _rowed(t):
 _ops = None
 
 
+def _first_order():
+    """A backward pass records nothing (gradient mode is on in one only to differentiate it again)."""
+    if _torch_module.is_grad_enabled():
+        raise NdvmError(3, "the network operators have no second derivatives")
+
+
 def _make_ops():
     global _ops
-    torch = _torch()
-    once = torch.autograd.function.once_differentiable
+    torch = _torch_module or _start()
 
     class Norm(torch.autograd.Function):
         @staticmethod
@@ -310,10 +364,10 @@ def _make_ops():
             return y
 
         @staticmethod
-        @once
         def backward(ctx, dy):
+            _first_order()
             x, weight, stats = ctx.saved_tensors
-            return layer_norm_backward(_rowed(dy), x, weight, stats, ctx.needs_input_grad[:3], wtype=ctx.wtype) + (None,)
+            return layer_norm_backward(_rowed(dy), x, weight, stats, ctx.needs_input_grad, wtype=ctx.wtype) + (None,)
 
     class Drop(torch.autograd.Function):
         @staticmethod
@@ -322,10 +376,10 @@ def _make_ops():
             return dropout_forward(x, p, seed, offset, residual)
 
         @staticmethod
-        @once
         def backward(ctx, dy):
-            dx = dropout_backward(_rowed(dy), *ctx.draw) if ctx.needs_input_grad[0] else None
-            return dx, None, None, None, dy if ctx.needs_input_grad[4] else None
+            _first_order()
+            wants = ctx.needs_input_grad
+            return (dropout_forward(_rowed(dy), *ctx.draw) if wants[0] else None, None, None, None, dy if wants[4] else None)
 
     class Gated(torch.autograd.Function):
         @staticmethod
@@ -335,16 +389,21 @@ def _make_ops():
             return gated_forward(x, w_gate, w_up, activation)
 
         @staticmethod
-        @once
         def backward(ctx, dh):
-            return gated_backward(_rowed(dh), *ctx.saved_tensors, ctx.activation, ctx.needs_input_grad[:3]) + (None,)
+            _first_order()
+            return gated_backward(_rowed(dh), *ctx.saved_tensors, ctx.activation, ctx.needs_input_grad) + (None,)
 
-    _ops = Norm, Drop, Gated
+    _ops = Norm.apply, Drop.apply, Gated.apply
     return _ops
 
 
 def _recorded(*tensors):
-    return _torch().is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if not (_torch_module or _start()).is_grad_enabled():
+        return False
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return True
+    return False
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
@@ -352,7 +411,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     x = _rowed(x)
     if not _recorded(x, weight, bias):
         return layer_norm_forward(x, weight, bias, eps, want_stats=False)[0]
-    return (_ops or _make_ops())[0].apply(x, weight, bias, eps)
+    return (_ops or _make_ops())[0](x, weight, bias, eps)
 
 
 def dropout(x, p, seed, offset=0, residual=None):
@@ -361,7 +420,7 @@ def dropout(x, p, seed, offset=0, residual=None):
     x, residual = _rowed(x), _rowed(residual)
     if not _recorded(x, residual):
         return dropout_forward(x, p, seed, offset, residual)
-    return (_ops or _make_ops())[1].apply(x, p, seed, offset, residual)
+    return (_ops or _make_ops())[1](x, p, seed, offset, residual)
 
 
 def gated(x, w_gate, w_up, activation="silu"):
@@ -369,7 +428,7 @@ def gated(x, w_gate, w_up, activation="silu"):
     x, w_gate, w_up = _rowed(x), _rowed(w_gate), _rowed(w_up)
     if not _recorded(x, w_gate, w_up):
         return gated_forward(x, w_gate, w_up, activation)
-    return (_ops or _make_ops())[2].apply(x, w_gate, w_up, activation)
+    return (_ops or _make_ops())[2](x, w_gate, w_up, activation)
 
 
 def check_operators():
