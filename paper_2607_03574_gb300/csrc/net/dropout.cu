@@ -14,15 +14,22 @@ constexpr int kThreads = 256;
 
 struct Words { uint32_t w[4]; };
 
+// A round's two products in full, as the widening multiply that the hardware has: through 64-bit integers the
+// compiler spends more (134 M bfloat16 elements with a residual: 156 us against 129).
+__device__ __forceinline__ void product(uint32_t a, uint32_t m, uint32_t* high, uint32_t* low) {
+  asm("{\n .reg .u64 t;\n mul.wide.u32 t, %2, %3;\n mov.b64 {%1, %0}, t;\n}" : "=r"(*high), "=r"(*low) : "r"(a), "r"(m));
+}
 __device__ __forceinline__ Words philox(uint64_t block, uint32_t k0, uint32_t k1) {
   uint32_t a = (uint32_t)block, b = (uint32_t)(block >> 32), c = 0, d = 0;
 #pragma unroll
   for (int r = 0; r < 10; r++) {
-    const uint64_t p = (uint64_t)a * 0xD2511F53u, q = (uint64_t)c * 0xCD9E8D57u;
-    a = (uint32_t)(q >> 32) ^ b ^ k0;
-    b = (uint32_t)q;
-    c = (uint32_t)(p >> 32) ^ d ^ k1;
-    d = (uint32_t)p;
+    uint32_t p1, p0, q1, q0;
+    product(a, 0xD2511F53u, &p1, &p0);
+    product(c, 0xCD9E8D57u, &q1, &q0);
+    a = q1 ^ b ^ k0;
+    b = q0;
+    c = p1 ^ d ^ k1;
+    d = p0;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
@@ -35,51 +42,61 @@ __device__ __forceinline__ T drop(const DropArgs& a, uint32_t word, T x, T r) {
   if (kResidual) y += to_f32(r);
   return from_f32<T>(y);
 }
+__device__ __forceinline__ float2 drop(const DropArgs& a, uint32_t w0, uint32_t w1, float2 x) {
+  const float2 y = mul(x, make_float2(a.scale, a.scale));
+  return make_float2(w0 >= a.threshold ? y.x : 0.0f, w1 >= a.threshold ? y.y : 0.0f);  // (chosen, not multiplied by 0)
+}
 
-// 16 bytes of x (and of the residual) a thread and step, kSteps of them in flight: for rows that start on
-// 16 bytes everywhere and hold whole vectors, and for one long row (a contiguous tensor) of any length.
-template <typename T, bool kResidual, int kSteps>
-__global__ void __launch_bounds__(kThreads) k_dropout_vectors(DropArgs a) {
+// 16 bytes of x (and of the residual) from its v-th vector on
+template <typename T, bool kResidual>
+__device__ __forceinline__ void drop_vector(const DropArgs& a, const T* x, const T* r, T* y, uint64_t block) {
   constexpr int V = 16 / sizeof(T);
-  using P = Pack<T, V>;
-  const int64_t vectors = a.cols / V;
-  const uint32_t k0 = (uint32_t)a.seed, k1 = (uint32_t)(a.seed >> 32);
-  for (int64_t row = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; row < a.rows; row += (int64_t)gridDim.y * blockDim.y) {
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-    const T* r = kResidual ? static_cast<const T*>(a.residual) + row * a.r_stride : nullptr;
-    T* y = static_cast<T*>(a.y) + row * a.y_stride;
-    const uint64_t first = a.offset / 4 + (uint64_t)(row * vectors) * (V / 4);
-    const int64_t v0 = (int64_t)blockIdx.x * blockDim.x * kSteps + threadIdx.x;
-    P px[kSteps], pr[kSteps];
+  Pack<T, V> p = load_pack<T, V>(x), pr;
+  if (kResidual) pr = load_pack<T, V>(r);
 #pragma unroll
-    for (int s = 0; s < kSteps; s++) {
-      const int64_t v = v0 + s * (int)blockDim.x;
-      if (v < vectors) {
-        px[s] = load_pack<T, V>(x + v * V);
-        if (kResidual) pr[s] = load_pack<T, V>(r + v * V);
-      }
+  for (int q = 0; q < V / 4; q++) {
+    const Words w = philox(block + q, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      float2 d = drop(a, w.w[e], w.w[e + 1], widen(p.v + q * 4 + e));
+      if (kResidual) d = add(d, widen(pr.v + q * 4 + e));
+      narrow(p.v + q * 4 + e, d);
     }
-#pragma unroll
-    for (int s = 0; s < kSteps; s++) {
-      const int64_t v = v0 + s * (int)blockDim.x;
-      if (v >= vectors) break;
-      P out;
-#pragma unroll
-      for (int q = 0; q < V / 4; q++) {
-        const Words w = philox(first + (uint64_t)v * (V / 4) + q, k0, k1);
-#pragma unroll
-        for (int e = 0; e < 4; e++) out.v[q * 4 + e] = drop<T, kResidual>(a, w.w[e], px[s].v[q * 4 + e], (kResidual ? pr : px)[s].v[q * 4 + e]);
-      }
-      store_pack(y + v * V, out);
-    }
-    // what a single row has beyond its vectors
-    const int64_t c = vectors * V + threadIdx.x;
-    if (blockIdx.x == 0 && c < a.cols) {
-      const Words w = philox(a.offset / 4 + (uint64_t)(c / 4), k0, k1);
+  }
+  store_pack(y, p);
+}
+
+// Contiguous tensors (one row of any length): bound by memory with a residual (134 M bfloat16 elements:
+// TODO).  One vector a thread: threads that took several, with the next loads in flight or not, were slower
+// (143 to 191 us; 127 at best).
+template <typename T, bool kResidual>
+__global__ void __launch_bounds__(kThreads, 5) k_dropout_flat(DropArgs a) {
+  constexpr int V = 16 / sizeof(T);
+  const T *x = static_cast<const T*>(a.x), *r = static_cast<const T*>(a.residual);
+  T* y = static_cast<T*>(a.y);
+  const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x, vectors = a.cols / V;
+  if (v < vectors) {
+    drop_vector<T, kResidual>(a, x + v * V, kResidual ? r + v * V : r, y + v * V, a.offset / 4 + (uint64_t)v * (V / 4));
+  } else if (v == vectors) {  // what is left beyond the vectors
+    for (int64_t c = vectors * V; c < a.cols; c++) {
+      const Words w = philox(a.offset / 4 + (uint64_t)(c / 4), (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
       const uint32_t word = c % 4 == 0 ? w.w[0] : c % 4 == 1 ? w.w[1] : c % 4 == 2 ? w.w[2] : w.w[3];
       y[c] = drop<T, kResidual>(a, word, x[c], kResidual ? r[c] : x[c]);
     }
   }
+}
+
+// rows of whole vectors that start on 16 bytes
+template <typename T, bool kResidual>
+__global__ void __launch_bounds__(kThreads, 5) k_dropout_rows(DropArgs a) {
+  constexpr int V = 16 / sizeof(T);
+  const int64_t v = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, vectors = a.cols / V;
+  if (v >= vectors) return;
+  for (int64_t row = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; row < a.rows; row += (int64_t)gridDim.y * blockDim.y)
+    drop_vector<T, kResidual>(a, static_cast<const T*>(a.x) + row * a.x_stride + v * V,
+                              kResidual ? static_cast<const T*>(a.residual) + row * a.r_stride + v * V : nullptr,
+                              static_cast<T*>(a.y) + row * a.y_stride + v * V,
+                              a.offset / 4 + (uint64_t)(row * vectors + v) * (V / 4));
 }
 
 // Any layout: a generator block a thread and step, of which the row's elements are taken (a block that
@@ -116,19 +133,22 @@ cudaError_t launch(DropArgs a, cudaStream_t s) {
   };
   const bool vectors = on16(a.x, a.x_stride) && on16(a.y, a.y_stride) && (!kResidual || on16(a.residual, a.r_stride)) &&
                        (a.rows == 1 || a.cols % V == 0);
+  if (vectors && a.rows == 1) {
+    const int64_t blocks = a.cols / V / kThreads + 1;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    k_dropout_flat<T, kResidual><<<(unsigned)blocks, kThreads, 0, s>>>(a);
+    return cudaGetLastError();
+  }
   // items of a row: its vectors, or the blocks it meets (one more where it starts inside a block)
-  const int64_t items = vectors ? std::max<int64_t>(a.cols / V, 1) : a.cols / 4 + 2;
-  // two steps a thread keep four 16-byte loads in flight; few items go one a thread over more blocks
-  const int steps = vectors && items * a.rows >= (int64_t)152 * 2048 * 2 ? 2 : 1;
+  const int64_t items = vectors ? a.cols / V : a.cols / 4 + 2;
   int bx = kThreads;
-  while (bx > 8 && bx / 2 * steps >= items) bx /= 2;
+  while (bx > 8 && bx / 2 >= items) bx /= 2;
   const dim3 block(bx, kThreads / bx);
-  const int64_t gx = (items + (int64_t)bx * steps - 1) / ((int64_t)bx * steps), gy = (a.rows + block.y - 1) / block.y;
+  const int64_t gx = (items + bx - 1) / bx, gy = (a.rows + block.y - 1) / block.y;
   if (gx > 0x7fffffff) return cudaErrorInvalidConfiguration;
   const dim3 grid((unsigned)gx, (unsigned)std::min<int64_t>(gy, 65535));
-  if (!vectors) k_dropout_elements<T, kResidual><<<grid, block, 0, s>>>(a);
-  else if (steps == 2) k_dropout_vectors<T, kResidual, 2><<<grid, block, 0, s>>>(a);
-  else k_dropout_vectors<T, kResidual, 1><<<grid, block, 0, s>>>(a);
+  if (vectors) k_dropout_rows<T, kResidual><<<grid, block, 0, s>>>(a);
+  else k_dropout_elements<T, kResidual><<<grid, block, 0, s>>>(a);
   return cudaGetLastError();
 }
 

@@ -14,22 +14,23 @@ namespace {
 
 // weights are of the activations' type or binary32
 template <typename T, int V>
-__device__ __forceinline__ void load_weight(float (&w)[V], const void* p, int f32, int64_t c, float none) {
+__device__ __forceinline__ void load_weight(Pairs<V> (&w)[kPairs<V>], const void* p, int f32, int64_t c, float none) {
   if (!p) {
 #pragma unroll
-    for (int e = 0; e < V; e++) w[e] = none;
+    for (int e = 0; e < kPairs<V>; e++) w[e] = both(none, w[e]);
   } else if (f32) {
-    constexpr int Q = V >= 4 ? 4 : 1;
+    if constexpr (V == 1) {
+      w[0] = static_cast<const float*>(p)[c];
+    } else {
 #pragma unroll
-    for (int q = 0; q < V; q += Q) {
-      const Pack<float, Q> v = load_pack<float, Q>(static_cast<const float*>(p) + c + q);
-#pragma unroll
-      for (int e = 0; e < Q; e++) w[q + e] = v.v[e];
+      for (int q = 0; q < V; q += 4) {
+        const Pack<float, 4> v = load_pack<float, 4>(static_cast<const float*>(p) + c + q);
+        w[q / 2] = make_float2(v.v[0], v.v[1]);
+        w[q / 2 + 1] = make_float2(v.v[2], v.v[3]);
+      }
     }
   } else {
-    const Pack<T, V> v = load_pack<T, V>(static_cast<const T*>(p) + c);
-#pragma unroll
-    for (int e = 0; e < V; e++) w[e] = to_f32(v.v[e]);
+    widen<T, V>(load_pack<T, V>(static_cast<const T*>(p) + c), w);
   }
 }
 
@@ -52,9 +53,11 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
 template <int kRow> constexpr int kBlock = kRow > 32 ? kRow : 128;  // threads a block
 
 // A row in the registers of kRow threads, N packs of V elements each: pack j of thread t holds the
-// columns (j kRow + t) V ...
-template <typename T, int V, int N, int kRow>
-__global__ void __launch_bounds__(kBlock<kRow>) k_forward(NormArgs a, int w_f32) {
+// columns (j kRow + t) V ...  kResident: blocks an SM should hold (registers a thread are cut to that).
+template <typename T, int V, int N, int kRow, int kResident>
+__global__ void __launch_bounds__(kBlock<kRow>, kResident) k_forward(NormArgs a, int w_f32) {
+  using P = Pairs<V>;
+  constexpr int H = kPairs<V>;
   __shared__ float part[2][32];
   const int t = threadIdx.x % kRow;
   const int64_t row = (int64_t)blockIdx.x * (kBlock<kRow> / kRow) + threadIdx.x / kRow;
@@ -62,38 +65,47 @@ __global__ void __launch_bounds__(kBlock<kRow>) k_forward(NormArgs a, int w_f32)
   const int cols = (int)a.cols;
   const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
   Pack<T, V> px[N];
-  float sum = 0.0f;
+  P sum = both(0.0f, P());
 #pragma unroll
   for (int j = 0; j < N; j++) {
     const int c = (j * kRow + t) * V;
     if (c < cols) px[j] = load_pack<T, V>(x + c);
   }
 #pragma unroll
-  for (int j = 0; j < N; j++)
-    if ((j * kRow + t) * V < cols)
+  for (int j = 0; j < N; j++) {
+    if ((j * kRow + t) * V >= cols) continue;
+    P v[H];
+    widen<T, V>(px[j], v);
 #pragma unroll
-      for (int e = 0; e < V; e++) sum += to_f32(px[j].v[e]);
-  const float mean = row_sum<kRow>(sum, part[0]) / (float)cols;
-  sum = 0.0f;
+    for (int e = 0; e < H; e++) sum = add(sum, v[e]);
+  }
+  const float mean = row_sum<kRow>(total(sum), part[0]) / (float)cols;
+  const P off = both(-mean, P());
+  sum = both(0.0f, P());
 #pragma unroll
-  for (int j = 0; j < N; j++)
-    if ((j * kRow + t) * V < cols)
+  for (int j = 0; j < N; j++) {
+    if ((j * kRow + t) * V >= cols) continue;
+    P v[H];
+    widen<T, V>(px[j], v);
 #pragma unroll
-      for (int e = 0; e < V; e++) {
-        const float d = to_f32(px[j].v[e]) - mean;
-        sum += d * d;
-      }
-  const float rstd = 1.0f / sqrtf(row_sum<kRow>(sum, part[1]) / (float)cols + a.eps);
+    for (int e = 0; e < H; e++) {
+      const P d = add(v[e], off);
+      sum = fma(d, d, sum);
+    }
+  }
+  const float rstd = 1.0f / sqrtf(row_sum<kRow>(total(sum), part[1]) / (float)cols + a.eps);
+  const P scale = both(rstd, P());
   T* y = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
   for (int j = 0; j < N; j++) {
     const int c = (j * kRow + t) * V;
     if (c >= cols) continue;
-    float w[V], b[V];
+    P v[H], w[H], b[H];
+    widen<T, V>(px[j], v);
     load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
     load_weight<T, V>(b, a.bias, w_f32, c, 0.0f);
 #pragma unroll
-    for (int e = 0; e < V; e++) px[j].v[e] = from_f32<T>((to_f32(px[j].v[e]) - mean) * rstd * w[e] + b[e]);
+    for (int e = 0; e < H; e++) narrow<T, V>(px[j], e, fma(mul(add(v[e], off), scale), w[e], b[e]));
     store_pack(y + c, px[j]);
   }
   if (t == 0 && a.stats) {
@@ -123,7 +135,7 @@ __global__ void __launch_bounds__(kLong) k_forward_long(NormArgs a, int w_f32) {
     float w[1], b[1];
     load_weight<T, 1>(w, a.weight, w_f32, c, 1.0f);
     load_weight<T, 1>(b, a.bias, w_f32, c, 0.0f);
-    y[c] = from_f32<T>((to_f32(x[c]) - mean) * rstd * w[0] + b[0]);
+    y[c] = from_f32<T>(fmaf((to_f32(x[c]) - mean) * rstd, w[0], b[0]));
   }
   if (threadIdx.x == 0 && a.stats) {
     a.stats[row] = mean;
@@ -133,18 +145,18 @@ __global__ void __launch_bounds__(kLong) k_forward_long(NormArgs a, int w_f32) {
 
 // Backward: a block takes every gridDim.x-th group of rows; the next row's loads are in flight while the
 // present one is worked on.  partial[block][0][c] = the block's sum of dy xh, [1][c] = of dy.
-template <typename T, int V, int N, int kRow>
-__global__ void __launch_bounds__(kBlock<kRow>) k_backward(NormArgs a, int w_f32) {
-  constexpr int kRows = kBlock<kRow> / kRow;
+template <typename T, int V, int N, int kRow, int kResident>
+__global__ void __launch_bounds__(kBlock<kRow>, kResident) k_backward(NormArgs a, int w_f32) {
+  using P = Pairs<V>;
+  constexpr int H = kPairs<V>, kRows = kBlock<kRow> / kRow;
   __shared__ float part[4][32];
   const int t = threadIdx.x % kRow, cols = (int)a.cols;
-  const bool sums = a.partial != nullptr;
   const float inv = 1.0f / (float)cols;
-  float dw[N][V], db[N][V];
+  P dw[N][H], db[N][H];
 #pragma unroll
   for (int j = 0; j < N; j++)
 #pragma unroll
-    for (int e = 0; e < V; e++) dw[j][e] = db[j][e] = 0.0f;
+    for (int e = 0; e < H; e++) dw[j][e] = db[j][e] = both(0.0f, P());
   Pack<T, V> nx[N], nd[N];
   float nmean = 0.0f, nrstd = 0.0f;
   const auto fetch = [&](int64_t row) {
@@ -168,43 +180,49 @@ __global__ void __launch_bounds__(kBlock<kRow>) k_backward(NormArgs a, int w_f32
   for (int turn = 0; row < a.rows; row += step, turn ^= 2) {
     Pack<T, V> px[N], pd[N];
     const float mean = nmean, rstd = nrstd;
+    const P off = both(-mean, P()), scale = both(rstd, P());
 #pragma unroll
     for (int j = 0; j < N; j++) px[j] = nx[j], pd[j] = nd[j];
     fetch(row + step);
-    float sg = 0.0f, sgx = 0.0f;
+    P sg = both(0.0f, P()), sgx = both(0.0f, P());
 #pragma unroll
     for (int j = 0; j < N; j++) {
       const int c = (j * kRow + t) * V;
       if (c >= cols) continue;
-      float w[V];
+      P w[H], x[H], d[H];
       load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
+      widen<T, V>(px[j], x);
+      widen<T, V>(pd[j], d);
 #pragma unroll
-      for (int e = 0; e < V; e++) {
-        const float d = to_f32(pd[j].v[e]), xh = (to_f32(px[j].v[e]) - mean) * rstd, g = d * w[e];
-        sg += g;
-        sgx += g * xh;
-        dw[j][e] += d * xh;
-        db[j][e] += d;
+      for (int e = 0; e < H; e++) {
+        const P xh = mul(add(x[e], off), scale), g = mul(d[e], w[e]);
+        sg = add(sg, g);
+        sgx = fma(g, xh, sgx);
+        dw[j][e] = fma(d[e], xh, dw[j][e]);
+        db[j][e] = add(db[j][e], d[e]);
       }
     }
     if (!a.dx) continue;
-    const float mg = row_sum<kRow>(sg, part[turn]) * inv, mgx = row_sum<kRow>(sgx, part[turn + 1]) * inv;
+    const float mg = row_sum<kRow>(total(sg), part[turn]) * inv, mgx = row_sum<kRow>(total(sgx), part[turn + 1]) * inv;
+    const P less = both(-mg, P()), slope = both(-mgx, P());
     T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
 #pragma unroll
     for (int j = 0; j < N; j++) {
       const int c = (j * kRow + t) * V;
       if (c >= cols) continue;
-      float w[V];
+      P w[H], x[H], d[H];
       load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
+      widen<T, V>(px[j], x);
+      widen<T, V>(pd[j], d);
 #pragma unroll
-      for (int e = 0; e < V; e++) {
-        const float xh = (to_f32(px[j].v[e]) - mean) * rstd;
-        px[j].v[e] = from_f32<T>(rstd * (to_f32(pd[j].v[e]) * w[e] - mg - xh * mgx));
+      for (int e = 0; e < H; e++) {
+        const P xh = mul(add(x[e], off), scale);
+        narrow<T, V>(px[j], e, mul(scale, fma(xh, slope, fma(d[e], w[e], less))));
       }
       store_pack(dx + c, px[j]);
     }
   }
-  if (!sums) return;
+  if (!a.partial) return;
   float* out = a.partial + (int64_t)blockIdx.x * 2 * cols;
   if constexpr (kRows == 1) {
 #pragma unroll
@@ -212,20 +230,20 @@ __global__ void __launch_bounds__(kBlock<kRow>) k_backward(NormArgs a, int w_f32
       const int c = (j * kRow + t) * V;
       if (c >= cols) continue;
 #pragma unroll
-      for (int e = 0; e < V; e++) {
-        out[c + e] = dw[j][e];
-        out[cols + c + e] = db[j][e];
+      for (int e = 0; e < H; e++) {
+        *reinterpret_cast<P*>(out + c + e * (V / H)) = dw[j][e];
+        *reinterpret_cast<P*>(out + cols + c + e * (V / H)) = db[j][e];
       }
     }
   } else {
-    __shared__ float all[kRows][2][N * V * kRow];
+    __shared__ __align__(16) float all[kRows][2][N * V * kRow];
 #pragma unroll
     for (int j = 0; j < N; j++)
 #pragma unroll
-      for (int e = 0; e < V; e++) {
-        const int c = (j * kRow + t) * V + e;
-        all[threadIdx.x / kRow][0][c] = dw[j][e];
-        all[threadIdx.x / kRow][1][c] = db[j][e];
+      for (int e = 0; e < H; e++) {
+        const int c = (j * kRow + t) * V + e * (V / H);
+        *reinterpret_cast<P*>(&all[threadIdx.x / kRow][0][c]) = dw[j][e];
+        *reinterpret_cast<P*>(&all[threadIdx.x / kRow][1][c]) = db[j][e];
       }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * cols; i += kBlock<kRow>) {
@@ -307,7 +325,7 @@ bool on16(const void* p, int64_t stride, int64_t rows, size_t elem) {
 }
 
 // The kernel variant for rows of `cols` elements: V elements a load (16 bytes where every row starts and
-// ends on 16 bytes, else 1), N loads a thread, kRow threads a row.  `f` is called with the three as
+// ends on 16 bytes, else 1), N loads a thread, kRow threads a row, blocks an SM.  `f` is called with them as
 // integral constants; false: the row is longer than any variant holds.
 template <int K> using Int = std::integral_constant<int, K>;
 
@@ -316,19 +334,19 @@ bool forward_variant(bool vectors, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
   if (vectors) {
     const int64_t packs = cols / V;  // a warp a row up to 8 loads a thread (no barriers), then blocks
-    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>());
-    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>());
-    else if (packs <= 128) f(Int<V>(), Int<4>(), Int<32>());
-    else if (packs <= 256) f(Int<V>(), Int<8>(), Int<32>());
-    else if (packs <= 512) f(Int<V>(), Int<4>(), Int<128>());
-    else if (packs <= 1024) f(Int<V>(), Int<4>(), Int<256>());
-    else if (packs <= 2048) f(Int<V>(), Int<4>(), Int<512>());
+    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<12>());
+    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<12>());
+    else if (packs <= 128) f(Int<V>(), Int<4>(), Int<32>(), Int<10>());
+    else if (packs <= 256) f(Int<V>(), Int<8>(), Int<32>(), Int<7>());
+    else if (packs <= 512) f(Int<V>(), Int<4>(), Int<128>(), Int<10>());
+    else if (packs <= 1024) f(Int<V>(), Int<4>(), Int<256>(), Int<5>());
+    else if (packs <= 2048) f(Int<V>(), Int<4>(), Int<512>(), Int<2>());
     else return false;
   } else {
-    if (cols <= 128) f(Int<1>(), Int<4>(), Int<32>());
-    else if (cols <= 512) f(Int<1>(), Int<16>(), Int<32>());
-    else if (cols <= 2048) f(Int<1>(), Int<16>(), Int<128>());
-    else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>());
+    if (cols <= 128) f(Int<1>(), Int<4>(), Int<32>(), Int<12>());
+    else if (cols <= 512) f(Int<1>(), Int<16>(), Int<32>(), Int<10>());
+    else if (cols <= 2048) f(Int<1>(), Int<16>(), Int<128>(), Int<10>());
+    else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>(), Int<2>());
     else return false;
   }
   return true;
@@ -339,20 +357,20 @@ bool backward_variant(bool vectors, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
   if (vectors) {
     const int64_t packs = cols / V;
-    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>());
-    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>());
-    else if (packs <= 128) f(Int<V>(), Int<1>(), Int<128>());
-    else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>());
-    else if (packs <= 512) f(Int<V>(), Int<2>(), Int<256>());
-    else if (packs <= 1024) f(Int<V>(), Int<2>(), Int<512>());
-    else if (packs <= 2048 && sizeof(T) == 4) f(Int<4>(), Int<4>(), Int<512>());  // (16-bit rows would not fit in 128 registers)
+    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<6>());
+    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<4>());
+    else if (packs <= 128) f(Int<V>(), Int<1>(), Int<128>(), Int<8>());
+    else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>(), Int<5>());
+    else if (packs <= 512) f(Int<V>(), Int<2>(), Int<256>(), Int<2>());
+    else if (packs <= 1024) f(Int<V>(), Int<2>(), Int<512>(), Int<1>());
+    else if (packs <= 2048 && sizeof(T) == 4) f(Int<4>(), Int<4>(), Int<512>(), Int<1>());  // (16-bit rows would not fit in 128 registers)
     else return false;
   } else {
-    if (cols <= 256) f(Int<1>(), Int<8>(), Int<32>());
-    else if (cols <= 1024) f(Int<1>(), Int<8>(), Int<128>());
-    else if (cols <= 2048) f(Int<1>(), Int<8>(), Int<256>());
-    else if (cols <= 4096) f(Int<1>(), Int<8>(), Int<512>());
-    else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>());
+    if (cols <= 256) f(Int<1>(), Int<8>(), Int<32>(), Int<5>());
+    else if (cols <= 1024) f(Int<1>(), Int<8>(), Int<128>(), Int<6>());
+    else if (cols <= 2048) f(Int<1>(), Int<8>(), Int<256>(), Int<3>());
+    else if (cols <= 4096) f(Int<1>(), Int<8>(), Int<512>(), Int<1>());
+    else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>(), Int<1>());
     else return false;
   }
   return true;
@@ -364,9 +382,9 @@ cudaError_t forward(const NormArgs& a, int w_f32, cudaStream_t s) {
   if (a.rows > 0x7fffffff) return cudaErrorInvalidConfiguration;
   const bool vectors = a.cols % (16 / sizeof(T)) == 0 && on16(a.x, a.x_stride, a.rows, sizeof(T)) &&
                        on16(a.y, a.y_stride, a.rows, sizeof(T)) && on16(a.weight) && on16(a.bias);
-  const bool held = forward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r) {
+  const bool held = forward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r, auto b) {
     constexpr int kRow = decltype(r)::value, kRows = kBlock<kRow> / kRow;
-    k_forward<T, decltype(v)::value, decltype(n)::value, kRow>
+    k_forward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value>
         <<<(unsigned)((a.rows + kRows - 1) / kRows), kBlock<kRow>, 0, s>>>(a, w_f32);
   });
   if (!held) k_forward_long<T><<<(unsigned)a.rows, kLong, 0, s>>>(a, w_f32);
@@ -383,17 +401,17 @@ cudaError_t backward(NormArgs a, int w_f32, cudaStream_t s) {
     const bool vectors = a.cols % (16 / sizeof(T)) == 0 && on16(a.x, a.x_stride, a.rows, sizeof(T)) &&
                          on16(a.dy, a.dy_stride, a.rows, sizeof(T)) && on16(a.weight) &&
                          (!a.dx || on16(a.dx, a.dx_stride, a.rows, sizeof(T)));
-    const bool held = backward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r) {
+    const bool held = backward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r, auto b) {
       constexpr int kRow = decltype(r)::value, kRows = kBlock<kRow> / kRow;
       // as many blocks as stay resident, or a block a group of rows where there are fewer
       static const int resident = [] {
-        int b = 0;
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&b, k_backward<T, decltype(v)::value, decltype(n)::value, kRow>,
+        int fit = 0;
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, k_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value>,
                                                       kBlock<kRow>, 0);
-        return std::clamp(b * kSms, kSms, kMostBlocks);
+        return std::clamp(fit * kSms, kSms, kMostBlocks);
       }();
       blocks = (int)std::min<int64_t>(resident, (a.rows + kRows - 1) / kRows);
-      k_backward<T, decltype(v)::value, decltype(n)::value, kRow><<<blocks, kBlock<kRow>, 0, s>>>(a, w_f32);
+      k_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value><<<blocks, kBlock<kRow>, 0, s>>>(a, w_f32);
     });
     if (!held) {
       if (a.dx) k_backward_long<T><<<(unsigned)a.rows, kLong, 0, s>>>(a, w_f32);
