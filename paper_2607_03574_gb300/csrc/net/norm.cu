@@ -143,14 +143,36 @@ __global__ void __launch_bounds__(kLong) k_forward_long(NormArgs a, int w_f32) {
   }
 }
 
-// Backward: a block takes every gridDim.x-th group of rows; the next row's loads are in flight while the
-// present one is worked on.  partial[block][0][c] = the block's sum of dy xh, [1][c] = of dy.
+// Two sums over the kRow threads of a group that shares a row, by the group's own barrier; `part` is another
+// one on the next call (a group's warp may still read this one then, but not on the call after).
+template <int kRow>
+__device__ __forceinline__ float2 group_sum(float a, float b, float2* part, int group) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    a += __shfl_xor_sync(~0u, a, o);
+    b += __shfl_xor_sync(~0u, b, o);
+  }
+  float2 s = make_float2(a, b);
+  if constexpr (kRow > 32) {
+    if (threadIdx.x % 32 == 0) part[threadIdx.x % kRow / 32] = s;
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kRow) : "memory");
+    s = part[0];
+#pragma unroll
+    for (int w = 1; w < kRow / 32; w++) s = add(s, part[w]);
+  }
+  return s;
+}
+
+// Backward: a group of kRow threads takes every so-manieth row; the next row's loads are in flight while
+// the present one is worked on.  partial[block][0][c] = the block's sum of dy xh, [1][c] = of dy.
+template <int kRow> constexpr int kBackBlock = kRow > 256 ? kRow : 256;
+
 template <typename T, int V, int N, int kRow, int kResident>
-__global__ void __launch_bounds__(kBlock<kRow>, kResident) k_backward(NormArgs a, int w_f32) {
+__global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_backward(NormArgs a, int w_f32) {
   using P = Pairs<V>;
-  constexpr int H = kPairs<V>, kRows = kBlock<kRow> / kRow;
-  __shared__ float part[4][32];
-  const int t = threadIdx.x % kRow, cols = (int)a.cols;
+  constexpr int H = kPairs<V>, kBlockRows = kBackBlock<kRow> / kRow;
+  __shared__ float2 part[2][kBlockRows][kRow / 32];
+  const int t = threadIdx.x % kRow, group = threadIdx.x / kRow, cols = (int)a.cols;
   const float inv = 1.0f / (float)cols;
   P dw[N][H], db[N][H];
 #pragma unroll
@@ -174,57 +196,49 @@ __global__ void __launch_bounds__(kBlock<kRow>, kResident) k_backward(NormArgs a
       }
     }
   };
-  const int64_t step = (int64_t)gridDim.x * kRows;
-  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kRow;
+  const int64_t step = (int64_t)gridDim.x * kBlockRows;
+  int64_t row = (int64_t)blockIdx.x * kBlockRows + group;
   fetch(row);
-  for (int turn = 0; row < a.rows; row += step, turn ^= 2) {
-    Pack<T, V> px[N], pd[N];
-    const float mean = nmean, rstd = nrstd;
-    const P off = both(-mean, P()), scale = both(rstd, P());
-#pragma unroll
-    for (int j = 0; j < N; j++) px[j] = nx[j], pd[j] = nd[j];
-    fetch(row + step);
-    P sg = both(0.0f, P()), sgx = both(0.0f, P());
+  for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
+    const float rstd = nrstd;
+    const P off = both(-nmean, P()), scale = both(rstd, P());
+    P xh[N][H], g[N][H], sg = both(0.0f, P()), sgx = both(0.0f, P());
 #pragma unroll
     for (int j = 0; j < N; j++) {
       const int c = (j * kRow + t) * V;
       if (c >= cols) continue;
-      P w[H], x[H], d[H];
+      P w[H];
       load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
-      widen<T, V>(px[j], x);
-      widen<T, V>(pd[j], d);
+      widen<T, V>(nx[j], xh[j]);
+      widen<T, V>(nd[j], g[j]);
 #pragma unroll
       for (int e = 0; e < H; e++) {
-        const P xh = mul(add(x[e], off), scale), g = mul(d[e], w[e]);
-        sg = add(sg, g);
-        sgx = fma(g, xh, sgx);
-        dw[j][e] = fma(d[e], xh, dw[j][e]);
-        db[j][e] = add(db[j][e], d[e]);
+        xh[j][e] = mul(add(xh[j][e], off), scale);
+        db[j][e] = add(db[j][e], g[j][e]);
+        dw[j][e] = fma(g[j][e], xh[j][e], dw[j][e]);
+        g[j][e] = mul(g[j][e], w[e]);
+        sg = add(sg, g[j][e]);
+        sgx = fma(g[j][e], xh[j][e], sgx);
       }
     }
+    fetch(row + step);
     if (!a.dx) continue;
-    const float mg = row_sum<kRow>(total(sg), part[turn]) * inv, mgx = row_sum<kRow>(total(sgx), part[turn + 1]) * inv;
-    const P less = both(-mg, P()), slope = both(-mgx, P());
+    const float2 s = group_sum<kRow>(total(sg), total(sgx), part[turn][group], group);
+    const P less = both(-s.x * inv, P()), slope = both(-s.y * inv, P());
     T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
 #pragma unroll
     for (int j = 0; j < N; j++) {
       const int c = (j * kRow + t) * V;
       if (c >= cols) continue;
-      P w[H], x[H], d[H];
-      load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
-      widen<T, V>(px[j], x);
-      widen<T, V>(pd[j], d);
+      Pack<T, V> out;
 #pragma unroll
-      for (int e = 0; e < H; e++) {
-        const P xh = mul(add(x[e], off), scale);
-        narrow<T, V>(px[j], e, mul(scale, fma(xh, slope, fma(d[e], w[e], less))));
-      }
-      store_pack(dx + c, px[j]);
+      for (int e = 0; e < H; e++) narrow<T, V>(out, e, mul(scale, fma(xh[j][e], slope, add(g[j][e], less))));
+      store_pack(dx + c, out);
     }
   }
   if (!a.partial) return;
   float* out = a.partial + (int64_t)blockIdx.x * 2 * cols;
-  if constexpr (kRows == 1) {
+  if constexpr (kBlockRows == 1) {
 #pragma unroll
     for (int j = 0; j < N; j++) {
       const int c = (j * kRow + t) * V;
@@ -235,23 +249,25 @@ __global__ void __launch_bounds__(kBlock<kRow>, kResident) k_backward(NormArgs a
         *reinterpret_cast<P*>(out + cols + c + e * (V / H)) = db[j][e];
       }
     }
-  } else {
-    __shared__ __align__(16) float all[kRows][2][N * V * kRow];
+  } else {  // the groups' sums one after another
+    __shared__ __align__(16) float all[2][N * V * kRow];
+    for (int q = 0; q < kBlockRows; q++) {
+      if (q == group) {
 #pragma unroll
-    for (int j = 0; j < N; j++)
+        for (int j = 0; j < N; j++)
 #pragma unroll
-      for (int e = 0; e < H; e++) {
-        const int c = (j * kRow + t) * V + e * (V / H);
-        *reinterpret_cast<P*>(&all[threadIdx.x / kRow][0][c]) = dw[j][e];
-        *reinterpret_cast<P*>(&all[threadIdx.x / kRow][1][c]) = db[j][e];
+          for (int e = 0; e < H; e++) {
+            const int c = (j * kRow + t) * V + e * (V / H);
+            P *w = reinterpret_cast<P*>(&all[0][c]), *b = reinterpret_cast<P*>(&all[1][c]);
+            *w = q ? add(*w, dw[j][e]) : dw[j][e];
+            *b = q ? add(*b, db[j][e]) : db[j][e];
+          }
       }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * cols; i += kBlock<kRow>) {
-      const int k = i >= cols, c = i - k * cols;
-      float s = all[0][k][c];
-#pragma unroll
-      for (int q = 1; q < kRows; q++) s += all[q][k][c];
-      out[i] = s;
+      __syncthreads();
+    }
+    for (int i = threadIdx.x; i < cols; i += kBackBlock<kRow>) {
+      out[i] = all[0][i];
+      out[cols + i] = all[1][i];
     }
   }
 }
@@ -357,17 +373,18 @@ bool backward_variant(bool vectors, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
   if (vectors) {
     const int64_t packs = cols / V;
-    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<6>());
-    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<4>());
-    else if (packs <= 128) f(Int<V>(), Int<1>(), Int<128>(), Int<8>());
-    else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>(), Int<5>());
+    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<3>());
+    else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<2>());
+    else if (packs <= 128) f(Int<V>(), Int<2>(), Int<64>(), Int<2>());
+    else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>(), Int<2>());
     else if (packs <= 512) f(Int<V>(), Int<2>(), Int<256>(), Int<2>());
     else if (packs <= 1024) f(Int<V>(), Int<2>(), Int<512>(), Int<1>());
     else if (packs <= 2048 && sizeof(T) == 4) f(Int<4>(), Int<4>(), Int<512>(), Int<1>());  // (16-bit rows would not fit in 128 registers)
     else return false;
   } else {
-    if (cols <= 256) f(Int<1>(), Int<8>(), Int<32>(), Int<5>());
-    else if (cols <= 1024) f(Int<1>(), Int<8>(), Int<128>(), Int<6>());
+    if (cols <= 256) f(Int<1>(), Int<8>(), Int<32>(), Int<3>());
+    else if (cols <= 512) f(Int<1>(), Int<8>(), Int<64>(), Int<3>());
+    else if (cols <= 1024) f(Int<1>(), Int<8>(), Int<128>(), Int<3>());
     else if (cols <= 2048) f(Int<1>(), Int<8>(), Int<256>(), Int<3>());
     else if (cols <= 4096) f(Int<1>(), Int<8>(), Int<512>(), Int<1>());
     else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>(), Int<1>());
@@ -402,16 +419,16 @@ cudaError_t backward(NormArgs a, int w_f32, cudaStream_t s) {
                          on16(a.dy, a.dy_stride, a.rows, sizeof(T)) && on16(a.weight) &&
                          (!a.dx || on16(a.dx, a.dx_stride, a.rows, sizeof(T)));
     const bool held = backward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r, auto b) {
-      constexpr int kRow = decltype(r)::value, kRows = kBlock<kRow> / kRow;
+      constexpr int kRow = decltype(r)::value, kThreads = kBackBlock<kRow>, kRows = kThreads / kRow;
       // as many blocks as stay resident, or a block a group of rows where there are fewer
       static const int resident = [] {
         int fit = 0;
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, k_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value>,
-                                                      kBlock<kRow>, 0);
+                                                      kThreads, 0);
         return std::clamp(fit * kSms, kSms, kMostBlocks);
       }();
       blocks = (int)std::min<int64_t>(resident, (a.rows + kRows - 1) / kRows);
-      k_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value><<<blocks, kBlock<kRow>, 0, s>>>(a, w_f32);
+      k_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value><<<blocks, kThreads, 0, s>>>(a, w_f32);
     });
     if (!held) {
       if (a.dx) k_backward_long<T><<<(unsigned)a.rows, kLong, 0, s>>>(a, w_f32);
