@@ -342,78 +342,99 @@ __global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitc
   }
 }
 
-// rows of `cols` elements to rows that start on 16 bytes (TMA reads no others)
+// Up to three matrices of `cols` columns to rows that start on 16 bytes (TMA reads no others): 8 elements a
+// thread, read one by one and stored together.
+struct PackArgs {
+  const void* from[3];
+  void* to[3];
+  int64_t stride[3], rows[3];
+  int64_t cols, pitch;
+};
 template <typename T>
-__global__ void __launch_bounds__(256) k_pack(const T* from, int64_t stride, int64_t rows, int64_t cols, T* to, int64_t pitch) {
-  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < cols; c += (int64_t)gridDim.x * 256)
-      to[r * pitch + c] = from[r * stride + c];
+__global__ void __launch_bounds__(256) k_pack(PackArgs a) {
+  const int w = blockIdx.y;
+  const T* from = static_cast<const T*>(a.from[w]);
+  const int64_t eights = a.pitch / 8, total = a.rows[w] * eights;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / eights, c = (i - row * eights) * 8;
+    const T* p = from + row * a.stride[w] + c;
+    Pack<T, 8> v;
+#pragma unroll
+    for (int e = 0; e < 8; e++) v.v[e] = c + e < a.cols ? p[e] : from_f32<T>(0.0f);
+    store_pack(static_cast<T*>(a.to[w]) + row * a.pitch + c, v);
+  }
 }
 
-// --------------------------------------------------------------------------- few rows: vectors
-// Up to 8 rows: the weights are read once and are nearly all the traffic, so a warp takes one row of each
-// weight, 16 bytes a lane and load, against every row of x (from L1), sums in registers.
-constexpr int kFewRows = 1;
-
-template <typename T, int R, int V, bool kBackward>
-__global__ void __launch_bounds__(256) k_few(GatedArgs a, T* dg, T* du, int64_t pitch) {
+// ------------------------------------------------------------------------------------ one row: vectors
+// The weights are read once and are nearly all the traffic: a warp takes kPer rows of each weight, 16 bytes a
+// lane and load, against x (from L1), sums in binary32.  (From two rows on the tensor cores are the faster: 8
+// rows, 2048 -> 8192, took 53 us this way and 17 us that way.)
+template <typename T, int V, int kPer, bool kBackward>
+__global__ void __launch_bounds__(128) k_one(GatedArgs a, T* dg, T* du) {
+  using P = Pairs<V>;
+  constexpr int H = kPairs<V>, kUnroll = 16 / (2 * kPer);
   const int lane = threadIdx.x % 32;
-  const int64_t j = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-  if (j >= a.n) return;
-  const T* wg = static_cast<const T*>(a.w_gate) + j * a.g_stride;
-  const T* wu = static_cast<const T*>(a.w_up) + j * a.u_stride;
+  const int64_t j0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / 32) * kPer;
+  if (j0 >= a.n) return;
+  const T *wg[kPer], *wu[kPer];
+  P g[kPer], u[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; q++) {
+    const int64_t j = j0 + q < a.n ? j0 + q : j0;
+    wg[q] = static_cast<const T*>(a.w_gate) + j * a.g_stride;
+    wu[q] = static_cast<const T*>(a.w_up) + j * a.u_stride;
+    g[q] = u[q] = both(0.0f, P());
+  }
   const T* x = static_cast<const T*>(a.x);
-  float g[R] = {}, u[R] = {};
-  constexpr int kUnroll = R > 2 ? 2 : 4;
 #pragma unroll kUnroll
   for (int64_t c = lane * V; c < a.k; c += 32 * V) {
-    const Pack<T, V> pg = load_pack<T, V>(wg + c), pu = load_pack<T, V>(wu + c);
+    P vx[H], vg[kPer][H], vu[kPer][H];
+    Pack<T, V> pg[kPer], pu[kPer];
 #pragma unroll
-    for (int r = 0; r < R; r++) {
-      if (R > 1 && r >= a.rows) break;
-      const Pack<T, V> px = load_pack<T, V>(x + r * a.x_stride + c);
+    for (int q = 0; q < kPer; q++) pg[q] = load_pack<T, V>(wg[q] + c), pu[q] = load_pack<T, V>(wu[q] + c);
+    widen<T, V>(load_pack<T, V>(x + c), vx);
 #pragma unroll
-      for (int e = 0; e < V; e++) {
-        g[r] += to_f32(px.v[e]) * to_f32(pg.v[e]);
-        u[r] += to_f32(px.v[e]) * to_f32(pu.v[e]);
+    for (int q = 0; q < kPer; q++) {
+      widen<T, V>(pg[q], vg[q]);
+      widen<T, V>(pu[q], vu[q]);
+#pragma unroll
+      for (int e = 0; e < H; e++) {
+        g[q] = fma(vx[e], vg[q][e], g[q]);
+        u[q] = fma(vx[e], vu[q][e], u[q]);
       }
     }
   }
 #pragma unroll
-  for (int r = 0; r < R; r++) {
+  for (int q = 0; q < kPer; q++) {
+    float sg = total(g[q]), su = total(u[q]);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-      g[r] += __shfl_xor_sync(~0u, g[r], o);
-      u[r] += __shfl_xor_sync(~0u, u[r], o);
+      sg += __shfl_xor_sync(~0u, sg, o);
+      su += __shfl_xor_sync(~0u, su, o);
     }
-  }
-#pragma unroll
-  for (int r = 0; r < R; r++) {
-    if (lane != r || r >= a.rows) continue;
+    const int64_t j = j0 + q;
+    if (lane != q || j >= a.n) continue;
     float act, da;
-    by_activation(a.act, [&](auto k) { activate<decltype(k)::value>(g[r], &act, &da); });
+    by_activation(a.act, [&](auto k) { activate<decltype(k)::value>(sg, &act, &da); });
     if (kBackward) {
-      const float dh = to_f32(static_cast<const T*>(a.dh)[r * a.dh_stride + j]);
-      dg[r * pitch + j] = from_f32<T>(dh * u[r] * da);
-      du[r * pitch + j] = from_f32<T>(dh * act);
+      const float dh = to_f32(static_cast<const T*>(a.dh)[j]);
+      dg[j] = from_f32<T>(dh * su * da);
+      du[j] = from_f32<T>(dh * act);
     } else {
-      static_cast<T*>(a.h)[r * a.h_stride + j] = from_f32<T>(act * u[r]);
+      static_cast<T*>(a.h)[j] = from_f32<T>(act * su);
     }
   }
 }
 
 template <typename T, bool kBackward>
-void few(const GatedArgs& a, bool vectors, T* dg, T* du, int64_t pitch, cudaStream_t s) {
-  const unsigned grid = (unsigned)((a.n + 7) / 8);
-  const auto go = [&](auto r) {
-    constexpr int R = decltype(r)::value;
-    if (vectors) k_few<T, R, 8, kBackward><<<grid, 256, 0, s>>>(a, dg, du, pitch);
-    else k_few<T, R, 1, kBackward><<<grid, 256, 0, s>>>(a, dg, du, pitch);
-  };
-  if (a.rows == 1) go(std::integral_constant<int, 1>());
-  else if (a.rows == 2) go(std::integral_constant<int, 2>());
-  else if (a.rows <= 4) go(std::integral_constant<int, 4>());
-  else go(std::integral_constant<int, 8>());
+void one(const GatedArgs& a, bool vectors, T* dg, T* du, cudaStream_t s) {
+  // two rows of each weight a warp halve the loads of x; fewer outputs than would fill the SMs go one a warp
+  const bool two = a.n >= 4096;
+  const unsigned grid = (unsigned)((a.n + (two ? 7 : 3)) / (two ? 8 : 4));
+  if (vectors && two) k_one<T, 8, 2, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
+  else if (vectors) k_one<T, 8, 1, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
+  else if (two) k_one<T, 1, 2, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
+  else k_one<T, 1, 1, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
 }
 
 // ------------------------------------------------------------------------------------ launches
@@ -564,14 +585,6 @@ struct Layout {
   }
 };
 
-template <typename T>
-void pack(const void*& p, int64_t& stride, int64_t rows, int64_t cols, void* to, int64_t pitch, cudaStream_t s) {
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(cols, 256), 1024), (unsigned)std::min<int64_t>(rows, 16384));
-  k_pack<T><<<grid, 256, 0, s>>>(static_cast<const T*>(p), stride, rows, cols, static_cast<T*>(to), pitch);
-  p = to;
-  stride = pitch;
-}
-
 bool all_ready(const GatedArgs& a) {
   return tma_ready(a.x, a.x_stride, a.rows, a.k) && tma_ready(a.w_gate, a.g_stride, a.n, a.k) &&
          tma_ready(a.w_up, a.u_stride, a.n, a.k);
@@ -580,10 +593,24 @@ bool all_ready(const GatedArgs& a) {
 template <typename T>
 void make_ready(GatedArgs& a, const Layout& l, bool x, bool weights, cudaStream_t s) {
   char* ws = static_cast<char*>(a.workspace);
-  if (x && !tma_ready(a.x, a.x_stride, a.rows, a.k)) pack<T>(a.x, a.x_stride, a.rows, a.k, ws + l.x, l.k_pitch, s);
-  if (!weights) return;
-  if (!tma_ready(a.w_gate, a.g_stride, a.n, a.k)) pack<T>(a.w_gate, a.g_stride, a.n, a.k, ws + l.gate, l.k_pitch, s);
-  if (!tma_ready(a.w_up, a.u_stride, a.n, a.k)) pack<T>(a.w_up, a.u_stride, a.n, a.k, ws + l.up, l.k_pitch, s);
+  PackArgs p{};
+  int count = 0;
+  int64_t most = 0;
+  const auto add = [&](const void*& from, int64_t& stride, int64_t rows, size_t at) {
+    if (tma_ready(from, stride, rows, a.k)) return;
+    p.from[count] = from; p.stride[count] = stride; p.rows[count] = rows; p.to[count] = ws + at;
+    most = std::max(most, rows);
+    from = ws + at;
+    stride = l.k_pitch;
+    count++;
+  };
+  if (x) add(a.x, a.x_stride, a.rows, l.x);
+  if (weights) add(a.w_gate, a.g_stride, a.n, l.gate), add(a.w_up, a.u_stride, a.n, l.up);
+  if (!count) return;
+  p.cols = a.k;
+  p.pitch = l.k_pitch;
+  const int64_t blocks = std::min<int64_t>(ceil_div(most * (l.k_pitch / 8), 256), kSms * 16);
+  k_pack<T><<<dim3((unsigned)blocks, (unsigned)count), 256, 0, s>>>(p);
 }
 
 // G and U, and h or dG and dU of them
@@ -603,8 +630,8 @@ cudaError_t products(const GatedArgs& a, void* out0, void* out1, int64_t stride,
 template <typename T>
 cudaError_t forward(GatedArgs a, cudaStream_t s) {
   if (a.rows == 0) return cudaSuccess;
-  if (a.rows <= kFewRows) {
-    few<T, false>(a, all_ready(a) && a.k % 8 == 0, nullptr, nullptr, 0, s);
+  if (a.rows == 1) {
+    one<T, false>(a, all_ready(a) && a.k % 8 == 0, nullptr, nullptr, s);
     return cudaGetLastError();
   }
   const Layout l(a.rows, a.k, a.n, false, !all_ready(a));
@@ -627,8 +654,8 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
   T* dg = reinterpret_cast<T*>(ws + l.grad);
   T* du = dg + a.rows * l.n_pitch;
   cudaError_t e;
-  if (a.rows <= kFewRows) {
-    few<T, true>(a, all_ready(a) && a.k % 8 == 0, dg, du, l.n_pitch, s);
+  if (a.rows == 1) {
+    one<T, true>(a, all_ready(a) && a.k % 8 == 0, dg, du, s);
     make_ready<T>(a, l, weights, a.dx != nullptr, s);
   } else {
     make_ready<T>(a, l, true, true, s);
@@ -672,7 +699,7 @@ cudaError_t launch_gated_backward(const GatedArgs& a, ndvm_dtype t, cudaStream_t
   return t == NDVM_F16 ? backward<__half>(a, s) : backward<__nv_bfloat16>(a, s);
 }
 size_t gated_workspace(int64_t rows, int64_t k, int64_t n, bool backward, bool copies) {
-  if (rows == 0 || (!backward && rows <= kFewRows)) return 0;
+  if (rows == 0 || (!backward && rows == 1)) return 0;
   return Layout(rows, k, n, backward, copies).total;
 }
 size_t gated_workspace(const GatedArgs& a, bool backward) { return gated_workspace(a.rows, a.k, a.n, backward, !all_ready(a)); }
