@@ -351,6 +351,25 @@ ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t r
                                 void* dw_gate, void* dw_up, void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * ndvm_gated_forward_keep, ndvm_gated_backward_kept -- the same pair with the pre-activations G = x Wg^T and
+ * U = x Wu^T kept in between instead of computed again.
+ *   kept : device, 16-byte aligned floats, 2 x rows rows (G's, then U's) of ndvm_gated_kept_stride(n), written by
+ *          the one and read by the other; NULL: nothing is kept, as above
+ * Keeping costs 8 bytes an element of h and saves a third of the backward pass's operations: it pays from about
+ * k = 1024 on, and for few rows.
+ */
+int64_t ndvm_gated_kept_stride(int64_t n);
+ndvm_status ndvm_gated_forward_keep(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                    const void* x, int64_t x_stride, const void* w_gate, int64_t g_stride,
+                                    const void* w_up, int64_t u_stride, void* h, int64_t h_stride, float* kept,
+                                    void* workspace, size_t ws_bytes, void* stream);
+ndvm_status ndvm_gated_backward_kept(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                     const void* dh, int64_t dh_stride, const void* x, int64_t x_stride,
+                                     const void* w_gate, int64_t g_stride, const void* w_up, int64_t u_stride,
+                                     const float* kept, void* dx, int64_t dx_stride, void* dw_gate, void* dw_up,
+                                     void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * ndvm_check_operators -- synchronize and report whether a kernel of the network operators gave up a wait on
  * the current device since the last check (NDVM_E_DEVICE_CHECK: its outputs are not valid); clears the flag.
  */

@@ -81,6 +81,11 @@ def load(build_if_missing: bool = True):
                                                   SZ, P]),
             "ndvm_gated_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, I64, P, I64, P, I64, P, I64, P, I64,
                                                    P, I64, P, P, P, SZ, P]),
+            "ndvm_gated_kept_stride": (I64, [I64]),
+            "ndvm_gated_forward_keep": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, I64, P, I64, P, I64, P, I64, P,
+                                                       I64, P, P, SZ, P]),
+            "ndvm_gated_backward_kept": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, I64, P, I64, P, I64, P, I64, P,
+                                                        I64, P, P, I64, P, P, P, SZ, P]),
             "ndvm_check_operators": (ctypes.c_int, []),
             "ndvm_launch_count": (ctypes.c_ulonglong, []),
             "ndvm_measure_fp64_peak": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double), P]),
@@ -432,4 +437,4 @@ def check_device(tape: Tape):
 
 
 from .network import (ACTIVATIONS, check_operators, dropout, dropout_backward, dropout_forward, gated, gated_backward,  # noqa: E402,F401
-                      gated_forward, layer_norm, layer_norm_backward, layer_norm_forward)
+                      gated_forward, gated_kept, layer_norm, layer_norm_backward, layer_norm_forward)

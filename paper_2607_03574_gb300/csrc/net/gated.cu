@@ -1,7 +1,7 @@
 // Gated projection h = act(G) U with G = x Wg^T, U = x Wu^T, and its backward pass:
 //   dU = dh act(G), dG = dh U act'(G), dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.
-// G and U are computed again in the backward pass rather than kept (8 bytes an element in binary32): they stay in
-// binary32 until dG and dU are rounded, once, to the operands' type, which the next products need.
+// The backward pass computes G and U again, or takes those that the forward pass kept: in binary32 (8 bytes an
+// element of h), so that dG and dU are rounded once, to the operands' type, which the next products need.
 //
 // All products run in one kernel frame (k_product): D[m, n] = sum over c of A[m, c] B[n, c], 128 rows a tile,
 // operands by TMA, sums in tensor memory.
@@ -62,6 +62,8 @@ template <int kN> constexpr int kSmem = kStages<kN> * kStageBytes<kN> + kReaders
 struct ProductArgs {
   CUtensorMap a[2], b[2];
   CUtensorMap o[2];              // the results (kGradient: dG and dU), or o[0] the split sums
+  CUtensorMap kept;              // kForward: where G and U go in binary32, if keep
+  int keep;
   int m, n, c;                   // rows and columns of the result, contraction of one segment
   int tiles_m, tiles_n, matrices;  // matrices: results of one shape, by the a's (kWeight: 1 or 2), else 1
   int steps, splits;             // contraction steps of a result, and how many parts they are cut into
@@ -84,6 +86,14 @@ __device__ __forceinline__ void stage_row(uint32_t buffer, int lane, const float
     for (int e = 0; e < 8; e++) o.t[e] = from_f32<T>(v[q * 8 + e]);
     tc::store16(buffer + lane * 64 + ((q ^ (lane >> 1 & 3)) << 4), o.u);
   }
+}
+// and as they are, a line of 128 bytes a row, in the 128-byte swizzle
+__device__ __forceinline__ void stage_row(uint32_t buffer, int lane, const float (&v)[32]) {
+#pragma unroll
+  for (int q = 0; q < 8; q++)
+    tc::store16(buffer + lane * 128 + ((q ^ (lane & 7)) << 4),
+                make_uint4(__float_as_uint(v[q * 4]), __float_as_uint(v[q * 4 + 1]), __float_as_uint(v[q * 4 + 2]),
+                           __float_as_uint(v[q * 4 + 3])));
 }
 // the buffer's rows to rows that start anywhere, a row at a time
 template <typename T>
@@ -254,6 +264,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           fetch(j + 64);
         }
         tc::tmem_loaded();
+        if (kMode == kForward && p.keep) {
+          if (lane == 0) tc::stores_read<0>();
+          __syncwarp();
+          stage_row(mine, lane, v);
+          tc::fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (row0 < p.m) tc::store_box(&p.kept, col, row0, 0, mine);
+            tc::stores_commit();
+            tc::stores_read<0>();
+          }
+          __syncwarp();
+          stage_row(mine, lane, u);
+          tc::fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (row0 < p.m) tc::store_box(&p.kept, col, row0, 1, mine);
+            tc::stores_commit();
+          }
+        }
         if (dual(kMode))
           by_activation(p.act, [&](auto act) {
 #pragma unroll
@@ -271,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           });
         // 4096 bytes hold two pieces of one result (then the other's copy may still be under way), or one
         // of dG and dU or of binary32 sums
-        const bool whole = kMode == kGradient || (!dual(kMode) && p.splits > 1);
+        const bool whole = kMode == kGradient || (kMode == kForward && p.keep) || (!dual(kMode) && p.splits > 1);
         const uint32_t to = mine + (whole ? 0 : buffer * 2048);
         if (lane == 0) {
           if (whole) tc::stores_read<0>();
@@ -279,11 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         }
         __syncwarp();
         if (!dual(kMode) && p.splits > 1) {
-#pragma unroll
-          for (int q = 0; q < 8; q++)  // binary32: a line of 128 bytes a row, in the 128-byte swizzle
-            tc::store16(to + lane * 128 + ((q ^ (lane & 7)) << 4),
-                        make_uint4(__float_as_uint(v[q * 4]), __float_as_uint(v[q * 4 + 1]), __float_as_uint(v[q * 4 + 2]),
-                                   __float_as_uint(v[q * 4 + 3])));
+          stage_row(to, lane, v);
           tc::fence_async();
           __syncwarp();
           if (lane == 0 && row0 < p.m) tc::store_box(&p.o[0], col, row0, it.split * p.matrices + it.matrix, to);
@@ -340,6 +366,51 @@ __global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitc
     for (int e = 0; e < 4; e++)
       if (c + e < n) out[e] = from_f32<T>(v[e]);
   }
+}
+
+// dG and dU of G and U that the forward pass kept: 8 columns a thread
+template <typename T, bool kVectors>
+__global__ void __launch_bounds__(256) k_gradient(const float* kept, int64_t kept_stride, const T* dh, int64_t dh_stride, int64_t rows,
+                                                  int64_t n, int act, T* dg, T* du, int64_t pitch) {
+  const int64_t eights = pitch / 8, total = rows * eights;
+  const float* up = kept + rows * kept_stride;
+  by_activation(act, [&](auto k) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+      const int64_t row = i / eights, c = (i - row * eights) * 8;
+      Pack<T, 8> d;
+      float4 g[2], u[2];
+      const bool all = c + 8 <= n;
+#pragma unroll
+      for (int q = 0; q < 2; q++) {
+        if (all || c + 4 * q < n) {  // (rows of G and U hold whole fours)
+          g[q] = *reinterpret_cast<const float4*>(kept + row * kept_stride + c + 4 * q);
+          u[q] = *reinterpret_cast<const float4*>(up + row * kept_stride + c + 4 * q);
+        } else {
+          g[q] = u[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+      }
+      if (kVectors && all) {
+        d = load_pack<T, 8>(dh + row * dh_stride + c);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) d.v[e] = c + e < n ? dh[row * dh_stride + c + e] : from_f32<T>(0.0f);
+      }
+      Pack<T, 8> og, ou;
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const float4 gq = g[e / 4], uq = u[e / 4];
+        const float ge = e % 4 == 0 ? gq.x : e % 4 == 1 ? gq.y : e % 4 == 2 ? gq.z : gq.w;
+        const float ue = e % 4 == 0 ? uq.x : e % 4 == 1 ? uq.y : e % 4 == 2 ? uq.z : uq.w;
+        float a, da;
+        activate<decltype(k)::value>(ge, &a, &da);
+        const float f = to_f32(d.v[e]);
+        og.v[e] = from_f32<T>(f * ue * da);
+        ou.v[e] = from_f32<T>(f * a);
+      }
+      store_pack(dg + row * pitch + c, og);
+      store_pack(du + row * pitch + c, ou);
+    }
+  });
 }
 
 // Up to three matrices of `cols` columns to rows that start on 16 bytes (TMA reads no others): 8 elements a
@@ -414,6 +485,10 @@ __global__ void __launch_bounds__(128) k_one(GatedArgs a, T* dg, T* du) {
     }
     const int64_t j = j0 + q;
     if (lane != q || j >= a.n) continue;
+    if (!kBackward && a.kept) {
+      a.kept[j] = sg;
+      a.kept[a.kept_stride + j] = su;
+    }
     float act, da;
     by_activation(a.act, [&](auto k) { activate<decltype(k)::value>(sg, &act, &da); });
     if (kBackward) {
@@ -622,6 +697,10 @@ cudaError_t products(const GatedArgs& a, void* out0, void* out1, int64_t stride,
       !map_matrix<T>(&p.b[1], a.w_up, a.n, a.k, a.u_stride, k.width / 2))
     return cudaErrorInvalidValue;
   p.m = (int)a.rows; p.n = (int)a.n; p.c = (int)a.k;
+  if (kMode == kForward && a.kept) {
+    p.keep = 1;
+    if (!map_partial(&p.kept, a.kept, 2, a.rows, a.n, a.kept_stride)) return cudaErrorInvalidValue;
+  }
   p.matrices = 1;
   p.act = a.act; p.out[0] = out0; p.out[1] = out1; p.stride = stride; p.dh = a.dh; p.dh_stride = a.dh_stride;
   return launch_product<T, kMode>(p, k, s);
@@ -654,7 +733,14 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
   T* dg = reinterpret_cast<T*>(ws + l.grad);
   T* du = dg + a.rows * l.n_pitch;
   cudaError_t e;
-  if (a.rows == 1) {
+  if (a.kept) {
+    make_ready<T>(a, l, weights, a.dx != nullptr, s);
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.rows * (l.n_pitch / 8), 256), kSms * 32);
+    const T* dh = static_cast<const T*>(a.dh);
+    const bool vectors = reinterpret_cast<uintptr_t>(dh) % 16 == 0 && (a.rows == 1 || a.dh_stride % 8 == 0);
+    if (vectors) k_gradient<T, true><<<(unsigned)blocks, 256, 0, s>>>(a.kept, a.kept_stride, dh, a.dh_stride, a.rows, a.n, a.act, dg, du, l.n_pitch);
+    else k_gradient<T, false><<<(unsigned)blocks, 256, 0, s>>>(a.kept, a.kept_stride, dh, a.dh_stride, a.rows, a.n, a.act, dg, du, l.n_pitch);
+  } else if (a.rows == 1) {
     one<T, true>(a, all_ready(a) && a.k % 8 == 0, dg, du, s);
     make_ready<T>(a, l, weights, a.dx != nullptr, s);
   } else {

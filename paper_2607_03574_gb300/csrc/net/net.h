@@ -44,6 +44,7 @@ struct GatedArgs {
   const void* dh; int64_t dh_stride;
   void* dx; int64_t dx_stride;
   void* dw_gate; void* dw_up;  // n x k, contiguous
+  float* kept; int64_t kept_stride;  // G and U in binary32 (2 x rows rows), or null
   void* workspace;
 };
 cudaError_t launch_gated_forward(const GatedArgs& a, ndvm_dtype t, cudaStream_t s);

@@ -142,16 +142,28 @@ size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backwa
   return gated_workspace(rows, k, n, backward != 0, !aligned);
 }
 
+int64_t ndvm_gated_kept_stride(int64_t n) { return n < 1 || n >= (int64_t)1 << 31 ? 0 : (n + 3) / 4 * 4; }
+
 ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,
                                int64_t x_stride, const void* w_gate, int64_t g_stride, const void* w_up,
                                int64_t u_stride, void* h, int64_t h_stride, void* workspace, size_t ws_bytes,
                                void* stream) {
+  return ndvm_gated_forward_keep(dtype, act, rows, k, n, x, x_stride, w_gate, g_stride, w_up, u_stride, h, h_stride, nullptr,
+                                 workspace, ws_bytes, stream);
+}
+
+ndvm_status ndvm_gated_forward_keep(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                    const void* x, int64_t x_stride, const void* w_gate, int64_t g_stride,
+                                    const void* w_up, int64_t u_stride, void* h, int64_t h_stride, float* kept,
+                                    void* workspace, size_t ws_bytes, void* stream) {
   if (ndvm_status s = gated_check(dtype, act, rows, k, n, x, x_stride, w_gate, g_stride, w_up, u_stride)) return s;
+  if (!aligned(kept, 16)) return bad("kept must be 16-byte aligned");
   if (rows == 0) return NDVM_OK;
   REFUSE(matrix_out(h, rows, n, h_stride, dtype));
   GatedArgs a{};
   a.rows = rows; a.k = k; a.n = n; a.x = x; a.x_stride = x_stride; a.w_gate = w_gate; a.w_up = w_up;
   a.g_stride = g_stride; a.u_stride = u_stride; a.act = act; a.h = h; a.h_stride = h_stride; a.workspace = workspace;
+  a.kept = kept; a.kept_stride = ndvm_gated_kept_stride(n);
   REFUSE(gated_room(a, false, workspace, ws_bytes));
   return done(launch_gated_forward(a, dtype, (cudaStream_t)stream), "gated projection launch");
 }
@@ -160,6 +172,15 @@ ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t r
                                 const void* dh, int64_t dh_stride, const void* x, int64_t x_stride, const void* w_gate,
                                 int64_t g_stride, const void* w_up, int64_t u_stride, void* dx, int64_t dx_stride,
                                 void* dw_gate, void* dw_up, void* workspace, size_t ws_bytes, void* stream) {
+  return ndvm_gated_backward_kept(dtype, act, rows, k, n, dh, dh_stride, x, x_stride, w_gate, g_stride, w_up, u_stride, nullptr,
+                                  dx, dx_stride, dw_gate, dw_up, workspace, ws_bytes, stream);
+}
+
+ndvm_status ndvm_gated_backward_kept(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                     const void* dh, int64_t dh_stride, const void* x, int64_t x_stride,
+                                     const void* w_gate, int64_t g_stride, const void* w_up, int64_t u_stride,
+                                     const float* kept, void* dx, int64_t dx_stride, void* dw_gate, void* dw_up,
+                                     void* workspace, size_t ws_bytes, void* stream) {
   if (ndvm_status s = gated_check(dtype, act, rows, k, n, x, x_stride, w_gate, g_stride, w_up, u_stride)) return s;
   if (rows > 0) {
     REFUSE(matrix_in(dh, rows, n, dh_stride, dtype));
@@ -167,10 +188,12 @@ ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t r
   }
   REFUSE(vector_in(dw_gate, dtype));
   REFUSE(vector_in(dw_up, dtype));
+  if (!aligned(kept, 16)) return bad("kept must be 16-byte aligned");
   GatedArgs a{};
   a.rows = rows; a.k = k; a.n = n; a.x = x; a.x_stride = x_stride; a.w_gate = w_gate; a.w_up = w_up;
   a.g_stride = g_stride; a.u_stride = u_stride; a.act = act; a.dh = dh; a.dh_stride = dh_stride; a.dx = dx;
   a.dx_stride = dx_stride; a.dw_gate = dw_gate; a.dw_up = dw_up; a.workspace = workspace;
+  a.kept = const_cast<float*>(kept); a.kept_stride = ndvm_gated_kept_stride(n);
   REFUSE(gated_room(a, true, workspace, ws_bytes));
   return done(launch_gated_backward(a, dtype, (cudaStream_t)stream), "gated projection launch");
 }

@@ -268,9 +268,26 @@ def _gated_operands(x, w_gate, w_up, activation, device):
     return act, rows, k, w_gate.shape[0], (px, xs, pg, gs, pu, us), ready
 
 
-def gated_forward(x, w_gate, w_up, activation="silu", h=None, workspace=None, stream=None):
-    """h = act(x w_gate^T) * (x w_up^T): x (..., k), both weights (n, k), h (..., n); 16-bit types.  Outputs
-    and the workspace that this call allocates belong to `stream`."""
+def gated_kept(x, w_gate, stream=None):
+    """A tensor for gated_forward's `kept`: float32 [2, rows, stride], a row's first n elements in use."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    return _new(torch, (2, _rows(x, "x")[0], lib.ndvm_gated_kept_stride(w_gate.shape[0])), torch.float32, _device(torch, x), stream)
+
+
+def _kept(torch, lib, kept, rows, n, device):
+    if kept is None:
+        return None
+    _given(kept, "kept", (2, rows, lib.ndvm_gated_kept_stride(n)), torch.float32, device)
+    if not kept.is_contiguous():
+        raise NdvmError(1, "kept must be contiguous")
+    return kept.data_ptr()
+
+
+def gated_forward(x, w_gate, w_up, activation="silu", h=None, kept=None, workspace=None, stream=None):
+    """h = act(x w_gate^T) * (x w_up^T): x (..., k), both weights (n, k), h (..., n); 16-bit types.  kept: a tensor of
+    gated_kept that receives the two products for gated_backward.  Outputs and the workspace that this call
+    allocates belong to `stream`."""
     torch = _torch_module or _start()
     lib = _nd._lib or load()
     device = _device(torch, x)
@@ -284,16 +301,17 @@ def gated_forward(x, w_gate, w_up, activation="silu", h=None, workspace=None, st
         hs = _rows(h, "h")[2]
     need = 0 if ready else lib.ndvm_gated_workspace_bytes(rows, k, n, 0, 0)
     ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
-    status = lib.ndvm_gated_forward(code, act, rows, k, n, *operands, h.data_ptr(), hs, wp, nbytes,
-                                    _stream(torch, stream, device))
+    status = lib.ndvm_gated_forward_keep(code, act, rows, k, n, *operands, h.data_ptr(), hs,
+                                         _kept(torch, lib, kept, rows, n, device), wp, nbytes, _stream(torch, stream, device))
     if status:
         _check(status)
     return h
 
 
 def gated_backward(dh, x, w_gate, w_up, activation="silu", wants=(True, True, True), dx=None, dw_gate=None, dw_up=None,
-                   workspace=None, stream=None):
-    """(dx, dw_gate, dw_up) of gated_forward; `wants` says which (the others are None)."""
+                   kept=None, workspace=None, stream=None):
+    """(dx, dw_gate, dw_up) of gated_forward; `wants` says which (the others are None).  kept: what the forward
+    call kept (None: the two products are computed again)."""
     torch = _torch_module or _start()
     lib = _nd._lib or load()
     device = _device(torch, x)
@@ -323,8 +341,9 @@ def gated_backward(dh, x, w_gate, w_up, activation="silu", wants=(True, True, Tr
         up = dw_up.data_ptr()
     need = lib.ndvm_gated_workspace_bytes(rows, k, n, 1, ready)
     ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
-    status = lib.ndvm_gated_backward(code, act, rows, k, n, dh.data_ptr(), _rows(dh, "dh")[2], *operands, xp, dxs, gp, up, wp,
-                                     nbytes, _stream(torch, stream, device))
+    status = lib.ndvm_gated_backward_kept(code, act, rows, k, n, dh.data_ptr(), _rows(dh, "dh")[2], *operands,
+                                          _kept(torch, lib, kept, rows, n, device), xp, dxs, gp, up, wp, nbytes,
+                                          _stream(torch, stream, device))
     if status:
         _check(status)
     return dx, dw_gate, dw_up

@@ -387,6 +387,26 @@ def test_gated_matches_64_bits(ndvm, cuda, rows, k, n, t):
             assert rel <= 3 * RMS[t], (name, rel)
 
 
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,k,n", GATED_SIZES[::2] + [(1, 40, 1001), (130, 72, 1001), (300, 1100, 136)])
+def test_gated_with_kept_products(ndvm, cuda, rows, k, n, t):
+    """The same bounds with the products kept; h has the bits of the call that keeps nothing."""
+    import torch
+    act = ["silu", "gelu", "relu", "sigmoid"][(rows + k + n) % 4]
+    x, wg, wu, dh = _gated_case(rows * 7919 + k * 31 + n, rows, k, n, t)
+    kept = ndvm.gated_kept(x, wg)
+    h = ndvm.gated_forward(x, wg, wu, act, kept=kept)
+    assert torch.equal(h, ndvm.gated_forward(x, wg, wu, act))
+    for i, w in enumerate((wg, wu)):  # G and U themselves, in binary32
+        exact = x.double() @ w.double().t()
+        _inside(kept[i, :, :n], exact, 2 * U * (k + 8) * (x.double().abs() @ w.double().abs().t()), "kept")
+    for d in (dh, _strided(dh, 3, 1)):
+        got = (h,) + ndvm.gated_backward(d, x, wg, wu, act, kept=kept)
+        want, err = _gated64(*(v.double() for v in (x, wg, wu, dh)), act, t)
+        for name, a, v, e in zip(("h", "dx", "dw_gate", "dw_up"), got, want, err):
+            _inside(a, v, _rounded(v, e, t), name)
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu", "sigmoid"])
 @pytest.mark.parametrize("rows", [1, 6, 200])
 def test_gated_activations(ndvm, cuda, act, rows):
@@ -615,6 +635,8 @@ def test_refusals(ndvm, cuda):
         lambda: ndvm.gated_backward(dh[:, :39], x, wg, wu),
         lambda: ndvm.gated_backward(dh, x, wg, wu, workspace=f[:4]),
         lambda: ndvm.gated_backward(dh, x, wg, wu, dw_gate=wg[:, :23]),
+        lambda: ndvm.gated_forward(x, wg, wu, kept=torch.empty(2, 8, 39, device="cuda")),
+        lambda: ndvm.gated_backward(dh, x, wg, wu, kept=torch.empty(2, 8, 40, device="cuda").half()),
     ]
     for i, call in enumerate(calls):
         with pytest.raises(E):
