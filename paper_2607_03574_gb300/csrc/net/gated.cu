@@ -54,10 +54,13 @@ __host__ __device__ constexpr bool a_rows(Mode m) { return m == kWeight; }
 __host__ __device__ constexpr bool b_rows(Mode m) { return m == kInput || m == kWeight; }
 __host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == kGradient; }
 
-template <int kN> constexpr int kStageBytes = (kM + kN) * kC * 2;
-template <int kN> constexpr int kStages = 196608 / kStageBytes<kN> < 8 ? 196608 / kStageBytes<kN> : 8;
-constexpr int kStaging = 4096;  // of each warp that reads sums: what its stores are made from
-template <int kN> constexpr int kSmem = kStages<kN> * kStageBytes<kN> + kReaders * kStaging + 1024 /* alignment */ + 256 /* barriers */;
+// A block's share: kN columns of sums for its 128 rows, of whose operand B a pair's blocks hold half each.
+template <int kN, int kCtas> constexpr int kStageBytes = (kM + kN / kCtas) * kC * 2;
+template <int kCtas> constexpr int kStaging = 4096 * kCtas;  // of each warp that reads sums: what its stores are made from
+template <int kN, int kCtas>
+constexpr int kStages = std::min(8, (229376 - kReaders * kStaging<kCtas>) / kStageBytes<kN, kCtas>);
+template <int kN, int kCtas>
+constexpr int kSmem = kStages<kN, kCtas> * kStageBytes<kN, kCtas> + kReaders * kStaging<kCtas> + 1024 /* alignment */ + 256 /* barriers */;
 
 struct ProductArgs {
   CUtensorMap a[2], b[2];
@@ -102,51 +105,54 @@ __device__ __forceinline__ void unstage(const char* buffer, int lane, T* out, in
     if (lane < cols) out[r * stride + lane] = *reinterpret_cast<const T*>(buffer + r * 64 + ((lane / 8 ^ (r >> 1 & 3)) << 4) + lane % 8 * 2);
 }
 
-template <typename T, Mode kMode, int kN>
+template <typename T, Mode kMode, int kN, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ ProductArgs p) {
   extern __shared__ char raw[];
-  constexpr int S = kStages<kN>;
+  constexpr int S = kStages<kN, kCtas>, kStage = kStageBytes<kN, kCtas>;
   constexpr uint32_t kABytes = kM * kC * 2;
   constexpr int kColumns = 2 * kN;  // of tensor memory: two tiles' sums
   constexpr int kOutN = dual(kMode) ? kN / 2 : kN;
   __shared__ uint32_t s_tmem;
   __shared__ int s_stop;
   const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
-  const uint32_t staging = base + S * kStageBytes<kN>, bars = staging + kReaders * kStaging;
+  const uint32_t staging = base + S * kStage, bars = staging + kReaders * kStaging<kCtas>;
   const auto full = [&](int i) { return bars + i * 8; };
   const auto empty = [&](int i) { return bars + (S + i) * 8; };
   const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
   const auto taken = [&](int i) { return bars + (2 * S + 2 + i) * 8; };  // and have been read
   const uint32_t drain = bars + (2 * S + 4) * 8;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int rank = kCtas == 1 ? 0 : (int)tc::cluster_rank(), unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
   volatile int* stop = &s_stop;
 
   if (threadIdx.x == 0) {
     s_stop = 0;
     for (int i = 0; i < S; i++) tc::barrier_init(full(i), 1), tc::barrier_init(empty(i), 1);
-    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), kReaders);
+    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), kReaders * kCtas);
     tc::barrier_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tc::tmem_alloc<kColumns>(tc::smem(&s_tmem));
+  if (warp == 1) tc::tmem_alloc<kCtas, kColumns>(tc::smem(&s_tmem));
   tc::fence_before();
   __syncthreads();
+  if (kCtas == 2) tc::cluster_sync();
   tc::fence_after();
   const uint32_t tmem = s_tmem;
 
   const int tiles = p.tiles_m * p.tiles_n, items = tiles * p.matrices * p.splits;
   const int segment = (p.c + kC - 1) / kC;  // steps of one segment
   struct Item { int m0, n0, matrix, split, from, to; };
-  // tiles in bands of 16 rows of tiles, down a band first: blocks that run together share operands in L2
+  constexpr int kBand = 16 / kCtas;
+  // tiles in bands of 2048 rows, down a band first: blocks that run together share operands in L2
   const auto item = [&](int i) {
     Item it;
     it.split = i / (tiles * p.matrices);
     i -= it.split * (tiles * p.matrices);
     it.matrix = i / tiles;
     i -= it.matrix * tiles;
-    const int band = i / (16 * p.tiles_n), first = band * 16, height = min(16, p.tiles_m - first);
-    i -= band * 16 * p.tiles_n;
-    it.m0 = (first + i % height) * kM;
+    const int band = i / (kBand * p.tiles_n), first = band * kBand, height = min(kBand, p.tiles_m - first);
+    i -= band * kBand * p.tiles_n;
+    it.m0 = ((first + i % height) * kCtas + rank) * kM;
     it.n0 = i / height * kOutN;
     it.from = (int)((int64_t)p.steps * it.split / p.splits);
     it.to = (int)((int64_t)p.steps * (it.split + 1) / p.splits);
@@ -159,61 +165,65 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     uint32_t phase = 0;
     int issued = 0;
     bool ok = true;
-    for (int i = blockIdx.x; ok && i < items; i += gridDim.x) {
+    for (int i = unit; ok && i < items; i += units) {
       const Item it = item(i);
       for (int s = it.from; s < it.to; s++) {
         if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, stop))) break;
-        const uint32_t a = base + stage * kStageBytes<kN>, b = a + kABytes, bar = full(stage);
-        tc::barrier_expect(bar, a_rows(kMode) ? kStageBytes<kN> : kStageBytes<kN> - kABytes + p.a_box * kC * 2);
+        const uint32_t a = base + stage * kStage, b = a + kABytes, bar = kCtas == 1 ? full(stage) : tc::in_first(full(stage));
+        const int bytes = a_rows(kMode) ? kStage : kStage - (int)kABytes + p.a_box * kC * 2;
+        if (rank == 0) tc::barrier_expect(full(stage), kCtas * bytes);
         const int seg = kMode == kInput ? s / segment : kMode == kWeight ? it.matrix : 0;
         const int c = (kMode == kInput ? s - seg * segment : s) * kC;
         if (a_rows(kMode)) {
-          for (int q = 0; q < kM / 64; q++) tc::load_box(a + q * 8192, &p.a[seg], it.m0 + q * 64, c, bar);
+          for (int q = 0; q < kM / 64; q++) tc::load_box<kCtas>(a + q * 8192, &p.a[seg], it.m0 + q * 64, c, bar);
         } else {
-          tc::load_box(a, &p.a[seg], c, it.m0, bar);
+          tc::load_box<kCtas>(a, &p.a[seg], c, it.m0, bar);
         }
-        if (dual(kMode)) {
-          tc::load_box(b, &p.b[0], c, it.n0, bar);
-          tc::load_box(b + kN / 2 * kC * 2, &p.b[1], c, it.n0, bar);
+        if (dual(kMode) && kCtas == 2) {
+          tc::load_box<kCtas>(b, &p.b[rank], c, it.n0, bar);
+        } else if (dual(kMode)) {
+          tc::load_box<kCtas>(b, &p.b[0], c, it.n0, bar);
+          tc::load_box<kCtas>(b + kN / 2 * kC * 2, &p.b[1], c, it.n0, bar);
         } else {
-          for (int q = 0; q < kN / 64; q++) tc::load_box(b + q * 8192, &p.b[kMode == kInput ? seg : 0], it.n0 + q * 64, c, bar);
+          for (int q = 0; q < kN / kCtas / 64; q++)
+            tc::load_box<kCtas>(b + q * 8192, &p.b[kMode == kInput ? seg : 0], it.n0 + rank * (kN / kCtas) + q * 64, c, bar);
         }
         issued++;
         if (++stage == S) stage = 0, phase ^= 1;
       }
     }
-    if (!ok)  // the copies in flight end before the block does
+    if (!ok && rank == 0)  // the copies in flight end before the block does (a pair's second waits for its first)
       for (int k = 1; k <= min(issued, S); k++) {
         const int at = (issued - k) % S, turn = (issued - k) / S;
         tc::barrier_drain(full(at), turn & 1);
       }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1 && lane == 0 && rank == 0) {
     // ---- products
-    constexpr uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, a_rows(kMode), b_rows(kMode), kM, kN);
+    constexpr uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, a_rows(kMode), b_rows(kMode), kM * kCtas, kN);
     int stage = 0, slot = 0;
     uint32_t phase = 0, slot_phase = 0;
     bool ok = true;
-    for (int i = blockIdx.x; ok && i < items; i += gridDim.x) {
+    for (int i = unit; ok && i < items; i += units) {
       const Item it = item(i);
       if (!(ok = tc::barrier_wait(taken(slot), slot_phase ^ 1, stop))) break;
       tc::fence_after();
       for (int s = it.from; s < it.to; s++) {
         if (!(ok = tc::barrier_wait(full(stage), phase, stop))) break;
         tc::fence_after();
-        const uint32_t at = base + stage * kStageBytes<kN>;
+        const uint32_t at = base + stage * kStage;
         const uint64_t a = tc::operand(at, a_rows(kMode)), b = tc::operand(at + kABytes, b_rows(kMode));
 #pragma unroll
         for (int q = 0; q < kC / 16; q++)  // 16 of the contraction: 32 bytes along a line, or 16 lines
-          tc::mma(tmem + slot * kN, a + q * (a_rows(kMode) ? 2048 >> 4 : 32 >> 4), b + q * (b_rows(kMode) ? 2048 >> 4 : 32 >> 4),
+          tc::mma<kCtas>(tmem + slot * kN, a + q * (a_rows(kMode) ? 2048 >> 4 : 32 >> 4), b + q * (b_rows(kMode) ? 2048 >> 4 : 32 >> 4),
                   desc, s > it.from || q > 0);
-        tc::commit(empty(stage));
+        tc::commit<kCtas>(empty(stage));
         if (++stage == S) stage = 0, phase ^= 1;
       }
-      tc::commit(done(slot));
+      tc::commit<kCtas>(done(slot));
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
     if (!ok) {  // the products in flight end before tensor memory is freed
-      tc::commit(drain);
+      tc::commit<kCtas>(drain);
       tc::barrier_drain(drain, 0);
     }
   } else if (warp >= 2) {
@@ -221,13 +231,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     // columns, by way of staging that asynchronous copies empty.  (Two warps a scheduler: one alone left the
     // latencies of the reads, the copies and dh in the open.  4096 rows, 1024 -> 4096: TODO)
     const int lanes = (warp % 4) * 32;
-    const uint32_t mine = staging + (warp - 2) * kStaging;
+    const uint32_t mine = staging + (warp - 2) * kStaging<kCtas>;
     const char* const mine_ptr = raw + (mine - tc::smem(raw));
     const int first = (warp - 2) / 4 * 32;
     int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
     const bool vec_dh = kMode == kGradient && reinterpret_cast<uintptr_t>(p.dh) % 16 == 0 && p.dh_stride % 8 == 0;
-    for (int i = blockIdx.x; i < items; i += gridDim.x) {
+    for (int i = unit; i < items; i += units) {
       const Item it = item(i);
       const int row0 = it.m0 + lanes, row = row0 + lane;
       Pack<T, 8> next[4];  // dh of the columns to come: asked for a piece ahead, the first before the wait for the sums
@@ -264,24 +274,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           fetch(j + 64);
         }
         tc::tmem_loaded();
-        if (kMode == kForward && p.keep) {
+        if (kMode == kForward && p.keep) {  // G and then U to memory, as binary32
           if (lane == 0) tc::stores_read<0>();
           __syncwarp();
           stage_row(mine, lane, v);
+          if (kCtas == 2) stage_row(mine + 4096, lane, u);
           tc::fence_async();
           __syncwarp();
           if (lane == 0) {
             if (row0 < p.m) tc::store_box(&p.kept, col, row0, 0, mine);
+            if (row0 < p.m && kCtas == 2) tc::store_box(&p.kept, col, row0, 1, mine + 4096);
             tc::stores_commit();
-            tc::stores_read<0>();
+            if (kCtas == 1) tc::stores_read<0>();
           }
-          __syncwarp();
-          stage_row(mine, lane, u);
-          tc::fence_async();
-          __syncwarp();
-          if (lane == 0) {
-            if (row0 < p.m) tc::store_box(&p.kept, col, row0, 1, mine);
-            tc::stores_commit();
+          if (kCtas == 1) {
+            __syncwarp();
+            stage_row(mine, lane, u);
+            tc::fence_async();
+            __syncwarp();
+            if (lane == 0) {
+              if (row0 < p.m) tc::store_box(&p.kept, col, row0, 1, mine);
+              tc::stores_commit();
+            }
           }
         }
         if (dual(kMode))
@@ -299,12 +313,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
               }
             }
           });
-        // 4096 bytes hold two pieces of one result (then the other's copy may still be under way), or one
-        // of dG and dU or of binary32 sums
-        const bool whole = kMode == kGradient || (kMode == kForward && p.keep) || (!dual(kMode) && p.splits > 1);
-        const uint32_t to = mine + (whole ? 0 : buffer * 2048);
+        // A piece takes 2048 bytes of 16-bit results, or 4096 for both of dG and dU or for binary32: the staging
+        // holds two (then the other's copy may still be under way) or one.
+        const bool large = kMode == kGradient || (!dual(kMode) && p.splits > 1);
+        const bool alone = (large && kCtas == 1) || (kMode == kForward && p.keep);
+        const uint32_t to = mine + (alone ? 0 : buffer * (large ? 4096 : 2048));
         if (lane == 0) {
-          if (whole) tc::stores_read<0>();
+          if (alone) tc::stores_read<0>();
           else tc::stores_read<1>();
         }
         __syncwarp();
@@ -334,7 +349,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
       }
       tc::fence_before();
       __syncwarp();
-      if (lane == 0) tc::barrier_arrive(taken(slot));
+      if (lane == 0) {
+        if (kCtas == 1) tc::barrier_arrive(taken(slot));
+        else tc::barrier_arrive_cluster(tc::in_first(taken(slot)));
+      }
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
     if (lane == 0) tc::stores_done();
@@ -342,8 +360,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   __syncwarp();
   __syncthreads();
   if (threadIdx.x == 0 && s_stop) g_stopped = 1;
+  __syncwarp();
+  tc::fence_before();
+  if (kCtas == 2) tc::cluster_sync();  // neither block's memory is in the other's use any more
   tc::fence_after();
-  if (warp == 1) tc::tmem_free<kColumns>(tmem);
+  if (warp == 1) tc::tmem_free<kCtas, kColumns>(tmem);
 }
 
 // the parts of split sums added up in order, and rounded: 4 columns a thread
@@ -560,52 +581,64 @@ bool map_partial(CUtensorMap* map, float* p, int64_t parts, int64_t m, int64_t n
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns of a tile's sums.  A round of tiles over the SMs takes about as long as its columns, narrower ones a
-// little longer (more bytes an operation: measured TODO).
-int tile_width(int64_t m, int64_t n, bool two) {
-  int best = 256;
-  double least = 1e300;
-  for (int w : {256, 128, 64}) {
-    const double rounds = (double)ceil_div(ceil_div(m, kM) * ceil_div(n, two ? w / 2 : w), kSms);
-    const double cost = rounds * (w == 256 ? 1.0 : w == 128 ? 0.6 : 0.4);
-    if (cost < least) least = cost, best = w;
-  }
-  return best;
-}
 // Parts that a result's contraction is cut into: enough for every SM to have one, none shorter than 8 steps.
 int split_count(int64_t tiles, int64_t steps) {
   if (tiles >= kSms) return 1;
   return (int)std::clamp<int64_t>(kSms / tiles, 1, std::max<int64_t>(steps / 8, 1));
 }
 
-template <typename T, Mode kMode, int kN>
+template <typename T, Mode kMode, int kN, int kCtas>
 cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
   static const cudaError_t set =
-      cudaFuncSetAttribute(k_product<T, kMode, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kN>);
+      cudaFuncSetAttribute(k_product<T, kMode, kN, kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kN, kCtas>);
   if (set != cudaSuccess) return set;
   const int items = p.tiles_m * p.tiles_n * p.matrices * p.splits;
-  k_product<T, kMode, kN><<<std::min(items, kSms), kThreads, kSmem<kN>, s>>>(p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3((unsigned)std::min(items, kSms / kCtas) * kCtas);
+  c.blockDim = dim3(kThreads);
+  c.dynamicSmemBytes = kSmem<kN, kCtas>;
+  c.stream = s;
+  cudaLaunchAttribute cluster{};
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = kCtas;
+  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  c.attrs = &cluster;
+  c.numAttrs = kCtas == 1 ? 0 : 1;
+  return cudaLaunchKernelEx(&c, k_product<T, kMode, kN, kCtas>, p);
 }
+
+// how a product of the given size is cut up: columns and rows of a tile's sums (256 rows are a pair's), parts
+struct Cut { int width, ctas, splits; };
 
 int a_box(int64_t m) { return (int)std::min<int64_t>(up(m, 8), kM); }
 
-// how a product of the given size is cut up (the weights' gradients as if both were wanted: one of them
-// alone has the same bits)
-struct Cut { int width, splits; };
+// A round of tiles over the SMs takes about as long as its columns; narrower tiles take a little longer for
+// them (more bytes an operation) and a pair's a little less (16384 x 2048 -> 8192 forward: 640 us alone, 598 in
+// pairs), if its contraction has 12 steps or more: pairs start and end together, which costs short ones (4096 x 256 ->
+// 1024: 9.1 us alone, 10.6 in pairs).  The weights' gradients are cut as if both were wanted: one of them alone
+// has the same bits.
 Cut cut(Mode mode, int64_t m, int64_t n, int64_t c) {
-  Cut k;
+  struct Shape { int width, ctas; double time; };
+  static constexpr Shape shapes[] = {{256, 2, 0.9}, {256, 1, 1.0}, {128, 1, 0.6}, {64, 1, 0.4}};
   const int matrices = mode == kWeight ? 2 : 1;
-  k.width = tile_width(m * matrices, n, dual(mode));
-  const int64_t tiles = matrices * ceil_div(m, kM) * ceil_div(n, dual(mode) ? k.width / 2 : k.width);
-  k.splits = dual(mode) ? 1 : split_count(tiles, ceil_div(c, kC) * (mode == kInput ? 2 : 1));
-  return k;
+  Cut best{};
+  double least = 1e300;
+  int64_t best_tiles = 0;
+  const int64_t steps = ceil_div(c, kC) * (mode == kInput ? 2 : 1);
+  for (const Shape& s : shapes) {
+    if (s.ctas == 2 && steps < 12) continue;
+    const int64_t tiles = matrices * ceil_div(m, kM * s.ctas) * ceil_div(n, dual(mode) ? s.width / 2 : s.width);
+    const double time = (double)ceil_div(tiles, kSms / s.ctas) * s.time;
+    if (time < least) least = time, best.width = s.width, best.ctas = s.ctas, best_tiles = tiles;
+  }
+  best.splits = dual(mode) ? 1 : split_count(best_tiles * best.ctas, steps);
+  return best;
 }
 
 template <typename T, Mode kMode>
 cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s) {
   const int out = dual(kMode) ? k.width / 2 : k.width;
-  p.tiles_m = (int)ceil_div(p.m, kM);
+  p.tiles_m = (int)ceil_div(p.m, kM * k.ctas);
   p.tiles_n = (int)ceil_div(p.n, out);
   p.steps = (int)ceil_div(p.c, kC) * (kMode == kInput ? 2 : 1);
   p.splits = k.splits;
@@ -622,9 +655,10 @@ cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s) {
     }
   }
   if ((int64_t)p.tiles_m * p.tiles_n * p.matrices * p.splits > 0x40000000) return cudaErrorInvalidConfiguration;
-  const cudaError_t e = k.width == 256   ? launch_width<T, kMode, 256>(p, s)
-                        : k.width == 128 ? launch_width<T, kMode, 128>(p, s)
-                                         : launch_width<T, kMode, 64>(p, s);
+  const cudaError_t e = k.ctas == 2      ? launch_width<T, kMode, 256, 2>(p, s)
+                        : k.width == 256 ? launch_width<T, kMode, 256, 1>(p, s)
+                        : k.width == 128 ? launch_width<T, kMode, 128, 1>(p, s)
+                                         : launch_width<T, kMode, 64, 1>(p, s);
   if (e != cudaSuccess || p.splits == 1) return e;
   const int64_t total = (int64_t)p.matrices * p.m * p.partial_pitch / 4;
   k_join<T><<<(unsigned)std::min<int64_t>(ceil_div(total, 256), kSms * 8), 256, 0, s>>>(
