@@ -19,19 +19,19 @@ struct Words { uint32_t w[4]; };
 __device__ __forceinline__ void product(uint32_t a, uint32_t m, uint32_t* high, uint32_t* low) {
   asm("{\n .reg .u64 t;\n mul.wide.u32 t, %2, %3;\n mov.b64 {%1, %0}, t;\n}" : "=r"(*high), "=r"(*low) : "r"(a), "r"(m));
 }
-__device__ __forceinline__ Words philox(uint64_t block, uint32_t k0, uint32_t k1) {
+// The rounds' keys are the launch's: the host works them out once (constant operands here).
+struct Keys { uint32_t k[10][2]; };
+__device__ __forceinline__ Words philox(uint64_t block, const Keys& keys) {
   uint32_t a = (uint32_t)block, b = (uint32_t)(block >> 32), c = 0, d = 0;
 #pragma unroll
   for (int r = 0; r < 10; r++) {
     uint32_t p1, p0, q1, q0;
     product(a, 0xD2511F53u, &p1, &p0);
     product(c, 0xCD9E8D57u, &q1, &q0);
-    a = q1 ^ b ^ k0;
+    a = q1 ^ b ^ keys.k[r][0];
     b = q0;
-    c = p1 ^ d ^ k1;
+    c = p1 ^ d ^ keys.k[r][1];
     d = p0;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
   }
   return {{a, b, c, d}};
 }
@@ -49,13 +49,13 @@ __device__ __forceinline__ float2 drop(const DropArgs& a, uint32_t w0, uint32_t 
 
 // 16 bytes of x (and of the residual) from its v-th vector on
 template <typename T, bool kResidual>
-__device__ __forceinline__ void drop_vector(const DropArgs& a, const T* x, const T* r, T* y, uint64_t block) {
+__device__ __forceinline__ void drop_vector(const DropArgs& a, const Keys& keys, const T* x, const T* r, T* y, uint64_t block) {
   constexpr int V = 16 / sizeof(T);
   Pack<T, V> p = load_pack<T, V>(x), pr;
   if (kResidual) pr = load_pack<T, V>(r);
 #pragma unroll
   for (int q = 0; q < V / 4; q++) {
-    const Words w = philox(block + q, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+    const Words w = philox(block + q, keys);
 #pragma unroll
     for (int e = 0; e < 4; e += 2) {
       float2 d = drop(a, w.w[e], w.w[e + 1], widen(p.v + q * 4 + e));
@@ -66,34 +66,37 @@ __device__ __forceinline__ void drop_vector(const DropArgs& a, const T* x, const
   store_pack(y, p);
 }
 
-// Contiguous tensors (one row of any length): bound by memory with a residual (134 M bfloat16 elements:
-// TODO).  One vector a thread: threads that took several, with the next loads in flight or not, were slower
-// (143 to 191 us; 127 at best).
+// Contiguous tensors (one row of any length).  With a residual bound by memory: 134 M bfloat16 elements in 113 us,
+// 7.1 TB/s; without, by the generator's instructions: 105 us, 5.1 TB/s (half as many a byte in binary32: 6.7 TB/s).
+// One vector a thread and all the threads an SM holds: with 40 of its 64 warps 126 us, with several vectors a
+// thread, the next one's loads in flight or not, 143 to 191 us.
 template <typename T, bool kResidual>
-__global__ void __launch_bounds__(kThreads, 5) k_dropout_flat(DropArgs a) {
+__global__ void __launch_bounds__(kThreads, 8) k_dropout_flat(const __grid_constant__ DropArgs a, const __grid_constant__ Keys keys) {
   constexpr int V = 16 / sizeof(T);
   const T *x = static_cast<const T*>(a.x), *r = static_cast<const T*>(a.residual);
   T* y = static_cast<T*>(a.y);
   const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x, vectors = a.cols / V;
   if (v < vectors) {
-    drop_vector<T, kResidual>(a, x + v * V, kResidual ? r + v * V : r, y + v * V, a.offset / 4 + (uint64_t)v * (V / 4));
+    drop_vector<T, kResidual>(a, keys, x + v * V, kResidual ? r + v * V : r, y + v * V, a.offset / 4 + (uint64_t)v * (V / 4));
   } else if (v == vectors) {  // what is left beyond the vectors
-    for (int64_t c = vectors * V; c < a.cols; c++) {
-      const Words w = philox(a.offset / 4 + (uint64_t)(c / 4), (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
-      const uint32_t word = c % 4 == 0 ? w.w[0] : c % 4 == 1 ? w.w[1] : c % 4 == 2 ? w.w[2] : w.w[3];
-      y[c] = drop<T, kResidual>(a, word, x[c], kResidual ? r[c] : x[c]);
+#pragma unroll 1
+    for (int64_t c = vectors * V; c < a.cols; c += 4) {
+      const Words w = philox(a.offset / 4 + (uint64_t)(c / 4), keys);
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        if (c + e < a.cols) y[c + e] = drop<T, kResidual>(a, w.w[e], x[c + e], kResidual ? r[c + e] : x[c + e]);
     }
   }
 }
 
 // rows of whole vectors that start on 16 bytes
 template <typename T, bool kResidual>
-__global__ void __launch_bounds__(kThreads, 5) k_dropout_rows(DropArgs a) {
+__global__ void __launch_bounds__(kThreads, 8) k_dropout_rows(const __grid_constant__ DropArgs a, const __grid_constant__ Keys keys) {
   constexpr int V = 16 / sizeof(T);
   const int64_t v = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, vectors = a.cols / V;
   if (v >= vectors) return;
   for (int64_t row = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; row < a.rows; row += (int64_t)gridDim.y * blockDim.y)
-    drop_vector<T, kResidual>(a, static_cast<const T*>(a.x) + row * a.x_stride + v * V,
+    drop_vector<T, kResidual>(a, keys, static_cast<const T*>(a.x) + row * a.x_stride + v * V,
                               kResidual ? static_cast<const T*>(a.residual) + row * a.r_stride + v * V : nullptr,
                               static_cast<T*>(a.y) + row * a.y_stride + v * V,
                               a.offset / 4 + (uint64_t)(row * vectors + v) * (V / 4));
@@ -102,8 +105,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_dropout_rows(DropArgs a) {
 // Any layout: a generator block a thread and step, of which the row's elements are taken (a block that
 // two rows share is drawn for both).
 template <typename T, bool kResidual>
-__global__ void __launch_bounds__(kThreads) k_dropout_elements(DropArgs a) {
-  const uint32_t k0 = (uint32_t)a.seed, k1 = (uint32_t)(a.seed >> 32);
+__global__ void __launch_bounds__(kThreads) k_dropout_elements(const __grid_constant__ DropArgs a, const __grid_constant__ Keys keys) {
   for (int64_t row = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; row < a.rows; row += (int64_t)gridDim.y * blockDim.y) {
     const int64_t i0 = row * a.cols, g = i0 / 4 + (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int64_t c0 = g * 4 - i0;  // the column of the block's first word
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(kThreads) k_dropout_elements(DropArgs a) {
     const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
     const T* r = kResidual ? static_cast<const T*>(a.residual) + row * a.r_stride : x;
     T* y = static_cast<T*>(a.y) + row * a.y_stride;
-    const Words w = philox(a.offset / 4 + (uint64_t)g, k0, k1);
+    const Words w = philox(a.offset / 4 + (uint64_t)g, keys);
 #pragma unroll
     for (int e = 0; e < 4; e++) {
       const int64_t c = c0 + e;
@@ -123,6 +125,11 @@ __global__ void __launch_bounds__(kThreads) k_dropout_elements(DropArgs a) {
 template <typename T, bool kResidual>
 cudaError_t launch(DropArgs a, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T);
+  Keys keys;
+  for (int r = 0; r < 10; r++) {
+    keys.k[r][0] = (uint32_t)a.seed + (uint32_t)r * 0x9E3779B9u;
+    keys.k[r][1] = (uint32_t)(a.seed >> 32) + (uint32_t)r * 0xBB67AE85u;
+  }
   auto dense = [&](int64_t stride) { return a.rows == 1 || stride == a.cols; };
   if (dense(a.x_stride) && dense(a.y_stride) && (!kResidual || dense(a.r_stride))) {
     a.cols *= a.rows;  // one row
@@ -136,7 +143,7 @@ cudaError_t launch(DropArgs a, cudaStream_t s) {
   if (vectors && a.rows == 1) {
     const int64_t blocks = a.cols / V / kThreads + 1;
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    k_dropout_flat<T, kResidual><<<(unsigned)blocks, kThreads, 0, s>>>(a);
+    k_dropout_flat<T, kResidual><<<(unsigned)blocks, kThreads, 0, s>>>(a, keys);
     return cudaGetLastError();
   }
   // items of a row: its vectors, or the blocks it meets (one more where it starts inside a block)
@@ -147,8 +154,8 @@ cudaError_t launch(DropArgs a, cudaStream_t s) {
   const int64_t gx = (items + bx - 1) / bx, gy = (a.rows + block.y - 1) / block.y;
   if (gx > 0x7fffffff) return cudaErrorInvalidConfiguration;
   const dim3 grid((unsigned)gx, (unsigned)std::min<int64_t>(gy, 65535));
-  if (vectors) k_dropout_rows<T, kResidual><<<grid, block, 0, s>>>(a);
-  else k_dropout_elements<T, kResidual><<<grid, block, 0, s>>>(a);
+  if (vectors) k_dropout_rows<T, kResidual><<<grid, block, 0, s>>>(a, keys);
+  else k_dropout_elements<T, kResidual><<<grid, block, 0, s>>>(a, keys);
   return cudaGetLastError();
 }
 
