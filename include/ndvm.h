@@ -267,8 +267,9 @@ ndvm_status ndvm_measure_op_cost(int fn, int iters, double* ns_per_call, void* s
  *     the next (at least a row's length, or 0 for an input whose rows are all the same memory).
  *     Pointers are aligned to their element type; other alignments only cost speed.
  *   - Everything is computed in binary32 and rounded to the output's type once, except where said.
- *   - Sums are added up in an order that depends on the sizes alone: the same call gives the same
- *     bits again.
+ *   - Sums are added up in an order that depends on the sizes, strides and alignment alone: the same
+ *     call gives the same bits again.
+ *   - The first call of an operator on a device loads its kernels: make it before any stream capture.
  *   - Errors: NDVM_E_INVALID_ARG for null pointers, sizes, strides, alignment or a workspace that
  *     is too small; NDVM_E_UNSUPPORTED for a type the operator does not take.  Outputs may not
  *     overlap inputs, except ndvm_dropout's y, which may be x or residual.
@@ -324,7 +325,7 @@ typedef enum { NDVM_ACT_SILU = 0, NDVM_ACT_GELU = 1, NDVM_ACT_RELU = 2, NDVM_ACT
  * one kernel: x is rows x k, w_gate and w_up are n x k, h is rows x n.
  *   dtype : every matrix (F16, BF16; sums in binary32)
  *   act   : silu g / (1 + e^-g), gelu g (1 + erf(g / sqrt 2)) / 2, relu, or sigmoid
- *   rows  : 0 is allowed and does nothing;  k, n : at least 1; rows, k and n below 2^31
+ *   rows  : 0 is allowed and does nothing;  k, n : at least 1; rows, k and n at most 2^30
  *   workspace : device, 256-byte aligned, ndvm_gated_workspace_bytes(..., 0, ...) bytes (NULL if that is 0)
  */
 ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,

@@ -10,6 +10,8 @@
 //   dx        A = dG, B = Wg^T, then A = dU, B = Wu^T into the same sums
 //   dW        A = dG^T (or dU^T), B = x^T
 // Transposes are read as they lie: the operand's rows are contiguous instead of its contraction.
+#include <atomic>
+
 #include "net.h"
 #include "tc.cuh"
 #include "types.cuh"
@@ -589,9 +591,15 @@ int split_count(int64_t tiles, int64_t steps) {
 
 template <typename T, Mode kMode, int kN, int kCtas>
 cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
-  static const cudaError_t set =
-      cudaFuncSetAttribute(k_product<T, kMode, kN, kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kN, kCtas>);
-  if (set != cudaSuccess) return set;
+  static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may take its shared memory
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  if (device >= 64 || !(allowed.load(std::memory_order_relaxed) >> device & 1)) {
+    e = cudaFuncSetAttribute(k_product<T, kMode, kN, kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kN, kCtas>);
+    if (e != cudaSuccess) return e;
+    if (device < 64) allowed.fetch_or((uint64_t)1 << device, std::memory_order_relaxed);
+  }
   const int items = p.tiles_m * p.tiles_n * p.matrices * p.splits;
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)std::min(items, kSms / kCtas) * kCtas);

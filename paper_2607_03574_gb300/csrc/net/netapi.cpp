@@ -118,12 +118,13 @@ ndvm_status ndvm_dropout(ndvm_dtype dtype, int64_t rows, int64_t cols, const voi
   return done(launch_dropout(a, dtype, (cudaStream_t)stream), "dropout launch");
 }
 
+static constexpr int64_t kGatedMost = (int64_t)1 << 30;  // rows, k and n (a tile's coordinates are 32-bit)
+
 static ndvm_status gated_check(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,
                                int64_t x_stride, const void* w_gate, int64_t g_stride, const void* w_up, int64_t u_stride) {
   if (dtype != NDVM_F16 && dtype != NDVM_BF16) return set_error(NDVM_E_UNSUPPORTED, "the gated projection takes F16 and BF16");
   if (act < NDVM_ACT_SILU || act > NDVM_ACT_SIGMOID) return bad("unknown activation");
-  constexpr int64_t most = ((int64_t)1 << 31) - 1;
-  if (rows < 0 || k < 1 || n < 1 || rows > most || k > most || n > most) return bad("bad rows, k or n");
+  if (rows < 0 || k < 1 || n < 1 || rows > kGatedMost || k > kGatedMost || n > kGatedMost) return bad("bad rows, k or n");
   if (rows > 0) REFUSE(matrix_in(x, rows, k, x_stride, dtype));
   REFUSE(matrix_in(w_gate, n, k, g_stride, dtype));
   REFUSE(matrix_in(w_up, n, k, u_stride, dtype));
@@ -137,12 +138,11 @@ static const char* gated_room(const GatedArgs& a, bool backward, const void* wor
 }
 
 size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backward, int aligned) {
-  constexpr int64_t most = ((int64_t)1 << 31) - 1;
-  if (rows < 0 || k < 1 || n < 1 || rows > most || k > most || n > most) return 0;
+  if (rows < 0 || k < 1 || n < 1 || rows > kGatedMost || k > kGatedMost || n > kGatedMost) return 0;
   return gated_workspace(rows, k, n, backward != 0, !aligned);
 }
 
-int64_t ndvm_gated_kept_stride(int64_t n) { return n < 1 || n >= (int64_t)1 << 31 ? 0 : (n + 3) / 4 * 4; }
+int64_t ndvm_gated_kept_stride(int64_t n) { return n < 1 || n > kGatedMost ? 0 : (n + 3) / 4 * 4; }
 
 ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,
                                int64_t x_stride, const void* w_gate, int64_t g_stride, const void* w_up,

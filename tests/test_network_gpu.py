@@ -387,6 +387,21 @@ def test_gated_matches_64_bits(ndvm, cuda, rows, k, n, t):
             assert rel <= 3 * RMS[t], (name, rel)
 
 
+@pytest.mark.parametrize("rows,k,n", [(5003, 2008, 2601), (4999, 2003, 2600), (2300, 1024, 4100)])
+def test_gated_of_many_tiles(ndvm, cuda, rows, k, n):
+    """Sizes of several rounds of the largest tiles in every product, ragged at every edge."""
+    import torch
+    x, wg, wu, dh = _gated_case(rows, rows, k, n, "bf16")
+    want, err = _gated64(*(v.double() for v in (x, wg, wu, dh)), "silu", "bf16")
+    bounds = [_rounded(v, e, "bf16") for v, e in zip(want, err)]
+    for kept in (None, ndvm.gated_kept(x, wg)):
+        got = (ndvm.gated_forward(x, wg, wu, kept=kept),) + ndvm.gated_backward(dh, x, wg, wu, kept=kept)
+        for name, a, v, b in zip(("h", "dx", "dw_gate", "dw_up"), got, want, bounds):
+            _inside(a, v, b, name)
+            assert float((a.double() - v).norm() / v.norm()) <= 3 * RMS["bf16"], name
+    ndvm.check_operators()
+
+
 @pytest.mark.parametrize("t", ["bf16", "f16"])
 @pytest.mark.parametrize("rows,k,n", GATED_SIZES[::2] + [(1, 40, 1001), (130, 72, 1001), (300, 1100, 136)])
 def test_gated_with_kept_products(ndvm, cuda, rows, k, n, t):
@@ -586,6 +601,24 @@ def test_differentiable_ops_take_any_layout(ndvm, cuda):
     dy2 = ndvm.gated_backward(torch.full_like(h2, 2.0), y2, wg, wu.contiguous(), "sigmoid")[0]
     dx2, dw2, _ = ndvm.layer_norm_backward(dy2, x2, w.detach(), stats)
     assert torch.equal(x.grad.reshape(30, 72), dx2) and torch.equal(w.grad, dw2)
+
+
+def test_empty_inputs_through_autograd(ndvm, cuda):
+    import torch
+    x = torch.empty(0, 24, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    w = torch.ones(24, device="cuda", requires_grad=True)
+    g, u = (torch.ones(40, 24, device="cuda", dtype=torch.bfloat16, requires_grad=True) for _ in range(2))
+    h = ndvm.dropout(ndvm.gated(ndvm.layer_norm(x, w), g, u), 0.1, 1)
+    dx, dw, dg, du = torch.autograd.grad(h, (x, w, g, u), torch.empty_like(h))
+    assert dx.shape == (0, 24) and not dw.any() and not dg.any() and not du.any()
+
+
+def test_no_second_derivatives(ndvm, cuda):
+    import torch
+    x = torch.randn(4, 8, device="cuda", requires_grad=True)
+    for y in (ndvm.layer_norm(x), ndvm.dropout(x, 0.5, 1)):
+        with pytest.raises(ndvm.NdvmError):
+            torch.autograd.grad(y, x, torch.ones_like(y), create_graph=True)
 
 
 def test_refusals(ndvm, cuda):
