@@ -58,7 +58,9 @@ __host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == k
 
 // A block's share: kN columns of sums for its 128 rows, of whose operand B a pair's blocks hold half each.
 template <int kN, int kCtas> constexpr int kStageBytes = (kM + kN / kCtas) * kC * 2;
-template <int kCtas> constexpr int kStaging = 4096 * kCtas;  // of each warp that reads sums: what its stores are made from
+// of each warp that reads sums: what its stores are made from (twice as much for a block alone would cost it a stage:
+// 16384 x 512 -> 2048 forward 54 -> 58 us)
+template <int kCtas> constexpr int kStaging = 4096 * kCtas;
 template <int kN, int kCtas>
 constexpr int kStages = std::min(8, (229376 - kReaders * kStaging<kCtas>) / kStageBytes<kN, kCtas>);
 template <int kN, int kCtas>
@@ -231,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   } else if (warp >= 2) {
     // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, every other 32
     // columns, by way of staging that asynchronous copies empty.  (Two warps a scheduler: one alone left the
-    // latencies of the reads, the copies and dh in the open.  4096 rows, 1024 -> 4096: TODO)
+    // latencies of the reads, the copies and dh in the open: backward of 4096 x 1024 -> 4096 174 and 159 us.)
     const int lanes = (warp % 4) * 32;
     const uint32_t mine = staging + (warp - 2) * kStaging<kCtas>;
     const char* const mine_ptr = raw + (mine - tc::smem(raw));
@@ -315,14 +317,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
               }
             }
           });
-        // A piece takes 2048 bytes of 16-bit results, or 4096 for both of dG and dU or for binary32: the staging
-        // holds two (then the other's copy may still be under way) or one.
-        const bool large = kMode == kGradient || (!dual(kMode) && p.splits > 1);
-        const bool alone = (large && kCtas == 1) || (kMode == kForward && p.keep);
-        const uint32_t to = mine + (alone ? 0 : buffer * (large ? 4096 : 2048));
+        // A piece takes 2048 bytes of 16-bit results, or 4096 for both of dG and dU or for binary32; while it is
+        // made, the copies of as many others as the staging holds may be under way (none where it held G and U).
+        constexpr int kSmall = kStaging<kCtas> / 2048, kLarge = kStaging<kCtas> / 4096;
+        const bool large = kMode == kGradient || (!dual(kMode) && p.splits > 1), alone = kMode == kForward && p.keep;
+        const uint32_t to = mine + (alone ? 0 : large ? buffer % kLarge * 4096 : buffer * 2048);
         if (lane == 0) {
           if (alone) tc::stores_read<0>();
-          else tc::stores_read<1>();
+          else if (large) tc::stores_read<kLarge - 1>();
+          else tc::stores_read<kSmall - 1>();
         }
         __syncwarp();
         if (!dual(kMode) && p.splits > 1) {
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           }
         }
         if (lane == 0) tc::stores_commit();
-        buffer ^= 1;
+        buffer = (buffer + 1) % kSmall;
       }
       tc::fence_before();
       __syncwarp();
@@ -583,12 +586,6 @@ bool map_partial(CUtensorMap* map, float* p, int64_t parts, int64_t m, int64_t n
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Parts that a result's contraction is cut into: enough for every SM to have one, none shorter than 8 steps.
-int split_count(int64_t tiles, int64_t steps) {
-  if (tiles >= kSms) return 1;
-  return (int)std::clamp<int64_t>(kSms / tiles, 1, std::max<int64_t>(steps / 8, 1));
-}
-
 template <typename T, Mode kMode, int kN, int kCtas>
 cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may take its shared memory
@@ -620,26 +617,26 @@ struct Cut { int width, ctas, splits; };
 
 int a_box(int64_t m) { return (int)std::min<int64_t>(up(m, 8), kM); }
 
-// A round of tiles over the SMs takes about as long as its columns; narrower tiles take a little longer for
-// them (more bytes an operation) and a pair's a little less (16384 x 2048 -> 8192 forward: 640 us alone, 598 in
-// pairs), if its contraction has 12 steps or more: pairs start and end together, which costs short ones (4096 x 256 ->
-// 1024: 9.1 us alone, 10.6 in pairs).  The weights' gradients are cut as if both were wanted: one of them alone
-// has the same bits.
+// The shape with the least estimated time, in steps of a tile 256 wide (0.27 us): a round of tiles takes its
+// steps and about 8 more to fill and empty; narrower tiles' steps are shorter, but not in proportion (more bytes an
+// operation), a pair's a little shorter (16384 x 2048 -> 8192 forward: 640 us alone, 598 in pairs) if there are 12 or
+// more (pairs start and end together: 4096 x 256 -> 1024 takes 9.1 us alone, 10.6 in pairs).  Where tiles are fewer than
+// SMs, a contraction is cut into parts of 8 steps or more, which costs the launch that joins them.  The weights'
+// gradients are cut as if both were wanted: one of them alone has the same bits.
 Cut cut(Mode mode, int64_t m, int64_t n, int64_t c) {
-  struct Shape { int width, ctas; double time; };
+  struct Shape { int width, ctas; double step; };
   static constexpr Shape shapes[] = {{256, 2, 0.9}, {256, 1, 1.0}, {128, 1, 0.6}, {64, 1, 0.4}};
   const int matrices = mode == kWeight ? 2 : 1;
+  const int64_t steps = ceil_div(c, kC) * (mode == kInput ? 2 : 1);
   Cut best{};
   double least = 1e300;
-  int64_t best_tiles = 0;
-  const int64_t steps = ceil_div(c, kC) * (mode == kInput ? 2 : 1);
   for (const Shape& s : shapes) {
     if (s.ctas == 2 && steps < 12) continue;
-    const int64_t tiles = matrices * ceil_div(m, kM * s.ctas) * ceil_div(n, dual(mode) ? s.width / 2 : s.width);
-    const double time = (double)ceil_div(tiles, kSms / s.ctas) * s.time;
-    if (time < least) least = time, best.width = s.width, best.ctas = s.ctas, best_tiles = tiles;
+    const int64_t units = kSms / s.ctas, tiles = matrices * ceil_div(m, kM * s.ctas) * ceil_div(n, dual(mode) ? s.width / 2 : s.width);
+    const int64_t splits = dual(mode) || tiles >= units ? 1 : std::clamp<int64_t>(units / tiles, 1, std::max<int64_t>(steps / 8, 1));
+    const double time = (double)ceil_div(tiles * splits, units) * ((double)ceil_div(steps, splits) * s.step + 8) + (splits > 1 ? 13 : 0);
+    if (time < least) least = time, best = Cut{s.width, s.ctas, (int)splits};
   }
-  best.splits = dual(mode) ? 1 : split_count(best_tiles * best.ctas, steps);
   return best;
 }
 

@@ -405,7 +405,7 @@ def _make_ops():
         def forward(ctx, x, w_gate, w_up, activation):
             # The two products are kept (8 bytes an element of h) where that is the faster: a long contraction, or
             # so few elements that they stay in L2.  Forward and backward, computed again / kept: 16384 x 2048 -> 8192
-            # 2666 / 2252 us, 4096 x 1024 -> 4096 192 / 187, 16384 x 1024 -> 4096 693 / 709, 16 x 2048 -> 8192 79 / 68.
+            # 2599 / 2255 us, 4096 x 1024 -> 4096 194 / 188, 16384 x 512 -> 2048 243 / 251, 16 x 2048 -> 8192 67 / 57.
             k, n = x.shape[-1], w_gate.shape[0]
             kept = gated_kept(x, w_gate) if k >= 1536 or x.numel() // max(k, 1) * n <= 1 << 24 else None
             ctx.save_for_backward(x, w_gate, w_up, kept)
