@@ -21,19 +21,36 @@ namespace {
 
 __device__ int g_stopped;  // a wait in k_product ran out (ndvm_check_operators)
 
+// act(g) and act'(g), two at a time.  1 / (1 + e^-g) is the hardware's power of two and reciprocal (off by a
+// few units of binary32's last place, and by a share of |g| of them where the value itself vanishes).
+__device__ __forceinline__ float power2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 template <int kAct>
-__device__ __forceinline__ void activate(float g, float* a, float* da) {
+__device__ __forceinline__ void activate(float2 g, float2* a, float2* da) {
+  const float2 one = make_float2(1.0f, 1.0f);
   if constexpr (kAct == NDVM_ACT_RELU) {
-    *a = g > 0.0f ? g : (g != g ? g : 0.0f);
-    *da = g > 0.0f ? 1.0f : 0.0f;
+    *a = make_float2(g.x > 0.0f ? g.x : (g.x != g.x ? g.x : 0.0f), g.y > 0.0f ? g.y : (g.y != g.y ? g.y : 0.0f));
+    *da = make_float2(g.x > 0.0f ? 1.0f : 0.0f, g.y > 0.0f ? 1.0f : 0.0f);
   } else if constexpr (kAct == NDVM_ACT_GELU) {
-    const float cdf = 0.5f * (1.0f + erff(g * 0.70710678f));
-    *a = g * cdf;
-    *da = cdf + g * __expf(-0.5f * g * g) * 0.39894228f;
+    const float2 half = make_float2(0.5f, 0.5f);
+    const float2 cdf = fma(make_float2(erff(g.x * 0.70710678f), erff(g.y * 0.70710678f)), half, half);
+    const float2 q = mul(mul(g, g), make_float2(-0.72134752f, -0.72134752f));  // -g^2 / 2 in powers of two
+    *a = mul(g, cdf);
+    *da = fma(mul(g, make_float2(power2(q.x), power2(q.y))), make_float2(0.39894228f, 0.39894228f), cdf);
   } else {
-    const float s = __fdividef(1.0f, 1.0f + __expf(-g));
-    *a = kAct == NDVM_ACT_SILU ? g * s : s;
-    *da = kAct == NDVM_ACT_SILU ? s * (1.0f + g * (1.0f - s)) : s * (1.0f - s);
+    const float2 q = mul(g, make_float2(-1.44269504f, -1.44269504f));
+    const float2 d = add(make_float2(power2(q.x), power2(q.y)), one), s = make_float2(reciprocal(d.x), reciprocal(d.y));
+    const float2 rest = fma(s, make_float2(-1.0f, -1.0f), one);  // 1 - s
+    *a = kAct == NDVM_ACT_SILU ? mul(g, s) : s;
+    *da = kAct == NDVM_ACT_SILU ? fma(*a, rest, s) : mul(s, rest);
   }
 }
 // f(activation as a constant): one branch around a loop over many elements, not one in each
@@ -90,7 +107,7 @@ __device__ __forceinline__ void stage_row(uint32_t buffer, int lane, const float
   for (int q = 0; q < 4; q++) {
     union { uint4 u; T t[8]; } o;
 #pragma unroll
-    for (int e = 0; e < 8; e++) o.t[e] = from_f32<T>(v[q * 8 + e]);
+    for (int e = 0; e < 8; e += 2) narrow(o.t + e, make_float2(v[q * 8 + e], v[q * 8 + e + 1]));
     tc::store16(buffer + lane * 64 + ((q ^ (lane >> 1 & 3)) << 4), o.u);
   }
 }
@@ -241,25 +258,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
     const bool vec_dh = kMode == kGradient && reinterpret_cast<uintptr_t>(p.dh) % 16 == 0 && p.dh_stride % 8 == 0;
-    for (int i = unit; i < items; i += units) {
-      const Item it = item(i);
-      const int row0 = it.m0 + lanes, row = row0 + lane;
-      Pack<T, 8> next[4];  // dh of the columns to come: asked for a piece ahead, the first before the wait for the sums
-      const auto fetch = [&](int j) {
-        if (kMode != kGradient || row >= p.m || j >= kOutN) return;
-        const T* from = static_cast<const T*>(p.dh) + row * p.dh_stride + it.n0 + j;
-        const int count = p.n - it.n0 - j;
+    Pack<T, 8> next[4];  // dh of the columns to come: asked for a piece ahead
+    const auto fetch = [&](const Item& of, int j) {
+      const int row = of.m0 + lanes + lane, count = p.n - of.n0 - j;
+      if (row >= p.m) return;
+      const T* from = static_cast<const T*>(p.dh) + row * p.dh_stride + of.n0 + j;
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-          if (vec_dh && q * 8 + 8 <= count) {
-            next[q] = load_pack<T, 8>(from + q * 8);
-          } else {
+      for (int q = 0; q < 4; q++) {
+        if (vec_dh && q * 8 + 8 <= count) {
+          next[q] = load_pack<T, 8>(from + q * 8);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; e++) next[q].v[e] = q * 8 + e < count ? from[q * 8 + e] : from_f32<T>(0.0f);
-          }
+          for (int e = 0; e < 8; e++) next[q].v[e] = q * 8 + e < count ? from[q * 8 + e] : from_f32<T>(0.0f);
         }
-      };
-      fetch(first);
+      }
+    };
+    Item it{}, following{};
+    if (unit < items) following = item(unit);
+    if (kMode == kGradient && unit < items && first < kOutN) fetch(following, first);
+    for (int i = unit; i < items; i += units) {
+      it = following;
+      if (i + units < items) following = item(i + units);
+      const int row0 = it.m0 + lanes;
+      bool asked = false;  // for the following tile's dh
       // (the whole warp goes on or gives up: reading tensor memory is a warp's instruction)
       if (!__all_sync(~0u, tc::barrier_wait(done(slot), slot_phase, stop))) break;
       tc::fence_after();
@@ -275,7 +296,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         if (kMode == kGradient) {
 #pragma unroll
           for (int q = 0; q < 4; q++) dh[q] = next[q];
-          fetch(j + 64);
+          if (j + 64 < kOutN && col + 64 < p.n) fetch(it, j + 64);
+          else asked = true, fetch(following, first);
         }
         tc::tmem_loaded();
         if (kMode == kForward && p.keep) {  // G and then U to memory, as binary32
@@ -305,16 +327,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         if (dual(kMode))
           by_activation(p.act, [&](auto act) {
 #pragma unroll
-            for (int e = 0; e < 32; e++) {
-              float a, da;
-              activate<decltype(act)::value>(v[e], &a, &da);
+            for (int e = 0; e < 32; e += 2) {
+              const float2 up = make_float2(u[e], u[e + 1]);
+              float2 a, da, out;
+              activate<decltype(act)::value>(make_float2(v[e], v[e + 1]), &a, &da);
               if (kMode == kForward) {
-                v[e] = a * u[e];
+                out = mul(a, up);
               } else {
-                const float d = to_f32(dh[e / 8].v[e % 8]);
-                v[e] = d * u[e] * da;
-                u[e] = d * a;
+                const float2 d = widen(dh[e / 8].v + e % 8), other = mul(d, a);
+                out = mul(mul(d, up), da);
+                u[e] = other.x, u[e + 1] = other.y;
               }
+              v[e] = out.x, v[e + 1] = out.y;
             }
           });
         // A piece takes 2048 bytes of 16-bit results, or 4096 for both of dG and dU or for binary32; while it is
@@ -352,6 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         if (lane == 0) tc::stores_commit();
         buffer = (buffer + 1) % kSmall;
       }
+      if (kMode == kGradient && !asked) fetch(following, first);  // (no columns of this tile were this warp's)
       tc::fence_before();
       __syncwarp();
       if (lane == 0) {
@@ -423,15 +448,15 @@ __global__ void __launch_bounds__(256) k_gradient(const float* kept, int64_t kep
       }
       Pack<T, 8> og, ou;
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
+      for (int e = 0; e < 8; e += 2) {
         const float4 gq = g[e / 4], uq = u[e / 4];
-        const float ge = e % 4 == 0 ? gq.x : e % 4 == 1 ? gq.y : e % 4 == 2 ? gq.z : gq.w;
-        const float ue = e % 4 == 0 ? uq.x : e % 4 == 1 ? uq.y : e % 4 == 2 ? uq.z : uq.w;
-        float a, da;
+        const float2 ge = e % 4 ? make_float2(gq.z, gq.w) : make_float2(gq.x, gq.y);
+        const float2 ue = e % 4 ? make_float2(uq.z, uq.w) : make_float2(uq.x, uq.y);
+        float2 a, da;
         activate<decltype(k)::value>(ge, &a, &da);
-        const float f = to_f32(d.v[e]);
-        og.v[e] = from_f32<T>(f * ue * da);
-        ou.v[e] = from_f32<T>(f * a);
+        const float2 f = widen(d.v + e);
+        narrow(og.v + e, mul(mul(f, ue), da));
+        narrow(ou.v + e, mul(f, a));
       }
       store_pack(dg + row * pitch + c, og);
       store_pack(du + row * pitch + c, ou);
@@ -516,7 +541,11 @@ __global__ void __launch_bounds__(128) k_one(GatedArgs a, T* dg, T* du) {
       a.kept[a.kept_stride + j] = su;
     }
     float act, da;
-    by_activation(a.act, [&](auto k) { activate<decltype(k)::value>(sg, &act, &da); });
+    by_activation(a.act, [&](auto k) {
+      float2 act2, da2;
+      activate<decltype(k)::value>(make_float2(sg, sg), &act2, &da2);
+      act = act2.x, da = da2.x;
+    });
     if (kBackward) {
       const float dh = to_f32(static_cast<const T*>(a.dh)[j]);
       dg[j] = from_f32<T>(dh * su * da);
