@@ -335,8 +335,8 @@ ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t ro
 
 /*
  * ndvm_gated_workspace_bytes -- device workspace of a forward (backward = 0) or backward (1) call.
- * aligned = 1: x, w_gate and w_up start on 16 bytes and their row strides are multiples of 8 elements and
- * not 0; otherwise 0, which adds room for copies that are.  0 on invalid sizes.
+ * aligned = 1: x, w_gate, w_up (and dh) start on 16 bytes and their row strides are multiples of 8 elements
+ * and not 0; otherwise 0, which adds room for copies that are.  0 on invalid sizes.
  */
 size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backward, int aligned);
 

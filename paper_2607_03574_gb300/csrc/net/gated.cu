@@ -75,17 +75,20 @@ __host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == k
 
 // A block's share: kN columns of sums for its 128 rows, of whose operand B a pair's blocks hold half each.
 template <int kN, int kCtas> constexpr int kStageBytes = (kM + kN / kCtas) * kC * 2;
-// of each warp that reads sums: what its stores are made from (twice as much for a block alone would cost it a stage:
-// 16384 x 512 -> 2048 forward 54 -> 58 us)
-template <int kCtas> constexpr int kStaging = 4096 * kCtas;
-template <int kN, int kCtas>
-constexpr int kStages = std::min(8, (229376 - kReaders * kStaging<kCtas>) / kStageBytes<kN, kCtas>);
-template <int kN, int kCtas>
-constexpr int kSmem = kStages<kN, kCtas> * kStageBytes<kN, kCtas> + kReaders * kStaging<kCtas> + 1024 /* alignment */ + 256 /* barriers */;
+// Of each warp that reads sums: what its stores are made from (twice as much for a block alone would cost it a stage:
+// 16384 x 512 -> 2048 forward 54 -> 58 us), and two pieces of dh that it has asked for.
+template <Mode kMode, int kCtas> constexpr int kStaging = kMode == kGradient ? 4096 : 4096 * kCtas;
+template <Mode kMode> constexpr int kAsked = kMode == kGradient ? 4096 : 0;
+template <Mode kMode, int kN, int kCtas>
+constexpr int kStages = std::min(8, (229376 - kReaders * (kStaging<kMode, kCtas> + kAsked<kMode>)) / kStageBytes<kN, kCtas>);
+template <Mode kMode, int kN, int kCtas>
+constexpr int kSmem = kStages<kMode, kN, kCtas> * kStageBytes<kN, kCtas> + kReaders * (kStaging<kMode, kCtas> + kAsked<kMode>) +
+                      1024 /* alignment */ + 384 /* barriers */;
 
 struct ProductArgs {
   CUtensorMap a[2], b[2];
   CUtensorMap o[2];              // the results (kGradient: dG and dU), or o[0] the split sums
+  CUtensorMap dh;                // kGradient
   CUtensorMap kept;              // kForward: where G and U go in binary32, if keep
   int keep;
   int m, n, c;                   // rows and columns of the result, contraction of one segment
@@ -95,7 +98,6 @@ struct ProductArgs {
   int a_box;                     // rows of A that a tile loads (fewer than 128 where the result has fewer)
   int copies;                    // results are stored by copies (their rows start on 16 bytes)
   void* out[2]; int64_t stride;  // kWeight: both matrices'; kGradient: dG and dU; else out[0]
-  const void* dh; int64_t dh_stride;
   float* partial; int64_t partial_pitch;  // splits > 1: [split][matrix][m][pitch]
 };
 
@@ -129,19 +131,21 @@ __device__ __forceinline__ void unstage(const char* buffer, int lane, T* out, in
 template <typename T, Mode kMode, int kN, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ ProductArgs p) {
   extern __shared__ char raw[];
-  constexpr int S = kStages<kN, kCtas>, kStage = kStageBytes<kN, kCtas>;
+  constexpr int S = kStages<kMode, kN, kCtas>, kStage = kStageBytes<kN, kCtas>;
   constexpr uint32_t kABytes = kM * kC * 2;
   constexpr int kColumns = 2 * kN;  // of tensor memory: two tiles' sums
   constexpr int kOutN = dual(kMode) ? kN / 2 : kN;
   __shared__ uint32_t s_tmem;
   __shared__ int s_stop;
   const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
-  const uint32_t staging = base + S * kStage, bars = staging + kReaders * kStaging<kCtas>;
+  const uint32_t staging = base + S * kStage, asked_at = staging + kReaders * kStaging<kMode, kCtas>;
+  const uint32_t bars = asked_at + kReaders * kAsked<kMode>;
   const auto full = [&](int i) { return bars + i * 8; };
   const auto empty = [&](int i) { return bars + (S + i) * 8; };
   const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
   const auto taken = [&](int i) { return bars + (2 * S + 2 + i) * 8; };  // and have been read
   const uint32_t drain = bars + (2 * S + 4) * 8;
+  const auto dh_in = [&](int reader, int b) { return bars + (2 * S + 5 + 2 * reader + b) * 8; };  // a piece of dh has come
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int rank = kCtas == 1 ? 0 : (int)tc::cluster_rank(), unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
   volatile int* stop = &s_stop;
@@ -151,6 +155,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     for (int i = 0; i < S; i++) tc::barrier_init(full(i), 1), tc::barrier_init(empty(i), 1);
     for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), kReaders * kCtas);
     tc::barrier_init(drain, 1);
+    if (kMode == kGradient)
+      for (int i = 0; i < 2 * kReaders; i++) tc::barrier_init(dh_in(i / 2, i % 2), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tc::tmem_alloc<kCtas, kColumns>(tc::smem(&s_tmem));
@@ -252,41 +258,54 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     // columns, by way of staging that asynchronous copies empty.  (Two warps a scheduler: one alone left the
     // latencies of the reads, the copies and dh in the open: backward of 4096 x 1024 -> 4096 174 and 159 us.)
     const int lanes = (warp % 4) * 32;
-    const uint32_t mine = staging + (warp - 2) * kStaging<kCtas>;
+    const uint32_t mine = staging + (warp - 2) * kStaging<kMode, kCtas>;
     const char* const mine_ptr = raw + (mine - tc::smem(raw));
     const int first = (warp - 2) / 4 * 32;
     int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
-    const bool vec_dh = kMode == kGradient && reinterpret_cast<uintptr_t>(p.dh) % 16 == 0 && p.dh_stride % 8 == 0;
-    Pack<T, 8> next[4];  // dh of the columns to come: asked for a piece ahead
-    const auto fetch = [&](const Item& of, int j) {
-      const int row = of.m0 + lanes + lane, count = p.n - of.n0 - j;
-      if (row >= p.m) return;
-      const T* from = static_cast<const T*>(p.dh) + row * p.dh_stride + of.n0 + j;
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        if (vec_dh && q * 8 + 8 <= count) {
-          next[q] = load_pack<T, 8>(from + q * 8);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; e++) next[q].v[e] = q * 8 + e < count ? from[q * 8 + e] : from_f32<T>(0.0f);
-        }
+    // kGradient: the pieces of dh that this warp needs, in the order it needs them, two of them asked for ahead
+    const int reader = warp - 2;
+    struct Place { int i, j; Item it; } ask{unit, first, {}};
+    const auto settle = [&] {  // past the tiles that have no columns of this warp's
+      while (ask.i < items && ask.it.n0 + first >= p.n) {
+        ask.i += units;
+        if (ask.i < items) ask.it = item(ask.i);
       }
     };
-    Item it{}, following{};
-    if (unit < items) following = item(unit);
-    if (kMode == kGradient && unit < items && first < kOutN) fetch(following, first);
-    for (int i = unit; i < items; i += units) {
-      it = following;
-      if (i + units < items) following = item(i + units);
+    int asked = 0, had = 0;
+    const auto ask_next = [&] {
+      if (ask.i >= items) return;
+      if (lane == 0) {
+        const uint32_t bar = dh_in(reader, asked & 1);
+        tc::barrier_expect(bar, 2048);
+        tc::load_box<1>(asked_at + reader * kAsked<kMode> + (asked & 1) * 2048, &p.dh, ask.it.n0 + ask.j, ask.it.m0 + lanes, bar);
+      }
+      asked++;
+      ask.j += 64;
+      if (ask.j >= kOutN || ask.it.n0 + ask.j >= p.n) {
+        ask.j = first;
+        ask.i += units;
+        if (ask.i < items) ask.it = item(ask.i);
+        settle();
+      }
+    };
+    if (kMode == kGradient) {
+      if (first >= kOutN) ask.i = items;
+      if (ask.i < items) ask.it = item(ask.i);
+      settle();
+      ask_next();
+      ask_next();
+    }
+    bool ok = true;
+    for (int i = unit; ok && i < items; i += units) {
+      const Item it = item(i);
       const int row0 = it.m0 + lanes;
-      bool asked = false;  // for the following tile's dh
       // (the whole warp goes on or gives up: reading tensor memory is a warp's instruction)
       if (!__all_sync(~0u, tc::barrier_wait(done(slot), slot_phase, stop))) break;
       tc::fence_after();
       const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
 #pragma unroll 1
-      for (int j = first; j < kOutN; j += 64) {
+      for (int j = first; ok && j < kOutN; j += 64) {
         const int col = it.n0 + j, count = min(32, p.n - col);
         if (count <= 0) break;
         float v[32], u[32];
@@ -294,10 +313,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         tc::tmem_load32(v, at + j);
         if (dual(kMode)) tc::tmem_load32(u, at + kN / 2 + j);
         if (kMode == kGradient) {
+          const int b = had & 1;
+          ok = __all_sync(~0u, tc::barrier_wait(dh_in(reader, b), had >> 1 & 1, stop));
+          const char* from = raw + (asked_at - tc::smem(raw)) + reader * kAsked<kMode> + b * 2048 + lane * 64;
 #pragma unroll
-          for (int q = 0; q < 4; q++) dh[q] = next[q];
-          if (j + 64 < kOutN && col + 64 < p.n) fetch(it, j + 64);
-          else asked = true, fetch(following, first);
+          for (int q = 0; q < 4; q++) dh[q] = load_pack<T, 8>(reinterpret_cast<const T*>(from + ((q ^ (lane >> 1 & 3)) << 4)));
+          __syncwarp();
+          if (ok) had++, ask_next();
         }
         tc::tmem_loaded();
         if (kMode == kForward && p.keep) {  // G and then U to memory, as binary32
@@ -343,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           });
         // A piece takes 2048 bytes of 16-bit results, or 4096 for both of dG and dU or for binary32; while it is
         // made, the copies of as many others as the staging holds may be under way (none where it held G and U).
-        constexpr int kSmall = kStaging<kCtas> / 2048, kLarge = kStaging<kCtas> / 4096;
+        constexpr int kSmall = kStaging<kMode, kCtas> / 2048, kLarge = kStaging<kMode, kCtas> / 4096;
         const bool large = kMode == kGradient || (!dual(kMode) && p.splits > 1), alone = kMode == kForward && p.keep;
         const uint32_t to = mine + (alone ? 0 : large ? buffer % kLarge * 4096 : buffer * 2048);
         if (lane == 0) {
@@ -376,7 +398,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         if (lane == 0) tc::stores_commit();
         buffer = (buffer + 1) % kSmall;
       }
-      if (kMode == kGradient && !asked) fetch(following, first);  // (no columns of this tile were this warp's)
       tc::fence_before();
       __syncwarp();
       if (lane == 0) {
@@ -385,7 +406,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
       }
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
-    if (lane == 0) tc::stores_done();
+    if (lane == 0) {
+      tc::stores_done();
+      if (kMode == kGradient)  // (pieces that a launch that gave up has left)
+        for (; had < asked; had++) tc::barrier_drain(dh_in(reader, had & 1), had >> 1 & 1);
+    }
   }
   __syncwarp();
   __syncthreads();
@@ -593,16 +618,16 @@ Encode encoder() {
 }
 
 // A matrix of `rows` rows of `cols` contiguous elements, read in boxes of 64 columns and `box` rows in the
-// 128-byte swizzle; or written in boxes of 32 by 32 (of 64 bytes a row: the 64-byte swizzle).
+// 128-byte swizzle; or in boxes of 32 by 32 (results, and dh: 64 bytes a row, the 64-byte swizzle).
 template <typename T>
-bool map_matrix(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box, bool written = false) {
+bool map_matrix(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride, int box, bool piece = false) {
   if (!encoder()) return false;
   if (rows == 1) stride = up(cols, 8);  // (never taken)
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t boxes[2] = {written ? 32u : 64u, (cuuint32_t)box}, ones[2] = {1, 1};
+  const cuuint32_t boxes[2] = {piece ? 32u : 64u, (cuuint32_t)box}, ones[2] = {1, 1};
   const CUtensorMapDataType type = std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   return encoder()(map, type, 2, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   written ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   piece ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // split sums: `parts` matrices of m rows, written in boxes of 32 by 32
@@ -622,7 +647,7 @@ cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
   if (device >= 64 || !(allowed.load(std::memory_order_relaxed) >> device & 1)) {
-    e = cudaFuncSetAttribute(k_product<T, kMode, kN, kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kN, kCtas>);
+    e = cudaFuncSetAttribute(k_product<T, kMode, kN, kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kMode, kN, kCtas>);
     if (e != cudaSuccess) return e;
     if (device < 64) allowed.fetch_or((uint64_t)1 << device, std::memory_order_relaxed);
   }
@@ -630,7 +655,7 @@ cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)std::min(items, kSms / kCtas) * kCtas);
   c.blockDim = dim3(kThreads);
-  c.dynamicSmemBytes = kSmem<kN, kCtas>;
+  c.dynamicSmemBytes = kSmem<kMode, kN, kCtas>;
   c.stream = s;
   cudaLaunchAttribute cluster{};
   cluster.id = cudaLaunchAttributeClusterDimension;
@@ -704,7 +729,7 @@ cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s) {
 // take turns).
 struct Layout {
   int64_t k_pitch, n_pitch;
-  size_t x, gate, up, grad, partial, total;
+  size_t x, gate, up, dh, grad, partial, total;
   Layout(int64_t rows, int64_t k, int64_t n, bool backward, bool copies) {
     k_pitch = ndvm::up(k, 8);
     n_pitch = ndvm::up(n, 8);
@@ -717,6 +742,7 @@ struct Layout {
     x = take(copies ? rows * k_pitch * 2 : 0);
     gate = take(copies ? n * k_pitch * 2 : 0);
     up = take(copies ? n * k_pitch * 2 : 0);
+    dh = take(copies && backward ? rows * n_pitch * 2 : 0);
     grad = take(backward ? 2 * rows * n_pitch * 2 : 0);
     int64_t parts = 0;
     if (backward && rows > 0) {
@@ -729,8 +755,14 @@ struct Layout {
 };
 
 bool all_ready(const GatedArgs& a) {
-  return tma_ready(a.x, a.x_stride, a.rows, a.k) && tma_ready(a.w_gate, a.g_stride, a.n, a.k) &&
+  return (!a.dh || tma_ready(a.dh, a.dh_stride, a.rows, a.n)) && tma_ready(a.x, a.x_stride, a.rows, a.k) && tma_ready(a.w_gate, a.g_stride, a.n, a.k) &&
          tma_ready(a.w_up, a.u_stride, a.n, a.k);
+}
+
+template <typename T>
+void launch_pack(const PackArgs& p, int count, int64_t most_rows, cudaStream_t s) {
+  const int64_t blocks = std::min<int64_t>(ceil_div(most_rows * (p.pitch / 8), 256), kSms * 16);
+  k_pack<T><<<dim3((unsigned)blocks, (unsigned)count), 256, 0, s>>>(p);
 }
 
 template <typename T>
@@ -749,11 +781,9 @@ void make_ready(GatedArgs& a, const Layout& l, bool x, bool weights, cudaStream_
   };
   if (x) add(a.x, a.x_stride, a.rows, l.x);
   if (weights) add(a.w_gate, a.g_stride, a.n, l.gate), add(a.w_up, a.u_stride, a.n, l.up);
-  if (!count) return;
   p.cols = a.k;
   p.pitch = l.k_pitch;
-  const int64_t blocks = std::min<int64_t>(ceil_div(most * (l.k_pitch / 8), 256), kSms * 16);
-  k_pack<T><<<dim3((unsigned)blocks, (unsigned)count), 256, 0, s>>>(p);
+  if (count) launch_pack<T>(p, count, most, s);
 }
 
 // G and U, and h or dG and dU of them
@@ -770,7 +800,8 @@ cudaError_t products(const GatedArgs& a, void* out0, void* out1, int64_t stride,
     if (!map_partial(&p.kept, a.kept, 2, a.rows, a.n, a.kept_stride)) return cudaErrorInvalidValue;
   }
   p.matrices = 1;
-  p.act = a.act; p.out[0] = out0; p.out[1] = out1; p.stride = stride; p.dh = a.dh; p.dh_stride = a.dh_stride;
+  if (kMode == kGradient && !map_matrix<T>(&p.dh, a.dh, a.rows, a.n, a.dh_stride, 32, true)) return cudaErrorInvalidValue;
+  p.act = a.act; p.out[0] = out0; p.out[1] = out1; p.stride = stride;
   return launch_product<T, kMode>(p, k, s);
 }
 
@@ -813,6 +844,15 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
     make_ready<T>(a, l, weights, a.dx != nullptr, s);
   } else {
     make_ready<T>(a, l, true, true, s);
+    if (!tma_ready(a.dh, a.dh_stride, a.rows, a.n)) {
+      PackArgs p{};
+      p.from[0] = a.dh; p.stride[0] = a.dh_stride; p.rows[0] = a.rows; p.to[0] = ws + l.dh;
+      p.cols = a.n;
+      p.pitch = l.n_pitch;
+      launch_pack<T>(p, 1, a.rows, s);
+      a.dh = ws + l.dh;
+      a.dh_stride = l.n_pitch;
+    }
     if ((e = products<T, kGradient>(a, dg, du, l.n_pitch, s)) != cudaSuccess) return e;
   }
   ProductArgs p{};

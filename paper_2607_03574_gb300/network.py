@@ -339,9 +339,10 @@ def gated_backward(dh, x, w_gate, w_up, activation="silu", wants=(True, True, Tr
         gp = dw_gate.data_ptr()
     if dw_up is not None:
         up = dw_up.data_ptr()
-    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 1, ready)
+    ph, hs = dh.data_ptr(), _rows(dh, "dh")[2]
+    need = lib.ndvm_gated_workspace_bytes(rows, k, n, 1, int(ready and (ph | 2 * hs) % 16 == 0 and hs != 0))
     ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
-    status = lib.ndvm_gated_backward_kept(code, act, rows, k, n, dh.data_ptr(), _rows(dh, "dh")[2], *operands,
+    status = lib.ndvm_gated_backward_kept(code, act, rows, k, n, ph, hs, *operands,
                                           _kept(torch, lib, kept, rows, n, device), xp, dxs, gp, up, wp, nbytes,
                                           _stream(torch, stream, device))
     if status:
