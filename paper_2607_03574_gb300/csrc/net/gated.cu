@@ -489,26 +489,39 @@ __global__ void __launch_bounds__(256) k_gradient(const float* kept, int64_t kep
   });
 }
 
-// Up to three matrices of `cols` columns to rows that start on 16 bytes (TMA reads no others): 8 elements a
-// thread, read one by one and stored together.
+// Up to three matrices of `cols` columns to rows that start on 16 bytes (TMA reads no others): a warp a row, 16 bytes
+// a lane, out of the one or two aligned 16-byte blocks that hold them (only blocks with bytes of the row are read).
 struct PackArgs {
   const void* from[3];
   void* to[3];
   int64_t stride[3], rows[3];
   int64_t cols, pitch;
 };
-template <typename T>
-__global__ void __launch_bounds__(256) k_pack(PackArgs a) {
-  const int w = blockIdx.y;
-  const T* from = static_cast<const T*>(a.from[w]);
-  const int64_t eights = a.pitch / 8, total = a.rows[w] * eights;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / eights, c = (i - row * eights) * 8;
-    const T* p = from + row * a.stride[w] + c;
-    Pack<T, 8> v;
+__global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a) {
+  const int w = blockIdx.y, lane = threadIdx.x % 32;
+  for (int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; row < a.rows[w]; row += (int64_t)gridDim.x * 8) {
+    const char* from = static_cast<const char*>(a.from[w]) + row * a.stride[w] * 2;
+    char* to = static_cast<char*>(a.to[w]) + row * a.pitch * 2;
+    const int off = (int)(reinterpret_cast<uintptr_t>(from) % 16);  // even, the same for all of the row's pieces
+    const int64_t bytes = a.cols * 2;
+    for (int64_t c = lane * 16; c < a.pitch * 2; c += 32 * 16) {
+      const uint4* block = reinterpret_cast<const uint4*>(from + c - off);
+      uint32_t v[9] = {};
+      const uint4 p = block[0];
+      v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
+      if (off + (bytes - c) > 16) {
+        const uint4 q = block[1];
+        v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
+      }
+      // (a row's last piece may end in what lies behind the row: columns that no tensor map has)
 #pragma unroll
-    for (int e = 0; e < 8; e++) v.v[e] = c + e < a.cols ? p[e] : from_f32<T>(0.0f);
-    store_pack(static_cast<T*>(a.to[w]) + row * a.pitch + c, v);
+      for (int i = 0; i < 7; i++) v[i] = off & 8 ? v[i + 2] : v[i];
+#pragma unroll
+      for (int i = 0; i < 5; i++) v[i] = off & 4 ? v[i + 1] : v[i];
+      const int bits = off % 4 * 8;
+      *reinterpret_cast<uint4*>(to + c) = make_uint4(__funnelshift_r(v[0], v[1], bits), __funnelshift_r(v[1], v[2], bits),
+                                                     __funnelshift_r(v[2], v[3], bits), __funnelshift_r(v[3], v[4], bits));
+    }
   }
 }
 
@@ -759,13 +772,11 @@ bool all_ready(const GatedArgs& a) {
          tma_ready(a.w_up, a.u_stride, a.n, a.k);
 }
 
-template <typename T>
 void launch_pack(const PackArgs& p, int count, int64_t most_rows, cudaStream_t s) {
-  const int64_t blocks = std::min<int64_t>(ceil_div(most_rows * (p.pitch / 8), 256), kSms * 16);
-  k_pack<T><<<dim3((unsigned)blocks, (unsigned)count), 256, 0, s>>>(p);
+  const int64_t blocks = std::min<int64_t>(ceil_div(most_rows, 8), kSms * 32);
+  k_pack<<<dim3((unsigned)blocks, (unsigned)count), 256, 0, s>>>(p);
 }
 
-template <typename T>
 void make_ready(GatedArgs& a, const Layout& l, bool x, bool weights, cudaStream_t s) {
   char* ws = static_cast<char*>(a.workspace);
   PackArgs p{};
@@ -783,7 +794,7 @@ void make_ready(GatedArgs& a, const Layout& l, bool x, bool weights, cudaStream_
   if (weights) add(a.w_gate, a.g_stride, a.n, l.gate), add(a.w_up, a.u_stride, a.n, l.up);
   p.cols = a.k;
   p.pitch = l.k_pitch;
-  if (count) launch_pack<T>(p, count, most, s);
+  if (count) launch_pack(p, count, most, s);
 }
 
 // G and U, and h or dG and dU of them
@@ -813,7 +824,7 @@ cudaError_t forward(GatedArgs a, cudaStream_t s) {
     return cudaGetLastError();
   }
   const Layout l(a.rows, a.k, a.n, false, !all_ready(a));
-  make_ready<T>(a, l, true, true, s);
+  make_ready(a, l, true, true, s);
   return products<T, kForward>(a, a.h, nullptr, a.h_stride, s);
 }
 
@@ -833,7 +844,7 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
   T* du = dg + a.rows * l.n_pitch;
   cudaError_t e;
   if (a.kept) {
-    make_ready<T>(a, l, weights, a.dx != nullptr, s);
+    make_ready(a, l, weights, a.dx != nullptr, s);
     const int64_t blocks = std::min<int64_t>(ceil_div(a.rows * (l.n_pitch / 8), 256), kSms * 32);
     const T* dh = static_cast<const T*>(a.dh);
     const bool vectors = reinterpret_cast<uintptr_t>(dh) % 16 == 0 && (a.rows == 1 || a.dh_stride % 8 == 0);
@@ -841,15 +852,15 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
     else k_gradient<T, false><<<(unsigned)blocks, 256, 0, s>>>(a.kept, a.kept_stride, dh, a.dh_stride, a.rows, a.n, a.act, dg, du, l.n_pitch);
   } else if (a.rows == 1) {
     one<T, true>(a, all_ready(a) && a.k % 8 == 0, dg, du, s);
-    make_ready<T>(a, l, weights, a.dx != nullptr, s);
+    make_ready(a, l, weights, a.dx != nullptr, s);
   } else {
-    make_ready<T>(a, l, true, true, s);
+    make_ready(a, l, true, true, s);
     if (!tma_ready(a.dh, a.dh_stride, a.rows, a.n)) {
       PackArgs p{};
       p.from[0] = a.dh; p.stride[0] = a.dh_stride; p.rows[0] = a.rows; p.to[0] = ws + l.dh;
       p.cols = a.n;
       p.pitch = l.n_pitch;
-      launch_pack<T>(p, 1, a.rows, s);
+      launch_pack(p, 1, a.rows, s);
       a.dh = ws + l.dh;
       a.dh_stride = l.n_pitch;
     }

@@ -405,10 +405,11 @@ def _make_ops():
         @staticmethod
         def forward(ctx, x, w_gate, w_up, activation):
             # The two products are kept (8 bytes an element of h) where that is the faster: a long contraction, or
-            # so few elements that they stay in L2.  Forward and backward, computed again / kept: 16384 x 2048 -> 8192
-            # 2599 / 2255 us, 4096 x 1024 -> 4096 194 / 188, 16384 x 512 -> 2048 243 / 251, 16 x 2048 -> 8192 67 / 57.
+            # few elements.  Forward and backward, computed again / kept: 16384 x 2048 -> 8192 2636 / 2353 us,
+            # 16 x 2048 -> 8192 67 / 57, 1501 x 333 -> 777 53 / 46; but 4096 x 1024 -> 4096 185 / 187, 4096 x 256 -> 1024
+            # 46 / 48, 16384 x 1024 -> 4096 654 / 704.
             k, n = x.shape[-1], w_gate.shape[0]
-            kept = gated_kept(x, w_gate) if k >= 1536 or x.numel() // max(k, 1) * n <= 1 << 24 else None
+            kept = gated_kept(x, w_gate) if k >= 1536 or x.numel() // max(k, 1) * n <= 1 << 21 else None
             ctx.save_for_backward(x, w_gate, w_up, kept)
             ctx.activation = activation
             return gated_forward(x, w_gate, w_up, activation, kept=kept)
