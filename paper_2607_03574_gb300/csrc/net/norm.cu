@@ -34,12 +34,18 @@ __device__ __forceinline__ void load_weight(Pairs<V> (&w)[kPairs<V>], const void
   }
 }
 
+// the lanes of this thread's group of kRow, or of its warp
+template <int kRow>
+__device__ __forceinline__ uint32_t group_lanes() {
+  return kRow >= 32 ? ~0u : ((1u << (kRow & 31)) - 1) << (threadIdx.x % 32 / kRow * kRow);
+}
+
 // Sums over the kRow threads that share a row: a warp's shuffles, then the warps' sums in shared memory
 // (`part` is the caller's, another one for each sum of a row, so one barrier a sum is enough).
 template <int kRow>
 __device__ __forceinline__ float row_sum(float v, float* part) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+  for (int o = (kRow < 32 ? kRow : 32) / 2; o; o >>= 1) v += __shfl_xor_sync(group_lanes<kRow>(), v, o);
   if constexpr (kRow > 32) {
     if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = v;
     __syncthreads();
@@ -61,7 +67,7 @@ __global__ void __launch_bounds__(kBlock<kRow>, kResident) k_forward(NormArgs a,
   __shared__ float part[2][32];
   const int t = threadIdx.x % kRow;
   const int64_t row = (int64_t)blockIdx.x * (kBlock<kRow> / kRow) + threadIdx.x / kRow;
-  if (row >= a.rows) return;  // (whole warps; with a block a row, no block)
+  if (row >= a.rows) return;  // (whole groups; with a block a row, no block)
   const int cols = (int)a.cols;
   const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
   Pack<T, V> px[N];
@@ -148,9 +154,9 @@ __global__ void __launch_bounds__(kLong) k_forward_long(NormArgs a, int w_f32) {
 template <int kRow>
 __device__ __forceinline__ float2 group_sum(float a, float b, float2* part, int group) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    a += __shfl_xor_sync(~0u, a, o);
-    b += __shfl_xor_sync(~0u, b, o);
+  for (int o = (kRow < 32 ? kRow : 32) / 2; o; o >>= 1) {
+    a += __shfl_xor_sync(group_lanes<kRow>(), a, o);
+    b += __shfl_xor_sync(group_lanes<kRow>(), b, o);
   }
   float2 s = make_float2(a, b);
   if constexpr (kRow > 32) {
@@ -171,7 +177,7 @@ template <typename T, int V, int N, int kRow, int kResident>
 __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_backward(NormArgs a, int w_f32) {
   using P = Pairs<V>;
   constexpr int H = kPairs<V>, kBlockRows = kBackBlock<kRow> / kRow;
-  __shared__ float2 part[2][kBlockRows][kRow / 32];
+  __shared__ float2 part[2][kBlockRows][kRow > 32 ? kRow / 32 : 1];
   const int t = threadIdx.x % kRow, group = threadIdx.x / kRow, cols = (int)a.cols;
   const float inv = 1.0f / (float)cols;
   P dw[N][H], db[N][H];
@@ -349,8 +355,10 @@ template <typename T, typename F>
 bool forward_variant(bool vectors, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
   if (vectors) {
-    const int64_t packs = cols / V;  // a warp a row up to 8 loads a thread (no barriers), then blocks
-    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<12>());
+    const int64_t packs = cols / V;  // a quarter of a warp, then a warp a row up to 8 loads a thread (no barriers), then blocks
+    if (packs <= 8) f(Int<V>(), Int<1>(), Int<8>(), Int<12>());
+    else if (packs <= 16) f(Int<V>(), Int<2>(), Int<8>(), Int<12>());
+    else if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<12>());
     else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<12>());
     else if (packs <= 128) f(Int<V>(), Int<4>(), Int<32>(), Int<10>());
     else if (packs <= 256) f(Int<V>(), Int<8>(), Int<32>(), Int<7>());
@@ -359,7 +367,8 @@ bool forward_variant(bool vectors, int64_t cols, F&& f) {
     else if (packs <= 2048) f(Int<V>(), Int<4>(), Int<512>(), Int<2>());
     else return false;
   } else {
-    if (cols <= 128) f(Int<1>(), Int<4>(), Int<32>(), Int<12>());
+    if (cols <= 64) f(Int<1>(), Int<8>(), Int<8>(), Int<12>());
+    else if (cols <= 128) f(Int<1>(), Int<4>(), Int<32>(), Int<12>());
     else if (cols <= 512) f(Int<1>(), Int<16>(), Int<32>(), Int<10>());
     else if (cols <= 2048) f(Int<1>(), Int<16>(), Int<128>(), Int<10>());
     else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>(), Int<2>());
@@ -373,7 +382,9 @@ bool backward_variant(bool vectors, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
   if (vectors) {
     const int64_t packs = cols / V;
-    if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<3>());
+    if (packs <= 8) f(Int<V>(), Int<1>(), Int<8>(), Int<3>());
+    else if (packs <= 16) f(Int<V>(), Int<2>(), Int<8>(), Int<2>());
+    else if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<3>());
     else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<2>());
     else if (packs <= 128) f(Int<V>(), Int<2>(), Int<64>(), Int<2>());
     else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>(), Int<2>());
@@ -382,7 +393,8 @@ bool backward_variant(bool vectors, int64_t cols, F&& f) {
     else if (packs <= 2048 && sizeof(T) == 4) f(Int<4>(), Int<4>(), Int<512>(), Int<1>());  // (16-bit rows would not fit in 128 registers)
     else return false;
   } else {
-    if (cols <= 256) f(Int<1>(), Int<8>(), Int<32>(), Int<3>());
+    if (cols <= 64) f(Int<1>(), Int<8>(), Int<8>(), Int<3>());
+    else if (cols <= 256) f(Int<1>(), Int<8>(), Int<32>(), Int<3>());
     else if (cols <= 512) f(Int<1>(), Int<8>(), Int<64>(), Int<3>());
     else if (cols <= 1024) f(Int<1>(), Int<8>(), Int<128>(), Int<3>());
     else if (cols <= 2048) f(Int<1>(), Int<8>(), Int<256>(), Int<3>());
