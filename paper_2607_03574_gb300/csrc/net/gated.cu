@@ -1,7 +1,8 @@
 // Gated projection h = act(G) U with G = x Wg^T, U = x Wu^T, and its backward pass:
 //   dU = dh act(G), dG = dh U act'(G), dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.
 // The backward pass computes G and U again, or takes those that the forward pass kept: in binary32 (8 bytes an
-// element of h), so that dG and dU are rounded once, to the operands' type, which the next products need.
+// element of h), so that dG and dU are rounded once, to the operands' type, which the next products need (and
+// where there are few of them, not even that: in_halves).
 //
 // All products run in one kernel frame (k_product): D[m, n] = sum over c of A[m, c] B[n, c], 128 rows a tile,
 // operands by TMA, sums in tensor memory.
@@ -86,16 +87,18 @@ constexpr int kSmem = kStages<kMode, kN, kCtas> * kStageBytes<kN, kCtas> + kRead
                       1024 /* alignment */ + 384 /* barriers */;
 
 struct ProductArgs {
-  CUtensorMap a[2], b[2];
+  CUtensorMap a[4], b[2];        // kWeight: a's are gate's parts, then up's
   CUtensorMap o[2];              // the results (kGradient: dG and dU), or o[0] the split sums
   CUtensorMap dh;                // kGradient
   CUtensorMap kept;              // kForward: where G and U go in binary32, if keep
   int keep;
   int m, n, c;                   // rows and columns of the result, contraction of one segment
   int tiles_m, tiles_n, matrices;  // matrices: results of one shape, by the a's (kWeight: 1 or 2), else 1
+  int parts;                     // kWeight: segments of a matrix (dG, or its two halves)
   int steps, splits;             // contraction steps of a result, and how many parts they are cut into
   int act;
   int a_box;                     // rows of A that a tile loads (fewer than 128 where the result has fewer)
+  int sums;                      // results are binary32 sums, which k_join finishes
   int copies;                    // results are stored by copies (their rows start on 16 bytes)
   void* out[2]; int64_t stride;  // kWeight: both matrices'; kGradient: dG and dU; else out[0]
   float* partial; int64_t partial_pitch;  // splits > 1: [split][matrix][m][pitch]
@@ -199,8 +202,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         const uint32_t a = base + stage * kStage, b = a + kABytes, bar = kCtas == 1 ? full(stage) : tc::in_first(full(stage));
         const int bytes = a_rows(kMode) ? kStage : kStage - (int)kABytes + p.a_box * kC * 2;
         if (rank == 0) tc::barrier_expect(full(stage), kCtas * bytes);
-        const int seg = kMode == kInput ? s / segment : kMode == kWeight ? it.matrix : 0;
-        const int c = (kMode == kInput ? s - seg * segment : s) * kC;
+        const int part = kMode == kInput || kMode == kWeight ? s / segment : 0, seg = kMode == kWeight ? it.matrix * p.parts + part : part;
+        const int c = (s - part * segment) * kC;
         if (a_rows(kMode)) {
           for (int q = 0; q < kM / 64; q++) tc::load_box<kCtas>(a + q * 8192, &p.a[seg], it.m0 + q * 64, c, bar);
         } else {
@@ -366,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         // A piece takes 2048 bytes of 16-bit results, or 4096 for both of dG and dU or for binary32; while it is
         // made, the copies of as many others as the staging holds may be under way (none where it held G and U).
         constexpr int kSmall = kStaging<kMode, kCtas> / 2048, kLarge = kStaging<kMode, kCtas> / 4096;
-        const bool large = kMode == kGradient || (!dual(kMode) && p.splits > 1), alone = kMode == kForward && p.keep;
+        const bool large = kMode == kGradient || (!dual(kMode) && p.sums), alone = kMode == kForward && p.keep;
         const uint32_t to = mine + (alone ? 0 : large ? buffer % kLarge * 4096 : buffer * 2048);
         if (lane == 0) {
           if (alone) tc::stores_read<0>();
@@ -374,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           else tc::stores_read<kSmall - 1>();
         }
         __syncwarp();
-        if (!dual(kMode) && p.splits > 1) {
+        if (!dual(kMode) && p.sums) {
           stage_row(to, lane, v);
           tc::fence_async();
           __syncwarp();
@@ -422,20 +425,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   if (warp == 1) tc::tmem_free<kCtas, kColumns>(tmem);
 }
 
-// the parts of split sums added up in order, and rounded: 4 columns a thread
+// the parts of split sums added up in order, and rounded: 4 columns a thread.  fold: each matrix's rows come
+// twice, and are added up too.
 template <typename T>
-__global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitch, int splits, int matrices, int64_t m, int64_t n,
-                                              T* out0, T* out1, int64_t stride) {
-  const int64_t quads = pitch / 4, total = matrices * m * quads;
+__global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitch, int splits, int matrices, int fold, int64_t m,
+                                              int64_t n, T* out0, T* out1, int64_t stride) {
+  const int64_t quads = pitch / 4, total = matrices * m * quads, part = total << fold;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const float* p = partial + i * 4;
-    float4 s = *reinterpret_cast<const float4*>(p);
-#pragma unroll 4
-    for (int k = 1; k < splits; k++) {
-      const float4 v = *reinterpret_cast<const float4*>(p + k * total * 4);
-      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-    }
     const int64_t row = i / quads, c = (i - row * quads) * 4;
+    const float* p = partial + (i + (fold && row >= m ? m * quads : 0)) * 4;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int k = 0; k < splits; k++) {
+      const float4 v = *reinterpret_cast<const float4*>(p + k * part * 4);
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+      if (fold) {
+        const float4 l = *reinterpret_cast<const float4*>(p + (k * part + m * quads) * 4);
+        s.x += l.x, s.y += l.y, s.z += l.z, s.w += l.w;
+      }
+    }
     T* out = row >= m ? out1 + (row - m) * stride + c : out0 + row * stride + c;
     const float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
@@ -444,10 +452,17 @@ __global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitc
   }
 }
 
-// dG and dU of G and U that the forward pass kept: 8 columns a thread
+// what rounding v to the operands' type leaves, rounded too (0 beside what is not finite)
+template <typename T>
+__device__ __forceinline__ T rest_of(float v, T rounded) {
+  const float r = to_f32(rounded);
+  return from_f32<T>(fabsf(r) <= 3.0e38f ? v - r : 0.0f);
+}
+// dG and dU of G and U that the forward pass kept: 8 columns a thread.  halves: and what their rounding left, `rows`
+// rows further on.
 template <typename T, bool kVectors>
 __global__ void __launch_bounds__(256) k_gradient(const float* kept, int64_t kept_stride, const T* dh, int64_t dh_stride, int64_t rows,
-                                                  int64_t n, int act, T* dg, T* du, int64_t pitch) {
+                                                  int64_t n, int act, T* dg, T* du, int64_t pitch, bool halves) {
   const int64_t eights = pitch / 8, total = rows * eights;
   const float* up = kept + rows * kept_stride;
   by_activation(act, [&](auto k) {
@@ -471,7 +486,7 @@ __global__ void __launch_bounds__(256) k_gradient(const float* kept, int64_t kep
 #pragma unroll
         for (int e = 0; e < 8; e++) d.v[e] = c + e < n ? dh[row * dh_stride + c + e] : from_f32<T>(0.0f);
       }
-      Pack<T, 8> og, ou;
+      Pack<T, 8> og, ou, lg, lu;
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         const float4 gq = g[e / 4], uq = u[e / 4];
@@ -480,8 +495,17 @@ __global__ void __launch_bounds__(256) k_gradient(const float* kept, int64_t kep
         float2 a, da;
         activate<decltype(k)::value>(ge, &a, &da);
         const float2 f = widen(d.v + e);
-        narrow(og.v + e, mul(mul(f, ue), da));
-        narrow(ou.v + e, mul(f, a));
+        const float2 vg = mul(mul(f, ue), da), vu = mul(f, a);
+        narrow(og.v + e, vg);
+        narrow(ou.v + e, vu);
+        if (halves) {
+          lg.v[e] = rest_of(vg.x, og.v[e]), lg.v[e + 1] = rest_of(vg.y, og.v[e + 1]);
+          lu.v[e] = rest_of(vu.x, ou.v[e]), lu.v[e + 1] = rest_of(vu.y, ou.v[e + 1]);
+        }
+      }
+      if (halves) {
+        store_pack(dg + (rows + row) * pitch + c, lg);
+        store_pack(du + (rows + row) * pitch + c, lu);
       }
       store_pack(dg + row * pitch + c, og);
       store_pack(du + row * pitch + c, ou);
@@ -526,11 +550,11 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
 }
 
 // ------------------------------------------------------------------------------------ one row: vectors
-// The weights are read once and are nearly all the traffic: a warp takes kPer rows of each weight, 16 bytes a
+// Forward alone.  The weights are read once and are nearly all the traffic: a warp takes kPer rows of each weight, 16 bytes a
 // lane and load, against x (from L1), sums in binary32.  (From two rows on the tensor cores are the faster: 8
 // rows, 2048 -> 8192, took 53 us this way and 17 us that way.)
-template <typename T, int V, int kPer, bool kBackward>
-__global__ void __launch_bounds__(128) k_one(GatedArgs a, T* dg, T* du) {
+template <typename T, int V, int kPer>
+__global__ void __launch_bounds__(128) k_one(GatedArgs a) {
   using P = Pairs<V>;
   constexpr int H = kPairs<V>, kUnroll = 16 / (2 * kPer);
   const int lane = threadIdx.x % 32;
@@ -574,35 +598,27 @@ __global__ void __launch_bounds__(128) k_one(GatedArgs a, T* dg, T* du) {
     }
     const int64_t j = j0 + q;
     if (lane != q || j >= a.n) continue;
-    if (!kBackward && a.kept) {
+    if (a.kept) {
       a.kept[j] = sg;
       a.kept[a.kept_stride + j] = su;
     }
-    float act, da;
     by_activation(a.act, [&](auto k) {
-      float2 act2, da2;
-      activate<decltype(k)::value>(make_float2(sg, sg), &act2, &da2);
-      act = act2.x, da = da2.x;
+      float2 act, da;
+      activate<decltype(k)::value>(make_float2(sg, sg), &act, &da);
+      static_cast<T*>(a.h)[j] = from_f32<T>(act.x * su);
     });
-    if (kBackward) {
-      const float dh = to_f32(static_cast<const T*>(a.dh)[j]);
-      dg[j] = from_f32<T>(dh * su * da);
-      du[j] = from_f32<T>(dh * act);
-    } else {
-      static_cast<T*>(a.h)[j] = from_f32<T>(act * su);
-    }
   }
 }
 
-template <typename T, bool kBackward>
-void one(const GatedArgs& a, bool vectors, T* dg, T* du, cudaStream_t s) {
+template <typename T>
+void one(const GatedArgs& a, bool vectors, cudaStream_t s) {
   // two rows of each weight a warp halve the loads of x; fewer outputs than would fill the SMs go one a warp
   const bool two = a.n >= 4096;
   const unsigned grid = (unsigned)((a.n + (two ? 7 : 3)) / (two ? 8 : 4));
-  if (vectors && two) k_one<T, 8, 2, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
-  else if (vectors) k_one<T, 8, 1, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
-  else if (two) k_one<T, 1, 2, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
-  else k_one<T, 1, 1, kBackward><<<grid, 128, 0, s>>>(a, dg, du);
+  if (vectors && two) k_one<T, 8, 2><<<grid, 128, 0, s>>>(a);
+  else if (vectors) k_one<T, 8, 1><<<grid, 128, 0, s>>>(a);
+  else if (two) k_one<T, 1, 2><<<grid, 128, 0, s>>>(a);
+  else k_one<T, 1, 1><<<grid, 128, 0, s>>>(a);
 }
 
 // ------------------------------------------------------------------------------------ launches
@@ -690,11 +706,11 @@ int a_box(int64_t m) { return (int)std::min<int64_t>(up(m, 8), kM); }
 // more (pairs start and end together: 4096 x 256 -> 1024 takes 9.1 us alone, 10.6 in pairs).  Where tiles are fewer than
 // SMs, a contraction is cut into parts of 8 steps or more, which costs the launch that joins them.  The weights'
 // gradients are cut as if both were wanted: one of them alone has the same bits.
-Cut cut(Mode mode, int64_t m, int64_t n, int64_t c) {
+Cut cut(Mode mode, int64_t m, int64_t n, int64_t c, int parts = 1) {
   struct Shape { int width, ctas; double step; };
   static constexpr Shape shapes[] = {{256, 2, 0.9}, {256, 1, 1.0}, {128, 1, 0.6}, {64, 1, 0.4}};
   const int matrices = mode == kWeight ? 2 : 1;
-  const int64_t steps = ceil_div(c, kC) * (mode == kInput ? 2 : 1);
+  const int64_t steps = ceil_div(c, kC) * (mode == kInput ? 2 : mode == kWeight ? parts : 1);
   Cut best{};
   double least = 1e300;
   for (const Shape& s : shapes) {
@@ -708,15 +724,16 @@ Cut cut(Mode mode, int64_t m, int64_t n, int64_t c) {
 }
 
 template <typename T, Mode kMode>
-cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s) {
+cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s, bool fold = false) {
   const int out = dual(kMode) ? k.width / 2 : k.width;
   p.tiles_m = (int)ceil_div(p.m, kM * k.ctas);
   p.tiles_n = (int)ceil_div(p.n, out);
-  p.steps = (int)ceil_div(p.c, kC) * (kMode == kInput ? 2 : 1);
+  p.steps = (int)ceil_div(p.c, kC) * (kMode == kInput ? 2 : kMode == kWeight ? p.parts : 1);
   p.splits = k.splits;
   p.a_box = a_rows(kMode) ? kM : a_box(p.m);
   p.copies = 1;
-  if (p.splits > 1) {
+  p.sums = p.splits > 1 || fold;
+  if (p.sums) {
     p.partial_pitch = up(p.n, 4);
     if (!map_partial(&p.o[0], p.partial, (int64_t)p.splits * p.matrices, p.m, p.n, p.partial_pitch)) return cudaErrorInvalidValue;
   } else {
@@ -731,21 +748,29 @@ cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s) {
                         : k.width == 256 ? launch_width<T, kMode, 256, 1>(p, s)
                         : k.width == 128 ? launch_width<T, kMode, 128, 1>(p, s)
                                          : launch_width<T, kMode, 64, 1>(p, s);
-  if (e != cudaSuccess || p.splits == 1) return e;
-  const int64_t total = (int64_t)p.matrices * p.m * p.partial_pitch / 4;
+  if (e != cudaSuccess || !p.sums) return e;
+  const int64_t m = fold ? p.m / 2 : p.m, total = (int64_t)p.matrices * m * p.partial_pitch / 4;
   k_join<T><<<(unsigned)std::min<int64_t>(ceil_div(total, 256), kSms * 8), 256, 0, s>>>(
-      p.partial, p.partial_pitch, p.splits, p.matrices, p.m, p.n, static_cast<T*>(p.out[0]), static_cast<T*>(p.out[1]), p.stride);
+      p.partial, p.partial_pitch, p.splits, p.matrices, fold, m, p.n, static_cast<T*>(p.out[0]), static_cast<T*>(p.out[1]), p.stride);
   return cudaGetLastError();
 }
+
+// Few elements: dG and dU are handed on in two halves of 16 bits, so that nothing is lost before the last
+// rounding.  (Over many elements the rounding of dG and dU adds to the results' own as squares add, 1.41 times in
+// all; over few it scatters, to more than twice: 4096 elements leave 1.2 to 1.55, 16384 1.37 to 1.49.)  It costs little
+// there: dx has the halves' rows one after the other in its tiles, the weights' gradients twice the steps.
+bool in_halves(int64_t rows, int64_t k, int64_t n) { return rows * std::min(n, k) <= 16384 || n * k <= 4096; }
 
 // The workspace: aligned copies of what TMA cannot read, dG and dU, and split sums (dx's and the weights'
 // take turns).
 struct Layout {
   int64_t k_pitch, n_pitch;
-  size_t x, gate, up, dh, grad, partial, total;
+  int parts;
+  size_t x, gate, up, dh, grad, partial, kept, h, total;
   Layout(int64_t rows, int64_t k, int64_t n, bool backward, bool copies) {
     k_pitch = ndvm::up(k, 8);
     n_pitch = ndvm::up(n, 8);
+    parts = in_halves(rows, k, n) ? 2 : 1;
     total = 0;
     const auto take = [&](int64_t bytes) {
       const size_t at = total;
@@ -756,14 +781,17 @@ struct Layout {
     gate = take(copies ? n * k_pitch * 2 : 0);
     up = take(copies ? n * k_pitch * 2 : 0);
     dh = take(copies && backward ? rows * n_pitch * 2 : 0);
-    grad = take(backward ? 2 * rows * n_pitch * 2 : 0);
-    int64_t parts = 0;
+    grad = take(backward ? 2 * parts * rows * n_pitch * 2 : 0);
+    int64_t sums = 0;
     if (backward && rows > 0) {
-      const Cut i = cut(kInput, rows, k, n), w = cut(kWeight, n, k, rows);
-      if (i.splits > 1) parts = i.splits * rows * ndvm::up(k, 4);
-      if (w.splits > 1) parts = std::max(parts, 2 * w.splits * n * ndvm::up(k, 4));
+      const Cut i = cut(kInput, rows * parts, k, n), w = cut(kWeight, n, k, rows, parts);
+      if (i.splits > 1 || parts > 1) sums = i.splits * parts * rows * ndvm::up(k, 4);
+      if (w.splits > 1) sums = std::max(sums, 2 * w.splits * n * ndvm::up(k, 4));
     }
-    partial = take(parts * 4);
+    partial = take(sums * 4);
+    // halves are made from G and U in binary32: where the forward pass has not kept them, it runs again
+    kept = take(backward && parts > 1 ? 2 * rows * ndvm::up(n, 4) * 4 : 0);
+    h = take(backward && parts > 1 ? rows * n_pitch * 2 : 0);
   }
 };
 
@@ -820,7 +848,7 @@ template <typename T>
 cudaError_t forward(GatedArgs a, cudaStream_t s) {
   if (a.rows == 0) return cudaSuccess;
   if (a.rows == 1) {
-    one<T, false>(a, all_ready(a) && a.k % 8 == 0, nullptr, nullptr, s);
+    one<T>(a, all_ready(a) && a.k % 8 == 0, s);
     return cudaGetLastError();
   }
   const Layout l(a.rows, a.k, a.n, false, !all_ready(a));
@@ -841,18 +869,26 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
   const Layout l(a.rows, a.k, a.n, true, !all_ready(a));
   char* ws = static_cast<char*>(a.workspace);
   T* dg = reinterpret_cast<T*>(ws + l.grad);
-  T* du = dg + a.rows * l.n_pitch;
+  T* du = dg + l.parts * a.rows * l.n_pitch;
   cudaError_t e;
+  if (l.parts > 1 && !a.kept) {
+    GatedArgs f = a;
+    f.dh = nullptr;
+    f.kept = reinterpret_cast<float*>(ws + l.kept);
+    f.kept_stride = up(a.n, 4);
+    f.h = ws + l.h;
+    f.h_stride = l.n_pitch;
+    if ((e = forward<T>(f, s)) != cudaSuccess) return e;
+    a.kept = f.kept;
+    a.kept_stride = f.kept_stride;
+  }
   if (a.kept) {
     make_ready(a, l, weights, a.dx != nullptr, s);
     const int64_t blocks = std::min<int64_t>(ceil_div(a.rows * (l.n_pitch / 8), 256), kSms * 32);
     const T* dh = static_cast<const T*>(a.dh);
     const bool vectors = reinterpret_cast<uintptr_t>(dh) % 16 == 0 && (a.rows == 1 || a.dh_stride % 8 == 0);
-    if (vectors) k_gradient<T, true><<<(unsigned)blocks, 256, 0, s>>>(a.kept, a.kept_stride, dh, a.dh_stride, a.rows, a.n, a.act, dg, du, l.n_pitch);
-    else k_gradient<T, false><<<(unsigned)blocks, 256, 0, s>>>(a.kept, a.kept_stride, dh, a.dh_stride, a.rows, a.n, a.act, dg, du, l.n_pitch);
-  } else if (a.rows == 1) {
-    one<T, true>(a, all_ready(a) && a.k % 8 == 0, dg, du, s);
-    make_ready(a, l, weights, a.dx != nullptr, s);
+    const auto kernel = vectors ? k_gradient<T, true> : k_gradient<T, false>;
+    kernel<<<(unsigned)blocks, 256, 0, s>>>(a.kept, a.kept_stride, dh, a.dh_stride, a.rows, a.n, a.act, dg, du, l.n_pitch, l.parts > 1);
   } else {
     make_ready(a, l, true, true, s);
     if (!tma_ready(a.dh, a.dh_stride, a.rows, a.n)) {
@@ -868,23 +904,27 @@ cudaError_t backward(GatedArgs a, cudaStream_t s) {
   }
   ProductArgs p{};
   p.partial = reinterpret_cast<float*>(ws + l.partial);
+  p.parts = l.parts;
   if (a.dx) {
-    const Cut k = cut(kInput, a.rows, a.k, a.n);
-    const int box = a_box(a.rows);
-    if (!map_matrix<T>(&p.a[0], dg, a.rows, a.n, l.n_pitch, box) || !map_matrix<T>(&p.a[1], du, a.rows, a.n, l.n_pitch, box) ||
+    const int64_t m = a.rows * l.parts;
+    const Cut k = cut(kInput, m, a.k, a.n);
+    const int box = a_box(m);
+    if (!map_matrix<T>(&p.a[0], dg, m, a.n, l.n_pitch, box) || !map_matrix<T>(&p.a[1], du, m, a.n, l.n_pitch, box) ||
         !map_matrix<T>(&p.b[0], a.w_gate, a.n, a.k, a.g_stride, 64) || !map_matrix<T>(&p.b[1], a.w_up, a.n, a.k, a.u_stride, 64))
       return cudaErrorInvalidValue;
-    p.m = (int)a.rows; p.n = (int)a.k; p.c = (int)a.n; p.matrices = 1;
+    p.m = (int)m; p.n = (int)a.k; p.c = (int)a.n; p.matrices = 1;
     p.out[0] = a.dx; p.out[1] = nullptr; p.stride = a.dx_stride;
-    if ((e = launch_product<T, kInput>(p, k, s)) != cudaSuccess) return e;
+    if ((e = launch_product<T, kInput>(p, k, s, l.parts > 1)) != cudaSuccess) return e;
   }
   if (weights) {
-    const Cut k = cut(kWeight, a.n, a.k, a.rows);
+    const Cut k = cut(kWeight, a.n, a.k, a.rows, l.parts);
     p.matrices = 0;
     for (int w = 0; w < 2; w++) {
       void* out = w ? a.dw_up : a.dw_gate;
       if (!out) continue;
-      if (!map_matrix<T>(&p.a[p.matrices], w ? du : dg, a.rows, a.n, l.n_pitch, 64)) return cudaErrorInvalidValue;
+      for (int half = 0; half < l.parts; half++)
+        if (!map_matrix<T>(&p.a[p.matrices * l.parts + half], (w ? du : dg) + half * a.rows * l.n_pitch, a.rows, a.n, l.n_pitch, 64))
+          return cudaErrorInvalidValue;
       p.out[p.matrices++] = out;
     }
     if (!map_matrix<T>(&p.b[0], a.x, a.rows, a.k, a.x_stride, 64)) return cudaErrorInvalidValue;

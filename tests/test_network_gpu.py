@@ -422,6 +422,28 @@ def test_gated_with_kept_products(ndvm, cuda, rows, k, n, t):
             _inside(a, v, _rounded(v, e, t), name)
 
 
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,k,n", [(1, 64, 16), (1, 48, 1000), (2, 2048, 640), (5, 33, 77), (64, 64, 64), (200, 80, 81), (900, 40, 100)])
+def test_gated_gradients_of_few_elements_are_rounded_once(ndvm, cuda, rows, k, n, t):
+    """Over few elements dG and dU are handed on in two halves (together 2^-15 or closer): the gradients are those
+    of the binary32 chain with one rounding, so no further from the exact ones than half a unit in the last place and
+    the small bounds of the halves and sums."""
+    import torch
+    x, wg, wu, dh = _gated_case(rows + 17 * n, rows, k, n, t)
+    want, _ = _gated64(*(v.double() for v in (x, wg, wu, dh)), "silu", t)
+    _, err = _gated64(*(v.double() for v in (x, wg, wu, dh)), "silu", "f32")  # bounds without the 16-bit rounding between
+    g, u = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+    a, da, _, _ = _act64("silu", g, 0)
+    left = {"bf16": 2.0 ** -16, "f16": 2.0 ** -22}[t]  # of dG and dU; and half's smallest step
+    dg, du = ((dh.double() * v).abs() * left + (2.0 ** -24 if t == "f16" else 0) for v in (u * da, a))
+    more = (dg @ wg.double().abs() + du @ wu.double().abs(), dg.t() @ x.double().abs(), du.t() @ x.double().abs())
+    for kept in (None, ndvm.gated_kept(x, wg)):
+        ndvm.gated_forward(x, wg, wu, kept=kept)
+        got = ndvm.gated_backward(dh, x, wg, wu, kept=kept)
+        for name, b, v, e, m in zip(("dx", "dw_gate", "dw_up"), got, want[1:], err[1:], more):
+            _inside(b, v, _rounded(v, e + m, t), name)
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu", "sigmoid"])
 @pytest.mark.parametrize("rows", [1, 6, 200])
 def test_gated_activations(ndvm, cuda, act, rows):
