@@ -759,7 +759,7 @@ cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s, bool fo
 // rounding.  (Over many elements the rounding of dG and dU adds to the results' own as squares add, 1.41 times in
 // all; over few it scatters, to more than twice: 4096 elements leave 1.2 to 1.55, 16384 1.37 to 1.49.)  It costs little
 // there: dx has the halves' rows one after the other in its tiles, the weights' gradients twice the steps.
-bool in_halves(int64_t rows, int64_t k, int64_t n) { return rows * std::min(n, k) <= 16384 || n * k <= 4096; }
+bool in_halves(int64_t rows, int64_t k, int64_t n) { return rows * std::min(n, k) <= 16384 || n * k <= 2048; }
 
 // The workspace: aligned copies of what TMA cannot read, dG and dU, and split sums (dx's and the weights'
 // take turns).

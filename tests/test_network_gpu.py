@@ -423,7 +423,7 @@ def test_gated_with_kept_products(ndvm, cuda, rows, k, n, t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16"])
-@pytest.mark.parametrize("rows,k,n", [(1, 64, 16), (1, 48, 1000), (2, 2048, 640), (5, 33, 77), (64, 64, 64), (200, 80, 81), (900, 40, 100)])
+@pytest.mark.parametrize("rows,k,n", [(1, 64, 16), (1, 48, 1000), (2, 2048, 640), (5, 33, 77), (64, 64, 64), (200, 80, 81), (900, 40, 50)])
 def test_gated_gradients_of_few_elements_are_rounded_once(ndvm, cuda, rows, k, n, t):
     """Over few elements dG and dU are handed on in two halves (together 2^-15 or closer): the gradients are those
     of the binary32 chain with one rounding, so no further from the exact ones than half a unit in the last place and
