@@ -279,7 +279,7 @@ ndvm_status ndvm_measure_op_cost(int fn, int iters, double* ns_per_call, void* s
  * ndvm_layer_norm_forward -- y = (x - mean) * rstd * weight + bias over each row of `cols` elements,
  * mean and variance (of the differences, not of the squares) over the row, rstd = 1 / sqrt(variance + eps).
  *   dtype  : x and y (F32, F16, BF16);  wtype : weight and bias, dtype or F32
- *   rows   : 0 is allowed and does nothing;  cols : at least 1
+ *   rows   : 0 is allowed and does nothing, below 2^31;  cols : at least 1
  *   weight, bias : device, cols values, or NULL for 1 and 0
  *   eps    : not negative, finite
  *   stats  : device, 2 x rows floats for the backward pass (all means, then all rstd), or NULL
@@ -325,7 +325,7 @@ typedef enum { NDVM_ACT_SILU = 0, NDVM_ACT_GELU = 1, NDVM_ACT_RELU = 2, NDVM_ACT
  * one kernel: x is rows x k, w_gate and w_up are n x k, h is rows x n.
  *   dtype : every matrix (F16, BF16; sums in binary32)
  *   act   : silu g / (1 + e^-g), gelu g (1 + erf(g / sqrt 2)) / 2, relu, or sigmoid
- *   rows  : 0 is allowed and does nothing;  k, n : at least 1; rows, k and n at most 2^30
+ *   rows  : 0 is allowed and does nothing;  k, n : at least 1; rows, k and n at most 2^28
  *   workspace : device, 256-byte aligned, ndvm_gated_workspace_bytes(..., 0, ...) bytes (NULL if that is 0)
  */
 ndvm_status ndvm_gated_forward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,

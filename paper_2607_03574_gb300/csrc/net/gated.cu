@@ -222,11 +222,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         if (++stage == S) stage = 0, phase ^= 1;
       }
     }
-    if (!ok && rank == 0)  // the copies in flight end before the block does (a pair's second waits for its first)
-      for (int k = 1; k <= min(issued, S); k++) {
-        const int at = (issued - k) % S, turn = (issued - k) / S;
-        tc::barrier_drain(full(at), turn & 1);
-      }
+    // The block stays until the products have let go of its stages (their arrivals come from outside, a pair's from
+    // the other block too); if the launch gives up, until its copies have landed (a pair's second waits for its first).
+    for (int k = min(issued, S); k >= 1; k--) {
+      const int at = (issued - k) % S, turn = (issued - k) / S;
+      if (ok) ok = tc::barrier_wait(empty(at), turn & 1, stop);
+      if (!ok && rank == 0) tc::barrier_drain(full(at), turn & 1);
+    }
   } else if (warp == 1 && lane == 0 && rank == 0) {
     // ---- products
     constexpr uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, a_rows(kMode), b_rows(kMode), kM * kCtas, kN);
@@ -324,7 +326,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           __syncwarp();
           if (ok) had++, ask_next();
         }
-        tc::tmem_loaded();
+        tc::tmem_loaded(v);
+        if (dual(kMode)) tc::tmem_loaded(u);
         if (kMode == kForward && p.keep) {  // G and then U to memory, as binary32
           if (lane == 0) tc::stores_read<0>();
           __syncwarp();

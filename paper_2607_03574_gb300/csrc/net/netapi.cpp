@@ -22,6 +22,7 @@ bool is_float(ndvm_dtype t) { return t == NDVM_F32 || t == NDVM_F16 || t == NDVM
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 constexpr int64_t kMost = (int64_t)1 << 48;  // elements a matrix spans at most
+constexpr int64_t kNormRows = ((int64_t)1 << 31) - 1;  // a block or more of them a launch
 
 bool spans(int64_t rows, int64_t cols, int64_t stride) {
   return stride >= 0 && (rows <= 1 || stride <= kMost / rows) && cols <= kMost;
@@ -58,7 +59,7 @@ ndvm_status ndvm_layer_norm_forward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t 
                                     int64_t y_stride, float* stats, void* stream) {
   if (!is_float(dtype) || (wtype != dtype && wtype != NDVM_F32))
     return set_error(NDVM_E_UNSUPPORTED, "layer norm takes F32, F16 and BF16, with weights of the same type or F32");
-  if (!sizes(rows, cols)) return bad("bad rows or cols");
+  if (!sizes(rows, cols) || rows > kNormRows) return bad("bad rows or cols");
   if (!(eps >= 0) || !std::isfinite(eps)) return bad("eps must be finite and not negative");
   if (rows == 0) return NDVM_OK;
   REFUSE(matrix_in(x, rows, cols, x_stride, dtype));
@@ -80,7 +81,7 @@ ndvm_status ndvm_layer_norm_backward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t
                                      void* workspace, size_t ws_bytes, void* stream) {
   if (!is_float(dtype) || (wtype != dtype && wtype != NDVM_F32))
     return set_error(NDVM_E_UNSUPPORTED, "layer norm takes F32, F16 and BF16, with weights of the same type or F32");
-  if (!sizes(rows, cols)) return bad("bad rows or cols");
+  if (!sizes(rows, cols) || rows > kNormRows) return bad("bad rows or cols");
   if (rows > 0) {
     REFUSE(matrix_in(dy, rows, cols, dy_stride, dtype));
     REFUSE(matrix_in(x, rows, cols, x_stride, dtype));
@@ -118,7 +119,7 @@ ndvm_status ndvm_dropout(ndvm_dtype dtype, int64_t rows, int64_t cols, const voi
   return done(launch_dropout(a, dtype, (cudaStream_t)stream), "dropout launch");
 }
 
-static constexpr int64_t kGatedMost = (int64_t)1 << 30;  // rows, k and n (a tile's coordinates are 32-bit)
+static constexpr int64_t kGatedMost = (int64_t)1 << 28;  // rows, k and n (a tile's coordinates are 32-bit, its sum's time bounded)
 
 static ndvm_status gated_check(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* x,
                                int64_t x_stride, const void* w_gate, int64_t g_stride, const void* w_up, int64_t u_stride) {

@@ -408,7 +408,6 @@ bool backward_variant(bool vectors, int64_t cols, F&& f) {
 template <typename T>
 cudaError_t forward(const NormArgs& a, int w_f32, cudaStream_t s) {
   if (a.rows == 0) return cudaSuccess;
-  if (a.rows > 0x7fffffff) return cudaErrorInvalidConfiguration;
   const bool vectors = a.cols % (16 / sizeof(T)) == 0 && on16(a.x, a.x_stride, a.rows, sizeof(T)) &&
                        on16(a.y, a.y_stride, a.rows, sizeof(T)) && on16(a.weight) && on16(a.bias);
   const bool held = forward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r, auto b) {
@@ -422,7 +421,6 @@ cudaError_t forward(const NormArgs& a, int w_f32, cudaStream_t s) {
 
 template <typename T>
 cudaError_t backward(NormArgs a, int w_f32, cudaStream_t s) {
-  if (a.rows > 0x7fffffff) return cudaErrorInvalidConfiguration;
   const bool sums = a.dweight || a.dbias;
   if (!sums) a.partial = nullptr;
   int blocks = 0;

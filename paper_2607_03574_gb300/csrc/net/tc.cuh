@@ -33,8 +33,9 @@ __device__ __forceinline__ uint64_t now_ns() {
   return t;
 }
 // Waits for the phase of `parity` to end; false once `*stop` is set, or after kWaitNs, which sets it: the
-// longest wait of a sound launch, for one tile's whole sum, is some milliseconds.
-constexpr uint64_t kWaitNs = 4000000000ull;
+// longest wait of a sound launch, for one tile's whole sum, is some milliseconds (seconds at the largest sizes that
+// the C ABI takes).
+constexpr uint64_t kWaitNs = 10000000000ull;
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
   if (barrier_try(bar, parity)) return true;
   const uint64_t start = now_ns();
@@ -159,7 +160,17 @@ __device__ __forceinline__ void tmem_load32(float (&v)[32], uint32_t addr) {
 #pragma unroll
   for (int i = 0; i < 32; i++) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// waits for the loads; what is done with their values comes after (they pass through)
+__device__ __forceinline__ void tmem_loaded(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]),
+                 "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]),
+                 "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]),
+                 "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]),
+                 "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]),
+                 "+f"(v[31])
+               :: "memory");
+}
 
 // Shared-memory descriptor of an operand in the 128-byte swizzle.  Contraction contiguous: a line of 128
 // bytes is 64 of the contraction, groups of 8 lines (rows or columns of the product) are 1024 bytes apart.

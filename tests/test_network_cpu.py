@@ -24,7 +24,7 @@ def norm(lib, dtype=BF16, wtype=BF16, rows=4, cols=8, x=A, xs=8, w=B, b=B, eps=1
 @pytest.mark.parametrize("change,status", [
     ({"dtype": F64}, UNSUPPORTED), ({"dtype": 9}, UNSUPPORTED), ({"wtype": F16}, UNSUPPORTED), ({"dtype": F32}, UNSUPPORTED),
     ({"rows": -1}, INVALID), ({"cols": 0}, INVALID), ({"rows": BIG}, INVALID), ({"cols": BIG}, INVALID),
-    ({"rows": 1 << 40, "cols": 1 << 40}, INVALID), ({"x": None}, INVALID), ({"y": None}, INVALID), ({"x": A + 1}, INVALID),
+    ({"rows": 1 << 40, "cols": 1 << 40}, INVALID), ({"rows": 1 << 31}, INVALID), ({"x": None}, INVALID), ({"y": None}, INVALID), ({"x": A + 1}, INVALID),
     ({"y": C + 1}, INVALID), ({"w": B + 1}, INVALID), ({"stats": C + 2}, INVALID), ({"xs": 7}, INVALID), ({"xs": -8}, INVALID),
     ({"ys": 0}, INVALID), ({"ys": 7}, INVALID), ({"xs": BIG}, INVALID), ({"eps": -1.0}, INVALID), ({"eps": float("nan")}, INVALID),
     ({"eps": float("inf")}, INVALID), ({"rows": 0, "x": None, "y": None}, OK)])
