@@ -1,22 +1,26 @@
 """Build the NDVM C-ABI library (libndvm.so) in-tree with nvcc for sm_103a.
 
 Translation units compile in parallel; the result is linked as one shared
-library with the CUDA runtime linked statically.  Run ``python -m
+library with the CUDA runtime linked statically, and a Python module on top of it
+(ndvm_torch.so) that holds the network operators' autograd nodes.  Run ``python -m
 paper_2607_03574_gb300.build`` or call :func:`build`.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libndvm.so")
+TORCH_OPS = os.path.join(OUT_DIR, "ndvm_torch.so")  # the network operators' autograd nodes (a Python module)
 
 SOURCES = ["tape.cpp", "trace_scheme.cpp", "trace_bytecode.cpp", "plan.cpp", "compact.cpp", "capi.cpp", "replay.cu", "scalar.cu", "matrix.cu",
            "net/netapi.cpp", "net/norm.cu", "net/dropout.cu", "net/gated.cu"]
@@ -38,10 +42,41 @@ def _deps() -> list[str]:
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(TORCH_OPS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_OPS))
     return any(os.path.getmtime(f) > t for f in _deps())
+
+
+def _torch_root() -> str:
+    spec = importlib.util.find_spec("torch")  # (not imported: that takes longer than finding it)
+    if spec is None:
+        raise RuntimeError("PyTorch not found: the network operators are built against it")
+    return list(spec.submodule_search_locations)[0]
+
+
+def _compile_torch_ops() -> str:
+    root, cuda = _torch_root(), os.path.dirname(os.path.dirname(_nvcc()))
+    obj = os.path.join(OUT_DIR, "net_torch_ops.cpp.o")
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", *("-I" + d for d in include), "-c",
+           os.path.join(CSRC, "net", "torch_ops.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compiling net/torch_ops.cpp failed:\n{r.stdout}\n{r.stderr}")
+    return obj
+
+
+def _link_torch_ops(obj: str) -> None:
+    lib = os.path.join(_torch_root(), "lib")
+    tmp = TORCH_OPS + f".tmp{os.getpid()}"
+    cmd = ["g++", "-shared", "-o", tmp, obj, "-L" + lib, "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ltorch_python",
+           "-L" + OUT_DIR, "-l:libndvm.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"linking ndvm_torch.so failed:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, TORCH_OPS)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -65,14 +100,17 @@ def build(force: bool = False, verbose: bool = False) -> str:
             print(r.stdout, r.stderr, file=sys.stderr)
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        torch_ops = ex.submit(_compile_torch_ops)
         objs = list(ex.map(compile_one, SOURCES))
+        torch_obj = torch_ops.result()
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-cudart", "static"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"linking libndvm.so failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    _link_torch_ops(torch_obj)
     return LIB
 
 

@@ -4,9 +4,10 @@
     h = gated(x, w_gate, w_up, "silu")               # act(x Wg^T) * (x Wu^T)
     z = dropout(h, p, seed, offset, residual=x)      # residual + dropout, the mask never stored
 
-These three are differentiable torch ops on the current stream, like ``loss_op(tape)``; each is
-made of raw calls (``*_forward``, ``*_backward``) that take outputs, a workspace and a stream and
-map one to one onto the C ABI (``ndvm_layer_norm_*``, ``ndvm_dropout``, ``ndvm_gated_*``).
+These three are differentiable torch ops on the current stream, like ``loss_op(tape)`` (their autograd
+nodes are in ``csrc/net/torch_ops.cpp``).  Under them are raw calls (``*_forward``, ``*_backward``) that take
+outputs, a workspace and a stream and map one to one onto the C ABI (``ndvm_layer_norm_*``,
+``ndvm_dropout``, ``ndvm_gated_*``).
 
 Layouts: the last dimension is contiguous and the leading ones are rows with one stride (a raw
 call refuses anything else, a differentiable op copies it).  Types: float32, float16 and bfloat16;
@@ -351,111 +352,60 @@ def gated_backward(dh, x, w_gate, w_up, activation="silu", wants=(True, True, Tr
 
 
 # ----------------------------------------------------------------------- differentiable ops
-def _rowed(t):
-    """t, or a contiguous copy where its layout is not rows of contiguous elements."""
-    if t is None or t.is_contiguous():
-        return t
-    try:
-        _rows(t, "")
-        return t
-    except NdvmError:
-        return t.contiguous()
-
-
 _ops = None
 
 
-def _first_order():
-    """A backward pass records nothing (gradient mode is on in one only to differentiate it again)."""
-    if _torch_module.is_grad_enabled():
-        raise NdvmError(3, "the network operators have no second derivatives")
-
-
-def _make_ops():
+def _load_ops():
+    """The module of autograd nodes (built beside the library)."""
     global _ops
-    torch = _torch_module or _start()
+    import importlib.machinery
+    import importlib.util
+    import os
 
-    class Norm(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, x, weight, bias, eps):
-            y, stats = layer_norm_forward(x, weight, bias, eps)
-            ctx.save_for_backward(x, weight, stats)
-            ctx.wtype = None if bias is None else bias.dtype
-            return y
-
-        @staticmethod
-        def backward(ctx, dy):
-            _first_order()
-            x, weight, stats = ctx.saved_tensors
-            return layer_norm_backward(_rowed(dy), x, weight, stats, ctx.needs_input_grad, wtype=ctx.wtype) + (None,)
-
-    class Drop(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, x, p, seed, offset, residual):
-            ctx.draw = (p, seed, offset)
-            return dropout_forward(x, p, seed, offset, residual)
-
-        @staticmethod
-        def backward(ctx, dy):
-            _first_order()
-            wants = ctx.needs_input_grad
-            return (dropout_forward(_rowed(dy), *ctx.draw) if wants[0] else None, None, None, None, dy if wants[4] else None)
-
-    class Gated(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, x, w_gate, w_up, activation):
-            # The two products are kept (8 bytes an element of h) where that is the faster: a long contraction, or
-            # few elements.  Forward and backward, computed again / kept: 16384 x 2048 -> 8192 2636 / 2353 us,
-            # 16 x 2048 -> 8192 67 / 57, 1501 x 333 -> 777 53 / 46; but 4096 x 1024 -> 4096 185 / 187, 4096 x 256 -> 1024
-            # 46 / 48, 16384 x 1024 -> 4096 654 / 704.
-            k, n = x.shape[-1], w_gate.shape[0]
-            kept = gated_kept(x, w_gate) if k >= 1536 or x.numel() // max(k, 1) * n <= 1 << 21 else None
-            ctx.save_for_backward(x, w_gate, w_up, kept)
-            ctx.activation = activation
-            return gated_forward(x, w_gate, w_up, activation, kept=kept)
-
-        @staticmethod
-        def backward(ctx, dh):
-            _first_order()
-            x, w_gate, w_up, kept = ctx.saved_tensors
-            return gated_backward(_rowed(dh), x, w_gate, w_up, ctx.activation, ctx.needs_input_grad, kept=kept) + (None,)
-
-    _ops = Norm.apply, Drop.apply, Gated.apply
-    return _ops
+    from . import build
+    _start()
+    load()
+    if not os.path.exists(build.TORCH_OPS):
+        raise NdvmError(6, f"the network operators' torch module is not built ({build.TORCH_OPS}); run paper_2607_03574_gb300.build")
+    loader = importlib.machinery.ExtensionFileLoader("ndvm_torch", build.TORCH_OPS)
+    ops = importlib.util.module_from_spec(importlib.util.spec_from_loader("ndvm_torch", loader))
+    loader.exec_module(ops)
+    _ops = ops
+    return ops
 
 
-def _recorded(*tensors):
-    if not (_torch_module or _start()).is_grad_enabled():
-        return False
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            return True
-    return False
+def _refuse(raw, *args):
+    """Raises what is wrong with an op's arguments: the raw call on them says it."""
+    raw(*args)
+    raise NdvmError(3, "the differentiable op does not take these arguments")
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """Layer norm over the last dimension as a differentiable op (gradients of x, weight and bias)."""
-    x = _rowed(x)
-    if not _recorded(x, weight, bias):
-        return layer_norm_forward(x, weight, bias, eps, want_stats=False)[0]
-    return (_ops or _make_ops())[0](x, weight, bias, eps)
+    try:
+        y = (_ops or _load_ops()).layer_norm(x, weight, bias, eps)
+    except TypeError:
+        y = None
+    return _refuse(layer_norm_forward, x, weight, bias, eps) if y is None else y
 
 
 def dropout(x, p, seed, offset=0, residual=None):
     """residual + dropout(x) as a differentiable op; see dropout_forward for what is drawn.  Give each call of
     a step its own offset range, and each step another seed or range."""
-    x, residual = _rowed(x), _rowed(residual)
-    if not _recorded(x, residual):
-        return dropout_forward(x, p, seed, offset, residual)
-    return (_ops or _make_ops())[1](x, p, seed, offset, residual)
+    try:
+        y = (_ops or _load_ops()).dropout(x, p, seed, offset, residual)
+    except TypeError:
+        y = None
+    return _refuse(dropout_forward, x, p, seed, offset, residual) if y is None else y
 
 
 def gated(x, w_gate, w_up, activation="silu"):
     """act(x w_gate^T) * (x w_up^T) as a differentiable op (gradients of x and both weights)."""
-    x, w_gate, w_up = _rowed(x), _rowed(w_gate), _rowed(w_up)
-    if not _recorded(x, w_gate, w_up):
-        return gated_forward(x, w_gate, w_up, activation)
-    return (_ops or _make_ops())[2](x, w_gate, w_up, activation)
+    try:
+        y = (_ops or _load_ops()).gated(x, w_gate, w_up, ACTIVATIONS.get(activation, -1))
+    except TypeError:
+        y = None
+    return _refuse(gated_forward, x, w_gate, w_up, activation) if y is None else y
 
 
 def check_operators():
