@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
     if (lane == 0) {
-      tc::stores_done();
+      tc::stores_read<0>();  // (what they write is there when the kernel ends)
       if (kMode == kGradient)  // (pieces that a launch that gave up has left)
         for (; had < asked; had++) tc::barrier_drain(dh_in(reader, had & 1), had >> 1 & 1);
     }

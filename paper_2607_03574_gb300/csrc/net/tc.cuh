@@ -99,7 +99,6 @@ __device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.co
 // until all but the last `kLeft` groups of this thread's stores have read their shared memory
 template <int kLeft>
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
-__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // makes this thread's writes to shared memory visible to the copies
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void store16(uint32_t to, uint4 v) {
