@@ -21,6 +21,8 @@ __device__ __forceinline__ void load_weight(Pairs<V> (&w)[kPairs<V>], const void
   } else if (f32) {
     if constexpr (V == 1) {
       w[0] = static_cast<const float*>(p)[c];
+    } else if constexpr (V == 2) {
+      w[0] = *reinterpret_cast<const float2*>(static_cast<const float*>(p) + c);
     } else {
 #pragma unroll
       for (int q = 0; q < V; q += 4) {
@@ -341,20 +343,28 @@ constexpr int kSms = 152;
 constexpr int kMostBlocks = kSms * 6;  // of k_backward: their column sums are what the workspace holds
 constexpr int kLongBlocks = 64;        // row ranges of k_columns_long
 
-bool on16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-bool on16(const void* p, int64_t stride, int64_t rows, size_t elem) {
-  return on16(p) && (rows <= 1 || (stride * (int64_t)elem) % 16 == 0);
+bool starts_on(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+// Elements a load: 16 bytes, two elements or one, whatever every row (and the weights) start and end on.
+template <typename T>
+int load_width(const NormArgs& a, int w_f32, std::initializer_list<std::pair<const void*, int64_t>> matrices) {
+  for (const int v : {16 / (int)sizeof(T), 2}) {
+    bool ok = a.cols % v == 0;
+    for (const auto& m : matrices) ok &= starts_on(m.first, v * sizeof(T)) && (a.rows <= 1 || m.second % v == 0);
+    const size_t w = v == 2 ? (w_f32 ? 8 : 2 * sizeof(T)) : 16;
+    if (ok && starts_on(a.weight, w) && starts_on(a.bias, w)) return v;
+  }
+  return 1;
 }
 
-// The kernel variant for rows of `cols` elements: V elements a load (16 bytes where every row starts and
-// ends on 16 bytes, else 1), N loads a thread, kRow threads a row, blocks an SM.  `f` is called with them as
-// integral constants; false: the row is longer than any variant holds.
+// The kernel variant for rows of `cols` elements: V elements a load, N loads a thread, kRow threads a row, blocks an
+// SM.  `f` is called with them as integral constants; false: the row is longer than any variant holds.  (Two
+// elements a load: 30000 x 2050 bfloat16 forward 94 us, with 2051 columns, one a load, 122.)
 template <int K> using Int = std::integral_constant<int, K>;
 
 template <typename T, typename F>
-bool forward_variant(bool vectors, int64_t cols, F&& f) {
+bool forward_variant(int width, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
-  if (vectors) {
+  if (width == V) {
     const int64_t packs = cols / V;  // a quarter of a warp, then a warp a row up to 8 loads a thread (no barriers), then blocks
     if (packs <= 8) f(Int<V>(), Int<1>(), Int<8>(), Int<12>());
     else if (packs <= 16) f(Int<V>(), Int<2>(), Int<8>(), Int<12>());
@@ -366,11 +376,19 @@ bool forward_variant(bool vectors, int64_t cols, F&& f) {
     else if (packs <= 1024) f(Int<V>(), Int<4>(), Int<256>(), Int<5>());
     else if (packs <= 2048) f(Int<V>(), Int<4>(), Int<512>(), Int<2>());
     else return false;
+  } else if (width == 2) {
+    if (cols <= 256) f(Int<2>(), Int<4>(), Int<32>(), Int<12>());
+    else if (cols <= 1024) f(Int<2>(), Int<16>(), Int<32>(), Int<8>());
+    else if (cols <= 2048) f(Int<2>(), Int<8>(), Int<128>(), Int<10>());
+    else if (cols <= 4096) f(Int<2>(), Int<8>(), Int<256>(), Int<5>());
+    else if (cols <= 8192) f(Int<2>(), Int<8>(), Int<512>(), Int<2>());
+    else return false;
   } else {
     if (cols <= 64) f(Int<1>(), Int<8>(), Int<8>(), Int<12>());
     else if (cols <= 128) f(Int<1>(), Int<4>(), Int<32>(), Int<12>());
     else if (cols <= 512) f(Int<1>(), Int<16>(), Int<32>(), Int<10>());
     else if (cols <= 2048) f(Int<1>(), Int<16>(), Int<128>(), Int<10>());
+    else if (cols <= 4096) f(Int<1>(), Int<16>(), Int<256>(), Int<5>());
     else if (cols <= 8192) f(Int<1>(), Int<16>(), Int<512>(), Int<2>());
     else return false;
   }
@@ -378,19 +396,27 @@ bool forward_variant(bool vectors, int64_t cols, F&& f) {
 }
 
 template <typename T, typename F>
-bool backward_variant(bool vectors, int64_t cols, F&& f) {
+bool backward_variant(int width, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
-  if (vectors) {
+  if (width == V) {
     const int64_t packs = cols / V;
     if (packs <= 8) f(Int<V>(), Int<1>(), Int<8>(), Int<3>());
     else if (packs <= 16) f(Int<V>(), Int<2>(), Int<8>(), Int<2>());
     else if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<3>());
     else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<2>());
     else if (packs <= 128) f(Int<V>(), Int<2>(), Int<64>(), Int<2>());
-    else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>(), Int<2>());
+    else if (packs <= 256) f(Int<V>(), Int<1>(), Int<256>(), Int<4>());  // (65536 x 2048 bf16 146 us; two loads, half the threads: 150)
     else if (packs <= 512) f(Int<V>(), Int<2>(), Int<256>(), Int<2>());
     else if (packs <= 1024) f(Int<V>(), Int<2>(), Int<512>(), Int<1>());
     else if (packs <= 2048 && sizeof(T) == 4) f(Int<4>(), Int<4>(), Int<512>(), Int<1>());  // (16-bit rows would not fit in 128 registers)
+    else return false;
+  } else if (width == 2) {
+    if (cols <= 256) f(Int<2>(), Int<4>(), Int<32>(), Int<3>());
+    else if (cols <= 512) f(Int<2>(), Int<4>(), Int<64>(), Int<3>());
+    else if (cols <= 1024) f(Int<2>(), Int<4>(), Int<128>(), Int<3>());
+    else if (cols <= 2048) f(Int<2>(), Int<4>(), Int<256>(), Int<3>());
+    else if (cols <= 4096) f(Int<2>(), Int<4>(), Int<512>(), Int<1>());
+    else if (cols <= 8192) f(Int<2>(), Int<8>(), Int<512>(), Int<1>());
     else return false;
   } else {
     if (cols <= 64) f(Int<1>(), Int<8>(), Int<8>(), Int<3>());
@@ -408,9 +434,8 @@ bool backward_variant(bool vectors, int64_t cols, F&& f) {
 template <typename T>
 cudaError_t forward(const NormArgs& a, int w_f32, cudaStream_t s) {
   if (a.rows == 0) return cudaSuccess;
-  const bool vectors = a.cols % (16 / sizeof(T)) == 0 && on16(a.x, a.x_stride, a.rows, sizeof(T)) &&
-                       on16(a.y, a.y_stride, a.rows, sizeof(T)) && on16(a.weight) && on16(a.bias);
-  const bool held = forward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r, auto b) {
+  const int width = load_width<T>(a, w_f32, {{a.x, a.x_stride}, {a.y, a.y_stride}});
+  const bool held = forward_variant<T>(width, a.cols, [&](auto v, auto n, auto r, auto b) {
     constexpr int kRow = decltype(r)::value, kRows = kBlock<kRow> / kRow;
     k_forward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value>
         <<<(unsigned)((a.rows + kRows - 1) / kRows), kBlock<kRow>, 0, s>>>(a, w_f32);
@@ -425,10 +450,8 @@ cudaError_t backward(NormArgs a, int w_f32, cudaStream_t s) {
   if (!sums) a.partial = nullptr;
   int blocks = 0;
   if (a.rows > 0 && (a.dx || sums)) {
-    const bool vectors = a.cols % (16 / sizeof(T)) == 0 && on16(a.x, a.x_stride, a.rows, sizeof(T)) &&
-                         on16(a.dy, a.dy_stride, a.rows, sizeof(T)) && on16(a.weight) &&
-                         (!a.dx || on16(a.dx, a.dx_stride, a.rows, sizeof(T)));
-    const bool held = backward_variant<T>(vectors, a.cols, [&](auto v, auto n, auto r, auto b) {
+    const int width = load_width<T>(a, w_f32, {{a.x, a.x_stride}, {a.dy, a.dy_stride}, {a.dx, a.dx ? a.dx_stride : 0}});
+    const bool held = backward_variant<T>(width, a.cols, [&](auto v, auto n, auto r, auto b) {
       constexpr int kRow = decltype(r)::value, kThreads = kBackBlock<kRow>, kRows = kThreads / kRow;
       // as many blocks as stay resident, or a block a group of rows where there are fewer
       static const int resident = [] {
