@@ -396,7 +396,7 @@ bool forward_variant(int width, int64_t cols, F&& f) {
 }
 
 template <typename T, typename F>
-bool backward_variant(int width, int64_t cols, F&& f) {
+bool backward_variant(int width, int64_t rows, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
   if (width == V) {
     const int64_t packs = cols / V;
@@ -405,7 +405,10 @@ bool backward_variant(int width, int64_t cols, F&& f) {
     else if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<3>());
     else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<2>());
     else if (packs <= 128) f(Int<V>(), Int<2>(), Int<64>(), Int<2>());
-    else if (packs <= 256) f(Int<V>(), Int<1>(), Int<256>(), Int<4>());  // (65536 x 2048 bf16 146 us; two loads, half the threads: 150)
+    // one load and twice the threads: more warps for many rows (65536 x 2048 bf16 146 us against 150), more column
+    // sums to join for few (4096 x 2048 19 us against 16)
+    else if (packs <= 256 && rows >= 32768) f(Int<V>(), Int<1>(), Int<256>(), Int<4>());
+    else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>(), Int<2>());
     else if (packs <= 512) f(Int<V>(), Int<2>(), Int<256>(), Int<2>());
     else if (packs <= 1024) f(Int<V>(), Int<2>(), Int<512>(), Int<1>());
     else if (packs <= 2048 && sizeof(T) == 4) f(Int<4>(), Int<4>(), Int<512>(), Int<1>());  // (16-bit rows would not fit in 128 registers)
@@ -451,7 +454,7 @@ cudaError_t backward(NormArgs a, int w_f32, cudaStream_t s) {
   int blocks = 0;
   if (a.rows > 0 && (a.dx || sums)) {
     const int width = load_width<T>(a, w_f32, {{a.x, a.x_stride}, {a.dy, a.dy_stride}, {a.dx, a.dx ? a.dx_stride : 0}});
-    const bool held = backward_variant<T>(width, a.cols, [&](auto v, auto n, auto r, auto b) {
+    const bool held = backward_variant<T>(width, a.rows, a.cols, [&](auto v, auto n, auto r, auto b) {
       constexpr int kRow = decltype(r)::value, kThreads = kBackBlock<kRow>, kRows = kThreads / kRow;
       // as many blocks as stay resident, or a block a group of rows where there are fewer
       static const int resident = [] {
