@@ -86,7 +86,7 @@ def _rounded(want, err, t):
 NORM_SIZES = [(1, 1), (3, 1), (1, 2), (5, 7), (2, 31), (33, 32), (7, 33), (64, 256), (9, 255), (130, 1000), (17, 1024),
               (40, 1025), (300, 1537), (3, 4096), (5, 5001), (2, 8192), (2, 8200), (3, 16384), (2, 16421), (1, 40000),
               (2, 70001), (20000, 24), (4999, 130), (3001, 64), (1003, 128), (777, 61), (33, 8), (5, 16), (50, 1002), (9, 4098), (21, 514), (301, 66), (2, 8190),
-              (13, 2050), (6, 250), (40000, 1100)]
+              (13, 2050), (6, 250), (33000, 1104), (33000, 600)]
 
 
 @pytest.mark.parametrize("t,wt", [("f32", "f32"), ("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
