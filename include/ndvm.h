@@ -272,7 +272,7 @@ ndvm_status ndvm_measure_op_cost(int fn, int iters, double* ns_per_call, void* s
  *   - The first call of an operator on a device loads its kernels: make it before any stream capture.
  *   - Errors: NDVM_E_INVALID_ARG for null pointers, sizes, strides, alignment or a workspace that
  *     is too small; NDVM_E_UNSUPPORTED for a type the operator does not take.  Outputs may not
- *     overlap inputs, except ndvm_dropout's y, which may be x or residual.
+ *     overlap inputs, except ndvm_dropout's y, which may be x or residual itself (address and stride).
  */
 
 /*
@@ -344,8 +344,8 @@ size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backwa
  * ndvm_gated_backward -- gradients of ndvm_gated_forward under the cotangent dh (rows x n).  The two
  * products are computed again; dG and dU are rounded to dtype before the products that make dx (rows x k)
  * and dw_gate, dw_up (n x k, contiguous), or, where there are few of them (rows * min(n, k) up to 16384 or
- * n * k up to 2048), split into two halves of dtype that lose nothing.  Each output may be NULL if not wanted; rows = 0 sets dw_gate
- * and dw_up to 0.
+ * n * k up to 2048), split into two halves of dtype that together lose next to nothing.  Each output may be
+ * NULL if not wanted; rows = 0 sets dw_gate and dw_up to 0.
  */
 ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
                                 const void* dh, int64_t dh_stride, const void* x, int64_t x_stride, const void* w_gate,
@@ -358,7 +358,7 @@ ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t r
  *   kept : device, 16-byte aligned floats, 2 x rows rows (G's, then U's) of ndvm_gated_kept_stride(n), written by
  *          the one and read by the other; NULL: nothing is kept, as above
  * Keeping costs 8 bytes an element of h and saves a third of the backward pass's operations: it pays from about
- * k = 1024 on, and for few rows.
+ * k = 1536 on, and where h has up to about 2^21 elements.
  */
 int64_t ndvm_gated_kept_stride(int64_t n);
 ndvm_status ndvm_gated_forward_keep(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,

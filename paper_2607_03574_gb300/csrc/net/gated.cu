@@ -758,7 +758,7 @@ cudaError_t launch_product(ProductArgs& p, const Cut& k, cudaStream_t s, bool fo
   return cudaGetLastError();
 }
 
-// Few elements: dG and dU are handed on in two halves of 16 bits, so that nothing is lost before the last
+// Few elements: dG and dU are handed on in two halves of 16 bits, so that next to nothing is lost before the last
 // rounding.  (Over many elements the rounding of dG and dU adds to the results' own as squares add, 1.41 times in
 // all; over few it scatters, to more than twice: 4096 elements leave 1.2 to 1.55, 16384 1.37 to 1.49.)  It costs little
 // there: dx has the halves' rows one after the other in its tiles, the weights' gradients twice the steps.
