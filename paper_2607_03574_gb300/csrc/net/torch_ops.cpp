@@ -5,6 +5,7 @@
 // A function returns None where an argument is not what the operator takes; the Python layer's raw call
 // then says what is wrong with it.
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -29,11 +30,13 @@ void set_error(int status, const char* message) {
   py::object e = type(status, message);
   PyErr_SetObject(type.ptr(), e.ptr());
 }
-void check_forward(int status) {  // (in a call from Python)
-  if (status == NDVM_OK) return;
+[[noreturn]] void raise_forward(int status, const char* message) {  // (in a call from Python)
   py::gil_scoped_acquire lock;
-  set_error(status, ndvm_last_error());
+  set_error(status, message);
   throw py::error_already_set();
+}
+void check_forward(int status) {
+  if (status != NDVM_OK) raise_forward(status, ndvm_last_error());
 }
 [[noreturn]] void raise_backward(int status, const char* message) {  // (in a thread of the autograd engine)
   py::gil_scoped_acquire lock;
@@ -45,9 +48,23 @@ void check_forward(int status) {  // (in a call from Python)
 void check_backward(int status) {
   if (status != NDVM_OK) raise_backward(status, ndvm_last_error());
 }
-// a backward pass records nothing (gradient mode is on in one only to differentiate it again)
-void first_order() {
+// Whether one of the tensors has a forward-mode tangent: a launch does not carry it on, and an output without one
+// would say that the derivative is 0.
+bool tangents(std::initializer_list<const Tensor*> ts) {
+  if (!c10::AutogradState::get_tls_state().get_fw_grad_mode()) return false;
+  for (const Tensor* t : ts)
+    if (t->defined() && t->_fw_grad(0).defined()) return true;
+  return false;
+}
+constexpr const char* kNoTangents = "the network operators have no forward-mode derivatives";
+// what an op refuses of its inputs before it reads them
+void check_inputs(std::initializer_list<const Tensor*> ts) {
+  if (tangents(ts)) raise_forward(NDVM_E_UNSUPPORTED, kNoTangents);
+}
+// A backward pass records nothing (gradient mode is on in one only to differentiate it again).
+void first_order(const Tensor& grad) {
   if (at::GradMode::is_enabled()) raise_backward(NDVM_E_UNSUPPORTED, "the network operators have no second derivatives");
+  if (tangents({&grad})) raise_backward(NDVM_E_UNSUPPORTED, kNoTangents);
 }
 
 int type_code(const Tensor& t) {
@@ -119,7 +136,7 @@ struct Norm : torch::autograd::Function<Norm> {
     return y;
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
-    first_order();
+    first_order(grads[0]);
     const variable_list saved = ctx->get_saved_variables();
     const Tensor &x = saved[0], &weight = saved[1], &stats = saved[2], dy = rowed(grads[0]);
     const Rows r(x);
@@ -147,6 +164,7 @@ Maybe layer_norm(const Tensor& given, const Maybe& w, const Maybe& b, double eps
     if (t->defined() && (!here(*t, device) || t->dim() != 1 || t->size(0) != x.size(-1) || !t->is_contiguous() || type_code(*t) < 0))
       return std::nullopt;
   if (weight.defined() && bias.defined() && weight.scalar_type() != bias.scalar_type()) return std::nullopt;
+  check_inputs({&x, &weight, &bias});
   return recorded({&x, &weight, &bias}) ? Norm::apply(x, w, b, eps) : norm_forward(x, weight, bias, eps, nullptr);
 }
 
@@ -170,7 +188,7 @@ struct Drop : torch::autograd::Function<Drop> {
     return y;
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
-    first_order();
+    first_order(grads[0]);
     Tensor dx, none;
     if (ctx->needs_input_grad(0)) {
       int status;
@@ -187,6 +205,7 @@ Maybe dropout(const Tensor& given, double p, uint64_t seed, uint64_t offset, con
   if (!here(given, device) || given.dim() == 0 || type_code(given) < 0) return std::nullopt;
   const Tensor x = rowed(given), residual = r && r->defined() ? rowed(*r) : Tensor();
   if (residual.defined() && (!here(residual, device) || residual.sizes() != x.sizes() || residual.scalar_type() != x.scalar_type())) return std::nullopt;
+  check_inputs({&x, &residual});
   if (recorded({&x, &residual})) return Drop::apply(x, residual.defined() ? Maybe(residual) : Maybe(), p, seed, offset);
   int status;
   Tensor y = drop(x, p, seed, offset, residual, &status);
@@ -233,7 +252,7 @@ struct Gated : torch::autograd::Function<Gated> {
     return h;
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
-    first_order();
+    first_order(grads[0]);
     const variable_list saved = ctx->get_saved_variables();
     const Tensor &x = saved[0], &w_gate = saved[1], &w_up = saved[2], &kept = saved[3], dh = rowed(grads[0]);
     const Operands o(x, w_gate, w_up);
@@ -259,6 +278,7 @@ Maybe gated(const Tensor& gx, const Tensor& gg, const Tensor& gu, int64_t act) {
   if (gg.sizes() != gu.sizes() || gg.size(1) != gx.size(-1)) return std::nullopt;
   if (act < 0 || type_code(gx) < 0 || gg.scalar_type() != gx.scalar_type() || gu.scalar_type() != gx.scalar_type()) return std::nullopt;
   const Tensor x = rowed(gx), w_gate = rowed(gg), w_up = rowed(gu);
+  check_inputs({&x, &w_gate, &w_up});
   return recorded({&x, &w_gate, &w_up}) ? Gated::apply(x, w_gate, w_up, act) : gated_forward(x, w_gate, w_up, act, Tensor());
 }
 

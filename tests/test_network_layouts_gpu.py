@@ -1,0 +1,40 @@
+"""Layouts that the differentiable network operators copy before they read them (GPU): whatever a raw call refuses."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _windows(rows, cols, seed):
+    """Overlapping rows: row i is elements i .. i + cols - 1 of one series."""
+    import torch
+    t = torch.randn(rows + cols - 1, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").bfloat16()
+    return t.unfold(0, cols, 1)
+
+
+def test_overlapping_rows_are_copied(ndvm, cuda):
+    """Sliding windows as x, residual, weights and cotangents, forward and backward: the bits of a contiguous copy's."""
+    import torch
+    x, r, dy, dh = _windows(37, 72, 1), _windows(37, 72, 2), _windows(37, 72, 3), _windows(37, 40, 4)
+    wg, wu = _windows(40, 72, 5), _windows(40, 72, 6)
+    w = torch.linspace(0.5, 1.5, 72, device="cuda")
+    calls = [(lambda x, w: ndvm.layer_norm(x, w), (x, w), dy), (ndvm.gated, (x, wg, wu), dh),
+             (lambda x, r: ndvm.dropout(x, 0.25, 9, 0, r), (x, r), dy)]
+    for call, args, cot in calls:
+        plain = [a.detach().contiguous().requires_grad_(True) for a in args]
+        want = call(*plain)
+        grads = torch.autograd.grad(want, plain, cot.contiguous())
+        with torch.no_grad():
+            assert torch.equal(call(*args), want)
+        leaves = [a.detach().requires_grad_(True) for a in args]
+        y = call(*leaves)
+        assert torch.equal(y, want)
+        for a, b in zip(torch.autograd.grad(y, leaves, cot), grads):
+            assert torch.equal(a, b)
+
+
+def test_raw_calls_name_the_overlapping_rows(ndvm, cuda):
+    x = _windows(8, 24, 1)
+    for call in (lambda: ndvm.layer_norm_forward(x), lambda: ndvm.dropout_forward(x, 0.1, 0), lambda: ndvm.gated_forward(x, x, x),
+                 lambda: ndvm.gated_forward(x.contiguous(), x, x.contiguous())):
+        with pytest.raises(ndvm.NdvmError, match="rows of contiguous elements"):
+            call()

@@ -1,0 +1,58 @@
+"""What the differentiable network operators do under torch's other ways of running a program (GPU): a mode in which
+a launch of theirs would silently be lost is refused."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _ops(ndvm):
+    """(name, call, its tensors): every operator with every tensor argument that it takes."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(5)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda").bfloat16()
+
+    x, r, w, b = randn(12, 24), randn(12, 24), randn(24), randn(24)
+    return [("layer_norm", ndvm.layer_norm, (x, w, b)), ("gated", ndvm.gated, (x, randn(40, 24), randn(40, 24))),
+            ("dropout", lambda x, r: ndvm.dropout(x, 0.25, 3, 8, r), (x, r))]
+
+
+@pytest.mark.parametrize("requires_grad", [False, True])
+def test_forward_mode_tangents_are_refused(ndvm, cuda, requires_grad):
+    """An input with a tangent (of any argument) raises: an output without one would say that the derivative is 0."""
+    import torch
+    from torch.autograd import forward_ad
+    for name, call, args in _ops(ndvm):
+        args = [a.clone().requires_grad_(requires_grad) for a in args]
+        want = call(*args)
+        with forward_ad.dual_level():
+            for i in range(len(args)):
+                duals = list(args)
+                duals[i] = forward_ad.make_dual(args[i], torch.ones_like(args[i]))
+                with pytest.raises(ndvm.NdvmError, match="forward-mode"):
+                    call(*duals)
+                    pytest.fail(f"{name}: argument {i} was not refused")
+            assert torch.equal(call(*args), want)  # (a level alone changes nothing)
+
+
+def test_forward_mode_through_the_backward_pass_is_refused(ndvm, cuda):
+    """A cotangent with a tangent (forward over reverse) raises too."""
+    import torch
+    from torch.autograd import forward_ad
+    for name, call, args in _ops(ndvm):
+        args = [a.clone().requires_grad_(True) for a in args]
+        y = call(*args)
+        with forward_ad.dual_level():
+            dy = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
+            with pytest.raises(ndvm.NdvmError, match="forward-mode"):
+                torch.autograd.grad(y, args[0], dy)
+                pytest.fail(name)
+
+
+def test_functional_jvp_raises(ndvm, cuda):
+    import torch
+    for name, call, args in _ops(ndvm):
+        with pytest.raises(RuntimeError):
+            torch.func.jvp(lambda x: call(x, *args[1:]), (args[0],), (torch.ones_like(args[0]),))
+            pytest.fail(name)
