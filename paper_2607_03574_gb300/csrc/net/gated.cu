@@ -517,30 +517,36 @@ __global__ void __launch_bounds__(256) k_gradient(const float* kept, int64_t kep
 }
 
 // Up to three matrices of `cols` columns to rows that start on 16 bytes (TMA reads no others): a warp a row, 16 bytes
-// a lane, out of the one or two aligned 16-byte blocks that hold them (only blocks with bytes of the row are read).
+// a lane, out of the one or two aligned 16-byte blocks that hold them.  What lies before and behind a row is not read
+// (it need not be the caller's): the blocks at its two ends are read element by element.
 struct PackArgs {
   const void* from[3];
   void* to[3];
   int64_t stride[3], rows[3];
   int64_t cols, pitch;
 };
+// the aligned 16 bytes at `block`, 0 where they are not of the row
+__device__ __forceinline__ uint4 row_block(const char* block, const char* row, const char* end) {
+  if (block >= row && block + 16 <= end) return *reinterpret_cast<const uint4*>(block);
+  uint32_t e[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    e[i] = block + 2 * i >= row && block + 2 * i < end ? *reinterpret_cast<const uint16_t*>(block + 2 * i) : 0;
+  return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+}
 __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a) {
   const int w = blockIdx.y, lane = threadIdx.x % 32;
   for (int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; row < a.rows[w]; row += (int64_t)gridDim.x * 8) {
     const char* from = static_cast<const char*>(a.from[w]) + row * a.stride[w] * 2;
     char* to = static_cast<char*>(a.to[w]) + row * a.pitch * 2;
     const int off = (int)(reinterpret_cast<uintptr_t>(from) % 16);  // even, the same for all of the row's pieces
-    const int64_t bytes = a.cols * 2;
+    const char* end = from + a.cols * 2;
     for (int64_t c = lane * 16; c < a.pitch * 2; c += 32 * 16) {
-      const uint4* block = reinterpret_cast<const uint4*>(from + c - off);
+      const char* block = from + c - off;
       uint32_t v[9] = {};
-      const uint4 p = block[0];
+      const uint4 p = row_block(block, from, end), q = off ? row_block(block + 16, from, end) : make_uint4(0, 0, 0, 0);
       v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
-      if (off + (bytes - c) > 16) {
-        const uint4 q = block[1];
-        v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
-      }
-      // (a row's last piece may end in what lies behind the row: columns that no tensor map has)
+      v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
 #pragma unroll
       for (int i = 0; i < 7; i++) v[i] = off & 8 ? v[i + 2] : v[i];
 #pragma unroll
