@@ -41,11 +41,22 @@ __device__ __forceinline__ void activate(float2 g, float2* a, float2* da) {
     *a = make_float2(g.x > 0.0f ? g.x : (g.x != g.x ? g.x : 0.0f), g.y > 0.0f ? g.y : (g.y != g.y ? g.y : 0.0f));
     *da = make_float2(g.x > 0.0f ? 1.0f : 0.0f, g.y > 0.0f ? 1.0f : 0.0f);
   } else if constexpr (kAct == NDVM_ACT_GELU) {
-    const float2 half = make_float2(0.5f, 0.5f);
-    const float2 cdf = fma(make_float2(erff(g.x * 0.70710678f), erff(g.y * 0.70710678f)), half, half);
+    // The normal distribution function by its tail, cdf(-|g|) = e^(-g^2 / 2) t Q(t) with t = 1 / (1 + 0.35 |g|): relative
+    // accuracy on both sides (1 + erf cancels below zero, to 4 % at -5 and to nothing from -5.5 on).  Q is the polynomial
+    // of degree 8 with the least largest relative error on 0 <= |g| <= 15 (3.2e-8), by reweighted least squares.
     const float2 q = mul(mul(g, g), make_float2(-0.72134752f, -0.72134752f));  // -g^2 / 2 in powers of two
+    const float2 e = make_float2(power2(q.x), power2(q.y));
+    const float2 d = make_float2(fmaf(fabsf(g.x), 0.35f, 1.0f), fmaf(fabsf(g.y), 0.35f, 1.0f));
+    const float2 t = make_float2(reciprocal(d.x), reciprocal(d.y));
+    constexpr float kQ[9] = {0.139621258f, 0.139864326f,  0.119815566f, 0.105574533f,   -0.0232631564f,
+                             0.15939188f,  -0.255900919f, 0.144060329f, -0.0291638281f};
+    float2 tail = make_float2(kQ[8], kQ[8]);
+#pragma unroll
+    for (int i = 7; i >= 0; i--) tail = fma(tail, t, make_float2(kQ[i], kQ[i]));
+    tail = mul(mul(e, t), tail);
+    const float2 cdf = make_float2(g.x < 0.0f ? tail.x : 1.0f - tail.x, g.y < 0.0f ? tail.y : 1.0f - tail.y);
     *a = mul(g, cdf);
-    *da = fma(mul(g, make_float2(power2(q.x), power2(q.y))), make_float2(0.39894228f, 0.39894228f), cdf);
+    *da = fma(mul(g, e), make_float2(0.39894228f, 0.39894228f), cdf);
   } else {
     const float2 q = mul(g, make_float2(-1.44269504f, -1.44269504f));
     const float2 d = add(make_float2(power2(q.x), power2(q.y)), one), s = make_float2(reciprocal(d.x), reciprocal(d.y));
