@@ -22,11 +22,11 @@ namespace {
 
 __device__ int g_stopped;  // a wait in k_product ran out (ndvm_check_operators)
 
-// act(g) and act'(g), two at a time.  1 / (1 + e^-g) is the hardware's power of two and reciprocal (off by a
-// few units of binary32's last place, and by a share of |g| of them where the value itself vanishes).
-__device__ __forceinline__ float power2(float x) {
+// act(g) and act'(g), two at a time: off by a few units of binary32's last place, and by a share of |g| (gelu: g^2) of
+// them where the value itself vanishes.  Powers of two and reciprocals are the hardware's.
+__device__ __forceinline__ float power2(float x) {  // (down to binary32's smallest)
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float reciprocal(float x) {
@@ -58,9 +58,12 @@ __device__ __forceinline__ void activate(float2 g, float2* a, float2* da) {
     *a = mul(g, cdf);
     *da = fma(mul(g, e), make_float2(0.39894228f, 0.39894228f), cdf);
   } else {
-    const float2 q = mul(g, make_float2(-1.44269504f, -1.44269504f));
-    const float2 d = add(make_float2(power2(q.x), power2(q.y)), one), s = make_float2(reciprocal(d.x), reciprocal(d.y));
-    const float2 rest = fma(s, make_float2(-1.0f, -1.0f), one);  // 1 - s
+    // s = 1 / (1 + e^-g) and 1 - s are r and e r, with e = e^-|g| and r = 1 / (1 + e), the one or the other way round: nothing
+    // cancels, overflows or is flushed in either tail
+    const float2 e = make_float2(power2(fabsf(g.x) * -1.44269504f), power2(fabsf(g.y) * -1.44269504f));
+    const float2 d = add(e, one), r = make_float2(reciprocal(d.x), reciprocal(d.y)), er = mul(e, r);
+    const float2 s = make_float2(g.x < 0.0f ? er.x : r.x, g.y < 0.0f ? er.y : r.y);
+    const float2 rest = make_float2(g.x < 0.0f ? r.x : er.x, g.y < 0.0f ? r.y : er.y);
     *a = kAct == NDVM_ACT_SILU ? mul(g, s) : s;
     *da = kAct == NDVM_ACT_SILU ? fma(*a, rest, s) : mul(s, rest);
   }

@@ -6,7 +6,7 @@ and U = 1 exactly, h = act(g), dU = act(g) and dG = act'(g) (dh = 1), and dx = (
 
 Bounds, derived from binary32 arithmetic (U = 2^-24): e^-|g| is the power of two of a product that is off by 1.3 U |g| in
 all, itself off by up to 4 U; a sum, a reciprocal and a product or two follow, a few U each: 16 U (1 + |g|) of the value.
-The normal distribution's density and tail: their logarithm moves by g^2 times the argument's 1.3 U; the error function
+The normal distribution's density and tail: their logarithm moves by g^2 times the argument's 1.3 U; the tail itself
 is off by 8 U: 16 U (1 + g^2).  Steps of 2^-149 (below 2^-126) are allowed for, times |g|; in dx, which a tensor core
 adds up, anything below 2^-125.  Then one rounding to bfloat16 for h and two for dx.
 """
@@ -81,3 +81,15 @@ def test_gelu_tails(ndvm, cuda, n, repeat, keep):
 @pytest.mark.parametrize("g", [-12.0, -8.0, -5.0, 4.0])
 def test_gelu_tails_of_one_row(ndvm, cuda, g):
     _run(ndvm, "gelu", [g], 1, False)
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("n,repeat", SHAPES)
+@pytest.mark.parametrize("act", ["silu", "sigmoid"])
+def test_logistic_tails(ndvm, cuda, act, n, repeat, keep):
+    _tails(act, n, repeat, keep, ndvm)
+
+
+@pytest.mark.parametrize("act,g", [("silu", -95.0), ("silu", -88.0), ("silu", 30.0), ("sigmoid", -80.0), ("sigmoid", 25.0)])
+def test_logistic_tails_of_one_row(ndvm, cuda, act, g):
+    _run(ndvm, act, [g], 1, False)
