@@ -6,10 +6,12 @@
 // then says what is wrong with it.
 #include <ATen/ATen.h>
 #include <c10/core/AutogradState.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include "../../../include/ndvm.h"
@@ -57,14 +59,23 @@ bool tangents(std::initializer_list<const Tensor*> ts) {
   return false;
 }
 constexpr const char* kNoTangents = "the network operators have no forward-mode derivatives";
+// Whether torch records a program here (torch.jit.trace, or torch.fx's proxies): it would record the allocation of an
+// output and not the launch that fills it.
+bool traced() {
+  return torch::jit::tracer::isTracing() || c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY).has_value() ||
+         c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::PreDispatch);
+}
+constexpr const char* kNoTraces = "the network operators cannot be traced: the trace would not hold their launches";
 // what an op refuses of its inputs before it reads them
 void check_inputs(std::initializer_list<const Tensor*> ts) {
   if (tangents(ts)) raise_forward(NDVM_E_UNSUPPORTED, kNoTangents);
+  if (traced()) raise_forward(NDVM_E_UNSUPPORTED, kNoTraces);
 }
 // A backward pass records nothing (gradient mode is on in one only to differentiate it again).
 void first_order(const Tensor& grad) {
   if (at::GradMode::is_enabled()) raise_backward(NDVM_E_UNSUPPORTED, "the network operators have no second derivatives");
   if (tangents({&grad})) raise_backward(NDVM_E_UNSUPPORTED, kNoTangents);
+  if (traced()) raise_backward(NDVM_E_UNSUPPORTED, kNoTraces);
 }
 
 int type_code(const Tensor& t) {

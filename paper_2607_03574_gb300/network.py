@@ -74,7 +74,12 @@ def _rows(t, name):
 
 
 def _device(torch, x):
-    """The index of x's device, which has to be the current one (the kernels launch there)."""
+    """The index of x's device, which has to be the current one (the kernels launch there).  Where torch records a
+    program, it would record an output's allocation and not the launch that fills it: refused."""
+    c = torch._C
+    if (c._get_tracing_state() is not None or c._get_dispatch_mode(c._TorchDispatchModeKey.PROXY) is not None
+            or c._dispatch_tls_is_dispatch_key_included(c.DispatchKey.PreDispatch)):
+        raise NdvmError(3, "the network operators cannot be traced: the trace would not hold their launches")
     device = x.get_device()
     if device < 0:
         raise NdvmError(1, "x must be a CUDA tensor (the network operators have no CPU path)")

@@ -56,3 +56,41 @@ def test_functional_jvp_raises(ndvm, cuda):
         with pytest.raises(RuntimeError):
             torch.func.jvp(lambda x: call(x, *args[1:]), (args[0],), (torch.ones_like(args[0]),))
             pytest.fail(name)
+
+
+def test_traces_are_refused(ndvm, cuda):
+    """A tracer sees the output's allocation and not the launch that fills it, so its program would return memory that
+    nothing wrote: the differentiable ops and the raw calls raise under one."""
+    import torch
+    from torch.fx.experimental.proxy_tensor import make_fx
+    raw = [("layer_norm_forward", lambda x, w, b: ndvm.layer_norm_forward(x, w, b)[0], _ops(ndvm)[0][2]),
+           ("gated_forward", ndvm.gated_forward, _ops(ndvm)[1][2]),
+           ("dropout_forward", lambda x, r: ndvm.dropout_forward(x, 0.25, 3, 8, r), _ops(ndvm)[2][2])]
+    for name, op, args in _ops(ndvm) + raw:
+        call = (lambda x, r: op(x, r)) if len(args) == 2 else (lambda x, a, b: op(x, a, b))  # (make_fx counts arguments)
+        want = call(*args)
+        for tracer in (lambda: torch.jit.trace(call, args, check_trace=False), lambda: make_fx(call)(*args),
+                       lambda: make_fx(call, pre_dispatch=True)(*args)):
+            with pytest.raises(ndvm.NdvmError, match="trace"):
+                tracer()
+                pytest.fail(f"{name} was traced")
+        assert torch.equal(call(*args), want)
+
+
+def test_traces_of_a_backward_pass_are_refused(ndvm, cuda):
+    """Also where the forward pass ran before the tracer came."""
+    import torch
+    from torch.fx.experimental.proxy_tensor import make_fx
+    for name, call, args in _ops(ndvm):
+        args = [a.clone().requires_grad_(True) for a in args]
+        y = call(*args)
+        dy = torch.ones_like(y)
+
+        def back(dy):
+            return torch.autograd.grad(y, args[:1], dy, retain_graph=True)[0]
+
+        want = back(dy)
+        with pytest.raises(ndvm.NdvmError, match="trace"):
+            make_fx(back)(dy)
+            pytest.fail(name)
+        assert torch.equal(back(dy), want)
