@@ -110,6 +110,7 @@ struct Rows {
       first = false;
       rows *= t.size(d);
     }
+    ok &= rows <= 1 || stride == 0 || stride >= cols;  // (rows that overlap, as those of sliding windows, are copied too)
   }
 };
 Tensor rowed(const Tensor& t) { return Rows(t).ok ? t : t.contiguous(); }

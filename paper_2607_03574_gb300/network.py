@@ -9,8 +9,8 @@ nodes are in ``csrc/net/torch_ops.cpp``).  Under them are raw calls (``*_forward
 outputs, a workspace and a stream and map one to one onto the C ABI (``ndvm_layer_norm_*``,
 ``ndvm_dropout``, ``ndvm_gated_*``).
 
-Layouts: the last dimension is contiguous and the leading ones are rows with one stride (a raw
-call refuses anything else, a differentiable op copies it).  Types: float32, float16 and bfloat16;
+Layouts: the last dimension is contiguous and the leading ones are rows with one stride, 0 or at least a
+row's length (a raw call refuses anything else, a differentiable op copies it).  Types: float32, float16 and bfloat16;
 the gated projection takes the 16-bit ones.  There is no CPU path.
 """
 from __future__ import annotations
@@ -68,8 +68,8 @@ def _rows(t, name):
             ok = False
         rows *= n
     step = cols if step is None else step
-    if not ok:
-        raise NdvmError(1, f"{name} must be rows of contiguous elements with one row stride")
+    if not ok or (rows > 1 and 0 < step < cols):
+        raise NdvmError(1, f"{name} must be rows of contiguous elements with one row stride (0, or at least a row's length)")
     return rows, cols, step
 
 
