@@ -171,13 +171,17 @@ Maybe layer_norm(const Tensor& given, const Maybe& w, const Maybe& b, double eps
   if (!given.is_cuda()) return std::nullopt;
   const int device = c10::cuda::current_device();
   if (!here(given, device) || given.dim() == 0 || type_code(given) < 0) return std::nullopt;
-  const Tensor x = rowed(given), weight = some(w), bias = some(b);
-  for (const Tensor* t : {&weight, &bias})
-    if (t->defined() && (!here(*t, device) || t->dim() != 1 || t->size(0) != x.size(-1) || !t->is_contiguous() || type_code(*t) < 0))
-      return std::nullopt;
+  const Tensor x = rowed(given);
+  Maybe vectors[2] = {w, b};
+  for (Maybe& v : vectors) {
+    if (!v || !v->defined()) continue;
+    if (!here(*v, device) || v->dim() != 1 || v->size(0) != x.size(-1) || type_code(*v) < 0) return std::nullopt;
+    v = v->contiguous();
+  }
+  const Tensor weight = some(vectors[0]), bias = some(vectors[1]);
   if (weight.defined() && bias.defined() && weight.scalar_type() != bias.scalar_type()) return std::nullopt;
   check_inputs({&x, &weight, &bias});
-  return recorded({&x, &weight, &bias}) ? Norm::apply(x, w, b, eps) : norm_forward(x, weight, bias, eps, nullptr);
+  return recorded({&x, &weight, &bias}) ? Norm::apply(x, vectors[0], vectors[1], eps) : norm_forward(x, weight, bias, eps, nullptr);
 }
 
 // --------------------------------------------------------------------------------------- dropout

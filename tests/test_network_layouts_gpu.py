@@ -38,3 +38,22 @@ def test_raw_calls_name_the_overlapping_rows(ndvm, cuda):
                  lambda: ndvm.gated_forward(x.contiguous(), x, x.contiguous())):
         with pytest.raises(ndvm.NdvmError, match="rows of contiguous elements"):
             call()
+
+
+def test_strided_weights_and_biases_are_copied(ndvm, cuda):
+    """A column of a matrix and a value that all columns share, as layer norm's weight and bias; their gradients go back
+    to where the values came from."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x, dy = (torch.randn(33, 72, generator=g, device="cuda").requires_grad_(True) for _ in range(2))
+    both = torch.randn(72, 3, generator=g, device="cuda").requires_grad_(True)
+    one = torch.full((1,), 0.25, device="cuda").requires_grad_(True)
+    plain = [both.detach()[:, 1].contiguous().requires_grad_(True), one.detach().expand(72).contiguous().requires_grad_(True)]
+    want = ndvm.layer_norm(x, *plain)
+    dw, db = torch.autograd.grad(want, plain, dy)
+    y = ndvm.layer_norm(x, both[:, 1], one.expand(72))
+    assert torch.equal(y, want)
+    dboth, done = torch.autograd.grad(y, (both, one), dy)
+    assert torch.equal(dboth[:, 1], dw) and not dboth[:, ::2].any() and torch.equal(done, db.sum().view(1))
+    with torch.no_grad():
+        assert torch.equal(ndvm.layer_norm(x, both[:, 1], one.expand(72)), want)
