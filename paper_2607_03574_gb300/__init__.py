@@ -47,7 +47,7 @@ def load(build_if_missing: bool = True):
         from . import build as _b
         path = _b.LIB
         if build_if_missing and _b._stale():
-            _b.build()
+            _b.build(torch_ops=False)
         if not os.path.exists(path):
             raise NdvmError(6, f"the NDVM CUDA library is not built ({path}); run paper_2607_03574_gb300.build")
         lib = ctypes.CDLL(path)

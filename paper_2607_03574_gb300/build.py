@@ -1,9 +1,10 @@
 """Build the NDVM C-ABI library (libndvm.so) in-tree with nvcc for sm_103a.
 
 Translation units compile in parallel; the result is linked as one shared
-library with the CUDA runtime linked statically, and a Python module on top of it
-(ndvm_torch.so) that holds the network operators' autograd nodes.  Run ``python -m
-paper_2607_03574_gb300.build`` or call :func:`build`.
+library with the CUDA runtime linked statically.  Where PyTorch is installed, a Python
+module on top of it (ndvm_torch.so) holds the network operators' autograd nodes; the
+library does not need it.  Run ``python -m paper_2607_03574_gb300.build`` or call
+:func:`build`.
 """
 from __future__ import annotations
 
@@ -21,6 +22,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libndvm.so")
 TORCH_OPS = os.path.join(OUT_DIR, "ndvm_torch.so")  # the network operators' autograd nodes (a Python module)
+TORCH_OPS_SOURCE = os.path.join(CSRC, "net", "torch_ops.cpp")
 
 SOURCES = ["tape.cpp", "trace_scheme.cpp", "trace_bytecode.cpp", "plan.cpp", "compact.cpp", "capi.cpp", "replay.cu", "scalar.cu", "matrix.cu",
            "net/netapi.cpp", "net/norm.cu", "net/dropout.cu", "net/gated.cu"]
@@ -34,34 +36,35 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the NDVM library needs the CUDA toolkit to build")
 
 
-def _deps() -> list[str]:
-    files = [os.path.join(d, f) for d in (CSRC, os.path.join(CSRC, "net")) for f in os.listdir(d)]
-    files.append(os.path.join(INCLUDE, "ndvm.h"))
-    files.append(os.path.abspath(__file__))
-    return files
+def _newer(target: str, files: list[str]) -> bool:
+    """Whether the target is missing or one of the files (or this one) was changed after it was made."""
+    return not os.path.exists(target) or any(os.path.getmtime(f) > os.path.getmtime(target) for f in (*files, os.path.abspath(__file__)))
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(TORCH_OPS):
-        return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_OPS))
-    return any(os.path.getmtime(f) > t for f in _deps())
+    files = [os.path.join(d, f) for d in (CSRC, os.path.join(CSRC, "net")) for f in os.listdir(d)]
+    files.remove(TORCH_OPS_SOURCE)
+    return _newer(LIB, [*files, os.path.join(INCLUDE, "ndvm.h")])
 
 
-def _torch_root() -> str:
+def _torch_ops_stale() -> bool:
+    return _newer(TORCH_OPS, [TORCH_OPS_SOURCE, os.path.join(INCLUDE, "ndvm.h")])
+
+
+def _torch_root() -> str | None:
     spec = importlib.util.find_spec("torch")  # (not imported: that takes longer than finding it)
-    if spec is None:
-        raise RuntimeError("PyTorch not found: the network operators are built against it")
-    return list(spec.submodule_search_locations)[0]
+    return list(spec.submodule_search_locations)[0] if spec else None
 
 
 def _compile_torch_ops() -> str:
     root, cuda = _torch_root(), os.path.dirname(os.path.dirname(_nvcc()))
+    if root is None:
+        raise RuntimeError("PyTorch not found: the network operators are built against it")
     obj = os.path.join(OUT_DIR, "net_torch_ops.cpp.o")
     include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", *("-I" + d for d in include), "-c",
-           os.path.join(CSRC, "net", "torch_ops.cpp"), "-o", obj]
+           TORCH_OPS_SOURCE, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"compiling net/torch_ops.cpp failed:\n{r.stdout}\n{r.stderr}")
@@ -79,8 +82,12 @@ def _link_torch_ops(obj: str) -> None:
     os.replace(tmp, TORCH_OPS)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
+def build(force: bool = False, verbose: bool = False, torch_ops: bool | None = None) -> str:
+    """Makes what is missing or out of date.  torch_ops: the autograd nodes' module too (None: where PyTorch is
+    installed); the library is made first and stands without it."""
+    library = force or _stale()
+    module = (_torch_root() is not None if torch_ops is None else torch_ops) and (force or _torch_ops_stale())
+    if not library and not module:
         return LIB
     os.makedirs(OUT_DIR, exist_ok=True)
     nvcc = _nvcc()
@@ -101,16 +108,17 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return obj
 
     with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        torch_ops = ex.submit(_compile_torch_ops)
-        objs = list(ex.map(compile_one, SOURCES))
-        torch_obj = torch_ops.result()
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-cudart", "static"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"linking libndvm.so failed:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, LIB)
-    _link_torch_ops(torch_obj)
+        torch_obj = ex.submit(_compile_torch_ops) if module else None
+        if library:
+            objs = list(ex.map(compile_one, SOURCES))
+            tmp = LIB + f".tmp{os.getpid()}"
+            cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-cudart", "static"]
+            r = subprocess.run(cmd, capture_output=True, text=True)
+            if r.returncode != 0:
+                raise RuntimeError(f"linking libndvm.so failed:\n{r.stdout}\n{r.stderr}")
+            os.replace(tmp, LIB)
+        if module:
+            _link_torch_ops(torch_obj.result())
     return LIB
 
 

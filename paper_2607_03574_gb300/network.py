@@ -361,17 +361,15 @@ _ops = None
 
 
 def _load_ops():
-    """The module of autograd nodes (built beside the library)."""
+    """The module of autograd nodes (built first if it is missing or out of date)."""
     global _ops
     import importlib.machinery
     import importlib.util
-    import os
 
     from . import build
     _start()
     load()
-    if not os.path.exists(build.TORCH_OPS):
-        raise NdvmError(6, f"the network operators' torch module is not built ({build.TORCH_OPS}); run paper_2607_03574_gb300.build")
+    build.build(torch_ops=True)
     loader = importlib.machinery.ExtensionFileLoader("ndvm_torch", build.TORCH_OPS)
     ops = importlib.util.module_from_spec(importlib.util.spec_from_loader("ndvm_torch", loader))
     loader.exec_module(ops)
