@@ -48,12 +48,33 @@ def _stale() -> bool:
 
 
 def _torch_ops_stale() -> bool:
-    return _newer(TORCH_OPS, [TORCH_OPS_SOURCE, os.path.join(INCLUDE, "ndvm.h")])
+    try:
+        with open(_torch_ops_record()) as f:
+            same = f.read() == _built_against()
+    except OSError:
+        same = False
+    return not same or _newer(TORCH_OPS, [TORCH_OPS_SOURCE, os.path.join(INCLUDE, "ndvm.h")])
 
 
 def _torch_root() -> str | None:
     spec = importlib.util.find_spec("torch")  # (not imported: that takes longer than finding it)
     return list(spec.submodule_search_locations)[0] if spec else None
+
+
+def _torch_ops_record() -> str:
+    return TORCH_OPS + ".for"
+
+
+def _built_against() -> str:
+    """The Python and the PyTorch (its place and its version file) that the module fits: another one's binary
+    interface is another."""
+    root = _torch_root()
+    try:
+        with open(os.path.join(root or "", "version.py")) as f:
+            version = f.read()
+    except OSError:
+        version = ""
+    return f"{sys.implementation.cache_tag}\n{root}\n{version}"
 
 
 def _compile_torch_ops() -> str:
@@ -80,6 +101,8 @@ def _link_torch_ops(obj: str) -> None:
     if r.returncode != 0:
         raise RuntimeError(f"linking ndvm_torch.so failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, TORCH_OPS)
+    with open(_torch_ops_record(), "w") as f:
+        f.write(_built_against())
 
 
 def build(force: bool = False, verbose: bool = False, torch_ops: bool | None = None) -> str:

@@ -91,3 +91,19 @@ def test_programs_are_traced_without_torch(ndvm):
             "print(nd.trace_build('(model (params a b) (* a b))').info()['n_params'])\n")
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "2", (r.stdout, r.stderr)
+
+
+def test_module_is_made_again_for_another_torch(build, monkeypatch, tmp_path):
+    """A module built against one PyTorch may not be loaded into another, however old its sources are."""
+    c = _commands(monkeypatch)
+    for version in ("2.0", "2.1"):
+        root = tmp_path / "torch"
+        root.mkdir(exist_ok=True)
+        (root / "version.py").write_text(f"__version__ = '{version}'\n")
+        monkeypatch.setattr(build, "_torch_root", lambda: str(root))
+        assert build._torch_ops_stale()
+        c.ran.clear()
+        build.build()
+        assert any(str(a).endswith("torch_ops.cpp") for cmd in c.ran for a in cmd) and not build._torch_ops_stale()
+    monkeypatch.setattr(build, "_torch_root", lambda: str(tmp_path / "elsewhere"))
+    assert build._torch_ops_stale()
