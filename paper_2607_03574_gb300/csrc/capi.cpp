@@ -975,6 +975,7 @@ ndvm_status host_replay(const ndvm_tape* tape, ndvm_dtype dtype, int64_t B, cons
                         int64_t n_obs, void* loss, void* grad, void* stream, bool sync) {
   ndvm_tape* t = const_cast<ndvm_tape*>(tape);
   if (!t) return fail(NDVM_E_INVALID_ARG, "null tape");
+  if (dtype != NDVM_F64 && dtype != NDVM_F32) return fail(NDVM_E_INVALID_ARG, "bad dtype");  // (before its size is used)
   if (B < 0 || n_obs < 0) return fail(NDVM_E_INVALID_ARG, "negative size");
   if (B == 0) return NDVM_OK;
   if (!loss || (t->tape.n_params > 0 && !params) || (n_obs > 0 && !obs)) return fail(NDVM_E_INVALID_ARG, "null argument");
