@@ -252,15 +252,15 @@ Tensor gated_forward(const Tensor& x, const Tensor& w_gate, const Tensor& w_up, 
   return h;
 }
 struct Gated : torch::autograd::Function<Gated> {
-  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w_gate, const Tensor& w_up, int64_t act) {
-    // The two products are kept (8 bytes an element of h) where that is the faster: a long contraction, or
-    // few elements.  Forward and backward, computed again / kept: 16384 x 2048 -> 8192 2636 / 2353 us, 16 x 2048 ->
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w_gate, const Tensor& w_up, int64_t act, int64_t keep) {
+    // The two products are kept (8 bytes an element of h) if the caller says so (keep 1; 0: not), or by default (-1) where
+    // that is the faster: a long contraction, or few elements.  Forward and backward, computed again / kept: 16384 x 2048 -> 8192 2636 / 2353 us, 16 x 2048 ->
     // 8192 67 / 57, 1501 x 333 -> 777 48 / 43; but 4096 x 1024 -> 4096 185 / 187, 4096 x 256 -> 1024 46 / 48, 16384 x 1024 ->
     // 4096 654 / 704.
     const Rows r(x);
     const int64_t n = w_gate.size(0);
     Tensor kept;
-    if (r.cols >= 1536 || r.rows * n <= (int64_t)1 << 21)
+    if (keep < 0 ? r.cols >= 1536 || r.rows * n <= (int64_t)1 << 21 : keep > 0)
       kept = at::empty({2, r.rows, ndvm_gated_kept_stride(n)}, x.options().dtype(at::kFloat));
     Tensor h = gated_forward(x, w_gate, w_up, act, kept);
     ctx->save_for_backward({x, w_gate, w_up, kept});
@@ -284,10 +284,10 @@ struct Gated : torch::autograd::Function<Gated> {
     check_backward(ndvm_gated_backward_kept((ndvm_dtype)type_code(x), (ndvm_activation)ctx->saved_data["act"].toInt(), o.x.rows, o.x.cols, n, in(dh),
                                             rh.stride, o.px, o.x.stride, o.pg, o.g.stride, o.pu, o.u.stride, static_cast<const float*>(in(kept)),
                                             out(dx), o.x.cols, out(dg), out(du), out(ws), need, stream_of(x.get_device())));
-    return {dx, dg, du, Tensor()};
+    return {dx, dg, du, Tensor(), Tensor()};
   }
 };
-Maybe gated(const Tensor& gx, const Tensor& gg, const Tensor& gu, int64_t act) {
+Maybe gated(const Tensor& gx, const Tensor& gg, const Tensor& gu, int64_t act, int64_t keep) {
   if (!gx.is_cuda()) return std::nullopt;
   const int device = c10::cuda::current_device();
   if (!here(gx, device) || !here(gg, device) || !here(gu, device) || gx.dim() == 0 || gg.dim() != 2 || gu.dim() != 2) return std::nullopt;
@@ -295,7 +295,7 @@ Maybe gated(const Tensor& gx, const Tensor& gg, const Tensor& gu, int64_t act) {
   if (act < 0 || type_code(gx) < 0 || gg.scalar_type() != gx.scalar_type() || gu.scalar_type() != gx.scalar_type()) return std::nullopt;
   const Tensor x = rowed(gx), w_gate = rowed(gg), w_up = rowed(gu);
   check_inputs({&x, &w_gate, &w_up});
-  return recorded({&x, &w_gate, &w_up}) ? Gated::apply(x, w_gate, w_up, act) : gated_forward(x, w_gate, w_up, act, Tensor());
+  return recorded({&x, &w_gate, &w_up}) ? Gated::apply(x, w_gate, w_up, act, keep) : gated_forward(x, w_gate, w_up, act, Tensor());
 }
 
 }  // namespace
@@ -310,8 +310,8 @@ PYBIND11_MODULE(ndvm_torch, m) {
     HANDLE_TH_ERRORS return dropout(x, p, seed, offset, residual);
     END_HANDLE_TH_ERRORS_PYBIND
   });
-  m.def("gated", [](const Tensor& x, const Tensor& w_gate, const Tensor& w_up, int64_t act) {
-    HANDLE_TH_ERRORS return gated(x, w_gate, w_up, act);
+  m.def("gated", [](const Tensor& x, const Tensor& w_gate, const Tensor& w_up, int64_t act, int64_t keep) {
+    HANDLE_TH_ERRORS return gated(x, w_gate, w_up, act, keep);
     END_HANDLE_TH_ERRORS_PYBIND
   });
 }

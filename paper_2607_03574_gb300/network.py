@@ -402,10 +402,12 @@ def dropout(x, p, seed, offset=0, residual=None):
     return _refuse(dropout_forward, x, p, seed, offset, residual) if y is None else y
 
 
-def gated(x, w_gate, w_up, activation="silu"):
-    """act(x w_gate^T) * (x w_up^T) as a differentiable op (gradients of x and both weights)."""
+def gated(x, w_gate, w_up, activation="silu", keep=None):
+    """act(x w_gate^T) * (x w_up^T) as a differentiable op (gradients of x and both weights).  keep: whether the two
+    products are held for the backward pass, as float32 (8 bytes an element of the result), instead of computed
+    again; None: where that is the faster (k >= 1536, or results of up to 2^21 elements)."""
     try:
-        y = (_ops or _load_ops()).gated(x, w_gate, w_up, ACTIVATIONS.get(activation, -1))
+        y = (_ops or _load_ops()).gated(x, w_gate, w_up, ACTIVATIONS.get(activation, -1), -1 if keep is None else int(bool(keep)))
     except TypeError:
         y = None
     return _refuse(gated_forward, x, w_gate, w_up, activation) if y is None else y
