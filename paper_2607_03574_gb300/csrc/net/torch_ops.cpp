@@ -113,7 +113,8 @@ struct Rows {
     ok &= rows <= 1 || stride == 0 || stride >= cols;  // (rows that overlap, as those of sliding windows, are copied too)
   }
 };
-Tensor rowed(const Tensor& t) { return Rows(t).ok ? t : t.contiguous(); }
+// (resolve_neg: the imaginary part of a conjugate is a view whose memory holds the opposite sign)
+Tensor rowed(const Tensor& t) { return (Rows(t).ok ? t : t.contiguous()).resolve_neg(); }
 
 void* stream_of(int device) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 const void* in(const Tensor& t) { return t.defined() ? t.const_data_ptr() : nullptr; }
@@ -176,7 +177,7 @@ Maybe layer_norm(const Tensor& given, const Maybe& w, const Maybe& b, double eps
   for (Maybe& v : vectors) {
     if (!v || !v->defined()) continue;
     if (!here(*v, device) || v->dim() != 1 || v->size(0) != x.size(-1) || type_code(*v) < 0) return std::nullopt;
-    v = v->contiguous();
+    v = v->contiguous().resolve_neg();
   }
   const Tensor weight = some(vectors[0]), bias = some(vectors[1]);
   if (weight.defined() && bias.defined() && weight.scalar_type() != bias.scalar_type()) return std::nullopt;

@@ -48,6 +48,8 @@ def _rows(t, name):
     shape = t.shape
     if not shape:
         raise NdvmError(1, f"{name} must have at least one dimension")
+    if t.is_neg():
+        raise NdvmError(1, f"{name}'s memory holds the opposite sign (a view of a conjugate): use resolve_neg()")
     cols = shape[-1]
     if t.is_contiguous():
         if len(shape) == 2:
@@ -108,7 +110,7 @@ def _vector(t, name, cols, device):
     """The address of a vector of `cols` elements, or None."""
     if t is None:
         return None
-    if t.shape != (cols,) or not t.is_contiguous():
+    if t.shape != (cols,) or not t.is_contiguous() or t.is_neg():
         raise NdvmError(1, f"{name} must be a contiguous vector of {cols} elements")
     _same_device(device, t, name)
     return t.data_ptr()

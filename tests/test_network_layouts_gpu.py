@@ -57,3 +57,18 @@ def test_strided_weights_and_biases_are_copied(ndvm, cuda):
     assert torch.equal(dboth[:, 1], dw) and not dboth[:, ::2].any() and torch.equal(done, db.sum().view(1))
     with torch.no_grad():
         assert torch.equal(ndvm.layer_norm(x, both[:, 1], one.expand(72)), want)
+
+
+def test_lazily_negated_views(ndvm, cuda):
+    """The imaginary part of a conjugate is a view whose memory holds the opposite sign: copied, or refused by a raw call."""
+    import torch
+    z = torch.randn(9, 1, generator=torch.Generator(device="cuda").manual_seed(8), device="cuda", dtype=torch.complex64)
+    x = z.conj().imag
+    assert x.is_neg()
+    assert torch.equal(ndvm.dropout(x, 0.0, 1), -z.imag) and torch.equal(ndvm.dropout(-z.imag, 0.0, 1, 0, x), -2 * z.imag)
+    one, bias = torch.ones(5, 1, device="cuda"), z[0].conj().imag
+    assert torch.equal(ndvm.layer_norm(one, None, bias), (-z[0].imag).expand(5, 1))
+    y = torch.ones(9, 1, device="cuda", requires_grad=True)
+    assert torch.equal(torch.autograd.grad(ndvm.dropout(y, 0.0, 1), y, x)[0], -z.imag)
+    with pytest.raises(ndvm.NdvmError, match="resolve_neg"):
+        ndvm.dropout_forward(x, 0.0, 1)
