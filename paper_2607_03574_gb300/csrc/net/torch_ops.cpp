@@ -25,6 +25,7 @@ namespace {
 
 using Maybe = std::optional<Tensor>;
 Tensor some(const Maybe& t) { return t ? *t : Tensor(); }
+Maybe maybe(const Tensor& t) { return t.defined() ? Maybe(t) : Maybe(); }
 
 // sets the package's NdvmError as the pending Python error (with the interpreter's lock)
 void set_error(int status, const char* message) {
@@ -62,8 +63,11 @@ constexpr const char* kNoTangents = "the network operators have no forward-mode 
 // Whether torch records a program here (torch.jit.trace, or torch.fx's proxies): it would record the allocation of an
 // output and not the launch that fills it.
 bool traced() {
-  return torch::jit::tracer::isTracing() || c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY).has_value() ||
-         c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::PreDispatch);
+  if (torch::jit::tracer::isTracing()) return true;
+  const c10::DispatchKeySet on = c10::impl::tls_local_dispatch_key_set().included_;
+  if (on.has(c10::DispatchKey::PreDispatch)) return true;
+  return on.has(c10::DispatchKey::Python) &&  // (a mode of some kind is on)
+         c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY).has_value();
 }
 constexpr const char* kNoTraces = "the network operators cannot be traced: the trace would not hold their launches";
 // what an op refuses of its inputs before it reads them
@@ -114,7 +118,11 @@ struct Rows {
   }
 };
 // (resolve_neg: the imaginary part of a conjugate is a view whose memory holds the opposite sign)
-Tensor rowed(const Tensor& t) { return (Rows(t).ok ? t : t.contiguous()).resolve_neg(); }
+Tensor resolved(const Tensor& t) { return t.is_neg() ? t.resolve_neg() : t; }
+Tensor rowed(const Tensor& t) {
+  if (Rows(t).ok && !t.is_neg()) return t;
+  return resolved(t.contiguous());
+}
 
 void* stream_of(int device) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 const void* in(const Tensor& t) { return t.defined() ? t.const_data_ptr() : nullptr; }
@@ -173,16 +181,15 @@ Maybe layer_norm(const Tensor& given, const Maybe& w, const Maybe& b, double eps
   const int device = c10::cuda::current_device();
   if (!here(given, device) || given.dim() == 0 || type_code(given) < 0) return std::nullopt;
   const Tensor x = rowed(given);
-  Maybe vectors[2] = {w, b};
-  for (Maybe& v : vectors) {
-    if (!v || !v->defined()) continue;
-    if (!here(*v, device) || v->dim() != 1 || v->size(0) != x.size(-1) || type_code(*v) < 0) return std::nullopt;
-    v = v->contiguous().resolve_neg();
+  Tensor weight = some(w), bias = some(b);
+  for (Tensor* t : {&weight, &bias}) {
+    if (!t->defined()) continue;
+    if (!here(*t, device) || t->dim() != 1 || t->size(0) != x.size(-1) || type_code(*t) < 0) return std::nullopt;
+    if (!t->is_contiguous() || t->is_neg()) *t = resolved(t->contiguous());
   }
-  const Tensor weight = some(vectors[0]), bias = some(vectors[1]);
   if (weight.defined() && bias.defined() && weight.scalar_type() != bias.scalar_type()) return std::nullopt;
   check_inputs({&x, &weight, &bias});
-  return recorded({&x, &weight, &bias}) ? Norm::apply(x, vectors[0], vectors[1], eps) : norm_forward(x, weight, bias, eps, nullptr);
+  return recorded({&x, &weight, &bias}) ? Norm::apply(x, maybe(weight), maybe(bias), eps) : norm_forward(x, weight, bias, eps, nullptr);
 }
 
 // --------------------------------------------------------------------------------------- dropout
@@ -223,7 +230,7 @@ Maybe dropout(const Tensor& given, double p, uint64_t seed, uint64_t offset, con
   const Tensor x = rowed(given), residual = r && r->defined() ? rowed(*r) : Tensor();
   if (residual.defined() && (!here(residual, device) || residual.sizes() != x.sizes() || residual.scalar_type() != x.scalar_type())) return std::nullopt;
   check_inputs({&x, &residual});
-  if (recorded({&x, &residual})) return Drop::apply(x, residual.defined() ? Maybe(residual) : Maybe(), p, seed, offset);
+  if (recorded({&x, &residual})) return Drop::apply(x, maybe(residual), p, seed, offset);
   int status;
   Tensor y = drop(x, p, seed, offset, residual, &status);
   check_forward(status);

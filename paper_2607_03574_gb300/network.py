@@ -25,12 +25,16 @@ ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 
 _torch_module = None
 _types = {}
+_modes = None  # torch's questions that _recorded asks
 
 
 def _start():
     """torch and the library, looked up once (the calls below are short beside an import's lookups)."""
-    global _torch_module
+    global _torch_module, _modes
     torch = _torch()
+    c = torch._C
+    _modes = (c._get_tracing_state, c._len_torch_dispatch_stack, c._dispatch_tls_is_dispatch_key_included, c.DispatchKey.PreDispatch,
+              c._get_dispatch_mode, c._TorchDispatchModeKey.PROXY)
     _types.update({torch.float32: 1, torch.float16: 2, torch.bfloat16: 3})
     _torch_module = torch
     return torch
@@ -48,9 +52,9 @@ def _rows(t, name):
     shape = t.shape
     if not shape:
         raise NdvmError(1, f"{name} must have at least one dimension")
-    if t.is_neg():
-        raise NdvmError(1, f"{name}'s memory holds the opposite sign (a view of a conjugate): use resolve_neg()")
     cols = shape[-1]
+    if cols == 1 and t.is_neg():  # (with more columns such a view is not contiguous)
+        raise NdvmError(1, f"{name}'s memory holds the opposite sign (a view of a conjugate): use resolve_neg()")
     if t.is_contiguous():
         if len(shape) == 2:
             return shape[0], cols, cols
@@ -75,12 +79,16 @@ def _rows(t, name):
     return rows, cols, step
 
 
+def _recorded():
+    """Whether torch records a program here (torch.jit.trace, or torch.fx's proxies): it would record an output's
+    allocation and not the launch that fills it."""
+    tracing, depth, included, pre_dispatch, mode, proxy = _modes
+    return tracing() is not None or included(pre_dispatch) or (depth() > 0 and mode(proxy) is not None)
+
+
 def _device(torch, x):
-    """The index of x's device, which has to be the current one (the kernels launch there).  Where torch records a
-    program, it would record an output's allocation and not the launch that fills it: refused."""
-    c = torch._C
-    if (c._get_tracing_state() is not None or c._get_dispatch_mode(c._TorchDispatchModeKey.PROXY) is not None
-            or c._dispatch_tls_is_dispatch_key_included(c.DispatchKey.PreDispatch)):
+    """The index of x's device, which has to be the current one (the kernels launch there)."""
+    if _recorded():
         raise NdvmError(3, "the network operators cannot be traced: the trace would not hold their launches")
     device = x.get_device()
     if device < 0:
@@ -110,7 +118,7 @@ def _vector(t, name, cols, device):
     """The address of a vector of `cols` elements, or None."""
     if t is None:
         return None
-    if t.shape != (cols,) or not t.is_contiguous() or t.is_neg():
+    if t.shape != (cols,) or not t.is_contiguous() or (cols == 1 and t.is_neg()):
         raise NdvmError(1, f"{name} must be a contiguous vector of {cols} elements")
     _same_device(device, t, name)
     return t.data_ptr()
