@@ -344,7 +344,8 @@ size_t ndvm_gated_workspace_bytes(int64_t rows, int64_t k, int64_t n, int backwa
  * ndvm_gated_backward -- gradients of ndvm_gated_forward under the cotangent dh (rows x n).  The two
  * products are computed again; dG and dU are rounded to dtype before the products that make dx (rows x k)
  * and dw_gate, dw_up (n x k, contiguous), or, where there are few of them (rows * min(n, k) up to 16384 or
- * n * k up to 2048), split into two halves of dtype that together lose next to nothing.  Each output may be
+ * n * k up to 2048), split into two halves of dtype that together lose next to nothing.  In F16 they are
+ * infinite beyond 65504 and lose digits below 6e-5, as a stored half does (scale dh accordingly).  Each output may be
  * NULL if not wanted; rows = 0 sets dw_gate and dw_up to 0.
  */
 ndvm_status ndvm_gated_backward(ndvm_dtype dtype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,

@@ -66,9 +66,10 @@ __device__ __forceinline__ void drop_vector(const DropArgs& a, const Keys& keys,
   store_pack(y, p);
 }
 
-// Contiguous tensors (one row of any length).  With a residual bound by memory: 134 M bfloat16 elements in 113 us,
-// 7.1 TB/s; without, by the generator's instructions: 105 us, 5.1 TB/s (half as many a byte in binary32: 6.7 TB/s).
-// One vector a thread and all the threads an SM holds: with 40 of its 64 warps 126 us, with several vectors a
+// Contiguous tensors (one row of any length).  With a residual bound by memory: 134 M bfloat16 elements in 114 us,
+// 7.1 TB/s; without, by the generator's instructions: 107 us, 5.0 TB/s (the pipe of the widening multiplies is busy 69 % of
+// the time, that of the xors 59 %; a warp waits 8.8 cycles an instruction for a pipe or its dispatch, 2.6 for memory).
+// Binary32 has half as many a byte and waits for memory again, 6.4 TB/s.  One vector a thread and all the threads an SM holds: with 40 of its 64 warps 126 us, with several vectors a
 // thread, the next one's loads in flight or not, 143 to 191 us.
 template <typename T, bool kResidual>
 __global__ void __launch_bounds__(kThreads, 8) k_dropout_flat(const __grid_constant__ DropArgs a, const __grid_constant__ Keys keys) {

@@ -405,8 +405,9 @@ bool backward_variant(int width, int64_t rows, int64_t cols, F&& f) {
     else if (packs <= 32) f(Int<V>(), Int<1>(), Int<32>(), Int<3>());
     else if (packs <= 64) f(Int<V>(), Int<2>(), Int<32>(), Int<2>());
     else if (packs <= 128) f(Int<V>(), Int<2>(), Int<64>(), Int<2>());
-    // one load and twice the threads: more warps for many rows (65536 x 2048 bf16 146 us against 150), more column
-    // sums to join for few (4096 x 2048 19 us against 16)
+    // one load and twice the threads: more warps for many rows, more column sums to join for few.  bf16, us, one load
+    // against two: 2048 columns 18.2 / 15.4 at 4096 rows, 45.1 / 43.2 at 16384, 78.5 / 78.3 at 32768, 146 / 150 at 65536;
+    // 1536 columns 16.6 / 15.1, 38.5 / 39.0, 67.7 / 70.6, 125 / 133
     else if (packs <= 256 && rows >= 32768) f(Int<V>(), Int<1>(), Int<256>(), Int<4>());
     else if (packs <= 256) f(Int<V>(), Int<2>(), Int<128>(), Int<2>());
     else if (packs <= 512) f(Int<V>(), Int<2>(), Int<256>(), Int<2>());

@@ -262,9 +262,10 @@ Tensor gated_forward(const Tensor& x, const Tensor& w_gate, const Tensor& w_up, 
 struct Gated : torch::autograd::Function<Gated> {
   static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w_gate, const Tensor& w_up, int64_t act, int64_t keep) {
     // The two products are kept (8 bytes an element of h) if the caller says so (keep 1; 0: not), or by default (-1) where
-    // that is the faster: a long contraction, or few elements.  Forward and backward, computed again / kept: 16384 x 2048 -> 8192 2636 / 2353 us, 16 x 2048 ->
-    // 8192 67 / 57, 1501 x 333 -> 777 48 / 43; but 4096 x 1024 -> 4096 185 / 187, 4096 x 256 -> 1024 46 / 48, 16384 x 1024 ->
-    // 4096 654 / 704.
+    // that is the faster: a long contraction, or few elements.  Forward and backward, computed again / kept:
+    // 16384 x 2048 -> 8192 2660 / 2357 us, 4096 x 2048 -> 8192 648 / 596, 16 x 2048 -> 8192 67 / 57, 1501 x 333 -> 777 49 / 44;
+    // but 4096 x 1024 -> 4096 194 / 198, 4096 x 256 -> 1024 47 / 50, 16384 x 1024 -> 4096 687 / 725, 100000 x 256 -> 512
+    // 238 / 310.
     const Rows r(x);
     const int64_t n = w_gate.size(0);
     Tensor kept;
