@@ -12,6 +12,9 @@ outputs, a workspace and a stream and map one to one onto the C ABI (``ndvm_laye
 Layouts: the last dimension is contiguous and the leading ones are rows with one stride, 0 or at least a
 row's length (a raw call refuses anything else, a differentiable op copies it).  Types: float32, float16 and bfloat16;
 the gated projection takes the 16-bit ones.  There is no CPU path.
+
+No second derivatives and no forward mode, and neither torch.jit.trace nor torch.fx can record a call: each of these
+raises.  ``check_operators()`` says whether a kernel has given up a wait, after which its outputs are not valid.
 """
 from __future__ import annotations
 
