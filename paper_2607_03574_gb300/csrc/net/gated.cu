@@ -725,8 +725,8 @@ int a_box(int64_t m) { return (int)std::min<int64_t>(up(m, 8), kM); }
 
 // The shape with the least estimated time, in steps of a tile 256 wide (0.27 us): a round of tiles takes its
 // steps and about 8 more to fill and empty; narrower tiles' steps are shorter, but not in proportion (more bytes an
-// operation), a pair's a little shorter (16384 x 2048 -> 8192 forward: 640 us alone, 598 in pairs) if there are 12 or
-// more (pairs start and end together: 4096 x 256 -> 1024 takes 9.1 us alone, 10.6 in pairs).  Where tiles are fewer than
+// operation), a pair's a little shorter (16384 x 2048 -> 8192 forward: 630 us alone, 576 in pairs) if there are 12 or
+// more (pairs start and end together: 4096 x 256 -> 1024 takes 9.2 us alone, 10.6 in pairs).  Where tiles are fewer than
 // SMs, a contraction is cut into parts of 8 steps or more, which costs the launch that joins them.  The weights'
 // gradients are cut as if both were wanted: one of them alone has the same bits.
 Cut cut(Mode mode, int64_t m, int64_t n, int64_t c, int parts = 1) {
