@@ -341,6 +341,7 @@ __global__ void __launch_bounds__(1024) k_columns_join(const float* partial, int
 
 constexpr int kSms = 152;
 constexpr int kMostBlocks = kSms * 6;  // of k_backward: their column sums are what the workspace holds
+constexpr int64_t kHeld = 8192;        // columns that k_backward holds at most (backward_variant); from there on
 constexpr int kLongBlocks = 64;        // row ranges of k_columns_long
 
 bool starts_on(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -398,6 +399,7 @@ bool forward_variant(int width, int64_t cols, F&& f) {
 template <typename T, typename F>
 bool backward_variant(int width, int64_t rows, int64_t cols, F&& f) {
   constexpr int V = 16 / sizeof(T);
+  if (cols > kHeld) return false;
   if (width == V) {
     const int64_t packs = cols / V;
     if (packs <= 8) f(Int<V>(), Int<1>(), Int<8>(), Int<3>());
@@ -492,7 +494,7 @@ cudaError_t launch_norm_backward(const NormArgs& a, ndvm_dtype t, ndvm_dtype wt,
   return t == NDVM_F32 ? backward<float>(a, f, s) : t == NDVM_F16 ? backward<__half>(a, f, s) : backward<__nv_bfloat16>(a, f, s);
 }
 size_t norm_workspace(int64_t rows, int64_t cols) {
-  return (size_t)std::clamp<int64_t>(rows, 1, kMostBlocks) * (size_t)cols * 2 * sizeof(float);
+  return (size_t)std::clamp<int64_t>(rows, 1, cols > kHeld ? kLongBlocks : kMostBlocks) * (size_t)cols * 2 * sizeof(float);
 }
 
 }  // namespace ndvm
