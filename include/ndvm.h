@@ -318,7 +318,8 @@ ndvm_status ndvm_dropout(ndvm_dtype dtype, int64_t rows, int64_t cols, const voi
                          const void* residual, int64_t r_stride, double p, uint64_t seed, uint64_t offset, void* y,
                          int64_t y_stride, void* stream);
 
-typedef enum { NDVM_ACT_SILU = 0, NDVM_ACT_GELU = 1, NDVM_ACT_RELU = 2, NDVM_ACT_SIGMOID = 3 } ndvm_activation;
+/* NDVM_ACT_NONE (act(z) = z) is for the dense layers alone. */
+typedef enum { NDVM_ACT_SILU = 0, NDVM_ACT_GELU = 1, NDVM_ACT_RELU = 2, NDVM_ACT_SIGMOID = 3, NDVM_ACT_NONE = 4 } ndvm_activation;
 
 /*
  * ndvm_gated_forward -- h = act(x Wg^T) * (x Wu^T), both products, the activation and the product in
@@ -371,6 +372,109 @@ ndvm_status ndvm_gated_backward_kept(ndvm_dtype dtype, ndvm_activation act, int6
                                      const void* w_gate, int64_t g_stride, const void* w_up, int64_t u_stride,
                                      const float* kept, void* dx, int64_t dx_stride, void* dw_gate, void* dw_up,
                                      void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * ndvm_rms_norm_forward -- y = s * rstd * weight over each row of `cols` elements, s = x + residual rounded to
+ * dtype (x where residual is NULL), rstd = 1 / sqrt(mean(s^2) + eps).
+ *   dtype  : x, residual, y and sum (F32, F16, BF16);  wtype : weight, dtype or F32
+ *   rows   : 0 is allowed and does nothing, below 2^31 - 128;  cols : at least 1
+ *   weight : device, cols values, or NULL for 1
+ *   sum    : receives s (it may be x or residual; y may be either where sum is not), or NULL; only with a residual
+ *   rstd   : device, rows floats for the backward pass, or NULL
+ */
+ndvm_status ndvm_rms_norm_forward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* x,
+                                  int64_t x_stride, const void* residual, int64_t r_stride, const void* weight, double eps,
+                                  void* y, int64_t y_stride, void* sum, int64_t sum_stride, float* rstd, void* stream);
+
+/* ndvm_rms_norm_workspace_bytes -- device workspace that ndvm_rms_norm_backward needs for dweight. */
+size_t ndvm_rms_norm_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * ndvm_rms_norm_backward -- gradients of ndvm_rms_norm_forward under the cotangents dy and dsum (NULL: 0).
+ *   s, weight, rstd : as the forward pass had and wrote them (s: its sum, or x)
+ *   dx      : the gradient of x and of the residual;  dweight : of wtype; each NULL if not wanted; rows = 0 sets dweight to 0
+ *   workspace : device, 16-byte aligned; may be NULL when dweight is
+ */
+ndvm_status ndvm_rms_norm_backward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* dy,
+                                   int64_t dy_stride, const void* dsum, int64_t dsum_stride, const void* s, int64_t s_stride,
+                                   const void* weight, const float* rstd, void* dx, int64_t dx_stride, void* dweight,
+                                   void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * 8-bit blocks -- 32 consecutive elements of a row (the last block may be shorter) share a scale 2^e, the least from
+ * e = -127 on with which none is over 448 in size; an element is the nearest e4m3 value to v / 2^e, ties to even.  A block
+ * with an infinity or a NaN is NaN throughout.
+ *   values : device, 16-byte aligned, a byte an element; row stride a multiple of 16 that holds a row.  Bytes of a row
+ *            behind its last element, up to a multiple of 16, are written as 0.
+ *   scales : device, 16-byte aligned, ndvm_quantized_scale_bytes: e + 127 (255: NaN) as bytes
+ *            [row / 128][column / 128][row % 32][row / 32 % 4][column / 32 % 4]; those of no block are written as 0, and
+ *            are not read.
+ *
+ * ndvm_quantize makes them of rows (F32, F16, BF16).  ndvm_dequantize writes what they stand for, rounded to dtype; what
+ * rounding lifts beyond dtype's largest finite value becomes that value.  ndvm_rms_norm_quantized makes them of
+ * ndvm_rms_norm_forward's y, which is not rounded in between.
+ */
+size_t ndvm_quantized_scale_bytes(int64_t rows, int64_t cols);
+ndvm_status ndvm_quantize(ndvm_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride, uint8_t* values,
+                          int64_t v_stride, uint8_t* scales, void* stream);
+ndvm_status ndvm_dequantize(ndvm_dtype dtype, int64_t rows, int64_t cols, const uint8_t* values, int64_t v_stride,
+                            const uint8_t* scales, void* x, int64_t x_stride, void* stream);
+ndvm_status ndvm_rms_norm_quantized(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* x,
+                                    int64_t x_stride, const void* residual, int64_t r_stride, const void* weight, double eps,
+                                    uint8_t* values, int64_t v_stride, uint8_t* scales, void* sum, int64_t sum_stride,
+                                    void* stream);
+
+/*
+ * ndvm_linear_forward -- y = act(z) + residual with z = x w^T + bias, in one kernel (two where a long contraction is
+ * split): x is rows x k, w is n x k, y and residual are rows x n.
+ *   dtype    : every matrix (F16, BF16; sums in binary32);  btype : bias, dtype or F32
+ *   act      : as the gated projection's, or NDVM_ACT_NONE
+ *   rows     : 0 is allowed and does nothing;  k, n : at least 1; rows, k and n at most 2^28
+ *   bias     : device, n values, or NULL;  residual : or NULL; y may be residual
+ *   z        : receives z for the backward pass, which needs it if act is not NDVM_ACT_NONE: device, 16-byte aligned floats,
+ *              rows rows of ndvm_linear_kept_stride(n); or z_values and z_scales: z as 8-bit blocks whose row stride is n
+ *              up to a multiple of 16; or all NULL
+ *   workspace : device, 256-byte aligned, ndvm_linear_workspace_bytes bytes (NULL if that is 0)
+ */
+int64_t ndvm_linear_kept_stride(int64_t n);
+ndvm_status ndvm_linear_forward(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                const void* x, int64_t x_stride, const void* w, int64_t w_stride, const void* bias,
+                                const void* residual, int64_t r_stride, void* y, int64_t y_stride, float* z,
+                                uint8_t* z_values, uint8_t* z_scales, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * ndvm_linear_workspace_bytes -- device workspace of a forward (backward = 0) or backward (1) call.  aligned = 1: x, w (and
+ * dy) start on 16 bytes and their row strides are multiples of 8 elements that hold a row; otherwise 0, which adds room
+ * for copies that are.  held = 1: the backward call has x as 8-bit blocks.  0 on invalid sizes.
+ */
+size_t ndvm_linear_workspace_bytes(ndvm_activation act, int64_t rows, int64_t k, int64_t n, int backward, int aligned, int held);
+
+/*
+ * ndvm_linear_backward -- gradients of ndvm_linear_forward under the cotangent dy (which is the residual's gradient).
+ * dz = dy act'(z) is rounded to dtype before the products that make dx (rows x k) and dw (n x k, contiguous), or, where there
+ * are few elements (rows * min(n, k) up to 16384 or n * k up to 2048), split into two halves of dtype that together lose next
+ * to nothing; dbias (btype) sums it unrounded.  In F16 dz is infinite beyond 65504 and loses digits below 6e-5.
+ *   x        : as the forward call had it, or NULL and x_values, x_scales: as 8-bit blocks, rounded to dtype (neither is read
+ *              without dw);  w is not read without dx
+ *   z, z_values, z_scales : as the forward call wrote them
+ *   dx, dw, dbias : each NULL if not wanted; rows = 0 sets dw and dbias to 0
+ */
+ndvm_status ndvm_linear_backward(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                 const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const uint8_t* x_values,
+                                 int64_t xv_stride, const uint8_t* x_scales, const void* w, int64_t w_stride, const float* z,
+                                 const uint8_t* z_values, const uint8_t* z_scales, void* dx, int64_t dx_stride, void* dw,
+                                 void* dbias, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * ndvm_linear_quantized -- ndvm_linear_forward of x and w in 8-bit blocks (dtype: y and residual, F16 or BF16): the products
+ * of what the blocks stand for, sums in binary32.
+ */
+size_t ndvm_linear_quantized_workspace_bytes(int64_t rows, int64_t k, int64_t n);
+ndvm_status ndvm_linear_quantized(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                  const uint8_t* x_values, int64_t xv_stride, const uint8_t* x_scales,
+                                  const uint8_t* w_values, int64_t wv_stride, const uint8_t* w_scales, const void* bias,
+                                  const void* residual, int64_t r_stride, void* y, int64_t y_stride, void* workspace,
+                                  size_t ws_bytes, void* stream);
 
 /*
  * ndvm_check_operators -- synchronize and report whether a kernel of the network operators gave up a wait on

@@ -51,7 +51,7 @@ def load(build_if_missing: bool = True):
         if not os.path.exists(path):
             raise NdvmError(6, f"the NDVM CUDA library is not built ({path}); run paper_2607_03574_gb300.build")
         lib = ctypes.CDLL(path)
-        P, I64, I32, SZ, U64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t, ctypes.c_uint64
+        C, P, I64, I32, SZ, U64 = ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t, ctypes.c_uint64
         sig = {
             "ndvm_trace_build": (ctypes.c_int, [ctypes.c_char_p, SZ, ctypes.c_int, ctypes.POINTER(P)]),
             "ndvm_tape_info": (ctypes.c_int, [P, ctypes.POINTER(I64), ctypes.POINTER(I32), ctypes.POINTER(I64),
@@ -86,6 +86,20 @@ def load(build_if_missing: bool = True):
                                                        I64, P, P, SZ, P]),
             "ndvm_gated_backward_kept": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, I64, I64, I64, P, I64, P, I64, P, I64, P,
                                                         I64, P, P, I64, P, P, P, SZ, P]),
+            "ndvm_rms_norm_forward": (C, [C, C, I64, I64, P, I64, P, I64, P, ctypes.c_double, P, I64, P, I64, P, P]),
+            "ndvm_rms_norm_workspace_bytes": (SZ, [I64, I64]),
+            "ndvm_rms_norm_backward": (C, [C, C, I64, I64, P, I64, P, I64, P, I64, P, P, P, I64, P, P, SZ, P]),
+            "ndvm_quantized_scale_bytes": (SZ, [I64, I64]),
+            "ndvm_quantize": (C, [C, I64, I64, P, I64, P, I64, P, P]),
+            "ndvm_dequantize": (C, [C, I64, I64, P, I64, P, P, I64, P]),
+            "ndvm_rms_norm_quantized": (C, [C, C, I64, I64, P, I64, P, I64, P, ctypes.c_double, P, I64, P, P, I64, P]),
+            "ndvm_linear_kept_stride": (I64, [I64]),
+            "ndvm_linear_workspace_bytes": (SZ, [C, I64, I64, I64, C, C, C]),
+            "ndvm_linear_forward": (C, [C, C, C, I64, I64, I64, P, I64, P, I64, P, P, I64, P, I64, P, P, P, P, SZ, P]),
+            "ndvm_linear_backward": (C, [C, C, C, I64, I64, I64, P, I64, P, I64, P, I64, P, P, I64, P, P, P, P, I64, P, P, P, SZ,
+                                         P]),
+            "ndvm_linear_quantized_workspace_bytes": (SZ, [I64, I64, I64]),
+            "ndvm_linear_quantized": (C, [C, C, C, I64, I64, I64, P, I64, P, P, I64, P, P, P, I64, P, I64, P, SZ, P]),
             "ndvm_check_operators": (ctypes.c_int, []),
             "ndvm_launch_count": (ctypes.c_ulonglong, []),
             "ndvm_measure_fp64_peak": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double), P]),
@@ -436,5 +450,8 @@ def check_device(tape: Tape):
     _check(load().ndvm_check_device(tape.handle))
 
 
-from .network import (ACTIVATIONS, check_operators, dropout, dropout_backward, dropout_forward, gated, gated_backward,  # noqa: E402,F401
-                      gated_forward, gated_kept, layer_norm, layer_norm_backward, layer_norm_forward)
+from .network import (ACTIVATIONS, Quantized, check_operators, dropout, dropout_backward, dropout_forward, gated,  # noqa: E402,F401
+                      gated_backward, gated_forward, gated_kept, layer_norm, layer_norm_backward, layer_norm_forward, linear,
+                      linear_backward, linear_forward, linear_kept, linear_quantized, linear_quantized_forward, quantize,
+                      quantize_forward, rms_norm, rms_norm_backward, rms_norm_forward, rms_norm_quantized,
+                      rms_norm_quantized_forward)

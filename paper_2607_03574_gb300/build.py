@@ -25,7 +25,7 @@ TORCH_OPS = os.path.join(OUT_DIR, "ndvm_torch.so")  # the network operators' aut
 TORCH_OPS_SOURCE = os.path.join(CSRC, "net", "torch_ops.cpp")
 
 SOURCES = ["tape.cpp", "trace_scheme.cpp", "trace_bytecode.cpp", "plan.cpp", "compact.cpp", "capi.cpp", "replay.cu", "scalar.cu", "matrix.cu",
-           "net/netapi.cpp", "net/norm.cu", "net/dropout.cu", "net/gated.cu"]
+           "net/netapi.cpp", "net/norm.cu", "net/dropout.cu", "net/product.cu", "net/gated.cu", "net/rms.cu", "net/linear.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

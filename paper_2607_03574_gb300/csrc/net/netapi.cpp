@@ -199,12 +199,219 @@ ndvm_status ndvm_gated_backward_kept(ndvm_dtype dtype, ndvm_activation act, int6
   return done(launch_gated_backward(a, dtype, (cudaStream_t)stream), "gated projection launch");
 }
 
+// ------------------------------------------------------------------- root-mean-square norm, 8-bit blocks
+static constexpr int64_t kBlockMost = (int64_t)1 << 40;  // elements of a row
+
+static const char* blocks(const void* values, int64_t rows, int64_t cols, int64_t v_stride, const void* scales) {
+  if (!values || !scales) return "null values or scales of 8-bit blocks";
+  if (!aligned(values, 16) || !aligned(scales, 16)) return "values or scales of 8-bit blocks are not 16-byte aligned";
+  if (cols > kBlockMost || !spans(rows, cols, v_stride) || (rows > 1 && (v_stride % 16 || v_stride < (cols + 15) / 16 * 16)))
+    return "the row stride of 8-bit blocks must be a multiple of 16 that holds a row";
+  return nullptr;
+}
+static const char* kRmsTypes = "rms norm takes F32, F16 and BF16, with weights of the same type or F32";
+
+static ndvm_status rms_forward(RmsArgs& a, ndvm_dtype dtype, ndvm_dtype wtype, double eps, void* stream) {
+  if (!is_float(dtype) || (wtype != dtype && wtype != NDVM_F32)) return set_error(NDVM_E_UNSUPPORTED, kRmsTypes);
+  if (!sizes(a.rows, a.cols) || a.rows > kNormRows - 127) return bad("bad rows or cols");
+  if (!(eps >= 0) || !std::isfinite(eps)) return bad("eps must be finite and not negative");
+  if (a.rows == 0) return NDVM_OK;
+  REFUSE(matrix_in(a.x, a.rows, a.cols, a.x_stride, dtype));
+  if (a.residual) REFUSE(matrix_in(a.residual, a.rows, a.cols, a.r_stride, dtype));
+  if (a.sum && !a.residual) return bad("a sum is written where there is a residual");
+  if (a.sum) REFUSE(matrix_out(a.sum, a.rows, a.cols, a.sum_stride, dtype));
+  REFUSE(vector_in(a.weight, wtype));
+  REFUSE(vector_in(a.rstd, NDVM_F32));
+  a.eps = (float)eps;
+  return done(launch_rms_forward(a, dtype, wtype, (cudaStream_t)stream), "rms norm launch");
+}
+
+ndvm_status ndvm_rms_norm_forward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* x,
+                                  int64_t x_stride, const void* residual, int64_t r_stride, const void* weight, double eps,
+                                  void* y, int64_t y_stride, void* sum, int64_t sum_stride, float* rstd, void* stream) {
+  if (sizes(rows, cols) && rows > 0 && is_float(dtype)) REFUSE(matrix_out(y, rows, cols, y_stride, dtype));
+  RmsArgs a{};
+  a.rows = rows; a.cols = cols; a.x = x; a.x_stride = x_stride; a.residual = residual; a.r_stride = r_stride; a.weight = weight;
+  a.y = y; a.y_stride = y_stride; a.sum = sum; a.sum_stride = sum_stride; a.rstd = rstd;
+  return rms_forward(a, dtype, wtype, eps, stream);
+}
+
+ndvm_status ndvm_rms_norm_quantized(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* x,
+                                    int64_t x_stride, const void* residual, int64_t r_stride, const void* weight, double eps,
+                                    uint8_t* values, int64_t v_stride, uint8_t* scales, void* sum, int64_t sum_stride,
+                                    void* stream) {
+  if (sizes(rows, cols) && rows > 0) REFUSE(blocks(values, rows, cols, v_stride, scales));
+  RmsArgs a{};
+  a.rows = rows; a.cols = cols; a.x = x; a.x_stride = x_stride; a.residual = residual; a.r_stride = r_stride; a.weight = weight;
+  a.values = values; a.v_stride = v_stride; a.v_cols = (cols + 15) / 16 * 16; a.scales = scales; a.sum = sum; a.sum_stride = sum_stride;
+  return rms_forward(a, dtype, wtype, eps, stream);
+}
+
+size_t ndvm_rms_norm_workspace_bytes(int64_t rows, int64_t cols) { return sizes(rows, cols) ? rms_workspace(rows, cols) : 0; }
+
+ndvm_status ndvm_rms_norm_backward(ndvm_dtype dtype, ndvm_dtype wtype, int64_t rows, int64_t cols, const void* dy,
+                                   int64_t dy_stride, const void* dsum, int64_t dsum_stride, const void* s, int64_t s_stride,
+                                   const void* weight, const float* rstd, void* dx, int64_t dx_stride, void* dweight,
+                                   void* workspace, size_t ws_bytes, void* stream) {
+  if (!is_float(dtype) || (wtype != dtype && wtype != NDVM_F32)) return set_error(NDVM_E_UNSUPPORTED, kRmsTypes);
+  if (!sizes(rows, cols) || rows > kNormRows) return bad("bad rows or cols");
+  if (rows > 0) {
+    REFUSE(matrix_in(dy, rows, cols, dy_stride, dtype));
+    REFUSE(matrix_in(s, rows, cols, s_stride, dtype));
+    if (dsum) REFUSE(matrix_in(dsum, rows, cols, dsum_stride, dtype));
+    if (!rstd || !aligned(rstd, 4)) return bad("rstd is null or not aligned");
+    if (dx) REFUSE(matrix_out(dx, rows, cols, dx_stride, dtype));
+  }
+  REFUSE(vector_in(weight, wtype));
+  REFUSE(vector_in(dweight, wtype));
+  if (dweight && (!workspace || !aligned(workspace, 16) || ws_bytes < rms_workspace(rows, cols)))
+    return bad("the workspace is null, not 16-byte aligned or smaller than ndvm_rms_norm_workspace_bytes");
+  RmsArgs a{};
+  a.rows = rows; a.cols = cols; a.x = s; a.x_stride = s_stride; a.weight = weight; a.rstd = const_cast<float*>(rstd);
+  a.dy = dy; a.dy_stride = dy_stride; a.dsum = dsum; a.dsum_stride = dsum_stride; a.dx = dx; a.dx_stride = dx_stride;
+  a.dweight = dweight; a.partial = static_cast<float*>(workspace);
+  return done(launch_rms_backward(a, dtype, wtype, (cudaStream_t)stream), "rms norm launch");
+}
+
+size_t ndvm_quantized_scale_bytes(int64_t rows, int64_t cols) {
+  return sizes(rows, cols) && cols <= kBlockMost ? (size_t)((rows + 127) / 128) * (size_t)((cols + 127) / 128) * 512 : 0;
+}
+
+static ndvm_status convert(bool back, ndvm_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,
+                           const uint8_t* values, int64_t v_stride, const uint8_t* scales, void* stream) {
+  if (!is_float(dtype)) return set_error(NDVM_E_UNSUPPORTED, "8-bit blocks are made of F32, F16 and BF16");
+  if (!sizes(rows, cols) || rows > kNormRows - 127) return bad("bad rows or cols");
+  if (rows == 0) return NDVM_OK;
+  REFUSE(back ? matrix_out(x, rows, cols, x_stride, dtype) : matrix_in(x, rows, cols, x_stride, dtype));
+  REFUSE(blocks(values, rows, cols, v_stride, scales));
+  RmsArgs a{};
+  a.rows = rows; a.cols = cols; a.values = const_cast<uint8_t*>(values); a.v_stride = v_stride; a.v_cols = (cols + 15) / 16 * 16;
+  a.scales = const_cast<uint8_t*>(scales);
+  if (back) a.y = const_cast<void*>(x), a.y_stride = x_stride;
+  else a.x = x, a.x_stride = x_stride;
+  return back ? done(launch_dequantize(a, dtype, (cudaStream_t)stream), "dequantize launch")
+              : done(launch_quantize(a, dtype, (cudaStream_t)stream), "quantize launch");
+}
+
+ndvm_status ndvm_quantize(ndvm_dtype dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride, uint8_t* values,
+                          int64_t v_stride, uint8_t* scales, void* stream) {
+  return convert(false, dtype, rows, cols, x, x_stride, values, v_stride, scales, stream);
+}
+
+ndvm_status ndvm_dequantize(ndvm_dtype dtype, int64_t rows, int64_t cols, const uint8_t* values, int64_t v_stride,
+                            const uint8_t* scales, void* x, int64_t x_stride, void* stream) {
+  return convert(true, dtype, rows, cols, x, x_stride, values, v_stride, scales, stream);
+}
+
+// ---------------------------------------------------------------------------------------- dense layers
+static bool linear_sizes(int64_t rows, int64_t k, int64_t n) {
+  return rows >= 0 && k >= 1 && n >= 1 && rows <= kGatedMost && k <= kGatedMost && n <= kGatedMost;
+}
+static ndvm_status linear_check(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activation act, int64_t rows, int64_t k, int64_t n, const void* bias) {
+  if ((dtype != NDVM_F16 && dtype != NDVM_BF16) || (btype != dtype && btype != NDVM_F32))
+    return set_error(NDVM_E_UNSUPPORTED, "dense layers take F16 and BF16, with a bias of the same type or F32");
+  if (act < NDVM_ACT_SILU || act > NDVM_ACT_NONE) return bad("unknown activation");
+  if (!linear_sizes(rows, k, n)) return bad("bad rows, k or n");
+  REFUSE(vector_in(bias, btype));
+  return NDVM_OK;
+}
+static const char* linear_room(size_t need, const void* workspace, size_t ws_bytes) {
+  return need && (!workspace || !aligned(workspace, 256) || ws_bytes < need)
+             ? "the workspace is null, not 256-byte aligned or smaller than its ..._workspace_bytes" : nullptr;
+}
+// z as it is kept: in binary32 or as 8-bit blocks
+static const char* kept_z(LinearArgs& a, float* z, uint8_t* z_values, uint8_t* z_scales) {
+  if (z && z_values) return "z is kept in binary32 or as 8-bit blocks, not both";
+  if (!aligned(z, 16)) return "z must be 16-byte aligned";
+  a.z_pitch = (a.n + 15) / 16 * 16;
+  if (z_values || z_scales)
+    if (const char* m = blocks(z_values, a.rows, a.n, a.z_pitch, z_scales)) return m;
+  a.z = z; a.z_stride = ndvm_linear_kept_stride(a.n);
+  a.z_values = z_values; a.z_scales = z_scales;
+  return nullptr;
+}
+
+int64_t ndvm_linear_kept_stride(int64_t n) { return n < 1 || n > kGatedMost ? 0 : (n + 3) / 4 * 4; }
+
+size_t ndvm_linear_workspace_bytes(ndvm_activation act, int64_t rows, int64_t k, int64_t n, int backward, int aligned, int held) {
+  if (!linear_sizes(rows, k, n) || act < NDVM_ACT_SILU || act > NDVM_ACT_NONE) return 0;
+  return linear_workspace(rows, k, n, act, backward != 0, !aligned, held != 0);
+}
+
+ndvm_status ndvm_linear_forward(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                const void* x, int64_t x_stride, const void* w, int64_t w_stride, const void* bias,
+                                const void* residual, int64_t r_stride, void* y, int64_t y_stride, float* z,
+                                uint8_t* z_values, uint8_t* z_scales, void* workspace, size_t ws_bytes, void* stream) {
+  if (ndvm_status s = linear_check(dtype, btype, act, rows, k, n, bias)) return s;
+  if (rows == 0) return NDVM_OK;
+  REFUSE(matrix_in(x, rows, k, x_stride, dtype));
+  REFUSE(matrix_in(w, n, k, w_stride, dtype));
+  if (residual) REFUSE(matrix_in(residual, rows, n, r_stride, dtype));
+  REFUSE(matrix_out(y, rows, n, y_stride, dtype));
+  LinearArgs a{};
+  a.rows = rows; a.k = k; a.n = n; a.x = x; a.x_stride = x_stride; a.w = w; a.w_stride = w_stride; a.bias = bias;
+  a.bias_f32 = btype == NDVM_F32; a.act = act; a.residual = residual; a.r_stride = r_stride; a.y = y; a.y_stride = y_stride;
+  a.workspace = workspace;
+  REFUSE(kept_z(a, z, z_values, z_scales));
+  REFUSE(linear_room(linear_workspace(a, false), workspace, ws_bytes));
+  return done(launch_linear_forward(a, dtype, (cudaStream_t)stream), "dense layer launch");
+}
+
+ndvm_status ndvm_linear_backward(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                 const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, const uint8_t* x_values,
+                                 int64_t xv_stride, const uint8_t* x_scales, const void* w, int64_t w_stride, const float* z,
+                                 const uint8_t* z_values, const uint8_t* z_scales, void* dx, int64_t dx_stride, void* dw,
+                                 void* dbias, void* workspace, size_t ws_bytes, void* stream) {
+  if (ndvm_status s = linear_check(dtype, btype, act, rows, k, n, dbias)) return s;
+  REFUSE(vector_in(dw, dtype));
+  LinearArgs a{};
+  a.rows = rows; a.k = k; a.n = n; a.dy = dy; a.dy_stride = dy_stride; a.x = x; a.x_stride = x_stride; a.x_values = x_values;
+  a.xv_stride = xv_stride; a.x_scales = x_scales; a.w = w; a.w_stride = w_stride; a.act = act; a.bias_f32 = btype == NDVM_F32;
+  a.dx = dx; a.dx_stride = dx_stride; a.dw = dw; a.dbias = dbias; a.workspace = workspace;
+  if (rows > 0) {
+    REFUSE(matrix_in(dy, rows, n, dy_stride, dtype));
+    if (x && x_values) return bad("x is given as it is or as 8-bit blocks, not both");
+    if (dw && x) REFUSE(matrix_in(x, rows, k, x_stride, dtype));
+    if (dw && !x) REFUSE(blocks(x_values, rows, k, xv_stride, x_scales));
+    if (dx) REFUSE(matrix_in(w, n, k, w_stride, dtype));
+    if (dx) REFUSE(matrix_out(dx, rows, k, dx_stride, dtype));
+    REFUSE(kept_z(a, const_cast<float*>(z), const_cast<uint8_t*>(z_values), const_cast<uint8_t*>(z_scales)));
+    if (act != NDVM_ACT_NONE && !z && !z_values) return bad("the gradients need the z that the forward call kept");
+  }
+  REFUSE(linear_room(linear_workspace(a, true), workspace, ws_bytes));
+  return done(launch_linear_backward(a, dtype, (cudaStream_t)stream), "dense layer launch");
+}
+
+size_t ndvm_linear_quantized_workspace_bytes(int64_t rows, int64_t k, int64_t n) {
+  return linear_sizes(rows, k, n) ? linear_blocks_workspace(rows, k, n) : 0;
+}
+
+ndvm_status ndvm_linear_quantized(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activation act, int64_t rows, int64_t k, int64_t n,
+                                  const uint8_t* x_values, int64_t xv_stride, const uint8_t* x_scales,
+                                  const uint8_t* w_values, int64_t wv_stride, const uint8_t* w_scales, const void* bias,
+                                  const void* residual, int64_t r_stride, void* y, int64_t y_stride, void* workspace,
+                                  size_t ws_bytes, void* stream) {
+  if (ndvm_status s = linear_check(dtype, btype, act, rows, k, n, bias)) return s;
+  if (rows == 0) return NDVM_OK;
+  REFUSE(blocks(x_values, rows, k, xv_stride, x_scales));
+  REFUSE(blocks(w_values, n, k, wv_stride, w_scales));
+  if (residual) REFUSE(matrix_in(residual, rows, n, r_stride, dtype));
+  REFUSE(matrix_out(y, rows, n, y_stride, dtype));
+  LinearArgs a{};
+  a.rows = rows; a.k = k; a.n = n; a.x_values = x_values; a.xv_stride = xv_stride; a.x_scales = x_scales; a.w_values = w_values;
+  a.wv_stride = wv_stride; a.w_scales = w_scales; a.bias = bias; a.bias_f32 = btype == NDVM_F32; a.act = act;
+  a.residual = residual; a.r_stride = r_stride; a.y = y; a.y_stride = y_stride; a.workspace = workspace;
+  REFUSE(linear_room(linear_blocks_workspace(rows, k, n), workspace, ws_bytes));
+  return done(launch_linear_blocks(a, dtype, (cudaStream_t)stream), "dense layer launch");
+}
+
 ndvm_status ndvm_check_operators(void) {
-  int flag = 0;
+  int flag = 0, linear = 0;
   cudaError_t e = cudaDeviceSynchronize();
-  if (e == cudaSuccess) e = gated_stopped(&flag);
+  if (e == cudaSuccess) e = product_stopped(&flag);
+  if (e == cudaSuccess) e = linear_stopped(&linear);
   if (e != cudaSuccess) return done(e, "read flag");
-  return flag ? set_error(NDVM_E_DEVICE_CHECK, "a kernel of the gated projection gave up waiting for its operands") : NDVM_OK;
+  return flag || linear ? set_error(NDVM_E_DEVICE_CHECK, "a kernel of the network operators gave up waiting for its operands") : NDVM_OK;
 }
 
 }  // extern "C"

@@ -86,6 +86,17 @@ __device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap* map, in
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
         ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
+template <int kCtas>
+__device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  if constexpr (kCtas == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(to), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
 // a box of shared memory to the tensor at (x, y[, z]); what lies outside it is left out
 __device__ __forceinline__ void store_box(const CUtensorMap* map, int x, int y, uint32_t from) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
@@ -135,6 +146,30 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
         "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
         ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
 }
+// The same for 32 of the contraction of e4m3 operands in 8-bit blocks: a and b's scales (a byte of a column of tensor
+// memory for each row, by the descriptor's scale ids) are powers of two.
+template <int kCtas>
+__device__ __forceinline__ void mma_blocks(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t a_scales, uint32_t b_scales, bool add) {
+  if constexpr (kCtas == 1)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+        ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add) : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+        ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add) : "memory");
+}
+// 512 bytes of shared memory (32 lanes of 16 bytes) to 4 columns of tensor memory, the same for each quarter of the lanes; products
+// issued later by this thread see them (a pair's blocks both copy, each its own)
+template <int kCtas>
+__device__ __forceinline__ void copy_scales(uint32_t to, uint32_t from) {
+  // no swizzle, groups of 8 lanes 128 bytes apart
+  const uint64_t desc = ((uint64_t)(from >> 4) & 0x3fff) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+  if constexpr (kCtas == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+}
 // arrives on the barrier (of a pair: on both blocks') when the products issued so far are done
 template <int kCtas>
 __device__ __forceinline__ void commit(uint32_t bar) {
@@ -183,6 +218,10 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, bool rows_contiguous)
 __host__ __device__ constexpr uint32_t instruction(bool bf16, bool a_rows, bool b_rows, int m, int n) {
   return 1u << 4 | (uint32_t)bf16 << 7 | (uint32_t)bf16 << 10 | (uint32_t)a_rows << 15 | (uint32_t)b_rows << 16 |
          (uint32_t)(n / 8) << 17 | (uint32_t)(m / 16) << 24;
+}
+// and for e4m3 operands in 8-bit blocks; id: which byte of their columns the scales are
+__host__ __device__ constexpr uint32_t instruction_blocks(int m, int n, int id) {
+  return (uint32_t)id << 4 | (uint32_t)(n / 8) << 17 | 1u << 23 | (uint32_t)(m / 128) << 27 | (uint32_t)id << 29;
 }
 
 }  // namespace tc

@@ -307,6 +307,252 @@ Maybe gated(const Tensor& gx, const Tensor& gg, const Tensor& gu, int64_t act, i
   return recorded({&x, &w_gate, &w_up}) ? Gated::apply(x, w_gate, w_up, act, keep) : gated_forward(x, w_gate, w_up, act, Tensor());
 }
 
+// ------------------------------------------------------------------------------------- rms norm
+// (x, weight or undefined, residual or undefined) as the operator takes them; false: not its arguments
+bool norm_arguments(const Tensor& given, const Maybe& w, const Maybe& r, Tensor* x, Tensor* weight, Tensor* residual) {
+  if (!given.is_cuda()) return false;
+  const int device = c10::cuda::current_device();
+  if (!here(given, device) || given.dim() == 0 || type_code(given) < 0) return false;
+  *x = rowed(given);
+  *weight = some(w);
+  if (weight->defined()) {
+    if (!here(*weight, device) || weight->dim() != 1 || weight->size(0) != x->size(-1) || type_code(*weight) < 0) return false;
+    if (!weight->is_contiguous() || weight->is_neg()) *weight = resolved(weight->contiguous());
+  }
+  if (r && r->defined()) {
+    if (!here(*r, device) || r->sizes() != x->sizes() || r->scalar_type() != x->scalar_type()) return false;
+    *residual = rowed(*r);
+  }
+  check_inputs({x, weight, residual});
+  return true;
+}
+int weight_code(const Tensor& weight, const Tensor& x) { return weight.defined() ? type_code(weight) : type_code(x); }
+
+// {y} or {y, sum}
+variable_list rms_forward(const Tensor& x, const Tensor& weight, const Tensor& residual, double eps, Tensor* rstd) {
+  const Rows r(x);
+  Tensor y = at::empty(x.sizes(), x.options()), sum;
+  if (residual.defined()) sum = at::empty(x.sizes(), x.options());
+  if (rstd) *rstd = at::empty({r.rows}, x.options().dtype(at::kFloat));
+  check_forward(ndvm_rms_norm_forward((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(weight, x), r.rows, r.cols, in(x), r.stride, in(residual),
+                                      residual.defined() ? Rows(residual).stride : 0, in(weight), eps, out(y), r.cols, out(sum), r.cols,
+                                      rstd ? static_cast<float*>(out(*rstd)) : nullptr, stream_of(x.get_device())));
+  return sum.defined() ? variable_list{y, sum} : variable_list{y};
+}
+struct RmsNorm : torch::autograd::Function<RmsNorm> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& x, const Maybe& w, const Maybe& r, double eps) {
+    const Tensor weight = some(w), residual = some(r);
+    Tensor rstd;
+    variable_list y = rms_forward(x, weight, residual, eps, &rstd);
+    ctx->save_for_backward({residual.defined() ? y[1] : x, weight, rstd});
+    ctx->saved_data["residual"] = residual.defined();
+    ctx->set_materialize_grads(false);
+    return y;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    for (const Tensor& g : grads)
+      if (g.defined()) first_order(g);
+    const variable_list saved = ctx->get_saved_variables();
+    const Tensor &s = saved[0], &weight = saved[1], &rstd = saved[2];
+    const bool residual = ctx->saved_data["residual"].toBool(), weighted = weight.defined();
+    const bool want_x = ctx->needs_input_grad(0), want_r = residual && ctx->needs_input_grad(weighted ? 2 : 1);
+    Tensor dx, dw;
+    if (weighted && ctx->needs_input_grad(1)) dw = at::empty({s.size(-1)}, weight.options());
+    if (!grads[0].defined()) {  // (the sum alone has a cotangent, or nothing has)
+      if (dw.defined()) dw.zero_();
+      dx = residual ? grads[1] : Tensor();
+    } else {
+      const Rows r(s);
+      const Tensor dy = rowed(grads[0]), dsum = residual && grads[1].defined() ? rowed(grads[1]) : Tensor();
+      if (want_x || want_r) dx = at::empty(s.sizes(), s.options());
+      const size_t need = dw.defined() ? ndvm_rms_norm_workspace_bytes(r.rows, r.cols) : 0;
+      Tensor ws = bytes(need, s);
+      check_backward(ndvm_rms_norm_backward((ndvm_dtype)type_code(s), (ndvm_dtype)weight_code(weight, s), r.rows, r.cols, in(dy), Rows(dy).stride,
+                                            in(dsum), dsum.defined() ? Rows(dsum).stride : 0, in(s), r.stride, in(weight),
+                                            static_cast<const float*>(in(rstd)), out(dx), r.cols, out(dw), out(ws), need, stream_of(s.get_device())));
+    }
+    return {want_x ? dx : Tensor(), dw, want_r ? dx : Tensor(), Tensor()};
+  }
+};
+std::optional<variable_list> rms_norm(const Tensor& given, const Maybe& w, double eps, const Maybe& r) {
+  Tensor x, weight, residual;
+  if (!norm_arguments(given, w, r, &x, &weight, &residual)) return std::nullopt;
+  return recorded({&x, &weight, &residual}) ? RmsNorm::apply(x, maybe(weight), maybe(residual), eps) : rms_forward(x, weight, residual, eps, nullptr);
+}
+
+// --------------------------------------------------------------------------------- 8-bit blocks
+constexpr const char* kNoGradient = "the operators on 8-bit blocks have no gradients: call them under torch.no_grad()";
+struct Blocks {
+  Tensor values, scales;  // values: rows of `stride` bytes
+  int64_t rows, cols, stride;
+  Blocks(const Tensor& like, int64_t rows, int64_t cols) : rows(rows), cols(cols), stride((cols + 15) / 16 * 16) {
+    values = at::empty({rows, stride}, like.options().dtype(at::kFloat8_e4m3fn));
+    scales = at::empty({(rows + 127) / 128, (cols + 127) / 128, 32, 4, 4}, like.options().dtype(at::kByte));
+  }
+  uint8_t* v() const { return static_cast<uint8_t*>(out(values)); }
+  uint8_t* s() const { return static_cast<uint8_t*>(out(scales)); }
+  Tensor shaped(at::IntArrayRef sizes) const {  // the values as a tensor of that shape
+    auto strides = sizes.vec();
+    int64_t step = stride;
+    strides.back() = 1;
+    for (int64_t d = (int64_t)sizes.size() - 2; d >= 0; d--) strides[d] = step, step *= std::max<int64_t>(sizes[d], 1);
+    return values.as_strided(sizes, strides);
+  }
+};
+using Held = std::tuple<Tensor, Tensor, int64_t, int64_t, int64_t>;  // values, scales, rows, cols, stride
+
+Blocks to_blocks(const Tensor& x) {
+  const Rows r(x);
+  Blocks b(x, r.rows, r.cols);
+  check_forward(ndvm_quantize((ndvm_dtype)type_code(x), r.rows, r.cols, in(x), r.stride, b.v(), b.stride, b.s(), stream_of(x.get_device())));
+  return b;
+}
+std::optional<Held> quantize(const Tensor& given) {
+  if (!given.is_cuda()) return std::nullopt;
+  if (!here(given, c10::cuda::current_device()) || given.dim() == 0 || type_code(given) < 0) return std::nullopt;
+  check_inputs({&given});
+  if (recorded({&given})) raise_forward(NDVM_E_UNSUPPORTED, kNoGradient);
+  const Tensor x = rowed(given);
+  const Blocks b = to_blocks(x);
+  return Held{b.shaped(x.sizes()), b.scales, b.rows, b.cols, b.stride};
+}
+std::optional<std::tuple<Tensor, Tensor, int64_t, int64_t, int64_t, Tensor>> rms_norm_quantized(const Tensor& given, const Maybe& w, double eps,
+                                                                                                const Maybe& r) {
+  Tensor x, weight, residual, sum;
+  if (!norm_arguments(given, w, r, &x, &weight, &residual)) return std::nullopt;
+  if (recorded({&x, &weight, &residual})) raise_forward(NDVM_E_UNSUPPORTED, kNoGradient);
+  const Rows rows(x);
+  const Blocks b(x, rows.rows, rows.cols);
+  if (residual.defined()) sum = at::empty(x.sizes(), x.options());
+  check_forward(ndvm_rms_norm_quantized((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(weight, x), rows.rows, rows.cols, in(x), rows.stride, in(residual),
+                                        residual.defined() ? Rows(residual).stride : 0, in(weight), eps, b.v(), b.stride, b.s(), out(sum), rows.cols,
+                                        stream_of(x.get_device())));
+  return std::make_tuple(b.shaped(x.sizes()), b.scales, b.rows, b.cols, b.stride, sum);
+}
+
+// ---------------------------------------------------------------------------------- dense layers
+bool ready(const Tensor& t, const Rows& r) { return (uintptr_t)in(t) % 16 == 0 && (r.rows <= 1 || (r.stride % 8 == 0 && r.stride >= r.cols)); }
+// bias (n) and residual (sizes) of a dense layer whose y has that type
+bool linear_extras(int device, const Maybe& b, const Maybe& r, int64_t n, at::IntArrayRef sizes, at::ScalarType type, Tensor* bias, Tensor* residual) {
+  *bias = some(b);
+  if (bias->defined()) {
+    if (!here(*bias, device) || bias->dim() != 1 || bias->size(0) != n || (bias->scalar_type() != type && bias->scalar_type() != at::kFloat)) return false;
+    if (!bias->is_contiguous() || bias->is_neg()) *bias = resolved(bias->contiguous());
+  }
+  if (r && r->defined()) {
+    if (!here(*r, device) || r->sizes() != sizes || r->scalar_type() != type) return false;
+    *residual = rowed(*r);
+  }
+  return true;
+}
+Tensor linear_forward(const Tensor& x, const Tensor& w, const Tensor& bias, int64_t act, const Tensor& residual, const Tensor& z, const Blocks* held) {
+  const Rows rx(x), rw(w);
+  const int64_t n = w.size(0);
+  auto shape = x.sizes().vec();
+  shape.back() = n;
+  Tensor y = at::empty(shape, x.options());
+  const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rx.rows, rx.cols, n, 0, ready(x, rx) && ready(w, rw), 0);
+  Tensor ws = bytes(need, x);
+  check_forward(ndvm_linear_forward((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(bias, x), (ndvm_activation)act, rx.rows, rx.cols, n, in(x), rx.stride,
+                                    in(w), rw.stride, in(bias), in(residual), residual.defined() ? Rows(residual).stride : 0, out(y), n,
+                                    static_cast<float*>(out(z)), held ? held->v() : nullptr, held ? held->s() : nullptr, out(ws), need,
+                                    stream_of(x.get_device())));
+  return y;
+}
+struct Linear : torch::autograd::Function<Linear> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Maybe& b, const Maybe& r, int64_t act, bool eight) {
+    const Tensor bias = some(b), residual = some(r);
+    const Rows rx(x);
+    const int64_t n = w.size(0);
+    Tensor z, y;
+    // what the gradients need: z of an activation, and x for w's
+    const bool activated = act != NDVM_ACT_NONE, wants_w = w.requires_grad(), wants_z = activated && (wants_w || x.requires_grad() || (bias.defined() && bias.requires_grad()));
+    if (eight) {
+      Tensor xv, xs, zs;
+      if (wants_w) {
+        const Blocks held = to_blocks(x);
+        xv = held.values, xs = held.scales;
+      }
+      std::optional<Blocks> blocks;
+      if (wants_z) blocks.emplace(x, rx.rows, n), z = blocks->values, zs = blocks->scales;
+      y = linear_forward(x, w, bias, act, residual, Tensor(), blocks ? &*blocks : nullptr);
+      ctx->save_for_backward({xv, xs, w, z, zs});
+    } else {
+      if (wants_z) z = at::empty({rx.rows, ndvm_linear_kept_stride(n)}, x.options().dtype(at::kFloat));
+      y = linear_forward(x, w, bias, act, residual, z, nullptr);
+      ctx->save_for_backward({wants_w ? x : Tensor(), Tensor(), w, z, Tensor()});
+    }
+    ctx->saved_data["act"] = act;
+    ctx->saved_data["x"] = x.sizes();
+    ctx->saved_data["eight"] = eight;
+    ctx->saved_data["bias"] = bias.defined() ? (int64_t)bias.scalar_type() : (int64_t)-1;
+    ctx->saved_data["residual"] = residual.defined();
+    return y;
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    first_order(grads[0]);
+    const variable_list saved = ctx->get_saved_variables();
+    const Tensor &x = saved[0], &xs = saved[1], &w = saved[2], &z = saved[3], &zs = saved[4], dy = rowed(grads[0]);
+    const int64_t act = ctx->saved_data["act"].toInt(), n = w.size(0), k = w.size(1), btype = ctx->saved_data["bias"].toInt();
+    const auto sizes = ctx->saved_data["x"].toIntVector();
+    const bool eight = ctx->saved_data["eight"].toBool(), biased = btype >= 0, residual = ctx->saved_data["residual"].toBool();
+    const Rows rd(dy), rw(w);
+    Tensor dx, dw, db;  // (the node's inputs are x, w and those of bias and residual that there are)
+    if (ctx->needs_input_grad(0)) dx = at::empty(sizes, dy.options());
+    if (ctx->needs_input_grad(1)) dw = at::empty({n, k}, dy.options());
+    if (biased && ctx->needs_input_grad(2)) db = at::empty({n}, dy.options().dtype((at::ScalarType)btype));
+    if (dx.defined() || dw.defined() || db.defined()) {
+      const bool held = eight && dw.defined();
+      std::optional<Rows> rx;
+      if (!eight && x.defined()) rx.emplace(x);
+      const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rd.rows, k, n, 1,
+                                                      (!rx || ready(x, *rx)) && ready(w, rw) && ready(dy, rd), held);
+      Tensor ws = bytes(need, dy);
+      check_backward(ndvm_linear_backward(
+          (ndvm_dtype)type_code(dy), db.defined() && btype == (int64_t)at::kFloat ? NDVM_F32 : (ndvm_dtype)type_code(dy), (ndvm_activation)act, rd.rows, k, n,
+          in(dy), rd.stride, rx ? in(x) : nullptr, rx ? rx->stride : 0, held ? static_cast<const uint8_t*>(in(x)) : nullptr, held ? x.size(-1) : 0,
+          held ? static_cast<const uint8_t*>(in(xs)) : nullptr, in(w), rw.stride, eight ? nullptr : static_cast<const float*>(in(z)),
+          eight ? static_cast<const uint8_t*>(in(z)) : nullptr, eight ? static_cast<const uint8_t*>(in(zs)) : nullptr, out(dx), k, out(dw), out(db), out(ws),
+          need, stream_of(dy.get_device())));
+    }
+    return {dx, dw, db, residual && ctx->needs_input_grad(biased ? 3 : 2) ? grads[0] : Tensor(), Tensor(), Tensor()};
+  }
+};
+Maybe linear(const Tensor& gx, const Tensor& gw, const Maybe& b, int64_t act, const Maybe& r, bool eight) {
+  if (!gx.is_cuda()) return std::nullopt;
+  const int device = c10::cuda::current_device();
+  if (!here(gx, device) || !here(gw, device) || gx.dim() == 0 || gw.dim() != 2 || gw.size(1) != gx.size(-1)) return std::nullopt;
+  if (type_code(gx) <= NDVM_F32 || gw.scalar_type() != gx.scalar_type()) return std::nullopt;
+  auto shape = gx.sizes().vec();
+  shape.back() = gw.size(0);
+  Tensor bias, residual;
+  if (!linear_extras(device, b, r, gw.size(0), shape, gx.scalar_type(), &bias, &residual)) return std::nullopt;
+  const Tensor x = rowed(gx), w = rowed(gw);
+  check_inputs({&x, &w, &bias, &residual});
+  if (recorded({&x, &w, &bias, &residual})) return Linear::apply(x, w, maybe(bias), maybe(residual), act, eight);
+  return linear_forward(x, w, bias, act, residual, Tensor(), nullptr);
+}
+Maybe linear_quantized(const Tensor& xv, const Tensor& xs, int64_t rows, int64_t k, int64_t x_stride, const Tensor& wv, const Tensor& ws, int64_t n,
+                       int64_t wk, int64_t w_stride, const Maybe& b, int64_t act, const Maybe& r, int64_t code) {
+  const int device = c10::cuda::current_device();
+  if (!here(xv, device) || !here(wv, device) || wv.dim() != 2 || wk != k || (code != NDVM_F16 && code != NDVM_BF16)) return std::nullopt;
+  const at::ScalarType type = code == NDVM_F16 ? at::kHalf : at::kBFloat16;
+  auto shape = xv.sizes().vec();
+  shape.back() = n;
+  Tensor bias, residual;
+  if (!linear_extras(device, b, r, n, shape, type, &bias, &residual)) return std::nullopt;
+  check_inputs({&xv, &wv, &bias, &residual});
+  if (recorded({&bias, &residual})) raise_forward(NDVM_E_UNSUPPORTED, kNoGradient);
+  Tensor y = at::empty(shape, xv.options().dtype(type));
+  const size_t need = ndvm_linear_quantized_workspace_bytes(rows, k, n);
+  Tensor room = bytes(need, xv);
+  check_forward(ndvm_linear_quantized((ndvm_dtype)type_code(y), (ndvm_dtype)weight_code(bias, y), (ndvm_activation)act, rows, k, n,
+                                      static_cast<const uint8_t*>(in(xv)), x_stride, static_cast<const uint8_t*>(in(xs)),
+                                      static_cast<const uint8_t*>(in(wv)), w_stride, static_cast<const uint8_t*>(in(ws)), in(bias), in(residual),
+                                      residual.defined() ? Rows(residual).stride : 0, out(y), n, out(room), need, stream_of(device)));
+  return y;
+}
+
 }  // namespace
 
 // (torch's errors as torch raises them)
@@ -321,6 +567,27 @@ PYBIND11_MODULE(ndvm_torch, m) {
   });
   m.def("gated", [](const Tensor& x, const Tensor& w_gate, const Tensor& w_up, int64_t act, int64_t keep) {
     HANDLE_TH_ERRORS return gated(x, w_gate, w_up, act, keep);
+    END_HANDLE_TH_ERRORS_PYBIND
+  });
+  m.def("rms_norm", [](const Tensor& x, const Maybe& weight, double eps, const Maybe& residual) {
+    HANDLE_TH_ERRORS return rms_norm(x, weight, eps, residual);
+    END_HANDLE_TH_ERRORS_PYBIND
+  });
+  m.def("quantize", [](const Tensor& x) {
+    HANDLE_TH_ERRORS return quantize(x);
+    END_HANDLE_TH_ERRORS_PYBIND
+  });
+  m.def("rms_norm_quantized", [](const Tensor& x, const Maybe& weight, double eps, const Maybe& residual) {
+    HANDLE_TH_ERRORS return rms_norm_quantized(x, weight, eps, residual);
+    END_HANDLE_TH_ERRORS_PYBIND
+  });
+  m.def("linear", [](const Tensor& x, const Tensor& w, const Maybe& bias, int64_t act, const Maybe& residual, bool eight) {
+    HANDLE_TH_ERRORS return linear(x, w, bias, act, residual, eight);
+    END_HANDLE_TH_ERRORS_PYBIND
+  });
+  m.def("linear_quantized", [](const Tensor& xv, const Tensor& xs, int64_t rows, int64_t k, int64_t x_stride, const Tensor& wv, const Tensor& ws, int64_t n,
+                               int64_t wk, int64_t w_stride, const Maybe& bias, int64_t act, const Maybe& residual, int64_t type) {
+    HANDLE_TH_ERRORS return linear_quantized(xv, xs, rows, k, x_stride, wv, ws, n, wk, w_stride, bias, act, residual, type);
     END_HANDLE_TH_ERRORS_PYBIND
   });
 }

@@ -7,6 +7,9 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
+
+#include "../status.h"
 
 namespace ndvm {
 
@@ -14,10 +17,19 @@ __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 
+template <typename T> constexpr ndvm_dtype kType = std::is_same<T, float>::value ? NDVM_F32 : std::is_same<T, __half>::value ? NDVM_F16 : NDVM_BF16;
+
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// what rounding v to the operands' type leaves, rounded too (0 beside what is not finite)
+template <typename T>
+__device__ __forceinline__ T rest_of(float v, T rounded) {
+  const float r = to_f32(rounded);
+  return from_f32<T>(fabsf(r) <= 3.0e38f ? v - r : 0.0f);
+}
 
 // V elements that are loaded and stored together (16 bytes, or one element)
 template <typename T, int V>

@@ -3,11 +3,19 @@
     y = layer_norm(x, weight, bias)                  # over the last dimension
     h = gated(x, w_gate, w_up, "silu")               # act(x Wg^T) * (x Wu^T)
     z = dropout(h, p, seed, offset, residual=x)      # residual + dropout, the mask never stored
+    y, x = rms_norm(x, weight, residual=h)           # of x + h, which is returned beside it
+    y = linear(x, w, bias, "silu", residual)         # act(x w^T + bias) + residual; keep="8bit": less is held for its gradient
 
-These three are differentiable torch ops on the current stream, like ``loss_op(tape)`` (their autograd
+These are differentiable torch ops on the current stream, like ``loss_op(tape)`` (their autograd
 nodes are in ``csrc/net/torch_ops.cpp``).  Under them are raw calls (``*_forward``, ``*_backward``) that take
 outputs, a workspace and a stream and map one to one onto the C ABI (``ndvm_layer_norm_*``,
-``ndvm_dropout``, ``ndvm_gated_*``).
+``ndvm_dropout``, ``ndvm_gated_*``, ``ndvm_rms_norm_*``, ``ndvm_linear_*``).
+
+A trained network is scored on 8-bit operands, without gradients:
+
+    q = quantize(w)                                  # once: 8-bit blocks (Quantized)
+    h, x = rms_norm_quantized(x, weight, residual=y)
+    y = linear_quantized(h, q, bias, "silu")
 
 Layouts: the last dimension is contiguous and the leading ones are rows with one stride, 0 or at least a
 row's length (a raw call refuses anything else, a differentiable op copies it).  Types: float32, float16 and bfloat16;
@@ -25,6 +33,7 @@ import paper_2607_03574_gb300 as _nd
 from . import NdvmError, _check, _on_stream, _torch, load
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
+_NONE = 4  # no activation (dense layers alone)
 
 _torch_module = None
 _types = {}
@@ -369,6 +378,364 @@ def gated_backward(dh, x, w_gate, w_up, activation="silu", wants=(True, True, Tr
     return dx, dw_gate, dw_up
 
 
+# ----------------------------------------------------------------------------------- rms norm
+def _rms_stats(rstd, rows, device):
+    _given(rstd, "rstd", (rows,), _torch_module.float32, device)
+    if not rstd.is_contiguous():
+        raise NdvmError(1, "rstd must be contiguous")
+    return rstd.data_ptr()
+
+
+def _like(t, name, x, device):
+    """(address, row stride) of a tensor of x's shape and type, or (None, 0)."""
+    if t is None:
+        return None, 0
+    _given(t, name, x.shape, x.dtype, device)
+    return t.data_ptr(), _rows(t, name)[2]
+
+
+def rms_norm_forward(x, weight=None, eps=1e-6, residual=None, y=None, sum=None, rstd=None, want_rstd=True, stream=None):
+    """(y, sum, rstd): s / sqrt(mean(s^2) + eps) * weight over the last dimension, s = x + residual rounded to x's type
+    (sum; None without a residual).  weight: a vector of x's type or float32.  rstd: float32 [rows] for the backward pass
+    (None with want_rstd=False).  sum may be x or residual.  Outputs this call allocates belong to `stream`."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
+    code = _type(x, "x")
+    rows, cols, xs = _rows(x, "x")
+    rp, rs = _like(residual, "residual", x, device)
+    if sum is not None and residual is None:
+        raise NdvmError(1, "a sum is written where there is a residual")
+    if y is None:
+        y = _new(torch, x.shape, x.dtype, device, stream)
+    if sum is None and residual is not None:
+        sum = _new(torch, x.shape, x.dtype, device, stream)
+    if rstd is None and want_rstd:
+        rstd = _new(torch, (rows,), torch.float32, device, stream)
+    yp, ys = _like(y, "y", x, device)
+    sp, ss = _like(sum, "sum", x, device)
+    status = lib.ndvm_rms_norm_forward(code, _weight_type(code, weight, None), rows, cols, x.data_ptr(), xs, rp, rs,
+                                       _vector(weight, "weight", cols, device), eps, yp, ys, sp, ss,
+                                       None if rstd is None else _rms_stats(rstd, rows, device), _stream(torch, stream, device))
+    if status:
+        _check(status)
+    return y, sum, rstd
+
+
+def rms_norm_backward(dy, s, weight, rstd, dsum=None, wants=(True, True), dx=None, dweight=None, wtype=None, workspace=None,
+                      stream=None):
+    """(dx, dweight) of rms_norm_forward, s being its sum (its x without a residual); dx is the residual's gradient too.
+    `wants` says which (the others are None).  dweight has weight's type (`wtype` where there is none; x's by default)."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, s)
+    code = _type(s, "s")
+    rows, cols, xs = _rows(s, "s")
+    dyp, dys = _like(dy, "dy", s, device)
+    dsp, dss = _like(dsum, "dsum", s, device)
+    wdtype = weight.dtype if weight is not None else (wtype or s.dtype)
+    if dx is None and wants[0]:
+        dx = _new(torch, s.shape, s.dtype, device, stream)
+    if dweight is None and wants[1]:
+        dweight = _new(torch, (cols,), wdtype, device, stream)
+    xp, dxs = _like(dx, "dx", s, device)
+    dwp = None
+    if dweight is not None:
+        _given(dweight, "dweight", (cols,), wdtype, device)
+        dwp = _vector(dweight, "dweight", cols, device)
+    need = lib.ndvm_rms_norm_workspace_bytes(rows, cols) if dwp is not None else 0
+    ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
+    status = lib.ndvm_rms_norm_backward(code, _weight_type(code, dweight if weight is None else weight, None), rows, cols, dyp, dys,
+                                        dsp, dss, s.data_ptr(), xs, _vector(weight, "weight", cols, device),
+                                        _rms_stats(rstd, rows, device), xp, dxs, dwp, wp, nbytes, _stream(torch, stream, device))
+    if status:
+        _check(status)
+    return dx, dweight
+
+
+# -------------------------------------------------------------------------------- 8-bit blocks
+class Quantized:
+    """A tensor in 8-bit blocks: 32 consecutive elements of the last dimension share a scale 2^e, the least from e = -127 on
+    with which none is over 448 in size; an element is the nearest e4m3 value to v / 2^e.  A block with an infinity or a
+    NaN is NaN.
+
+    values: float8_e4m3fn of the tensor's shape, rows with one stride that is a multiple of 16 and starts on 16 bytes.
+    scales: uint8 [rows / 128, columns / 128, 32, 4, 4] (both rounded up), e + 127 at [row / 128, column / 128, row % 32,
+    row / 32 % 4, column / 32 % 4].  quantize() and rms_norm_quantized() make them."""
+
+    __slots__ = ("values", "scales", "rows", "cols", "stride")
+
+    def __init__(self, values, scales):
+        torch = _torch_module or _start()
+        if values.dtype != torch.float8_e4m3fn or scales.dtype != torch.uint8:
+            raise NdvmError(3, "8-bit blocks are float8_e4m3fn values with uint8 scales")
+        if not values.is_cuda or scales.device != values.device:
+            raise NdvmError(1, "values and scales must be CUDA tensors of one device")
+        rows, cols, stride = _rows(values, "values")
+        if (rows > 1 and (stride % 16 or stride < cols)) or values.data_ptr() % 16:
+            raise NdvmError(1, "values must be rows that start on 16 bytes")
+        if scales.shape != (-(-rows // 128), -(-cols // 128), 32, 4, 4) or not scales.is_contiguous() or scales.data_ptr() % 16:
+            raise NdvmError(1, f"scales must be contiguous, of shape {(-(-rows // 128), -(-cols // 128), 32, 4, 4)}, and start on 16 bytes")
+        self.values, self.scales, self.rows, self.cols, self.stride = values, scales, rows, cols, stride
+
+    @classmethod
+    def _of(cls, values, scales, rows, cols, stride):
+        """(what this package has made needs no checks)"""
+        q = cls.__new__(cls)
+        q.values, q.scales, q.rows, q.cols, q.stride = values, scales, rows, cols, stride
+        return q
+
+    @property
+    def shape(self):
+        return self.values.shape
+
+    @property
+    def device(self):
+        return self.values.device
+
+    def __repr__(self):
+        return f"Quantized(shape={tuple(self.shape)}, device={self.device})"
+
+    def dequantize(self, dtype=None, out=None, stream=None):
+        """What the blocks stand for, rounded to dtype (float32 by default); what rounding lifts beyond its largest finite
+        value becomes that value."""
+        torch = _torch_module or _start()
+        lib = _nd._lib or load()
+        device = _device(torch, self.values)
+        if out is None:
+            out = _new(torch, self.shape, dtype or torch.float32, device, stream)
+        else:
+            _given(out, "out", self.shape, dtype or out.dtype, device)
+        status = lib.ndvm_dequantize(_type(out, "out"), self.rows, self.cols, self.values.data_ptr(), self.stride, self.scales.data_ptr(),
+                                     out.data_ptr(), _rows(out, "out")[2], _stream(torch, stream, device))
+        if status:
+            _check(status)
+        return out
+
+
+def _new_quantized(torch, shape, rows, cols, device, stream):
+    """Room for blocks of `shape`."""
+    pitch = -(-cols // 16) * 16
+    values = _new(torch, shape[:-1] + (pitch,), torch.float8_e4m3fn, device, stream)[..., :cols]
+    scales = _new(torch, (-(-rows // 128), -(-cols // 128), 32, 4, 4), torch.uint8, device, stream)
+    return Quantized._of(values, scales, rows, cols, pitch)
+
+
+def _given_quantized(q, name, shape, device):
+    if not isinstance(q, Quantized) or q.shape != shape:
+        raise NdvmError(1, f"{name} must be Quantized of shape {tuple(shape)}")
+    _same_device(device, q.values, name)
+
+
+def quantize_forward(x, out=None, stream=None):
+    """Quantized: 8-bit blocks of x (..., cols); float32, float16, bfloat16.  out: a Quantized of x's shape to write to."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
+    code = _type(x, "x")
+    rows, cols, xs = _rows(x, "x")
+    if out is None:
+        out = _new_quantized(torch, x.shape, rows, cols, device, stream)
+    else:
+        _given_quantized(out, "out", x.shape, device)
+    status = lib.ndvm_quantize(code, rows, cols, x.data_ptr(), xs, out.values.data_ptr(), out.stride, out.scales.data_ptr(),
+                               _stream(torch, stream, device))
+    if status:
+        _check(status)
+    return out
+
+
+def rms_norm_quantized_forward(x, weight=None, eps=1e-6, residual=None, out=None, sum=None, stream=None):
+    """(y, sum): rms_norm_forward with y as 8-bit blocks (Quantized) of what is not rounded in between."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
+    code = _type(x, "x")
+    rows, cols, xs = _rows(x, "x")
+    rp, rs = _like(residual, "residual", x, device)
+    if sum is not None and residual is None:
+        raise NdvmError(1, "a sum is written where there is a residual")
+    if sum is None and residual is not None:
+        sum = _new(torch, x.shape, x.dtype, device, stream)
+    sp, ss = _like(sum, "sum", x, device)
+    if out is None:
+        out = _new_quantized(torch, x.shape, rows, cols, device, stream)
+    else:
+        _given_quantized(out, "out", x.shape, device)
+    status = lib.ndvm_rms_norm_quantized(code, _weight_type(code, weight, None), rows, cols, x.data_ptr(), xs, rp, rs,
+                                         _vector(weight, "weight", cols, device), eps, out.values.data_ptr(), out.stride,
+                                         out.scales.data_ptr(), sp, ss, _stream(torch, stream, device))
+    if status:
+        _check(status)
+    return out, sum
+
+
+# -------------------------------------------------------------------------------- dense layers
+def _activation(activation):
+    if activation is None:
+        return _NONE
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise NdvmError(1, f"unknown activation {activation!r}: None or one of {', '.join(ACTIVATIONS)}")
+    return act
+
+
+def _matrix(w, name, x, k, device):
+    """(n, row stride) of a weight matrix (n, k) of x's type."""
+    if w.dim() != 2 or w.shape[1] != k:
+        raise NdvmError(1, f"{name} must be an (n, {k}) matrix")
+    if w.dtype != x.dtype:
+        raise NdvmError(1, f"x and {name} must have the same dtype")
+    _same_device(device, w, name)
+    return w.shape[0], _rows(w, name)[2]
+
+
+def _ready(pointer, stride, rows, cols):
+    """Whether the products can read a matrix of 16-bit elements where it lies."""
+    return pointer % 16 == 0 and (rows <= 1 or (stride % 8 == 0 and stride >= cols))
+
+
+def linear_kept(x, w, keep=None, stream=None):
+    """What linear_forward's `kept` takes: float32 [rows, stride], a row's first n elements in use, or with keep="8bit" a
+    Quantized [rows, n]."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    rows, n, device = _rows(x, "x")[0], w.shape[0], _device(torch, x)
+    if keep == "8bit":
+        return _new_quantized(torch, (rows, n), rows, n, device, stream)
+    if keep is not None:
+        raise NdvmError(1, f"unknown keep {keep!r}: None or '8bit'")
+    return _new(torch, (rows, lib.ndvm_linear_kept_stride(n)), torch.float32, device, stream)
+
+
+def _linear_kept(torch, lib, kept, rows, n, device):
+    """(z, z_values, z_scales) of linear_kept's tensor."""
+    if kept is None:
+        return None, None, None
+    if isinstance(kept, Quantized):
+        _given_quantized(kept, "kept", (rows, n), device)
+        if rows > 1 and kept.stride != -(-n // 16) * 16:
+            raise NdvmError(1, "kept must be one of linear_kept")
+        return None, kept.values.data_ptr(), kept.scales.data_ptr()
+    _given(kept, "kept", (rows, lib.ndvm_linear_kept_stride(n)), torch.float32, device)
+    if not kept.is_contiguous():
+        raise NdvmError(1, "kept must be contiguous")
+    return kept.data_ptr(), None, None
+
+
+def linear_forward(x, w, bias=None, activation=None, residual=None, y=None, kept=None, workspace=None, stream=None):
+    """y = act(x w^T + bias) + residual: x (..., k), w (n, k), bias (n) of x's type or float32, y and residual (..., n);
+    16-bit types.  kept: a tensor of linear_kept that receives x w^T + bias for linear_backward.  y may be residual.
+    Outputs and the workspace that this call allocates belong to `stream`."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, x)
+    code = _type(x, "x")
+    act = _activation(activation)
+    rows, k, xs = _rows(x, "x")
+    n, ws_ = _matrix(w, "w", x, k, device)
+    shape = x.shape[:-1] + (n,)
+    if y is None:
+        y, ys = _new(torch, shape, x.dtype, device, stream), n
+    else:
+        _given(y, "y", shape, x.dtype, device)
+        ys = _rows(y, "y")[2]
+    rp, rs = _like(residual, "residual", y, device)
+    need = lib.ndvm_linear_workspace_bytes(act, rows, k, n, 0, int(_ready(x.data_ptr(), xs, rows, k) and _ready(w.data_ptr(), ws_, n, k)), 0)
+    ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
+    status = lib.ndvm_linear_forward(code, _weight_type(code, None, bias), act, rows, k, n, x.data_ptr(), xs, w.data_ptr(), ws_,
+                                     _vector(bias, "bias", n, device), rp, rs, y.data_ptr(), ys,
+                                     *_linear_kept(torch, lib, kept, rows, n, device), wp, nbytes, _stream(torch, stream, device))
+    if status:
+        _check(status)
+    return y
+
+
+def linear_backward(dy, x, w, activation=None, wants=(True, True, True), dx=None, dw=None, dbias=None, btype=None, kept=None,
+                    workspace=None, stream=None):
+    """(dx, dw, dbias) of linear_forward; `wants` says which (the others are None; the residual's gradient is dy itself).
+    x: as the forward call had it, or a Quantized of it.  kept: what the forward call kept (needed with an activation).
+    dbias has dtype `btype` (x's by default)."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    device = _device(torch, w)
+    code = _type(w, "w")
+    act = _activation(activation)
+    held = isinstance(x, Quantized)
+    if held:
+        _same_device(device, x.values, "x")
+        rows, k, xs, xp = x.rows, x.cols, 0, None
+        n, ws_ = _matrix(w, "w", w, k, device)
+    else:
+        _same_device(device, x, "x")
+        rows, k, xs = _rows(x, "x")
+        n, ws_ = _matrix(w, "w", x, k, device)
+        xp = x.data_ptr()
+    _given(dy, "dy", x.shape[:-1] + (n,), w.dtype, device)
+    dys = _rows(dy, "dy")[2]
+    bdtype = btype or w.dtype
+    if dx is None and wants[0]:
+        dx = _new(torch, x.shape, w.dtype, device, stream)
+    if dw is None and wants[1]:
+        dw = _new(torch, (n, k), w.dtype, device, stream)
+    if dbias is None and wants[2]:
+        dbias = _new(torch, (n,), bdtype, device, stream)
+    dxp = dxs = dwp = dbp = None
+    if dx is not None:
+        _given(dx, "dx", x.shape, w.dtype, device)
+        dxp, dxs = dx.data_ptr(), _rows(dx, "dx")[2]
+    if dw is not None:
+        _given(dw, "dw", (n, k), w.dtype, device)
+        if not dw.is_contiguous():
+            raise NdvmError(1, "dw must be contiguous")
+        dwp = dw.data_ptr()
+    if dbias is not None:
+        _given(dbias, "dbias", (n,), bdtype, device)
+        dbp = _vector(dbias, "dbias", n, device)
+    ready = (held or _ready(xp, xs, rows, k)) and _ready(w.data_ptr(), ws_, n, k) and _ready(dy.data_ptr(), dys, rows, n)
+    need = lib.ndvm_linear_workspace_bytes(act, rows, k, n, 1, int(ready), int(held))
+    ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
+    status = lib.ndvm_linear_backward(code, _weight_type(code, None, dbias), act, rows, k, n, dy.data_ptr(), dys, xp, xs,
+                                      x.values.data_ptr() if held else None, x.stride if held else 0,
+                                      x.scales.data_ptr() if held else None, w.data_ptr(), ws_,
+                                      *_linear_kept(torch, lib, kept, rows, n, device), dxp, dxs or 0, dwp, dbp, wp, nbytes,
+                                      _stream(torch, stream, device))
+    if status:
+        _check(status)
+    return dx, dw, dbias
+
+
+def linear_quantized_forward(x, w, bias=None, activation=None, residual=None, dtype=None, y=None, workspace=None, stream=None):
+    """linear_forward of x (..., k) and w (n, k) in 8-bit blocks (Quantized).  dtype: of y and residual, bfloat16 (the
+    default where neither is given) or float16; bias of that type or float32."""
+    torch = _torch_module or _start()
+    lib = _nd._lib or load()
+    if not isinstance(x, Quantized) or not isinstance(w, Quantized):
+        raise NdvmError(1, "x and w must be Quantized")
+    device = _device(torch, x.values)
+    act = _activation(activation)
+    if len(w.shape) != 2 or w.cols != x.cols:
+        raise NdvmError(1, f"w must be an (n, {x.cols}) matrix")
+    _same_device(device, w.values, "w")
+    shape = x.shape[:-1] + (w.rows,)
+    if y is None:
+        y, ys = _new(torch, shape, dtype or (torch.bfloat16 if residual is None else residual.dtype), device, stream), w.rows
+    else:
+        _given(y, "y", shape, dtype or y.dtype, device)
+        ys = _rows(y, "y")[2]
+    code = _type(y, "y")
+    rp, rs = _like(residual, "residual", y, device)
+    need = lib.ndvm_linear_quantized_workspace_bytes(x.rows, x.cols, w.rows)
+    ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
+    status = lib.ndvm_linear_quantized(code, _weight_type(code, None, bias), act, x.rows, x.cols, w.rows, x.values.data_ptr(), x.stride,
+                                       x.scales.data_ptr(), w.values.data_ptr(), w.stride, w.scales.data_ptr(),
+                                       _vector(bias, "bias", w.rows, device), rp, rs, y.data_ptr(), ys, wp, nbytes,
+                                       _stream(torch, stream, device))
+    if status:
+        _check(status)
+    return y
+
+
 # ----------------------------------------------------------------------- differentiable ops
 _ops = None
 
@@ -424,6 +791,71 @@ def gated(x, w_gate, w_up, activation="silu", keep=None):
     except TypeError:
         y = None
     return _refuse(gated_forward, x, w_gate, w_up, activation) if y is None else y
+
+
+def rms_norm(x, weight=None, eps=1e-6, residual=None):
+    """s / sqrt(mean(s^2) + eps) * weight over the last dimension as a differentiable op, s = x.  With a residual, s = x +
+    residual rounded to their type, and the result is (y, s)."""
+    try:
+        y = (_ops or _load_ops()).rms_norm(x, weight, eps, residual)
+    except TypeError:
+        y = None
+    if y is None:
+        _refuse(rms_norm_forward, x, weight, eps, residual)
+    return y[0] if residual is None else tuple(y)
+
+
+def linear(x, w, bias=None, activation=None, residual=None, keep=None):
+    """act(x w^T + bias) + residual as a differentiable op (gradients of all four; 16-bit types, bias also float32).
+    With an activation, x w^T + bias is held for the backward pass as float32.  keep="8bit": it and x are held as
+    8-bit blocks instead (a bit over a byte an element each), and the gradients are those at what the blocks stand for."""
+    if keep is not None and keep != "8bit":
+        raise NdvmError(1, f"unknown keep {keep!r}: None or '8bit'")
+    act = _activation(activation)
+    try:
+        y = (_ops or _load_ops()).linear(x, w, bias, act, residual, keep is not None)
+    except TypeError:
+        y = None
+    return _refuse(linear_forward, x, w, bias, activation, residual) if y is None else y
+
+
+def quantize(x):
+    """8-bit blocks of x (..., cols), a Quantized: float32, float16, bfloat16, rows of any layout.  Has no gradient: raises
+    where one would be recorded."""
+    try:
+        q = (_ops or _load_ops()).quantize(x)
+    except TypeError:
+        q = None
+    return _refuse(quantize_forward, x) if q is None else Quantized._of(*q)
+
+
+def rms_norm_quantized(x, weight=None, eps=1e-6, residual=None):
+    """rms_norm whose y is a Quantized, made of what is not rounded in between; with a residual (y, s).  Has no gradient:
+    raises where one would be recorded."""
+    try:
+        q = (_ops or _load_ops()).rms_norm_quantized(x, weight, eps, residual)
+    except TypeError:
+        q = None
+    if q is None:
+        _refuse(rms_norm_quantized_forward, x, weight, eps, residual)
+    y = Quantized._of(*q[:5])
+    return y if residual is None else (y, q[5])
+
+
+def linear_quantized(x, w, bias=None, activation=None, residual=None, dtype=None):
+    """act(x w^T + bias) + residual of x (..., k) and w (n, k) in 8-bit blocks (Quantized), in dtype: bfloat16 or float16
+    (the residual's, or bfloat16, by default).  Has no gradient: raises where one would be recorded."""
+    act = _activation(activation)
+    y = None
+    if isinstance(x, Quantized) and isinstance(w, Quantized):
+        if dtype is None:
+            dtype = (_torch_module or _start()).bfloat16 if residual is None else residual.dtype
+        try:
+            y = (_ops or _load_ops()).linear_quantized(x.values, x.scales, x.rows, x.cols, x.stride, w.values, w.scales, w.rows, w.cols, w.stride,
+                                                       bias, act, residual, _types.get(dtype, 0))
+        except TypeError:
+            y = None
+    return _refuse(linear_quantized_forward, x, w, bias, activation, residual, dtype) if y is None else y
 
 
 def check_operators():
