@@ -58,6 +58,40 @@ __device__ __forceinline__ void activate(float2 g, float2* a, float2* da) {
     *da = kAct == NDVM_ACT_SILU ? fma(*a, rest, s) : mul(s, rest);
   }
 }
+// act(g) alone, as it is stored in 16 bits: fewer instructions than activate(), which the epilogue of a product counts.  Tails
+// keep their relative accuracy down to binary32's smallest here too (a power of two is the square of half the power's, which
+// is never flushed before the result is 0), and nothing is chosen by the sign where a maximum can do it.
+__device__ __forceinline__ float power2_normal(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <int kAct>
+__device__ __forceinline__ float2 activation(float2 g) {
+  if constexpr (kAct == NDVM_ACT_NONE) {
+    return g;
+  } else if constexpr (kAct == NDVM_ACT_RELU) {
+    return make_float2(g.x < 0.0f ? 0.0f : g.x, g.y < 0.0f ? 0.0f : g.y);  // (a NaN stays one)
+  } else if constexpr (kAct == NDVM_ACT_GELU) {
+    // max(g, 0) - |g| cdf(-|g|), the tail as in activate(); from |g| = 40 on it is 0
+    const float2 half = mul(mul(g, g), make_float2(-0.36067376f, -0.36067376f));
+    const float2 h = make_float2(power2_normal(half.x), power2_normal(half.y)), e = mul(h, h);
+    const float2 p = make_float2(fminf(fabsf(g.x), 40.0f), fminf(fabsf(g.y), 40.0f));
+    const float2 t = make_float2(reciprocal(fmaf(p.x, 0.35f, 1.0f)), reciprocal(fmaf(p.y, 0.35f, 1.0f)));
+    constexpr float kQ[9] = {0.139621258f, 0.139864326f,  0.119815566f, 0.105574533f,   -0.0232631564f,
+                             0.15939188f,  -0.255900919f, 0.144060329f, -0.0291638281f};
+    float2 tail = make_float2(kQ[8], kQ[8]);
+#pragma unroll
+    for (int i = 7; i >= 0; i--) tail = fma(tail, t, make_float2(kQ[i], kQ[i]));
+    tail = mul(mul(e, t), tail);
+    return make_float2(fmaf(-p.x, tail.x, fmaxf(g.x, 0.0f)), fmaf(-p.y, tail.y, fmaxf(g.y, 0.0f)));
+  } else {
+    const float2 h = make_float2(power2_normal(fabsf(g.x) * -0.72134752f), power2_normal(fabsf(g.y) * -0.72134752f)), e = mul(h, h);
+    const float2 d = add(e, make_float2(1.0f, 1.0f)), r = make_float2(reciprocal(d.x), reciprocal(d.y));
+    const float2 s = mul(r, make_float2(g.x < 0.0f ? e.x : 1.0f, g.y < 0.0f ? e.y : 1.0f));
+    return kAct == NDVM_ACT_SILU ? mul(g, s) : s;
+  }
+}
 // f(activation as a constant): one branch around a loop over many elements, not one in each
 template <typename F>
 __device__ __forceinline__ void by_activation(int act, F&& f) {

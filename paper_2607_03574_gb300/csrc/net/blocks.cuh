@@ -19,6 +19,11 @@ __host__ __device__ __forceinline__ int64_t scale_at(int64_t row, int64_t block,
 
 // The bits of |v|: they order as the values do, infinities and NaNs above all.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+__device__ __forceinline__ float larger(float a, float b) {  // of the sizes; a NaN wins
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return m;
+}
 // The scale of a block whose largest magnitude is `most`: with |v| = (1 + f) 2^x, 448 2^e = 1.75 2^(8 + e) is not below it
 // from e = x - 8 on, or x - 7 if 1 + f > 1.75.
 __device__ __forceinline__ uint32_t block_code(uint32_t most) {

@@ -22,19 +22,21 @@ namespace {
 __device__ int g_linear_stopped;  // a wait in k_linear ran out (ndvm_check_operators)
 
 // ---------------------------------------------------------------------------------- the product
-constexpr int kReaders = 8;                   // warps that read the sums: two for each quarter of a tile's rows
-constexpr int kThreads = 64 + 32 * kReaders;  // and one that loads, one that multiplies
+// Warps that read the sums: four (in 8 bits, whose tiles have at most 192 columns, three) for each quarter of a tile's rows, which
+// share its columns.
+template <bool kEight> constexpr int kReaders = kEight ? 12 : 16;
+template <bool kEight> constexpr int kThreads = 64 + 32 * kReaders<kEight>;  // and one that loads, one that multiplies
+constexpr int kRoom = 4096;                   // bytes of each: what its stores are made from
 constexpr int kLine = 128;                    // bytes of a row in a step: 64 elements of the contraction, or 128 in 8 bits
 
 template <int kN, int kCtas> constexpr int kTileBytes = (kM + kN / kCtas) * kLine;
 // scales of a step, in 8 bits: 128 rows' of A, and those of the one or two 128s of rows that B's lie in
 template <int kN> constexpr int kScaleTiles = kN > 128 ? 2 : 1;
 template <bool kEight, int kN> constexpr int kScaleBytes = kEight ? 512 * (1 + kScaleTiles<kN>) : 0;
-template <int kCtas> constexpr int kRoom = 4096 * kCtas;  // of each warp that reads sums: what its stores are made from
 template <bool kEight, int kN, int kCtas>
-constexpr int kSteps = std::min(8, (229376 - kReaders * kRoom<kCtas>) / (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>));
+constexpr int kSteps = std::min(8, (229376 - kReaders<kEight> * kRoom) / (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>));
 template <bool kEight, int kN, int kCtas>
-constexpr int kShared = kSteps<kEight, kN, kCtas> * (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>) + kReaders * kRoom<kCtas> +
+constexpr int kShared = kSteps<kEight, kN, kCtas> * (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>) + kReaders<kEight> * kRoom +
                         1024 /* alignment */ + 256 /* barriers */;
 // of tensor memory: two tiles' sums, and two steps' scales
 template <bool kEight, int kN> constexpr int kColumns = !kEight ? 2 * kN : kN == 64 ? 256 : 512;
@@ -51,7 +53,8 @@ struct ForwardArgs {
   int act, keep;
   int a_box;                        // rows of A that a tile loads (fewer than 128 where the result has fewer)
   int copies;                       // y is stored by copies (its rows start on 16 bytes)
-  int wide;                         // the residual's rows start on 16 bytes
+  int wide, bias_wide;              // the residual's rows, and the bias, start on 16 bytes
+  uint32_t band_magic, band_shift;  // i / (a band's tiles) = (i * magic) >> (32 + shift)
   const void* bias; int bias_f32;
   const void* residual; int64_t r_stride;
   void* out; int64_t stride;
@@ -84,10 +87,10 @@ __device__ __forceinline__ void stage_floats(uint32_t buffer, int lane, const fl
 
 // A block of a row (values beyond its end are 0) to e4m3, `room` (16 or 32) bytes of which are the row's
 __device__ __forceinline__ void keep_block(const float (&v)[32], uint8_t* values, int room, uint8_t* scale) {
-  uint32_t most = 0;
+  float most[4] = {};
 #pragma unroll
-  for (int e = 0; e < 32; e++) most = max(most, magnitude(v[e]));
-  const uint32_t code = block_code(most);
+  for (int e = 0; e < 32; e++) most[e % 4] = larger(most[e % 4], v[e]);
+  const uint32_t code = block_code(__float_as_uint(larger(larger(most[0], most[1]), larger(most[2], most[3]))));
   const float inverse = block_inverse(code);
   uint32_t q[8];
 #pragma unroll
@@ -97,18 +100,58 @@ __device__ __forceinline__ void keep_block(const float (&v)[32], uint8_t* values
   *scale = (uint8_t)code;
 }
 
+// 32 consecutive values of a row from memory, `count` of which there are; wide: they start on 16 bytes
+template <typename T>
+__device__ __forceinline__ void load32(Pack<T, 8> (&v)[4], const T* from, int count, bool wide) {
+  if (wide && count >= 32) {
+#pragma unroll
+    for (int q = 0; q < 4; q++) v[q] = load_pack<T, 8>(from + 8 * q);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; e++)
+      if (e < count) v[e / 8].v[e % 8] = from[e];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void add32(float (&v)[32], const Pack<T, 8> (&a)[4]) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 2) {
+    const float2 s = add(make_float2(v[e], v[e + 1]), widen(a[e / 8].v + e % 8));
+    v[e] = s.x, v[e + 1] = s.y;
+  }
+}
+// the same 32 values for every lane (a broadcast from L1)
+template <typename T>
+__device__ __forceinline__ void add_bias(float (&v)[32], const void* bias, int f32, int col, int count, bool wide) {
+  if (f32 && wide && count >= 32) {
+#pragma unroll
+    for (int q = 0; q < 8; q++) {
+      const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(bias) + col + 4 * q);
+      const float2 s = add(make_float2(v[4 * q], v[4 * q + 1]), make_float2(b.x, b.y)), t = add(make_float2(v[4 * q + 2], v[4 * q + 3]), make_float2(b.z, b.w));
+      v[4 * q] = s.x, v[4 * q + 1] = s.y, v[4 * q + 2] = t.x, v[4 * q + 3] = t.y;
+    }
+  } else if (f32) {
+#pragma unroll
+    for (int e = 0; e < 32; e++)
+      if (e < count) v[e] += static_cast<const float*>(bias)[col + e];
+  } else {
+    Pack<T, 8> b[4] = {};
+    load32<T>(b, static_cast<const T*>(bias) + col, count, wide);
+    add32<T>(v, b);
+  }
+}
+
 // One thread loads, one issues the products, eight warps read the sums of a tile while the next one's are made.  A block has
 // kN columns of sums for its 128 rows; a pair's blocks (kCtas = 2) hold half of those rows of B each.
 template <typename T, bool kEight, int kN, int kCtas>
-__global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ ForwardArgs p) {
+__global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_constant__ ForwardArgs p) {
   extern __shared__ char raw[];
   constexpr int S = kSteps<kEight, kN, kCtas>, kTile = kTileBytes<kN, kCtas>, kScales = kScaleBytes<kEight, kN>;
-  constexpr int kABytes = kM * kLine, kElements = kEight ? 128 : 64;  // of the contraction a step
+  constexpr int kABytes = kM * kLine, kElements = kEight ? 128 : 64, R = kReaders<kEight>;  // (of the contraction a step)
   __shared__ uint32_t s_tmem;
   __shared__ int s_stop;
-  __shared__ __align__(16) float s_bias[kReaders][32];
   const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
-  const uint32_t staging = base + S * kTile, scales = staging + kReaders * kRoom<kCtas>, bars = scales + S * kScales;
+  const uint32_t staging = base + S * kTile, scales = staging + R * kRoom, bars = scales + S * kScales;
   const auto full = [&](int i) { return bars + i * 8; };
   const auto empty = [&](int i) { return bars + (S + i) * 8; };
   const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
@@ -121,7 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
   if (threadIdx.x == 0) {
     s_stop = 0;
     for (int i = 0; i < S; i++) tc::barrier_init(full(i), 1), tc::barrier_init(empty(i), 1);
-    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), kReaders * kCtas);
+    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), R * kCtas);
     tc::barrier_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -138,12 +181,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
   // tiles in bands of 2048 rows, down a band first: blocks that run together share operands in L2
   const auto item = [&](int i) {
     Item it;
-    it.split = i / tiles;
+    it.split = p.splits > 1 ? i / tiles : 0;
     i -= it.split * tiles;
-    const int band = i / (kBand * p.tiles_n), first = band * kBand, height = min(kBand, p.tiles_m - first);
+    const int band = (int)((uint64_t)i * p.band_magic >> 32 >> p.band_shift), first = band * kBand, height = min(kBand, p.tiles_m - first);
     i -= band * kBand * p.tiles_n;
-    it.m0 = ((first + i % height) * kCtas + rank) * kM;
-    it.n0 = i / height * kN;
+    const int across = height == kBand ? i / kBand : i / height;
+    it.m0 = ((first + i - across * height) * kCtas + rank) * kM;
+    it.n0 = across * kN;
+    if (p.splits == 1) {
+      it.from = 0, it.to = p.steps;
+      return it;
+    }
     it.from = (int)((int64_t)p.steps * it.split / p.splits);
     it.to = (int)((int64_t)p.steps * (it.split + 1) / p.splits);
     return it;
@@ -224,29 +272,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
       tc::barrier_drain(drain, 0);
     }
   } else if (warp >= 2) {
-    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, every other 32 columns: a block
-    // of 32 columns of one row a thread.  Bias and residual are asked for a piece ahead.
+    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, and 32 columns at a time: a block
+    // of one row a thread.  The residual is asked for a piece ahead.  (What these warps do for each other is hide the waits between
+    // their instructions: 16384 x 256 -> 8192 took 120 us with eight of them, 147 with a bias in shared memory.)
     const int lanes = (warp % 4) * 32, reader = warp - 2, first = reader / 4 * 32;
-    const uint32_t mine = staging + reader * kRoom<kCtas>;
+    constexpr int kNext = R / 4 * 32;
+    const uint32_t mine = staging + reader * kRoom;
     const char* const mine_ptr = raw + (mine - tc::smem(raw));
-    const bool sums = p.splits > 1;
+    const bool sums = p.splits > 1, floats = !sums && p.keep == kFloats;
     int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
-    float next_bias = 0.0f;
     Pack<T, 8> next[4];
     const auto ask = [&](int row, int col) {
-      if (sums || col >= p.n) return;
-      if (col + lane < p.n) next_bias = bias_at<T>(p.bias, p.bias_f32, col + lane);
-      if (!p.residual || row >= p.m) return;
-      const T* from = static_cast<const T*>(p.residual) + row * p.r_stride + col;
-      if (p.wide && col + 32 <= p.n) {
-#pragma unroll
-        for (int q = 0; q < 4; q++) next[q] = load_pack<T, 8>(from + 8 * q);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 32; e++)
-          if (col + e < p.n) next[e / 8].v[e % 8] = from[e];
-      }
+      if (p.residual && !sums && col < p.n && row < p.m)
+        load32<T>(next, static_cast<const T*>(p.residual) + row * p.r_stride + col, p.n - col, p.wide);
     };
     for (int i = unit; i < items; i += units) {
       const Item it = item(i);
@@ -257,47 +296,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
       tc::fence_after();
       const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
 #pragma unroll 1
-      for (int j = first; j < kN; j += 64) {
+      for (int j = first; j < kN; j += kNext) {
         const int col = it.n0 + j, count = min(32, p.n - col);
         if (count <= 0) break;
         float v[32];
         tc::tmem_load32(v, at + j);
-        Pack<T, 8> residual[4];
-        if (!sums) {
-          s_bias[reader][lane] = next_bias;
-#pragma unroll
-          for (int q = 0; q < 4; q++) residual[q] = next[q];
-          if (j + 64 < kN) ask(row, col + 64);
-          __syncwarp();
+        // binary32 takes the staging whole, y half of it by turns
+        const uint32_t to = mine + (sums || floats ? 0 : (buffer++ & 1) * 2048);
+        if (lane == 0) {
+          if (sums || floats) tc::stores_read<0>();
+          else tc::stores_read<1>();
         }
+        __syncwarp();
         tc::tmem_loaded(v);
         if (sums) {
-          if (lane == 0) tc::stores_read<kCtas - 1>();
-          __syncwarp();
-          const uint32_t to = mine + (kCtas == 2 ? (buffer & 1) * 4096 : 0);
           stage_floats(to, lane, v);
           tc::fence_async();
           __syncwarp();
           if (lane == 0 && row0 < p.m) tc::store_box(&p.o, col, row0, it.split, to);
           if (lane == 0) tc::stores_commit();
-          buffer++;
           continue;
         }
-        if (p.bias) {
-#pragma unroll
-          for (int q = 0; q < 8; q++) {
-            const float4 b = *reinterpret_cast<const float4*>(&s_bias[reader][4 * q]);
-            v[4 * q] += b.x, v[4 * q + 1] += b.y, v[4 * q + 2] += b.z, v[4 * q + 3] += b.w;
-          }
-        }
-        // The staging takes z and then y, one after the other in a block alone (kRoom 4096), side by side in a pair's.
-        const bool floats = p.keep == kFloats;
+        if (p.bias) add_bias<T>(v, p.bias, p.bias_f32, col, count, p.bias_wide);
         if (floats) {
-          if (lane == 0) {
-            if (kCtas == 2) tc::stores_read<1>();  // (the last piece's y may be under way)
-            else tc::stores_read<0>();
-          }
-          __syncwarp();
           stage_floats(mine, lane, v);
           tc::fence_async();
           __syncwarp();
@@ -315,27 +336,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
         by_activation_or_none(p.act, [&](auto act) {
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            float2 a, da;
-            activate<decltype(act)::value>(make_float2(v[e], v[e + 1]), &a, &da);
+            const float2 a = activation<decltype(act)::value>(make_float2(v[e], v[e + 1]));
             v[e] = a.x, v[e + 1] = a.y;
           }
         });
         if (p.residual) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const float2 r = widen(residual[e / 8].v + e % 8);
-            v[e] += r.x, v[e + 1] += r.y;
-          }
+          add32<T>(v, next);
+          if (j + kNext < kN) ask(row, col + kNext);
         }
-        // y: 2048 bytes of the staging by turns
-        constexpr int kTurns = kRoom<kCtas> / 2048;
-        const uint32_t to = mine + (!floats ? buffer % kTurns * 2048 : kCtas == 2 ? 4096 + buffer % 2 * 2048 : 0);
-        if (lane == 0) {
-          if (!floats) tc::stores_read<kTurns - 1>();
-          else if (kCtas == 1) tc::stores_read<0>();
-          else tc::stores_read<2>();  // (z, the last piece's y)
+        if (floats) {
+          if (lane == 0) tc::stores_read<0>();
+          __syncwarp();
         }
-        __syncwarp();
         stage_narrow<T>(to, lane, v);
         if (p.copies) {
           tc::fence_async();
@@ -350,7 +362,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
             if (lane < count) out[r * p.stride + lane] = *reinterpret_cast<const T*>(from + r * 64 + ((lane / 8 ^ (r >> 1 & 3)) << 4) + lane % 8 * 2);
         }
         if (lane == 0) tc::stores_commit();
-        buffer++;
       }
       tc::fence_before();
       __syncwarp();
@@ -399,8 +410,7 @@ __global__ void __launch_bounds__(256) k_finish(const float* partial, int64_t pi
     by_activation_or_none(a.act, [&](auto act) {
 #pragma unroll
       for (int e = 0; e < 4; e += 2) {
-        float2 o, d;
-        activate<decltype(act)::value>(make_float2(v[e], v[e + 1]), &o, &d);
+        const float2 o = activation<decltype(act)::value>(make_float2(v[e], v[e + 1]));
         v[e] = o.x, v[e + 1] = o.y;
       }
     });
@@ -454,8 +464,7 @@ __global__ void __launch_bounds__(128) k_linear_one(LinearArgs a) {
     z += bias_at<T>(a.bias, a.bias_f32, j);
     if (a.z) a.z[j] = z;
     by_activation_or_none(a.act, [&](auto k) {
-      float2 act, da;
-      activate<decltype(k)::value>(make_float2(z, z), &act, &da);
+      const float2 act = activation<decltype(k)::value>(make_float2(z, z));
       const float r = a.residual ? to_f32(static_cast<const T*>(a.residual)[j]) : 0.0f;
       static_cast<T*>(a.y)[j] = from_f32<T>(act.x + r);
     });
@@ -609,7 +618,7 @@ cudaError_t launch_shape(const ForwardArgs& p, cudaStream_t s) {
   }
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)std::min(p.tiles_m * p.tiles_n * p.splits, kSms / kCtas) * kCtas);
-  c.blockDim = dim3(kThreads);
+  c.blockDim = dim3(kThreads<kEight>);
   c.dynamicSmemBytes = kShared<kEight, kN, kCtas>;
   c.stream = s;
   cudaLaunchAttribute cluster{};
@@ -637,6 +646,11 @@ cudaError_t product(const LinearArgs& a, const Cut& k, float* partial, cudaStrea
   p.bias = a.bias; p.bias_f32 = a.bias_f32;
   p.residual = a.residual; p.r_stride = a.r_stride;
   p.wide = a.residual && tma_ready(a.residual, a.r_stride, a.rows, 0);
+  p.bias_wide = reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
+  // floor(2^(32 + shift) / d) + 1 with 2^shift < d <= 2^(shift + 1): over by less than i / 2^(32 + shift), below 1 / d for i below 2^31
+  const uint32_t band = (uint32_t)(16 / k.ctas * p.tiles_n);
+  while (((uint64_t)2 << p.band_shift) < band) p.band_shift++;
+  p.band_magic = (uint32_t)(((uint64_t)1 << (32 + p.band_shift)) / band + 1);
   p.out = a.y; p.stride = a.y_stride;
   p.z_values = a.z_values; p.z_pitch = a.z_pitch; p.z_scales = a.z_scales;
   bool ok = true;
