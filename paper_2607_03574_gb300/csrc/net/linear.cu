@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
   const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
   const auto taken = [&](int i) { return bars + (2 * S + 2 + i) * 8; };  // and have been read
   const uint32_t drain = bars + (2 * S + 4) * 8;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(~0u, threadIdx.x / 32, 0), lane = threadIdx.x % 32;  // (the same for all of a warp, as the compiler sees)
   const int rank = kCtas == 1 ? 0 : (int)tc::cluster_rank(), unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
   volatile int* stop = &s_stop;
 
@@ -197,7 +197,9 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
     return it;
   };
 
-  if (warp == 0 && lane == 0) {
+  // (the whole warp waits, and goes on or gives up)
+  const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(~0u, tc::barrier_wait(bar, parity, stop)) != 0; };
+  if (warp == 0) {
     // ---- loads
     int stage = 0;
     uint32_t phase = 0;
@@ -207,16 +209,19 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
     for (int i = unit; ok && i < items; i += units) {
       const Item it = item(i);
       for (int s = it.from; s < it.to; s++) {
-        if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, stop))) break;
-        const uint32_t at = base + stage * kTile, bar = kCtas == 1 ? full(stage) : tc::in_first(full(stage));
-        if (rank == 0) tc::barrier_expect(full(stage), kCtas * bytes);
-        tc::load_box<kCtas>(at, &p.a, s * kElements, it.m0, bar);
-        tc::load_box<kCtas>(at + kABytes, &p.b, s * kElements, it.n0 + rank * (kN / kCtas), bar);
-        if constexpr (kEight) {  // (scales behind the last row of either are filled with 0; a pair's blocks both hold all of B's)
-          const uint32_t to = scales + stage * kScales;
-          tc::load_box<kCtas>(to, &p.a_scales, 0, s, it.m0 / 128, bar);
-          tc::load_box<kCtas>(to + 512, &p.b_scales, 0, s, it.n0 / 128, bar);
+        if (!(ok = wait(empty(stage), phase ^ 1))) break;
+        if (tc::elect()) {
+          const uint32_t at = base + stage * kTile, bar = kCtas == 1 ? full(stage) : tc::in_first(full(stage));
+          if (rank == 0) tc::barrier_expect(full(stage), kCtas * bytes);
+          tc::load_box<kCtas>(at, &p.a, s * kElements, it.m0, bar);
+          tc::load_box<kCtas>(at + kABytes, &p.b, s * kElements, it.n0 + rank * (kN / kCtas), bar);
+          if constexpr (kEight) {  // (scales behind the last row of either are filled with 0; a pair's blocks both hold all of B's)
+            const uint32_t to = scales + stage * kScales;
+            tc::load_box<kCtas>(to, &p.a_scales, 0, s, it.m0 / 128, bar);
+            tc::load_box<kCtas>(to + 512, &p.b_scales, 0, s, it.n0 / 128, bar);
+          }
         }
+        __syncwarp();
         issued++;
         if (++stage == S) stage = 0, phase ^= 1;
       }
@@ -225,10 +230,10 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
     // the other block too); if the launch gives up, until its copies have landed (a pair's second waits for its first).
     for (int k = min(issued, S); k >= 1; k--) {
       const int at = (issued - k) % S, turn = (issued - k) / S;
-      if (ok) ok = tc::barrier_wait(empty(at), turn & 1, stop);
+      if (ok) ok = wait(empty(at), turn & 1);
       if (!ok && rank == 0) tc::barrier_drain(full(at), turn & 1);
     }
-  } else if (warp == 1 && lane == 0 && rank == 0) {
+  } else if (warp == 1 && rank == 0) {
     // ---- products
     constexpr uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, false, false, kM * kCtas, kN);
     int stage = 0, slot = 0, turn = 0;
@@ -236,39 +241,43 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
     bool ok = true;
     for (int i = unit; ok && i < items; i += units) {
       const Item it = item(i);
-      if (!(ok = tc::barrier_wait(taken(slot), slot_phase ^ 1, stop))) break;
+      if (!(ok = wait(taken(slot), slot_phase ^ 1))) break;
       tc::fence_after();
       for (int s = it.from; s < it.to; s++) {
-        if (!(ok = tc::barrier_wait(full(stage), phase, stop))) break;
+        if (!(ok = wait(full(stage), phase))) break;
         tc::fence_after();
-        const uint32_t at = base + stage * kTile;
-        const uint64_t a = tc::operand(at, false), b = tc::operand(at + kABytes, false);
-        if constexpr (kEight) {
-          // scales to tensor memory, two steps' by turns; B's columns begin in the middle of a 128 where its tile does
-          const uint32_t from = scales + stage * kScales, to = tmem + 2 * kN + turn * 16;
-          tc::copy_scales<kCtas>(to, from);
+        if (tc::elect()) {
+          const uint32_t at = base + stage * kTile;
+          const uint64_t a = tc::operand(at, false), b = tc::operand(at + kABytes, false);
+          if constexpr (kEight) {
+            // scales to tensor memory, two steps' by turns; B's columns begin in the middle of a 128 where its tile does
+            const uint32_t from = scales + stage * kScales, to = tmem + 2 * kN + turn * 16, to_b = to + 4 + it.n0 % 128 / 32;
+            tc::copy_scales<kCtas>(to, from);
 #pragma unroll
-          for (int q = 0; q < kScaleTiles<kN>; q++) tc::copy_scales<kCtas>(to + 4 + 4 * q, from + 512 + 512 * q);
-          turn ^= 1;
-          const int blocks = min(4, (p.c - s * kElements + 31) / 32);  // (none behind the row's last: its scale need not be one)
+            for (int q = 0; q < kScaleTiles<kN>; q++) tc::copy_scales<kCtas>(to + 4 + 4 * q, from + 512 + 512 * q);
+            const int blocks = (p.c - s * kElements + 31) / 32;  // (none behind the row's last: its scale need not be one)
 #pragma unroll
-          for (int q = 0; q < 4; q++)
-            if (q < blocks)
-              tc::mma_blocks<kCtas>(tmem + slot * kN, a + q * (32 >> 4), b + q * (32 >> 4), tc::instruction_blocks(kM * kCtas, kN, q), to,
-                                    to + 4 + it.n0 % 128 / 32, s > it.from || q > 0);
-        } else {
+            for (int q = 0; q < 4; q++)
+              if (q < blocks)
+                tc::mma_blocks<kCtas>(tmem + slot * kN, a + q * (32 >> 4), b + q * (32 >> 4), tc::instruction_blocks(kM * kCtas, kN, q), to, to_b,
+                                      s > it.from || q > 0);
+          } else {
 #pragma unroll
-          for (int q = 0; q < 4; q++)  // 16 of the contraction: 32 bytes along a line
-            tc::mma<kCtas>(tmem + slot * kN, a + q * (32 >> 4), b + q * (32 >> 4), desc, s > it.from || q > 0);
+            for (int q = 0; q < 4; q++)  // 16 of the contraction: 32 bytes along a line
+              tc::mma<kCtas>(tmem + slot * kN, a + q * (32 >> 4), b + q * (32 >> 4), desc, s > it.from || q > 0);
+          }
+          tc::commit<kCtas>(empty(stage));
+          if (s + 1 == it.to) tc::commit<kCtas>(done(slot));
         }
-        tc::commit<kCtas>(empty(stage));
+        __syncwarp();
+        turn ^= 1;
         if (++stage == S) stage = 0, phase ^= 1;
       }
-      tc::commit<kCtas>(done(slot));
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
     if (!ok) {  // the products in flight end before tensor memory is freed
-      tc::commit<kCtas>(drain);
+      if (tc::elect()) tc::commit<kCtas>(drain);
+      __syncwarp();
       tc::barrier_drain(drain, 0);
     }
   } else if (warp >= 2) {
@@ -291,8 +300,7 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
       const Item it = item(i);
       const int row0 = it.m0 + lanes, row = row0 + lane;
       ask(row, it.n0 + first);
-      // (the whole warp goes on or gives up: reading tensor memory is a warp's instruction)
-      if (!__all_sync(~0u, tc::barrier_wait(done(slot), slot_phase, stop))) break;
+      if (!wait(done(slot), slot_phase)) break;
       tc::fence_after();
       const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
 #pragma unroll 1

@@ -74,6 +74,14 @@ __device__ __forceinline__ void barrier_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// One lane of a converged warp.  Copies, products and commits take their operands from registers that a warp shares; where the
+// compiler sees that one lane of a whole warp issues them, it computes those there (otherwise it goes over the lanes of a
+// divergent branch, operand by operand: a step of the products took 600 cycles more to issue than to run).
+__device__ __forceinline__ bool elect() {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
+  return ok != 0;
+}
 // a box of the tensor at (x, y) to shared memory; its bytes count on the barrier (which for a pair is in_first's)
 template <int kCtas>
 __device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
