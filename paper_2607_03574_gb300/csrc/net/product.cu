@@ -18,8 +18,9 @@ namespace {
 
 __device__ int g_stopped;  // a wait in k_product ran out (ndvm_check_operators)
 
-constexpr int kReaders = 8;       // warps that read the sums: two for each quarter of a tile's rows
-constexpr int kThreads = 64 + 32 * kReaders;  // and one that loads, one that multiplies
+// Warps that read the sums: two for each quarter of a tile's rows, or four where each needs little staging.
+template <Mode kMode> constexpr int kReaders = kMode == kForward || kMode == kGradient ? 8 : 16;
+template <Mode kMode> constexpr int kThreads = 64 + 32 * kReaders<kMode>;  // and one that loads, one that multiplies
 
 __host__ __device__ constexpr bool a_rows(Mode m) { return m == kWeight; }
 __host__ __device__ constexpr bool b_rows(Mode m) { return m == kInput || m == kWeight; }
@@ -29,12 +30,12 @@ __host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == k
 template <int kN, int kCtas> constexpr int kStageBytes = (kM + kN / kCtas) * kC * 2;
 // Of each warp that reads sums: what its stores are made from (twice as much for a block alone would cost it a stage:
 // 16384 x 512 -> 2048 forward 54 -> 58 us), and two pieces of dh that it has asked for.
-template <Mode kMode, int kCtas> constexpr int kStaging = kMode == kGradient ? 4096 : 4096 * kCtas;
+template <Mode kMode, int kCtas> constexpr int kStaging = kMode == kForward ? 4096 * kCtas : 4096;
 template <Mode kMode> constexpr int kAsked = kMode == kGradient ? 4096 : 0;
 template <Mode kMode, int kN, int kCtas>
-constexpr int kStages = std::min(8, (229376 - kReaders * (kStaging<kMode, kCtas> + kAsked<kMode>)) / kStageBytes<kN, kCtas>);
+constexpr int kStages = std::min(8, (229376 - kReaders<kMode> * (kStaging<kMode, kCtas> + kAsked<kMode>)) / kStageBytes<kN, kCtas>);
 template <Mode kMode, int kN, int kCtas>
-constexpr int kSmem = kStages<kMode, kN, kCtas> * kStageBytes<kN, kCtas> + kReaders * (kStaging<kMode, kCtas> + kAsked<kMode>) +
+constexpr int kSmem = kStages<kMode, kN, kCtas> * kStageBytes<kN, kCtas> + kReaders<kMode> * (kStaging<kMode, kCtas> + kAsked<kMode>) +
                       1024 /* alignment */ + 384 /* barriers */;
 
 // 32 values of a row to the staging buffer, in the 64-byte swizzle (a line of 64 bytes a row: the 16-byte
@@ -65,34 +66,34 @@ __device__ __forceinline__ void unstage(const char* buffer, int lane, T* out, in
 }
 
 template <typename T, Mode kMode, int kN, int kCtas>
-__global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ ProductArgs p) {
+__global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_constant__ ProductArgs p) {
   extern __shared__ char raw[];
-  constexpr int S = kStages<kMode, kN, kCtas>, kStage = kStageBytes<kN, kCtas>;
+  constexpr int S = kStages<kMode, kN, kCtas>, kStage = kStageBytes<kN, kCtas>, R = kReaders<kMode>, kNext = R / 4 * 32;
   constexpr uint32_t kABytes = kM * kC * 2;
   constexpr int kColumns = 2 * kN;  // of tensor memory: two tiles' sums
   constexpr int kOutN = dual(kMode) ? kN / 2 : kN;
   __shared__ uint32_t s_tmem;
   __shared__ int s_stop;
   const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
-  const uint32_t staging = base + S * kStage, asked_at = staging + kReaders * kStaging<kMode, kCtas>;
-  const uint32_t bars = asked_at + kReaders * kAsked<kMode>;
+  const uint32_t staging = base + S * kStage, asked_at = staging + R * kStaging<kMode, kCtas>;
+  const uint32_t bars = asked_at + R * kAsked<kMode>;
   const auto full = [&](int i) { return bars + i * 8; };
   const auto empty = [&](int i) { return bars + (S + i) * 8; };
   const auto done = [&](int i) { return bars + (2 * S + i) * 8; };       // a tile's sums are complete
   const auto taken = [&](int i) { return bars + (2 * S + 2 + i) * 8; };  // and have been read
   const uint32_t drain = bars + (2 * S + 4) * 8;
   const auto dh_in = [&](int reader, int b) { return bars + (2 * S + 5 + 2 * reader + b) * 8; };  // a piece of dh has come
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(~0u, threadIdx.x / 32, 0), lane = threadIdx.x % 32;  // (the same for all of a warp, as the compiler sees)
   const int rank = kCtas == 1 ? 0 : (int)tc::cluster_rank(), unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
   volatile int* stop = &s_stop;
 
   if (threadIdx.x == 0) {
     s_stop = 0;
     for (int i = 0; i < S; i++) tc::barrier_init(full(i), 1), tc::barrier_init(empty(i), 1);
-    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), kReaders * kCtas);
+    for (int i = 0; i < 2; i++) tc::barrier_init(done(i), 1), tc::barrier_init(taken(i), R * kCtas);
     tc::barrier_init(drain, 1);
     if (kMode == kGradient)
-      for (int i = 0; i < 2 * kReaders; i++) tc::barrier_init(dh_in(i / 2, i % 2), 1);
+      for (int i = 0; i < 2 * R; i++) tc::barrier_init(dh_in(i / 2, i % 2), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tc::tmem_alloc<kCtas, kColumns>(tc::smem(&s_tmem));
@@ -122,7 +123,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     return it;
   };
 
-  if (warp == 0 && lane == 0) {
+  // (the whole warp waits, and goes on or gives up)
+  const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(~0u, tc::barrier_wait(bar, parity, stop)) != 0; };
+  if (warp == 0) {
     // ---- loads
     int stage = 0;
     uint32_t phase = 0;
@@ -131,26 +134,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     for (int i = unit; ok && i < items; i += units) {
       const Item it = item(i);
       for (int s = it.from; s < it.to; s++) {
-        if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, stop))) break;
-        const uint32_t a = base + stage * kStage, b = a + kABytes, bar = kCtas == 1 ? full(stage) : tc::in_first(full(stage));
+        if (!(ok = wait(empty(stage), phase ^ 1))) break;
         const int bytes = a_rows(kMode) ? kStage : kStage - (int)kABytes + p.a_box * kC * 2;
-        if (rank == 0) tc::barrier_expect(full(stage), kCtas * bytes);
         const int part = kMode == kInput || kMode == kWeight ? s / segment : 0, seg = kMode == kWeight ? it.matrix * p.parts + part : part;
         const int c = (s - part * segment) * kC;
-        if (a_rows(kMode)) {
-          for (int q = 0; q < kM / 64; q++) tc::load_box<kCtas>(a + q * 8192, &p.a[seg], it.m0 + q * 64, c, bar);
-        } else {
-          tc::load_box<kCtas>(a, &p.a[seg], c, it.m0, bar);
+        if (tc::elect()) {
+          const uint32_t a = base + stage * kStage, b = a + kABytes, bar = kCtas == 1 ? full(stage) : tc::in_first(full(stage));
+          if (rank == 0) tc::barrier_expect(full(stage), kCtas * bytes);
+          if (a_rows(kMode)) {
+            for (int q = 0; q < kM / 64; q++) tc::load_box<kCtas>(a + q * 8192, &p.a[seg], it.m0 + q * 64, c, bar);
+          } else {
+            tc::load_box<kCtas>(a, &p.a[seg], c, it.m0, bar);
+          }
+          if (dual(kMode) && kCtas == 2) {
+            tc::load_box<kCtas>(b, &p.b[rank], c, it.n0, bar);
+          } else if (dual(kMode)) {
+            tc::load_box<kCtas>(b, &p.b[0], c, it.n0, bar);
+            tc::load_box<kCtas>(b + kN / 2 * kC * 2, &p.b[1], c, it.n0, bar);
+          } else {
+            for (int q = 0; q < kN / kCtas / 64; q++)
+              tc::load_box<kCtas>(b + q * 8192, &p.b[kMode == kInput ? seg : 0], it.n0 + rank * (kN / kCtas) + q * 64, c, bar);
+          }
         }
-        if (dual(kMode) && kCtas == 2) {
-          tc::load_box<kCtas>(b, &p.b[rank], c, it.n0, bar);
-        } else if (dual(kMode)) {
-          tc::load_box<kCtas>(b, &p.b[0], c, it.n0, bar);
-          tc::load_box<kCtas>(b + kN / 2 * kC * 2, &p.b[1], c, it.n0, bar);
-        } else {
-          for (int q = 0; q < kN / kCtas / 64; q++)
-            tc::load_box<kCtas>(b + q * 8192, &p.b[kMode == kInput ? seg : 0], it.n0 + rank * (kN / kCtas) + q * 64, c, bar);
-        }
+        __syncwarp();
         issued++;
         if (++stage == S) stage = 0, phase ^= 1;
       }
@@ -159,10 +165,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     // the other block too); if the launch gives up, until its copies have landed (a pair's second waits for its first).
     for (int k = min(issued, S); k >= 1; k--) {
       const int at = (issued - k) % S, turn = (issued - k) / S;
-      if (ok) ok = tc::barrier_wait(empty(at), turn & 1, stop);
+      if (ok) ok = wait(empty(at), turn & 1);
       if (!ok && rank == 0) tc::barrier_drain(full(at), turn & 1);
     }
-  } else if (warp == 1 && lane == 0 && rank == 0) {
+  } else if (warp == 1 && rank == 0) {
     // ---- products
     constexpr uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, a_rows(kMode), b_rows(kMode), kM * kCtas, kN);
     int stage = 0, slot = 0;
@@ -170,29 +176,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     bool ok = true;
     for (int i = unit; ok && i < items; i += units) {
       const Item it = item(i);
-      if (!(ok = tc::barrier_wait(taken(slot), slot_phase ^ 1, stop))) break;
+      if (!(ok = wait(taken(slot), slot_phase ^ 1))) break;
       tc::fence_after();
       for (int s = it.from; s < it.to; s++) {
-        if (!(ok = tc::barrier_wait(full(stage), phase, stop))) break;
+        if (!(ok = wait(full(stage), phase))) break;
         tc::fence_after();
-        const uint32_t at = base + stage * kStage;
-        const uint64_t a = tc::operand(at, a_rows(kMode)), b = tc::operand(at + kABytes, b_rows(kMode));
+        if (tc::elect()) {
+          const uint32_t at = base + stage * kStage;
+          const uint64_t a = tc::operand(at, a_rows(kMode)), b = tc::operand(at + kABytes, b_rows(kMode));
 #pragma unroll
-        for (int q = 0; q < kC / 16; q++)  // 16 of the contraction: 32 bytes along a line, or 16 lines
-          tc::mma<kCtas>(tmem + slot * kN, a + q * (a_rows(kMode) ? 2048 >> 4 : 32 >> 4), b + q * (b_rows(kMode) ? 2048 >> 4 : 32 >> 4),
-                  desc, s > it.from || q > 0);
-        tc::commit<kCtas>(empty(stage));
+          for (int q = 0; q < kC / 16; q++)  // 16 of the contraction: 32 bytes along a line, or 16 lines
+            tc::mma<kCtas>(tmem + slot * kN, a + q * (a_rows(kMode) ? 2048 >> 4 : 32 >> 4), b + q * (b_rows(kMode) ? 2048 >> 4 : 32 >> 4),
+                           desc, s > it.from || q > 0);
+          tc::commit<kCtas>(empty(stage));
+          if (s + 1 == it.to) tc::commit<kCtas>(done(slot));
+        }
+        __syncwarp();
         if (++stage == S) stage = 0, phase ^= 1;
       }
-      tc::commit<kCtas>(done(slot));
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
     if (!ok) {  // the products in flight end before tensor memory is freed
-      tc::commit<kCtas>(drain);
+      if (tc::elect()) tc::commit<kCtas>(drain);
+      __syncwarp();
       tc::barrier_drain(drain, 0);
     }
   } else if (warp >= 2) {
-    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, every other 32
+    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, 32
     // columns, by way of staging that asynchronous copies empty.  (Two warps a scheduler: one alone left the
     // latencies of the reads, the copies and dh in the open: backward of 4096 x 1024 -> 4096 174 and 159 us.)
     const int lanes = (warp % 4) * 32;
@@ -219,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         tc::load_box<1>(asked_at + reader * kAsked<kMode> + (asked & 1) * 2048, &p.dh, ask.it.n0 + ask.j, ask.it.m0 + lanes, bar);
       }
       asked++;
-      ask.j += 64;
+      ask.j += kNext;
       if (ask.j >= kOutN || ask.it.n0 + ask.j >= p.n) {
         ask.j = first;
         ask.i += units;
@@ -238,12 +248,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     for (int i = unit; ok && i < items; i += units) {
       const Item it = item(i);
       const int row0 = it.m0 + lanes;
-      // (the whole warp goes on or gives up: reading tensor memory is a warp's instruction)
-      if (!__all_sync(~0u, tc::barrier_wait(done(slot), slot_phase, stop))) break;
+      if (!wait(done(slot), slot_phase)) break;
       tc::fence_after();
       const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
 #pragma unroll 1
-      for (int j = first; ok && j < kOutN; j += 64) {
+      for (int j = first; ok && j < kOutN; j += kNext) {
         const int col = it.n0 + j, count = min(32, p.n - col);
         if (count <= 0) break;
         float v[32], u[32];
@@ -252,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         if (dual(kMode)) tc::tmem_load32(u, at + kN / 2 + j);
         if (kMode == kGradient) {
           const int b = had & 1;
-          ok = __all_sync(~0u, tc::barrier_wait(dh_in(reader, b), had >> 1 & 1, stop));
+          ok = wait(dh_in(reader, b), had >> 1 & 1);
           const char* from = raw + (asked_at - tc::smem(raw)) + reader * kAsked<kMode> + b * 2048 + lane * 64;
 #pragma unroll
           for (int q = 0; q < 4; q++) dh[q] = load_pack<T, 8>(reinterpret_cast<const T*>(from + ((q ^ (lane >> 1 & 3)) << 4)));
@@ -435,7 +444,7 @@ cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
   const int items = p.tiles_m * p.tiles_n * p.matrices * p.splits;
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)std::min(items, kSms / kCtas) * kCtas);
-  c.blockDim = dim3(kThreads);
+  c.blockDim = dim3(kThreads<kMode>);
   c.dynamicSmemBytes = kSmem<kMode, kN, kCtas>;
   c.stream = s;
   cudaLaunchAttribute cluster{};
