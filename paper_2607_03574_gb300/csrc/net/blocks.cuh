@@ -56,20 +56,27 @@ template <> __device__ __forceinline__ float largest<float>() { return 3.4028234
 template <> __device__ __forceinline__ float largest<__half>() { return 65504.0f; }
 template <> __device__ __forceinline__ float largest<__nv_bfloat16>() { return 3.3895313893e38f; }
 template <typename T>
-__device__ __forceinline__ float held(float v, float scale) {
-  const float h = v * scale;
-  return fabsf(h) > largest<T>() ? copysignf(largest<T>(), h) : h;
+__device__ __forceinline__ float2 held(float2 v, float scale, uint32_t code) {
+  float2 h = mul(v, make_float2(scale, scale));
+  if (code > (std::is_same<T, __half>::value ? 134u : 245u)) {  // (448 2^e is finite below)
+    h.x = fabsf(h.x) > largest<T>() ? copysignf(largest<T>(), h.x) : h.x;
+    h.y = fabsf(h.y) > largest<T>() ? copysignf(largest<T>(), h.y) : h.y;
+  }
+  return h;
 }
 
 // V elements of a row (those beyond its end are 0) to blocks: 32 / V consecutive lanes, `lanes` among them, share one.
 template <int V>
 __device__ __forceinline__ void store_block(const Pairs<V> (&v)[kPairs<V>], uint32_t lanes, uint8_t* values, bool inside, uint8_t* scale) {
-  uint32_t most = 0;
+  float size;
+  if constexpr (V == 1) {
+    size = v[0];
+  } else {
+    size = larger(v[0].x, v[0].y);
 #pragma unroll
-  for (int e = 0; e < kPairs<V>; e++) {
-    if constexpr (V == 1) most = magnitude(v[0]);
-    else most = max(most, max(magnitude(v[e].x), magnitude(v[e].y)));
+    for (int e = 1; e < kPairs<V>; e++) size = larger(size, larger(v[e].x, v[e].y));
   }
+  uint32_t most = magnitude(size);
 #pragma unroll
   for (int o = 16 / V; o; o >>= 1) most = max(most, __shfl_xor_sync(lanes, most, o));
   const uint32_t code = block_code(most);

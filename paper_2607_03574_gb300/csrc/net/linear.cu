@@ -432,61 +432,72 @@ __global__ void __launch_bounds__(256) k_finish(const float* partial, int64_t pi
 }
 
 // ------------------------------------------------------------------------------------ one row: vectors
-// w is read once and is nearly all the traffic: a warp takes kPer of its rows, 16 bytes a lane and load, against x (from L1).
-template <typename T, int V, int kPer>
-__global__ void __launch_bounds__(128) k_linear_one(LinearArgs a) {
+// w is read once and is nearly all the traffic, so what counts is how much of it is under way: kSplits warps share a row of w, 16
+// bytes a lane and eight loads at once, against x (from L1); a block's sums are joined in shared memory.
+template <typename T, int V, int kSplits>
+__global__ void __launch_bounds__(256) k_linear_one(LinearArgs a) {
   using P = Pairs<V>;
-  constexpr int H = kPairs<V>, kUnroll = 16 / kPer;
-  const int lane = threadIdx.x % 32;
-  const int64_t j0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / 32) * kPer;
-  if (j0 >= a.n) return;
-  const T* w[kPer];
-  P s[kPer];
+  constexpr int H = kPairs<V>, kUnroll = 8, kPer = 8 / kSplits;  // rows of w a block
+  __shared__ float part[8];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, split = warp % kSplits;
+  const int64_t j = (int64_t)blockIdx.x * kPer + warp / kSplits;
+  P s = both(0.0f, P());
+  if (j < a.n) {
+    const T *w = static_cast<const T*>(a.w) + j * a.w_stride, *x = static_cast<const T*>(a.x);
+    constexpr int kStep = kSplits * 32 * V;
+    for (int64_t c0 = (split * 32 + lane) * V; c0 < a.k; c0 += kUnroll * kStep) {
+      Pack<T, V> pw[kUnroll], px[kUnroll];
 #pragma unroll
-  for (int q = 0; q < kPer; q++) {
-    w[q] = static_cast<const T*>(a.w) + (j0 + q < a.n ? j0 + q : j0) * a.w_stride;
-    s[q] = both(0.0f, P());
-  }
-  const T* x = static_cast<const T*>(a.x);
-#pragma unroll kUnroll
-  for (int64_t c = lane * V; c < a.k; c += 32 * V) {
-    P vx[H], vw[H];
-    Pack<T, V> pw[kPer];
+      for (int u = 0; u < kUnroll; u++)
+        if (c0 + u * kStep < a.k) pw[u] = load_pack<T, V>(w + c0 + u * kStep);
 #pragma unroll
-    for (int q = 0; q < kPer; q++) pw[q] = load_pack<T, V>(w[q] + c);
-    widen<T, V>(load_pack<T, V>(x + c), vx);
+      for (int u = 0; u < kUnroll; u++)
+        if (c0 + u * kStep < a.k) px[u] = load_pack<T, V>(x + c0 + u * kStep);
 #pragma unroll
-    for (int q = 0; q < kPer; q++) {
-      widen<T, V>(pw[q], vw);
+      for (int u = 0; u < kUnroll; u++) {
+        if (c0 + u * kStep >= a.k) break;
+        P vx[H], vw[H];
+        widen<T, V>(px[u], vx);
+        widen<T, V>(pw[u], vw);
 #pragma unroll
-      for (int e = 0; e < H; e++) s[q] = fma(vx[e], vw[e], s[q]);
+        for (int e = 0; e < H; e++) s = fma(vx[e], vw[e], s);
+      }
     }
   }
+  float z = total(s);
 #pragma unroll
-  for (int q = 0; q < kPer; q++) {
-    float z = total(s[q]);
+  for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(~0u, z, o);
+  if constexpr (kSplits > 1) {
+    if (lane == 0) part[warp] = z;
+    __syncthreads();
+    if (split) return;
+    z = part[warp];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(~0u, z, o);
-    const int64_t j = j0 + q;
-    if (lane != q || j >= a.n) continue;
-    z += bias_at<T>(a.bias, a.bias_f32, j);
-    if (a.z) a.z[j] = z;
-    by_activation_or_none(a.act, [&](auto k) {
-      const float2 act = activation<decltype(k)::value>(make_float2(z, z));
-      const float r = a.residual ? to_f32(static_cast<const T*>(a.residual)[j]) : 0.0f;
-      static_cast<T*>(a.y)[j] = from_f32<T>(act.x + r);
-    });
+    for (int q = 1; q < kSplits; q++) z += part[warp + q];
   }
+  if (lane || j >= a.n) return;
+  z += bias_at<T>(a.bias, a.bias_f32, j);
+  if (a.z) a.z[j] = z;
+  by_activation_or_none(a.act, [&](auto k) {
+    const float2 act = activation<decltype(k)::value>(make_float2(z, z));
+    const float r = a.residual ? to_f32(static_cast<const T*>(a.residual)[j]) : 0.0f;
+    static_cast<T*>(a.y)[j] = from_f32<T>(act.x + r);
+  });
 }
 
+template <typename T, int V>
+void one_of(const LinearArgs& a, cudaStream_t s) {
+  // as many warps a row as 40 on each SM have room for, each with a batch of loads at least
+  const int64_t room = kSms * 40 / a.n, most = a.k / (8 * 32 * V);
+  if (std::min(room, most) >= 8) k_linear_one<T, V, 8><<<(unsigned)a.n, 256, 0, s>>>(a);
+  else if (std::min(room, most) >= 4) k_linear_one<T, V, 4><<<(unsigned)ceil_div(a.n, 2), 256, 0, s>>>(a);
+  else if (std::min(room, most) >= 2) k_linear_one<T, V, 2><<<(unsigned)ceil_div(a.n, 4), 256, 0, s>>>(a);
+  else k_linear_one<T, V, 1><<<(unsigned)ceil_div(a.n, 8), 256, 0, s>>>(a);
+}
 template <typename T>
 void one(const LinearArgs& a, bool vectors, cudaStream_t s) {
-  const bool many = a.n >= 2048;  // four rows of w a warp quarter the loads of x; fewer outputs go one a warp
-  const unsigned grid = (unsigned)((a.n + (many ? 15 : 3)) / (many ? 16 : 4));
-  if (vectors && many) k_linear_one<T, 8, 4><<<grid, 128, 0, s>>>(a);
-  else if (vectors) k_linear_one<T, 8, 1><<<grid, 128, 0, s>>>(a);
-  else if (many) k_linear_one<T, 1, 4><<<grid, 128, 0, s>>>(a);
-  else k_linear_one<T, 1, 1><<<grid, 128, 0, s>>>(a);
+  if (vectors) one_of<T, 8>(a, s);
+  else one_of<T, 1>(a, s);
 }
 
 // ----------------------------------------------------------------------------------------- dz and db
@@ -500,67 +511,82 @@ struct SlopeArgs {
   int halves;               // and what dz's rounding leaves, `rows` rows further on
   float* sums;              // [gridDim.y][n], or null
 };
-// 8 columns a thread, 256 a block, every so-manieth 8 rows; a block's 8 row sums are joined in shared memory.
-template <typename T, bool kVectors>
+// z of 8 columns of a row: two words of a block and its scale, or binary32
+struct HeldZ { uint2 q; uint32_t code; };
+// 8 columns a thread, 256 a block, every so-manieth 8 rows, kRows of them asked for at once; a block's 8 row sums are joined in
+// shared memory.  Bound by memory: 16384 x 8192 with z in binary32 and dz (1.07 GB) ran at 5.5 TB/s with two rows at once.
+template <typename T, bool kVectors, int kZ>
 __global__ void __launch_bounds__(256) k_slope(SlopeArgs a) {
+  constexpr int kRows = kZ == kNothing ? 8 : 4;
+  using Z = std::conditional_t<kZ == kFloats, Pack<float, 8>, HeldZ>;
   const int t = threadIdx.x % 32, r = threadIdx.x / 32;
-  const int64_t c = (int64_t)blockIdx.x * 256 + t * 8, chunks = (a.n + 127) / 128;
-  const bool all = c + 8 <= a.n;
+  const int64_t c = (int64_t)blockIdx.x * 256 + t * 8, chunks = (a.n + 127) / 128, step = (int64_t)gridDim.y * 8;
+  const bool all = c + 8 <= a.n, some = c < a.n;
   float2 sum[4] = {};
-  by_activation_or_none(a.act, [&](auto k) {
-#pragma unroll 2
-    for (int64_t row = (int64_t)blockIdx.y * 8 + r; row < a.rows; row += (int64_t)gridDim.y * 8) {
-      if (c >= a.n) break;
+  for (int64_t row0 = (int64_t)blockIdx.y * 8 + r; some && row0 < a.rows; row0 += kRows * step) {
+    Pack<T, 8> d[kRows];
+    Z held_z[kZ == kNothing ? 1 : kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; u++) {
+      const int64_t row = row0 + u * step;
+      if (row >= a.rows) continue;
       const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride + c;
-      Pack<T, 8> d;
       if (kVectors && all) {
-        d = load_pack<T, 8>(dy);
+        d[u] = load_pack<T, 8>(dy);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; e++) d.v[e] = c + e < a.n ? dy[e] : from_f32<T>(0.0f);
+        for (int e = 0; e < 8; e++) d[u].v[e] = c + e < a.n ? dy[e] : from_f32<T>(0.0f);
       }
-      float2 z[4] = {};
-      if constexpr (decltype(k)::value != NDVM_ACT_NONE) {
-        if (a.z) {  // (its rows hold whole fours)
+      if constexpr (kZ == kFloats) {  // (its rows hold whole fours)
 #pragma unroll
-          for (int q = 0; q < 2; q++) {
-            if (!all && c + 4 * q >= a.n) continue;
-            const float4 f = *reinterpret_cast<const float4*>(a.z + row * a.z_stride + c + 4 * q);
-            z[2 * q] = make_float2(f.x, f.y), z[2 * q + 1] = make_float2(f.z, f.w);
-          }
-        } else {
-          const uint2 q = *reinterpret_cast<const uint2*>(a.z_values + row * a.z_pitch + c);
-          const float scale = block_scale(a.z_scales[scale_at(row, c / 32, chunks)]);
-          const uint16_t pairs[4] = {(uint16_t)q.x, (uint16_t)(q.x >> 16), (uint16_t)q.y, (uint16_t)(q.y >> 16)};
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const float2 v = from_e4m3(pairs[e]);
-            z[e] = make_float2(held<float>(v.x, scale), held<float>(v.y, scale));
-          }
+        for (int q = 0; q < 2; q++) {
+          const float4 f = all || c + 4 * q < a.n ? *reinterpret_cast<const float4*>(a.z + row * a.z_stride + c + 4 * q) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          held_z[u].v[4 * q] = f.x, held_z[u].v[4 * q + 1] = f.y, held_z[u].v[4 * q + 2] = f.z, held_z[u].v[4 * q + 3] = f.w;
         }
-      }
-      Pack<T, 8> o, l;
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        float2 f, g;
-        activate<decltype(k)::value>(z[e], &f, &g);
-        const float2 v = mul(widen(d.v + 2 * e), g);
-        sum[e] = add(sum[e], v);
-        narrow(o.v + 2 * e, v);
-        if (a.halves) l.v[2 * e] = rest_of(v.x, o.v[2 * e]), l.v[2 * e + 1] = rest_of(v.y, o.v[2 * e + 1]);
-      }
-      if (!all) {  // (the pitch's last columns are 0)
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-          if (c + e >= a.n) o.v[e] = l.v[e] = from_f32<T>(0.0f);
-      }
-      if (a.dz) {
-        T* dz = static_cast<T*>(a.dz) + row * a.pitch + c;
-        store_pack(dz, o);
-        if (a.halves) store_pack(dz + a.rows * a.pitch, l);
+      } else if constexpr (kZ == kBlocks) {
+        held_z[u].q = *reinterpret_cast<const uint2*>(a.z_values + row * a.z_pitch + c);
+        held_z[u].code = a.z_scales[scale_at(row, c / 32, chunks)];
       }
     }
-  });
+    by_activation_or_none(kZ == kNothing ? NDVM_ACT_NONE : a.act, [&](auto k) {
+#pragma unroll
+      for (int u = 0; u < kRows; u++) {
+        const int64_t row = row0 + u * step;
+        if (row >= a.rows) break;
+        if constexpr (kZ == kNothing) {
+#pragma unroll
+          for (int e = 0; e < 4; e++) sum[e] = add(sum[e], widen(d[u].v + 2 * e));
+        } else {
+          Pack<T, 8> o, l;
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            float2 z, f, g;
+            if constexpr (kZ == kFloats) {
+              z = make_float2(held_z[u].v[2 * e], held_z[u].v[2 * e + 1]);
+            } else {
+              const float scale = block_scale(held_z[u].code);
+              z = from_e4m3((uint16_t)((e < 2 ? held_z[u].q.x : held_z[u].q.y) >> (e % 2 * 16)));
+              z = held<float>(z, scale, held_z[u].code);
+            }
+            activate<decltype(k)::value>(z, &f, &g);
+            const float2 v = mul(widen(d[u].v + 2 * e), g);
+            sum[e] = add(sum[e], v);
+            narrow(o.v + 2 * e, v);
+            if (a.halves) l.v[2 * e] = rest_of(v.x, o.v[2 * e]), l.v[2 * e + 1] = rest_of(v.y, o.v[2 * e + 1]);
+          }
+          if (!a.dz) continue;
+          if (!all) {  // (the pitch's last columns are 0)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              if (c + e >= a.n) o.v[e] = l.v[e] = from_f32<T>(0.0f);
+          }
+          T* dz = static_cast<T*>(a.dz) + row * a.pitch + c;
+          store_pack(dz, o);
+          if (a.halves) store_pack(dz + a.rows * a.pitch, l);
+        }
+      }
+    });
+  }
   if (!a.sums) return;
   __shared__ __align__(16) float2 all_sums[8][4][32];
 #pragma unroll
@@ -795,8 +821,14 @@ cudaError_t backward(LinearArgs a, cudaStream_t s) {
     d.sums = a.dbias ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
     const int64_t splits = slope_splits(a.rows, a.n);
     const dim3 grid((unsigned)ceil_div(a.n, 256), (unsigned)splits);
-    if (tma_ready(a.dy, a.dy_stride, a.rows, 0)) k_slope<T, true><<<grid, 256, 0, s>>>(d);
-    else k_slope<T, false><<<grid, 256, 0, s>>>(d);
+    const auto launch = [&](auto vectors) {
+      constexpr bool kVectors = decltype(vectors)::value;
+      if (!activated) k_slope<T, kVectors, kNothing><<<grid, 256, 0, s>>>(d);
+      else if (a.z) k_slope<T, kVectors, kFloats><<<grid, 256, 0, s>>>(d);
+      else k_slope<T, kVectors, kBlocks><<<grid, 256, 0, s>>>(d);
+    };
+    if (tma_ready(a.dy, a.dy_stride, a.rows, 0)) launch(std::true_type());
+    else launch(std::false_type());
     if (a.dbias) {
       const dim3 join((unsigned)ceil_div(a.n, 32)), block(32, 32);
       if (a.bias_f32) k_columns_join<<<join, block, 0, s>>>(d.sums, (int)splits, 1, a.n, static_cast<float*>(a.dbias), static_cast<float*>(nullptr));

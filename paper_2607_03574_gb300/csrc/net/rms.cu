@@ -6,6 +6,8 @@
 // All of it is bound by memory: forward reads x and the residual and writes s and y, backward reads s, dy and dsum and
 // writes dx.  A row is read once and held in the registers of the threads that share it, as in the layer norm; the stream
 // is rounded to its type before it is normalised, so that the backward pass sees from s alone what the forward pass saw.
+#include <atomic>
+
 #include "blocks.cuh"
 #include "net.h"
 #include "rows.cuh"
@@ -133,14 +135,28 @@ __global__ void __launch_bounds__(kLong) k_rms_forward_long(RmsArgs a, int w_f32
   if (!kBlocks && threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
 }
 
-// Backward, as the layer norm's: a group of kRow threads takes every so-manieth row, the next row's loads in flight while the
-// present one is worked on.  partial[block][c] = the block's sum of dy sh.
+// Backward: a group of kRow threads takes every so-manieth row.  Each thread asks for its part of the rows to come by asynchronous
+// copies, kDepth - 1 rows ahead, to shared memory that it alone reads: registers would hold one row ahead, which left the latency of
+// memory in the open (16384 x 1024 bf16 with a residual 37 us, 3.7 TB/s).  Rows off 16 bytes do take registers, one row ahead.
+// partial[block][c] = the block's sum of dy sh.
+template <int V, int N, int kRow, int kResident, int kBytes>
+constexpr int kDepth = V * kBytes != 16 ? 0 : std::min(4, 221184 / kResident / (3 * N * kBackBlock<kRow> * 16));
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
 template <typename T, int V, int N, int kRow, int kResident>
 __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(RmsArgs a, int w_f32) {
   using P = Pairs<V>;
-  constexpr int H = kPairs<V>, kBlockRows = kBackBlock<kRow> / kRow;
+  constexpr int H = kPairs<V>, kBlockRows = kBackBlock<kRow> / kRow, D = kDepth<V, N, kRow, kResident, sizeof(T)>;
+  extern __shared__ __align__(16) char ring[];  // [row ahead][array][pack][thread]
   __shared__ float2 part[2][kBlockRows][kRow > 32 ? kRow / 32 : 1];
-  const int t = threadIdx.x % kRow, group = threadIdx.x / kRow, cols = (int)a.cols;
+  const int t = threadIdx.x % kRow, group = threadIdx.x / kRow, cols = (int)a.cols, arrays = a.dsum ? 3 : 2;
   const float inv = 1.0f / (float)cols;
   P dw[N][H];
 #pragma unroll
@@ -149,28 +165,52 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
     for (int e = 0; e < H; e++) dw[j][e] = both(0.0f, P());
   Pack<T, V> nx[N], nd[N], ns[N];
   float nrstd = 0.0f;
-  const auto fetch = [&](int64_t row) {
-    if (row >= a.rows) return;
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-    const T* d = static_cast<const T*>(a.dy) + row * a.dy_stride;
-    const T* s = static_cast<const T*>(a.dsum) + row * a.dsum_stride;
-    nrstd = a.rstd[row];
+  const int64_t step = (int64_t)gridDim.x * kBlockRows;
+  const auto pack_at = [&](int slot, int array, int j) { return ((slot * arrays + array) * N + j) * kBackBlock<kRow> * 16 + (int)threadIdx.x * 16; };
+  // asks for a row; `slot` of the ring receives it
+  const auto fetch = [&](int64_t row, int slot) {
+    if (row < a.rows) {
+      const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+      const T* d = static_cast<const T*>(a.dy) + row * a.dy_stride;
+      const T* s = static_cast<const T*>(a.dsum) + row * a.dsum_stride;
 #pragma unroll
-    for (int j = 0; j < N; j++) {
-      const int c = (j * kRow + t) * V;
-      if (c < cols) {
-        nx[j] = load_pack<T, V>(x + c);
-        nd[j] = load_pack<T, V>(d + c);
-        if (a.dsum) ns[j] = load_pack<T, V>(s + c);
+      for (int j = 0; j < N; j++) {
+        const int c = (j * kRow + t) * V;
+        if (c >= cols) continue;
+        if constexpr (D > 0) {
+          const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring);
+          copy16(to + pack_at(slot, 0, j), x + c);
+          copy16(to + pack_at(slot, 1, j), d + c);
+          if (a.dsum) copy16(to + pack_at(slot, 2, j), s + c);
+        } else {
+          nx[j] = load_pack<T, V>(x + c);
+          nd[j] = load_pack<T, V>(d + c);
+          if (a.dsum) ns[j] = load_pack<T, V>(s + c);
+        }
       }
     }
+    if constexpr (D > 0) asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  const int64_t step = (int64_t)gridDim.x * kBlockRows;
+  const auto ask_rstd = [&](int64_t row) {
+    if (row < a.rows) nrstd = a.rstd[row];
+  };
   int64_t row = (int64_t)blockIdx.x * kBlockRows + group;
-  fetch(row);
+  ask_rstd(row);
+  if constexpr (D > 0) {
+#pragma unroll
+    for (int q = 0; q < D - 1; q++) fetch(row + q * step, q);
+  } else {
+    fetch(row, 0);
+  }
+  int slot = 0;
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
     const float rstd = nrstd;
     const P scale = both(rstd, P());
+    ask_rstd(row + step);
+    if constexpr (D > 0) {
+      fetch(row + (D - 1) * step, slot == 0 ? D - 1 : slot - 1);
+      copies_wait<D - 1>();
+    }
     P sh[N][H], g[N][H], sgs = both(0.0f, P());
     Pack<T, V> ds[N];
 #pragma unroll
@@ -179,6 +219,11 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
       if (c >= cols) continue;
       P w[H];
       load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
+      if constexpr (D > 0) {
+        nx[j] = load_pack<T, V>(reinterpret_cast<const T*>(ring + pack_at(slot, 0, j)));
+        nd[j] = load_pack<T, V>(reinterpret_cast<const T*>(ring + pack_at(slot, 1, j)));
+        if (a.dsum) ns[j] = load_pack<T, V>(reinterpret_cast<const T*>(ring + pack_at(slot, 2, j)));
+      }
       widen<T, V>(nx[j], sh[j]);
       widen<T, V>(nd[j], g[j]);
       ds[j] = ns[j];
@@ -190,7 +235,8 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
         sgs = fma(g[j][e], sh[j][e], sgs);
       }
     }
-    fetch(row + step);
+    if constexpr (D > 0) slot = slot + 1 == D ? 0 : slot + 1;
+    else fetch(row + step, 0);
     if (!a.dx) continue;
     const float2 s = group_sum<kRow>(total(sgs), 0.0f, part[turn][group], group);
     const P slope = both(-s.x * inv, P());
@@ -212,6 +258,7 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
       store_pack(dx + c, out);
     }
   }
+  if constexpr (D > 0) copies_wait<0>();
   if (!a.partial) return;
   float* out = a.partial + (int64_t)blockIdx.x * cols;
   if constexpr (kBlockRows == 1) {
@@ -284,6 +331,7 @@ __global__ void __launch_bounds__(256) k_quantize(RmsArgs a, int64_t share) {
   if (row >= whole(a.rows)) return;
   const bool real = row < a.rows;
   const T* x = static_cast<const T*>(a.x) + (real ? row : 0) * a.x_stride;
+  uint8_t *values = a.values + row * a.v_stride, *scales = a.scales + scale_at(row, 0, chunks);  // (a row's: 4 of every 512 bytes)
   const uint32_t lanes = (0xffffffffu >> (32 - 32 / V)) << (lane / (32 / V) * (32 / V));
   for (int64_t c0 = from + lane * V; c0 < to; c0 += kUnroll * 32 * V) {
     Pack<T, V> p[kUnroll];
@@ -303,7 +351,7 @@ __global__ void __launch_bounds__(256) k_quantize(RmsArgs a, int64_t share) {
 #pragma unroll
         for (int e = 0; e < H; e++) v[e] = both(0.0f, P());
       }
-      store_block<V>(v, lanes, a.values + row * a.v_stride + c, real && c < a.v_cols, a.scales + scale_at(row, c / 32, chunks));
+      store_block<V>(v, lanes, values + c, real && c < a.v_cols, scales + c / 128 * 512 + (c / 32 & 3));
     }
   }
 }
@@ -315,28 +363,43 @@ __global__ void __launch_bounds__(256) k_dequantize(RmsArgs a, int64_t share) {
   const int64_t from = blockIdx.y * share, to = min(from + share, a.cols);
   if (row >= a.rows) return;
   T* y = static_cast<T*>(a.y) + row * a.y_stride;
-#pragma unroll 4
-  for (int64_t c = from + lane * 8; c < to; c += 256) {
-    const uint2 q = *reinterpret_cast<const uint2*>(a.values + row * a.v_stride + c);
-    const float scale = block_scale(a.scales[scale_at(row, c / 32, chunks)]);
-    const uint16_t pairs[4] = {(uint16_t)q.x, (uint16_t)(q.x >> 16), (uint16_t)q.y, (uint16_t)(q.y >> 16)};
-    Pack<T, 8> out;
+  const uint8_t *values = a.values + row * a.v_stride, *scales = a.scales + scale_at(row, 0, chunks);
+  constexpr int kUnroll = 4;
+  for (int64_t c0 = from + lane * 8; c0 < to; c0 += kUnroll * 256) {
+    uint2 words[kUnroll];
+    uint32_t codes[kUnroll];
 #pragma unroll
-    for (int e = 0; e < 4; e++) {
-      const float2 v = from_e4m3(pairs[e]);
-      narrow(out.v + 2 * e, make_float2(held<T>(v.x, scale), held<T>(v.y, scale)));
+    for (int u = 0; u < kUnroll; u++) {
+      const int64_t c = c0 + u * 256;
+      if (c >= to) continue;
+      words[u] = *reinterpret_cast<const uint2*>(values + c);
+      codes[u] = scales[c / 128 * 512 + (c / 32 & 3)];
     }
-    if (kVectors && c + 8 <= a.cols) {
-      if constexpr (sizeof(T) == 2) {
-        store_pack(y + c, out);
-      } else {
-        *reinterpret_cast<float4*>(y + c) = make_float4(out.v[0], out.v[1], out.v[2], out.v[3]);
-        *reinterpret_cast<float4*>(y + c + 4) = make_float4(out.v[4], out.v[5], out.v[6], out.v[7]);
-      }
-    } else {
 #pragma unroll
-      for (int e = 0; e < 8; e++)
-        if (c + e < a.cols) y[c + e] = out.v[e];
+    for (int u = 0; u < kUnroll; u++) {
+      const int64_t c = c0 + u * 256;
+      if (c >= to) break;
+      const uint2 q = words[u];
+      const float scale = block_scale(codes[u]);
+      const uint16_t pairs[4] = {(uint16_t)q.x, (uint16_t)(q.x >> 16), (uint16_t)q.y, (uint16_t)(q.y >> 16)};
+      Pack<T, 8> out;
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float2 v = from_e4m3(pairs[e]);
+        narrow(out.v + 2 * e, held<T>(v, scale, codes[u]));
+      }
+      if (kVectors && c + 8 <= a.cols) {
+        if constexpr (sizeof(T) == 2) {
+          store_pack(y + c, out);
+        } else {
+          *reinterpret_cast<float4*>(y + c) = make_float4(out.v[0], out.v[1], out.v[2], out.v[3]);
+          *reinterpret_cast<float4*>(y + c + 4) = make_float4(out.v[4], out.v[5], out.v[6], out.v[7]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+          if (c + e < a.cols) y[c + e] = out.v[e];
+      }
     }
   }
 }
@@ -364,21 +427,31 @@ template <typename T>
 cudaError_t rms_backward(RmsArgs a, int w_f32, cudaStream_t s) {
   if (!a.dweight) a.partial = nullptr;
   int blocks = 0;
+  cudaError_t failed = cudaSuccess;
   if (a.rows > 0 && (a.dx || a.dweight)) {
     const int width = load_width<T>(a.rows, a.cols, w_f32, {a.weight},
                                     {{a.x, a.x_stride}, {a.dy, a.dy_stride}, {a.dsum, a.dsum ? a.dsum_stride : 0}, {a.dx, a.dx ? a.dx_stride : 0}});
     const bool held = backward_variant<T>(width, a.rows, a.cols, [&](auto v, auto n, auto r, auto b) {
       constexpr int kRow = decltype(r)::value, kThreads = kBackBlock<kRow>, kRows = kThreads / kRow;
+      constexpr auto kernel = k_rms_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value>;
+      constexpr int kRing = kDepth<decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value, sizeof(T)> * decltype(n)::value * kThreads * 16;
       // as many blocks as stay resident, or a block a group of rows where there are fewer
-      static const int resident = [] {
+      static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may take its shared memory
+      static std::atomic<int> resident{0};
+      int device = 0;
+      if (failed == cudaSuccess) failed = cudaGetDevice(&device);
+      if (failed == cudaSuccess && (device >= 64 || !(allowed.load(std::memory_order_acquire) >> device & 1))) {
+        if (kRing) failed = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kRing);
         int fit = 0;
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, k_rms_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value>,
-                                                      kThreads, 0);
-        return std::clamp(fit * kSms, kSms, kMostBlocks);
-      }();
-      blocks = (int)std::min<int64_t>(resident, (a.rows + kRows - 1) / kRows);
-      k_rms_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value><<<blocks, kThreads, 0, s>>>(a, w_f32);
+        if (failed == cudaSuccess) failed = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, kernel, kThreads, 3 * kRing);
+        resident.store(std::clamp(fit * kSms, kSms, kMostBlocks), std::memory_order_relaxed);
+        if (failed == cudaSuccess && device < 64) allowed.fetch_or((uint64_t)1 << device, std::memory_order_release);
+      }
+      if (failed != cudaSuccess) return;
+      blocks = (int)std::min<int64_t>(resident.load(std::memory_order_relaxed), (a.rows + kRows - 1) / kRows);
+      kernel<<<blocks, kThreads, (a.dsum ? 3 : 2) * kRing, s>>>(a, w_f32);
     });
+    if (failed != cudaSuccess) return failed;
     if (!held) {
       if (a.dx) k_rms_backward_long<T><<<(unsigned)a.rows, kLong, 0, s>>>(a, w_f32);
       blocks = (int)std::min<int64_t>(kLongBlocks, a.rows);
