@@ -92,6 +92,33 @@ __device__ __forceinline__ float2 activation(float2 g) {
     return kAct == NDVM_ACT_SILU ? mul(g, s) : s;
   }
 }
+// act'(g) alone, with fewer instructions than activate(): s (1 - s) is the same on both sides of 0.
+template <int kAct>
+__device__ __forceinline__ float2 derivative(float2 g) {
+  const float2 one = make_float2(1.0f, 1.0f);
+  if constexpr (kAct == NDVM_ACT_NONE) {
+    return one;
+  } else if constexpr (kAct == NDVM_ACT_RELU) {
+    return make_float2(g.x > 0.0f ? 1.0f : 0.0f, g.y > 0.0f ? 1.0f : 0.0f);
+  } else if constexpr (kAct == NDVM_ACT_GELU) {
+    const float2 half = mul(mul(g, g), make_float2(-0.36067376f, -0.36067376f));
+    const float2 h = make_float2(power2_normal(half.x), power2_normal(half.y)), e = mul(h, h);
+    const float2 t = make_float2(reciprocal(fmaf(fabsf(g.x), 0.35f, 1.0f)), reciprocal(fmaf(fabsf(g.y), 0.35f, 1.0f)));
+    constexpr float kQ[9] = {0.139621258f, 0.139864326f,  0.119815566f, 0.105574533f,   -0.0232631564f,
+                             0.15939188f,  -0.255900919f, 0.144060329f, -0.0291638281f};
+    float2 tail = make_float2(kQ[8], kQ[8]);
+#pragma unroll
+    for (int i = 7; i >= 0; i--) tail = fma(tail, t, make_float2(kQ[i], kQ[i]));
+    tail = mul(mul(e, t), tail);
+    const float2 cdf = make_float2(g.x < 0.0f ? tail.x : 1.0f - tail.x, g.y < 0.0f ? tail.y : 1.0f - tail.y);
+    return fma(mul(g, e), make_float2(0.39894228f, 0.39894228f), cdf);
+  } else {
+    const float2 h = make_float2(power2_normal(fabsf(g.x) * -0.72134752f), power2_normal(fabsf(g.y) * -0.72134752f)), e = mul(h, h);
+    const float2 d = add(e, one), r = make_float2(reciprocal(d.x), reciprocal(d.y)), er = mul(e, r);
+    if constexpr (kAct == NDVM_ACT_SIGMOID) return mul(er, r);
+    return fma(mul(g, er), r, make_float2(g.x < 0.0f ? er.x : r.x, g.y < 0.0f ? er.y : r.y));
+  }
+}
 // f(activation as a constant): one branch around a loop over many elements, not one in each
 template <typename F>
 __device__ __forceinline__ void by_activation(int act, F&& f) {

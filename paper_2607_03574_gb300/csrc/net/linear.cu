@@ -433,11 +433,11 @@ __global__ void __launch_bounds__(256) k_finish(const float* partial, int64_t pi
 
 // ------------------------------------------------------------------------------------ one row: vectors
 // w is read once and is nearly all the traffic, so what counts is how much of it is under way: kSplits warps share a row of w, 16
-// bytes a lane and eight loads at once, against x (from L1); a block's sums are joined in shared memory.
+// bytes a lane and four loads at once, against x (from L1); a block's sums are joined in shared memory.
 template <typename T, int V, int kSplits>
-__global__ void __launch_bounds__(256) k_linear_one(LinearArgs a) {
+__global__ void __launch_bounds__(256, 4) k_linear_one(LinearArgs a) {
   using P = Pairs<V>;
-  constexpr int H = kPairs<V>, kUnroll = 8, kPer = 8 / kSplits;  // rows of w a block
+  constexpr int H = kPairs<V>, kUnroll = 4, kPer = 8 / kSplits;  // rows of w a block
   __shared__ float part[8];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, split = warp % kSplits;
   const int64_t j = (int64_t)blockIdx.x * kPer + warp / kSplits;
@@ -446,18 +446,15 @@ __global__ void __launch_bounds__(256) k_linear_one(LinearArgs a) {
     const T *w = static_cast<const T*>(a.w) + j * a.w_stride, *x = static_cast<const T*>(a.x);
     constexpr int kStep = kSplits * 32 * V;
     for (int64_t c0 = (split * 32 + lane) * V; c0 < a.k; c0 += kUnroll * kStep) {
-      Pack<T, V> pw[kUnroll], px[kUnroll];
+      Pack<T, V> pw[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; u++)
         if (c0 + u * kStep < a.k) pw[u] = load_pack<T, V>(w + c0 + u * kStep);
 #pragma unroll
-      for (int u = 0; u < kUnroll; u++)
-        if (c0 + u * kStep < a.k) px[u] = load_pack<T, V>(x + c0 + u * kStep);
-#pragma unroll
       for (int u = 0; u < kUnroll; u++) {
         if (c0 + u * kStep >= a.k) break;
         P vx[H], vw[H];
-        widen<T, V>(px[u], vx);
+        widen<T, V>(load_pack<T, V>(x + c0 + u * kStep), vx);
         widen<T, V>(pw[u], vw);
 #pragma unroll
         for (int e = 0; e < H; e++) s = fma(vx[e], vw[e], s);
@@ -487,7 +484,7 @@ __global__ void __launch_bounds__(256) k_linear_one(LinearArgs a) {
 
 template <typename T, int V>
 void one_of(const LinearArgs& a, cudaStream_t s) {
-  // as many warps a row as 40 on each SM have room for, each with a batch of loads at least
+  // as many warps a row as 40 on each SM have room for, each with two batches of loads at least (8192 -> 1024 6.0 us, 10.0 with one)
   const int64_t room = kSms * 40 / a.n, most = a.k / (8 * 32 * V);
   if (std::min(room, most) >= 8) k_linear_one<T, V, 8><<<(unsigned)a.n, 256, 0, s>>>(a);
   else if (std::min(room, most) >= 4) k_linear_one<T, V, 4><<<(unsigned)ceil_div(a.n, 2), 256, 0, s>>>(a);
@@ -514,10 +511,11 @@ struct SlopeArgs {
 // z of 8 columns of a row: two words of a block and its scale, or binary32
 struct HeldZ { uint2 q; uint32_t code; };
 // 8 columns a thread, 256 a block, every so-manieth 8 rows, kRows of them asked for at once; a block's 8 row sums are joined in
-// shared memory.  Bound by memory: 16384 x 8192 with z in binary32 and dz (1.07 GB) ran at 5.5 TB/s with two rows at once.
+// shared memory.  Bound by memory where z is binary32 (16384 x 8192, db alone: 805 MB in 136 us), by the activation's instructions where it
+// is 8-bit blocks (402 MB, 136 us); two rows at once and three blocks an SM beat four and two (139 and 155 us).
 template <typename T, bool kVectors, int kZ>
-__global__ void __launch_bounds__(256) k_slope(SlopeArgs a) {
-  constexpr int kRows = kZ == kNothing ? 8 : 4;
+__global__ void __launch_bounds__(256, 3) k_slope(SlopeArgs a) {
+  constexpr int kRows = kZ == kNothing ? 8 : 2;
   using Z = std::conditional_t<kZ == kFloats, Pack<float, 8>, HeldZ>;
   const int t = threadIdx.x % 32, r = threadIdx.x / 32;
   const int64_t c = (int64_t)blockIdx.x * 256 + t * 8, chunks = (a.n + 127) / 128, step = (int64_t)gridDim.y * 8;
@@ -560,7 +558,7 @@ __global__ void __launch_bounds__(256) k_slope(SlopeArgs a) {
           Pack<T, 8> o, l;
 #pragma unroll
           for (int e = 0; e < 4; e++) {
-            float2 z, f, g;
+            float2 z;
             if constexpr (kZ == kFloats) {
               z = make_float2(held_z[u].v[2 * e], held_z[u].v[2 * e + 1]);
             } else {
@@ -568,8 +566,7 @@ __global__ void __launch_bounds__(256) k_slope(SlopeArgs a) {
               z = from_e4m3((uint16_t)((e < 2 ? held_z[u].q.x : held_z[u].q.y) >> (e % 2 * 16)));
               z = held<float>(z, scale, held_z[u].code);
             }
-            activate<decltype(k)::value>(z, &f, &g);
-            const float2 v = mul(widen(d[u].v + 2 * e), g);
+            const float2 v = mul(widen(d[u].v + 2 * e), derivative<decltype(k)::value>(z));
             sum[e] = add(sum[e], v);
             narrow(o.v + 2 * e, v);
             if (a.halves) l.v[2 * e] = rest_of(v.x, o.v[2 * e]), l.v[2 * e + 1] = rest_of(v.y, o.v[2 * e + 1]);

@@ -397,15 +397,6 @@ __global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitc
   }
 }
 
-// the aligned 16 bytes at `block`, 0 where they are not of the row
-__device__ __forceinline__ uint4 row_block(const char* block, const char* row, const char* end) {
-  if (block >= row && block + 16 <= end) return *reinterpret_cast<const uint4*>(block);
-  uint32_t e[8];
-#pragma unroll
-  for (int i = 0; i < 8; i++)
-    e[i] = block + 2 * i >= row && block + 2 * i < end ? *reinterpret_cast<const uint16_t*>(block + 2 * i) : 0;
-  return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-}
 __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a) {
   const int w = blockIdx.y, lane = threadIdx.x % 32;
   for (int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; row < a.rows[w]; row += (int64_t)gridDim.x * 8) {
@@ -414,18 +405,7 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
     const int off = (int)(reinterpret_cast<uintptr_t>(from) % 16);  // even, the same for all of the row's pieces
     const char* end = from + a.cols * 2;
     for (int64_t c = lane * 16; c < a.pitch * 2; c += 32 * 16) {
-      const char* block = from + c - off;
-      uint32_t v[9] = {};
-      const uint4 p = row_block(block, from, end), q = off ? row_block(block + 16, from, end) : make_uint4(0, 0, 0, 0);
-      v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
-      v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
-#pragma unroll
-      for (int i = 0; i < 7; i++) v[i] = off & 8 ? v[i + 2] : v[i];
-#pragma unroll
-      for (int i = 0; i < 5; i++) v[i] = off & 4 ? v[i + 1] : v[i];
-      const int bits = off % 4 * 8;
-      *reinterpret_cast<uint4*>(to + c) = make_uint4(__funnelshift_r(v[0], v[1], bits), __funnelshift_r(v[1], v[2], bits),
-                                                     __funnelshift_r(v[2], v[3], bits), __funnelshift_r(v[3], v[4], bits));
+      *reinterpret_cast<uint4*>(to + c) = row_bytes(from + c, from, end, off);
     }
   }
 }

@@ -320,11 +320,11 @@ __global__ void k_rms_columns_long(RmsArgs a) {
 }
 
 // ------------------------------------------------------------------------------------- 8-bit blocks
-// A warp a row (gridDim.y warps, each its share of whole 128s of the columns), V elements a lane.
-template <typename T, int V>
+// A warp a row (gridDim.y warps, each its share of whole 128s of the columns), 16 bytes a lane wherever the rows start.
+template <typename T, bool kVectors>
 __global__ void __launch_bounds__(256) k_quantize(RmsArgs a, int64_t share) {
+  constexpr int V = 16 / sizeof(T), H = kPairs<V>, kUnroll = 4;
   using P = Pairs<V>;
-  constexpr int H = kPairs<V>, kUnroll = 4;
   const int lane = threadIdx.x % 32;
   const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, chunks = (a.cols + 127) / 128;
   const int64_t from = blockIdx.y * share, to = min(from + share, chunks * 128);
@@ -332,13 +332,22 @@ __global__ void __launch_bounds__(256) k_quantize(RmsArgs a, int64_t share) {
   const bool real = row < a.rows;
   const T* x = static_cast<const T*>(a.x) + (real ? row : 0) * a.x_stride;
   uint8_t *values = a.values + row * a.v_stride, *scales = a.scales + scale_at(row, 0, chunks);  // (a row's: 4 of every 512 bytes)
+  const char *begin = reinterpret_cast<const char*>(x), *end = reinterpret_cast<const char*>(x + a.cols);
+  const int off = (int)(reinterpret_cast<uintptr_t>(x) % 16);
   const uint32_t lanes = (0xffffffffu >> (32 - 32 / V)) << (lane / (32 / V) * (32 / V));
   for (int64_t c0 = from + lane * V; c0 < to; c0 += kUnroll * 32 * V) {
     Pack<T, V> p[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; u++) {
       const int64_t c = c0 + u * 32 * V;
-      if (real && c < to && c < a.cols) p[u] = load_pack<T, V>(x + c);
+      if (!real || c >= to || c >= a.cols) continue;
+      if constexpr (kVectors) {
+        p[u] = load_pack<T, V>(x + c);
+      } else {
+        union { uint4 u; Pack<T, V> p; } b;
+        b.u = row_bytes(begin + c * sizeof(T), begin, end, off);
+        p[u] = b.p;
+      }
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; u++) {
@@ -358,35 +367,34 @@ __global__ void __launch_bounds__(256) k_quantize(RmsArgs a, int64_t share) {
 
 template <typename T, bool kVectors>
 __global__ void __launch_bounds__(256) k_dequantize(RmsArgs a, int64_t share) {
+  constexpr int kUnroll = 4;
+  __shared__ T staging[kVectors ? 1 : 8][256];
   const int lane = threadIdx.x % 32;
   const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, chunks = (a.cols + 127) / 128;
   const int64_t from = blockIdx.y * share, to = min(from + share, a.cols);
   if (row >= a.rows) return;
   T* y = static_cast<T*>(a.y) + row * a.y_stride;
   const uint8_t *values = a.values + row * a.v_stride, *scales = a.scales + scale_at(row, 0, chunks);
-  constexpr int kUnroll = 4;
-  for (int64_t c0 = from + lane * 8; c0 < to; c0 += kUnroll * 256) {
+  for (int64_t first = from; first < to; first += kUnroll * 256) {
     uint2 words[kUnroll];
     uint32_t codes[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; u++) {
-      const int64_t c = c0 + u * 256;
+      const int64_t c = first + u * 256 + lane * 8;
       if (c >= to) continue;
       words[u] = *reinterpret_cast<const uint2*>(values + c);
       codes[u] = scales[c / 128 * 512 + (c / 32 & 3)];
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; u++) {
-      const int64_t c = c0 + u * 256;
-      if (c >= to) break;
-      const uint2 q = words[u];
-      const float scale = block_scale(codes[u]);
-      const uint16_t pairs[4] = {(uint16_t)q.x, (uint16_t)(q.x >> 16), (uint16_t)q.y, (uint16_t)(q.y >> 16)};
+      const int64_t c0 = first + u * 256, c = c0 + lane * 8;
+      if (c0 >= to) break;
       Pack<T, 8> out;
+      if (c < to) {
+        const float scale = block_scale(codes[u]);
 #pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const float2 v = from_e4m3(pairs[e]);
-        narrow(out.v + 2 * e, held<T>(v, scale, codes[u]));
+        for (int e = 0; e < 4; e++)
+          narrow(out.v + 2 * e, held<T>(from_e4m3((uint16_t)((e < 2 ? words[u].x : words[u].y) >> (e % 2 * 16))), scale, codes[u]));
       }
       if (kVectors && c + 8 <= a.cols) {
         if constexpr (sizeof(T) == 2) {
@@ -395,10 +403,21 @@ __global__ void __launch_bounds__(256) k_dequantize(RmsArgs a, int64_t share) {
           *reinterpret_cast<float4*>(y + c) = make_float4(out.v[0], out.v[1], out.v[2], out.v[3]);
           *reinterpret_cast<float4*>(y + c + 4) = make_float4(out.v[4], out.v[5], out.v[6], out.v[7]);
         }
-      } else {
+      } else if (kVectors) {
 #pragma unroll
         for (int e = 0; e < 8; e++)
           if (c + e < a.cols) y[c + e] = out.v[e];
+      } else {  // by way of shared memory, so that a warp stores neighbours
+        T* mine = staging[threadIdx.x / 32];
+        if (c < to) {
+#pragma unroll
+          for (int e = 0; e < 8; e++) mine[lane * 8 + e] = out.v[e];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+          if (c0 + e * 32 + lane < a.cols) y[c0 + e * 32 + lane] = mine[e * 32 + lane];
+        __syncwarp();
       }
     }
   }
@@ -480,10 +499,8 @@ cudaError_t quantize(const RmsArgs& a, cudaStream_t s) {
   int64_t share;
   const dim3 grid = block_grid((a.rows + 127) / 128 * 128, a.cols, &share);
   const int width = load_width<T>(a.rows, a.cols, 0, {}, {{a.x, a.x_stride}});
-  constexpr int V = 16 / sizeof(T);
-  if (width == V) k_quantize<T, V><<<grid, 256, 0, s>>>(a, share);
-  else if (width == 2) k_quantize<T, 2><<<grid, 256, 0, s>>>(a, share);
-  else k_quantize<T, 1><<<grid, 256, 0, s>>>(a, share);
+  if (width == 16 / (int)sizeof(T)) k_quantize<T, true><<<grid, 256, 0, s>>>(a, share);
+  else k_quantize<T, false><<<grid, 256, 0, s>>>(a, share);
   return cudaGetLastError();
 }
 template <typename T>

@@ -57,6 +57,32 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
   }
 }
 
+// the aligned 16 bytes at `block`, 0 where they are not of the row
+__device__ __forceinline__ uint4 row_block(const char* block, const char* row, const char* end) {
+  if (block >= row && block + 16 <= end) return *reinterpret_cast<const uint4*>(block);
+  uint32_t e[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    e[i] = block + 2 * i >= row && block + 2 * i < end ? *reinterpret_cast<const uint16_t*>(block + 2 * i) : 0;
+  return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+}
+// 16 bytes at `at` of the row [row, end), 0 where they are not of it, out of the one or two aligned blocks that hold them; off: how
+// far the row starts behind such a block (even)
+__device__ __forceinline__ uint4 row_bytes(const char* at, const char* row, const char* end, int off) {
+  const char* block = at - off;
+  uint32_t v[9] = {};
+  const uint4 p = row_block(block, row, end), q = off ? row_block(block + 16, row, end) : make_uint4(0, 0, 0, 0);
+  v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w;
+  v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
+#pragma unroll
+  for (int i = 0; i < 7; i++) v[i] = off & 8 ? v[i + 2] : v[i];
+#pragma unroll
+  for (int i = 0; i < 5; i++) v[i] = off & 4 ? v[i + 1] : v[i];
+  const int bits = off % 4 * 8;
+  return make_uint4(__funnelshift_r(v[0], v[1], bits), __funnelshift_r(v[1], v[2], bits), __funnelshift_r(v[2], v[3], bits),
+                    __funnelshift_r(v[3], v[4], bits));
+}
+
 // Pairs of binary32 values, which one instruction adds, multiplies or fuses (sm_100 and later); a lone value
 // has the same operations, so a kernel is written once for packs of 8, 4 and 1 elements.
 __device__ __forceinline__ uint64_t bits(float2 v) {
