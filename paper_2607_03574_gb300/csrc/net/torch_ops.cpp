@@ -11,6 +11,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
 
@@ -339,71 +340,114 @@ variable_list rms_forward(const Tensor& x, const Tensor& weight, const Tensor& r
                                       rstd ? static_cast<float*>(out(*rstd)) : nullptr, stream_of(x.get_device())));
   return sum.defined() ? variable_list{y, sum} : variable_list{y};
 }
-struct RmsNorm : torch::autograd::Function<RmsNorm> {
-  static variable_list forward(AutogradContext* ctx, const Tensor& x, const Maybe& w, const Maybe& r, double eps) {
-    const Tensor weight = some(w), residual = some(r);
-    Tensor rstd;
-    variable_list y = rms_forward(x, weight, residual, eps, &rstd);
-    ctx->save_for_backward({residual.defined() ? y[1] : x, weight, rstd});
-    ctx->saved_data["residual"] = residual.defined();
-    ctx->set_materialize_grads(false);
-    return y;
+// The nodes of the norm and of the dense layers are plain ones: a Function's context costs 10 us more a pass (forward and backward
+// on small inputs: norm 148 us, dense layer 167; a plain product of torch 121).  Each is made when its outputs are there;
+// edges are those of its inputs in order, undefined ones among them.
+using torch::autograd::SavedVariable;
+template <typename N>
+std::shared_ptr<N> new_node(std::initializer_list<const Tensor*> inputs) {
+  std::shared_ptr<N> node(new N(), torch::autograd::deleteNode);
+  torch::autograd::edge_list edges;
+  edges.reserve(inputs.size());
+  for (const Tensor* t : inputs) edges.push_back(t->defined() ? torch::autograd::impl::gradient_edge(*t) : torch::autograd::Edge());
+  node->set_next_edges(std::move(edges));
+  return node;
+}
+
+struct RmsNormBackward : torch::autograd::Node {
+  SavedVariable s, weight;
+  Tensor rstd;
+  bool residual = false, weighted = false;
+  std::string name() const override { return "RmsNormBackward"; }
+  void release_variables() override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    s.reset_data();
+    weight.reset_data();
+    rstd.reset();
   }
-  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+  variable_list apply(variable_list&& grads) override {
+    std::lock_guard<std::mutex> lock(mutex_);
     for (const Tensor& g : grads)
       if (g.defined()) first_order(g);
-    const variable_list saved = ctx->get_saved_variables();
-    const Tensor &s = saved[0], &weight = saved[1], &rstd = saved[2];
-    const bool residual = ctx->saved_data["residual"].toBool(), weighted = weight.defined();
-    const bool want_x = ctx->needs_input_grad(0), want_r = residual && ctx->needs_input_grad(weighted ? 2 : 1);
+    const Tensor dsum = residual && grads[1].defined() ? rowed(grads[1]) : Tensor();
+    const bool want_x = task_should_compute_output(0), want_w = weighted && task_should_compute_output(1), want_r = residual && task_should_compute_output(2);
+    const Tensor saved = s.unpack(residual ? getptr() : nullptr), w = weighted ? weight.unpack() : Tensor();
     Tensor dx, dw;
-    if (weighted && ctx->needs_input_grad(1)) dw = at::empty({s.size(-1)}, weight.options());
+    if (want_w) dw = at::empty({saved.size(-1)}, w.options());
     if (!grads[0].defined()) {  // (the sum alone has a cotangent, or nothing has)
-      if (dw.defined()) dw.zero_();
+      if (want_w) dw.zero_();
       dx = residual ? grads[1] : Tensor();
     } else {
-      const Rows r(s);
-      const Tensor dy = rowed(grads[0]), dsum = residual && grads[1].defined() ? rowed(grads[1]) : Tensor();
-      if (want_x || want_r) dx = at::empty(s.sizes(), s.options());
-      const size_t need = dw.defined() ? ndvm_rms_norm_workspace_bytes(r.rows, r.cols) : 0;
-      Tensor ws = bytes(need, s);
-      check_backward(ndvm_rms_norm_backward((ndvm_dtype)type_code(s), (ndvm_dtype)weight_code(weight, s), r.rows, r.cols, in(dy), Rows(dy).stride,
-                                            in(dsum), dsum.defined() ? Rows(dsum).stride : 0, in(s), r.stride, in(weight),
-                                            static_cast<const float*>(in(rstd)), out(dx), r.cols, out(dw), out(ws), need, stream_of(s.get_device())));
+      const Rows r(saved);
+      const Tensor dy = rowed(grads[0]);
+      if (want_x || want_r) dx = at::empty(saved.sizes(), saved.options());
+      const size_t need = want_w ? ndvm_rms_norm_workspace_bytes(r.rows, r.cols) : 0;
+      Tensor ws = bytes(need, saved);
+      check_backward(ndvm_rms_norm_backward((ndvm_dtype)type_code(saved), (ndvm_dtype)weight_code(w, saved), r.rows, r.cols, in(dy), Rows(dy).stride,
+                                            in(dsum), dsum.defined() ? Rows(dsum).stride : 0, in(saved), r.stride, in(w),
+                                            static_cast<const float*>(in(rstd)), out(dx), r.cols, out(dw), out(ws), need,
+                                            stream_of(saved.get_device())));
     }
-    return {want_x ? dx : Tensor(), dw, want_r ? dx : Tensor(), Tensor()};
+    return {want_x ? dx : Tensor(), dw, want_r ? dx : Tensor()};
   }
 };
+variable_list rms_recorded(const Tensor& x, const Tensor& weight, const Tensor& residual, double eps) {
+  Tensor rstd;
+  variable_list y;
+  {
+    at::AutoDispatchBelowADInplaceOrView below;
+    y = rms_forward(x, weight, residual, eps, &rstd);
+  }
+  const auto node = new_node<RmsNormBackward>({&x, &weight, &residual});
+  node->residual = residual.defined();
+  node->weighted = weight.defined();
+  for (Tensor& t : y) torch::autograd::set_history(t, node);
+  node->s = residual.defined() ? SavedVariable(y[1], true) : SavedVariable(x, false);
+  if (weight.defined()) node->weight = SavedVariable(weight, false);
+  node->rstd = rstd;
+  return y;
+}
 std::optional<variable_list> rms_norm(const Tensor& given, const Maybe& w, double eps, const Maybe& r) {
   Tensor x, weight, residual;
   if (!norm_arguments(given, w, r, &x, &weight, &residual)) return std::nullopt;
-  return recorded({&x, &weight, &residual}) ? RmsNorm::apply(x, maybe(weight), maybe(residual), eps) : rms_forward(x, weight, residual, eps, nullptr);
+  return recorded({&x, &weight, &residual}) ? rms_recorded(x, weight, residual, eps) : rms_forward(x, weight, residual, eps, nullptr);
 }
 
 // --------------------------------------------------------------------------------- 8-bit blocks
 constexpr const char* kNoGradient = "the operators on 8-bit blocks have no gradients: call them under torch.no_grad()";
 struct Blocks {
-  Tensor values, scales;  // values: rows of `stride` bytes
+  Tensor values, scales;  // values: of the given shape, rows of `stride` bytes
   int64_t rows, cols, stride;
-  Blocks(const Tensor& like, int64_t rows, int64_t cols) : rows(rows), cols(cols), stride((cols + 15) / 16 * 16) {
-    values = at::empty({rows, stride}, like.options().dtype(at::kFloat8_e4m3fn));
+  Blocks(const Tensor& like, at::IntArrayRef sizes, int64_t rows) : rows(rows), cols(sizes.back()), stride((cols + 15) / 16 * 16) {
+    const auto options = like.options().dtype(at::kFloat8_e4m3fn);
+    if (stride == cols) {
+      values = at::empty(sizes, options);
+    } else {
+      auto strides = sizes.vec();
+      int64_t step = stride;
+      strides.back() = 1;
+      for (int64_t d = (int64_t)sizes.size() - 2; d >= 0; d--) strides[d] = step, step *= std::max<int64_t>(sizes[d], 1);
+      values = at::empty({rows, stride}, options).as_strided(sizes, strides);
+    }
     scales = at::empty({(rows + 127) / 128, (cols + 127) / 128, 32, 4, 4}, like.options().dtype(at::kByte));
   }
   uint8_t* v() const { return static_cast<uint8_t*>(out(values)); }
   uint8_t* s() const { return static_cast<uint8_t*>(out(scales)); }
-  Tensor shaped(at::IntArrayRef sizes) const {  // the values as a tensor of that shape
-    auto strides = sizes.vec();
-    int64_t step = stride;
-    strides.back() = 1;
-    for (int64_t d = (int64_t)sizes.size() - 2; d >= 0; d--) strides[d] = step, step *= std::max<int64_t>(sizes[d], 1);
-    return values.as_strided(sizes, strides);
-  }
 };
 using Held = std::tuple<Tensor, Tensor, int64_t, int64_t, int64_t>;  // values, scales, rows, cols, stride
 
+// (rows, cols, row stride) of what may be 8-bit blocks, or nothing
+std::optional<std::tuple<int64_t, int64_t, int64_t>> blocks_of(const Tensor& values, const Tensor& scales) {
+  if (!values.is_cuda() || values.scalar_type() != at::kFloat8_e4m3fn || scales.scalar_type() != at::kByte || scales.device() != values.device()) return std::nullopt;
+  const Rows r(values);
+  if (!r.ok || (r.rows > 1 && (r.stride % 16 || r.stride < r.cols)) || (uintptr_t)in(values) % 16) return std::nullopt;
+  const int64_t shape[5] = {(r.rows + 127) / 128, (r.cols + 127) / 128, 32, 4, 4};
+  if (scales.sizes() != at::IntArrayRef(shape) || !scales.is_contiguous() || (uintptr_t)in(scales) % 16) return std::nullopt;
+  return std::make_tuple(r.rows, r.cols, r.stride);
+}
 Blocks to_blocks(const Tensor& x) {
   const Rows r(x);
-  Blocks b(x, r.rows, r.cols);
+  Blocks b(x, x.sizes(), r.rows);
   check_forward(ndvm_quantize((ndvm_dtype)type_code(x), r.rows, r.cols, in(x), r.stride, b.v(), b.stride, b.s(), stream_of(x.get_device())));
   return b;
 }
@@ -414,7 +458,7 @@ std::optional<Held> quantize(const Tensor& given) {
   if (recorded({&given})) raise_forward(NDVM_E_UNSUPPORTED, kNoGradient);
   const Tensor x = rowed(given);
   const Blocks b = to_blocks(x);
-  return Held{b.shaped(x.sizes()), b.scales, b.rows, b.cols, b.stride};
+  return Held{b.values, b.scales, b.rows, b.cols, b.stride};
 }
 std::optional<std::tuple<Tensor, Tensor, int64_t, int64_t, int64_t, Tensor>> rms_norm_quantized(const Tensor& given, const Maybe& w, double eps,
                                                                                                 const Maybe& r) {
@@ -422,12 +466,12 @@ std::optional<std::tuple<Tensor, Tensor, int64_t, int64_t, int64_t, Tensor>> rms
   if (!norm_arguments(given, w, r, &x, &weight, &residual)) return std::nullopt;
   if (recorded({&x, &weight, &residual})) raise_forward(NDVM_E_UNSUPPORTED, kNoGradient);
   const Rows rows(x);
-  const Blocks b(x, rows.rows, rows.cols);
+  const Blocks b(x, x.sizes(), rows.rows);
   if (residual.defined()) sum = at::empty(x.sizes(), x.options());
   check_forward(ndvm_rms_norm_quantized((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(weight, x), rows.rows, rows.cols, in(x), rows.stride, in(residual),
                                         residual.defined() ? Rows(residual).stride : 0, in(weight), eps, b.v(), b.stride, b.s(), out(sum), rows.cols,
                                         stream_of(x.get_device())));
-  return std::make_tuple(b.shaped(x.sizes()), b.scales, b.rows, b.cols, b.stride, sum);
+  return std::make_tuple(b.values, b.scales, b.rows, b.cols, b.stride, sum);
 }
 
 // ---------------------------------------------------------------------------------- dense layers
@@ -459,65 +503,88 @@ Tensor linear_forward(const Tensor& x, const Tensor& w, const Tensor& bias, int6
                                     stream_of(x.get_device())));
   return y;
 }
-struct Linear : torch::autograd::Function<Linear> {
-  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Maybe& b, const Maybe& r, int64_t act, bool eight) {
-    const Tensor bias = some(b), residual = some(r);
-    const Rows rx(x);
-    const int64_t n = w.size(0);
-    Tensor z, y;
-    // what the gradients need: z of an activation, and x for w's
-    const bool activated = act != NDVM_ACT_NONE, wants_w = w.requires_grad(), wants_z = activated && (wants_w || x.requires_grad() || (bias.defined() && bias.requires_grad()));
-    if (eight) {
-      Tensor xv, xs, zs;
-      if (wants_w) {
-        const Blocks held = to_blocks(x);
-        xv = held.values, xs = held.scales;
-      }
-      std::optional<Blocks> blocks;
-      if (wants_z) blocks.emplace(x, rx.rows, n), z = blocks->values, zs = blocks->scales;
-      y = linear_forward(x, w, bias, act, residual, Tensor(), blocks ? &*blocks : nullptr);
-      ctx->save_for_backward({xv, xs, w, z, zs});
-    } else {
-      if (wants_z) z = at::empty({rx.rows, ndvm_linear_kept_stride(n)}, x.options().dtype(at::kFloat));
-      y = linear_forward(x, w, bias, act, residual, z, nullptr);
-      ctx->save_for_backward({wants_w ? x : Tensor(), Tensor(), w, z, Tensor()});
-    }
-    ctx->saved_data["act"] = act;
-    ctx->saved_data["x"] = x.sizes();
-    ctx->saved_data["eight"] = eight;
-    ctx->saved_data["bias"] = bias.defined() ? (int64_t)bias.scalar_type() : (int64_t)-1;
-    ctx->saved_data["residual"] = residual.defined();
-    return y;
+struct LinearBackward : torch::autograd::Node {
+  SavedVariable x, w;  // (x: where it is held as it is)
+  Tensor x_values, x_scales, z, z_scales;
+  std::vector<int64_t> sizes;  // x's
+  int64_t act = 0, pitch = 0;  // (of x's blocks)
+  at::ScalarType btype = at::kFloat;
+  bool eight = false, biased = false, wants_w = false;
+  std::string name() const override { return "LinearBackward"; }
+  void release_variables() override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    x.reset_data();
+    w.reset_data();
+    for (Tensor* t : {&x_values, &x_scales, &z, &z_scales}) t->reset();
   }
-  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+  variable_list apply(variable_list&& grads) override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    if (!grads[0].defined()) return {Tensor(), Tensor(), Tensor(), Tensor()};
     first_order(grads[0]);
-    const variable_list saved = ctx->get_saved_variables();
-    const Tensor &x = saved[0], &xs = saved[1], &w = saved[2], &z = saved[3], &zs = saved[4], dy = rowed(grads[0]);
-    const int64_t act = ctx->saved_data["act"].toInt(), n = w.size(0), k = w.size(1), btype = ctx->saved_data["bias"].toInt();
-    const auto sizes = ctx->saved_data["x"].toIntVector();
-    const bool eight = ctx->saved_data["eight"].toBool(), biased = btype >= 0, residual = ctx->saved_data["residual"].toBool();
-    const Rows rd(dy), rw(w);
-    Tensor dx, dw, db;  // (the node's inputs are x, w and those of bias and residual that there are)
-    if (ctx->needs_input_grad(0)) dx = at::empty(sizes, dy.options());
-    if (ctx->needs_input_grad(1)) dw = at::empty({n, k}, dy.options());
-    if (biased && ctx->needs_input_grad(2)) db = at::empty({n}, dy.options().dtype((at::ScalarType)btype));
+    const Tensor weight = w.unpack(), given = wants_w && !eight ? x.unpack() : Tensor();  // (which raise where they were released)
+    const Tensor dy = rowed(grads[0]);
+    const int64_t n = weight.size(0), k = weight.size(1);
+    const Rows rd(dy), rw(weight);
+    Tensor dx, dw, db;
+    if (task_should_compute_output(0)) dx = at::empty(sizes, dy.options());
+    if (task_should_compute_output(1)) dw = at::empty({n, k}, dy.options());
+    if (biased && task_should_compute_output(2)) db = at::empty({n}, dy.options().dtype(btype));
     if (dx.defined() || dw.defined() || db.defined()) {
       const bool held = eight && dw.defined();
       std::optional<Rows> rx;
-      if (!eight && x.defined()) rx.emplace(x);
+      if (given.defined()) rx.emplace(given);
       const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rd.rows, k, n, 1,
-                                                      (!rx || ready(x, *rx)) && ready(w, rw) && ready(dy, rd), held);
+                                                      (!rx || ready(given, *rx)) && ready(weight, rw) && ready(dy, rd), held);
       Tensor ws = bytes(need, dy);
       check_backward(ndvm_linear_backward(
-          (ndvm_dtype)type_code(dy), db.defined() && btype == (int64_t)at::kFloat ? NDVM_F32 : (ndvm_dtype)type_code(dy), (ndvm_activation)act, rd.rows, k, n,
-          in(dy), rd.stride, rx ? in(x) : nullptr, rx ? rx->stride : 0, held ? static_cast<const uint8_t*>(in(x)) : nullptr, held ? x.size(-1) : 0,
-          held ? static_cast<const uint8_t*>(in(xs)) : nullptr, in(w), rw.stride, eight ? nullptr : static_cast<const float*>(in(z)),
-          eight ? static_cast<const uint8_t*>(in(z)) : nullptr, eight ? static_cast<const uint8_t*>(in(zs)) : nullptr, out(dx), k, out(dw), out(db), out(ws),
-          need, stream_of(dy.get_device())));
+          (ndvm_dtype)type_code(dy), db.defined() && btype == at::kFloat ? NDVM_F32 : (ndvm_dtype)type_code(dy), (ndvm_activation)act, rd.rows, k, n,
+          in(dy), rd.stride, rx ? in(given) : nullptr, rx ? rx->stride : 0, held ? static_cast<const uint8_t*>(in(x_values)) : nullptr,
+          pitch, held ? static_cast<const uint8_t*>(in(x_scales)) : nullptr, in(weight), rw.stride,
+          eight ? nullptr : static_cast<const float*>(in(z)), eight ? static_cast<const uint8_t*>(in(z)) : nullptr,
+          eight ? static_cast<const uint8_t*>(in(z_scales)) : nullptr, out(dx), k, out(dw), out(db), out(ws), need, stream_of(dy.get_device())));
     }
-    return {dx, dw, db, residual && ctx->needs_input_grad(biased ? 3 : 2) ? grads[0] : Tensor(), Tensor(), Tensor()};
+    return {dx, dw, db, task_should_compute_output(3) ? grads[0] : Tensor()};
   }
 };
+Tensor linear_recorded(const Tensor& x, const Tensor& w, const Tensor& bias, const Tensor& residual, int64_t act, bool eight) {
+  const Rows rx(x);
+  const int64_t n = w.size(0);
+  // what the gradients need: z of an activation, and x for w's
+  const bool wants_w = w.requires_grad();
+  const bool wants_z = act != NDVM_ACT_NONE && (wants_w || x.requires_grad() || (bias.defined() && bias.requires_grad()));
+  Tensor y, z, x_values, x_scales, z_scales;
+  int64_t pitch = 0;
+  {
+    at::AutoDispatchBelowADInplaceOrView below;
+    std::optional<Blocks> blocks;
+    if (eight && wants_w) {
+      const Blocks held = to_blocks(x);
+      x_values = held.values, x_scales = held.scales, pitch = held.stride;
+    }
+    if (eight && wants_z) {
+      blocks.emplace(x, at::IntArrayRef({rx.rows, n}), rx.rows);
+      z = blocks->values, z_scales = blocks->scales;
+    } else if (wants_z) {
+      z = at::empty({rx.rows, ndvm_linear_kept_stride(n)}, x.options().dtype(at::kFloat));
+    }
+    y = linear_forward(x, w, bias, act, residual, eight ? Tensor() : z, blocks ? &*blocks : nullptr);
+  }
+  const auto node = new_node<LinearBackward>({&x, &w, &bias, &residual});
+  torch::autograd::set_history(y, node);
+  node->w = SavedVariable(w, false);
+  if (wants_w && !eight) node->x = SavedVariable(x, false);
+  node->x_values = x_values;
+  node->x_scales = x_scales;
+  node->pitch = pitch;
+  node->z = z;
+  node->z_scales = z_scales;
+  node->sizes = x.sizes().vec();
+  node->act = act;
+  node->eight = eight;
+  node->wants_w = wants_w;
+  if ((node->biased = bias.defined())) node->btype = bias.scalar_type();
+  return y;
+}
 Maybe linear(const Tensor& gx, const Tensor& gw, const Maybe& b, int64_t act, const Maybe& r, bool eight) {
   if (!gx.is_cuda()) return std::nullopt;
   const int device = c10::cuda::current_device();
@@ -529,7 +596,7 @@ Maybe linear(const Tensor& gx, const Tensor& gw, const Maybe& b, int64_t act, co
   if (!linear_extras(device, b, r, gw.size(0), shape, gx.scalar_type(), &bias, &residual)) return std::nullopt;
   const Tensor x = rowed(gx), w = rowed(gw);
   check_inputs({&x, &w, &bias, &residual});
-  if (recorded({&x, &w, &bias, &residual})) return Linear::apply(x, w, maybe(bias), maybe(residual), act, eight);
+  if (recorded({&x, &w, &bias, &residual})) return linear_recorded(x, w, bias, residual, act, eight);
   return linear_forward(x, w, bias, act, residual, Tensor(), nullptr);
 }
 Maybe linear_quantized(const Tensor& xv, const Tensor& xs, int64_t rows, int64_t k, int64_t x_stride, const Tensor& wv, const Tensor& ws, int64_t n,
@@ -575,6 +642,10 @@ PYBIND11_MODULE(ndvm_torch, m) {
   });
   m.def("quantize", [](const Tensor& x) {
     HANDLE_TH_ERRORS return quantize(x);
+    END_HANDLE_TH_ERRORS_PYBIND
+  });
+  m.def("blocks_of", [](const Tensor& values, const Tensor& scales) {
+    HANDLE_TH_ERRORS return blocks_of(values, scales);
     END_HANDLE_TH_ERRORS_PYBIND
   });
   m.def("rms_norm_quantized", [](const Tensor& x, const Maybe& weight, double eps, const Maybe& residual) {

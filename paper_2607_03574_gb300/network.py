@@ -466,6 +466,16 @@ class Quantized:
     __slots__ = ("values", "scales", "rows", "cols", "stride")
 
     def __init__(self, values, scales):
+        try:
+            sizes = (_ops or _load_ops()).blocks_of(values, scales)
+        except TypeError:
+            sizes = None
+        self.values, self.scales = values, scales
+        self.rows, self.cols, self.stride = sizes or self._sizes(values, scales)
+
+    @staticmethod
+    def _sizes(values, scales):
+        """(rows, cols, row stride), or what is wrong."""
         torch = _torch_module or _start()
         if values.dtype != torch.float8_e4m3fn or scales.dtype != torch.uint8:
             raise NdvmError(3, "8-bit blocks are float8_e4m3fn values with uint8 scales")
@@ -476,7 +486,7 @@ class Quantized:
             raise NdvmError(1, "values must be rows that start on 16 bytes")
         if scales.shape != (-(-rows // 128), -(-cols // 128), 32, 4, 4) or not scales.is_contiguous() or scales.data_ptr() % 16:
             raise NdvmError(1, f"scales must be contiguous, of shape {(-(-rows // 128), -(-cols // 128), 32, 4, 4)}, and start on 16 bytes")
-        self.values, self.scales, self.rows, self.cols, self.stride = values, scales, rows, cols, stride
+        return rows, cols, stride
 
     @classmethod
     def _of(cls, values, scales, rows, cols, stride):
