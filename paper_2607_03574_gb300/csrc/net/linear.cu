@@ -161,6 +161,10 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
   const int rank = kCtas == 1 ? 0 : (int)tc::cluster_rank(), unit = blockIdx.x / kCtas, units = gridDim.x / kCtas;
   volatile int* stop = &s_stop;
 
+  if (threadIdx.x == 32) {
+    tc::prefetch_map(&p.a), tc::prefetch_map(&p.b);
+    if (kEight) tc::prefetch_map(&p.a_scales), tc::prefetch_map(&p.b_scales);
+  }
   if (threadIdx.x == 0) {
     s_stop = 0;
     for (int i = 0; i < S; i++) tc::barrier_init(full(i), 1), tc::barrier_init(empty(i), 1);
@@ -723,7 +727,8 @@ bool x_ready(const LinearArgs& a) { return a.x && tma_ready(a.x, a.x_stride, a.r
 bool w_ready(const LinearArgs& a) { return tma_ready(a.w, a.w_stride, a.n, a.k); }
 bool dy_ready(const LinearArgs& a) { return tma_ready(a.dy, a.dy_stride, a.rows, a.n); }
 
-int64_t slope_splits(int64_t rows, int64_t n) { return std::clamp<int64_t>(kSms * 6 / ceil_div(n, 256), 1, ceil_div(rows, 8)); }
+// row ranges of k_slope: as many blocks as stay resident
+int64_t slope_splits(int64_t rows, int64_t n) { return std::clamp<int64_t>(kSms * 3 / ceil_div(n, 256), 1, ceil_div(rows, 8)); }
 
 struct Layout {
   int64_t k_pitch, n_pitch;

@@ -194,11 +194,19 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
   const auto ask_rstd = [&](int64_t row) {
     if (row < a.rows) nrstd = a.rstd[row];
   };
+  // weights stay in registers where the ring has left room for them
+  P w[N][H];
+  const auto ask_weight = [&](int j) {
+    const int c = (j * kRow + t) * V;
+    if (c < cols) load_weight<T, V>(w[j], a.weight, w_f32, c, 1.0f);
+  };
   int64_t row = (int64_t)blockIdx.x * kBlockRows + group;
   ask_rstd(row);
   if constexpr (D > 0) {
 #pragma unroll
     for (int q = 0; q < D - 1; q++) fetch(row + q * step, q);
+#pragma unroll
+    for (int j = 0; j < N; j++) ask_weight(j);
   } else {
     fetch(row, 0);
   }
@@ -217,8 +225,7 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
     for (int j = 0; j < N; j++) {
       const int c = (j * kRow + t) * V;
       if (c >= cols) continue;
-      P w[H];
-      load_weight<T, V>(w, a.weight, w_f32, c, 1.0f);
+      if constexpr (D == 0) ask_weight(j);
       if constexpr (D > 0) {
         nx[j] = load_pack<T, V>(reinterpret_cast<const T*>(ring + pack_at(slot, 0, j)));
         nd[j] = load_pack<T, V>(reinterpret_cast<const T*>(ring + pack_at(slot, 1, j)));
@@ -231,7 +238,7 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
       for (int e = 0; e < H; e++) {
         sh[j][e] = mul(sh[j][e], scale);
         dw[j][e] = fma(g[j][e], sh[j][e], dw[j][e]);
-        g[j][e] = mul(g[j][e], w[e]);
+        g[j][e] = mul(g[j][e], w[j][e]);
         sgs = fma(g[j][e], sh[j][e], sgs);
       }
     }

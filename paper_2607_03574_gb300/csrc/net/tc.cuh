@@ -82,6 +82,8 @@ __device__ __forceinline__ bool elect() {
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
   return ok != 0;
 }
+// asks for a tensor's map ahead of its first copy
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // a box of the tensor at (x, y) to shared memory; its bytes count on the barrier (which for a pair is in_first's)
 template <int kCtas>
 __device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
