@@ -95,7 +95,7 @@ def _compile_torch_ops() -> str:
 def _link_torch_ops(obj: str) -> None:
     lib = os.path.join(_torch_root(), "lib")
     tmp = TORCH_OPS + f".tmp{os.getpid()}"
-    cmd = ["g++", "-shared", "-o", tmp, obj, "-L" + lib, "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ltorch_python",
+    cmd = ["g++", "-shared", "-o", tmp, obj, "-L" + lib, "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-ltorch_python",
            "-L" + OUT_DIR, "-l:libndvm.so", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

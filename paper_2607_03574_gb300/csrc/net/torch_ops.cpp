@@ -5,6 +5,7 @@
 // A function returns None where an argument is not what the operator takes; the Python layer's raw call
 // then says what is wrong with it.
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/AutogradState.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -309,6 +310,10 @@ Maybe gated(const Tensor& gx, const Tensor& gg, const Tensor& gu, int64_t act, i
 }
 
 // ------------------------------------------------------------------------------------- rms norm
+// An uninitialised tensor beside `like`, straight from the allocator (dispatching it costs as much again).
+Tensor fresh(at::IntArrayRef sizes, const Tensor& like, at::ScalarType type) { return at::detail::empty_cuda(sizes, type, like.device(), std::nullopt); }
+Tensor fresh(at::IntArrayRef sizes, const Tensor& like) { return fresh(sizes, like, like.scalar_type()); }
+
 // (x, weight or undefined, residual or undefined) as the operator takes them; false: not its arguments
 bool norm_arguments(const Tensor& given, const Maybe& w, const Maybe& r, Tensor* x, Tensor* weight, Tensor* residual) {
   if (!given.is_cuda()) return false;
@@ -332,9 +337,9 @@ int weight_code(const Tensor& weight, const Tensor& x) { return weight.defined()
 // {y} or {y, sum}
 variable_list rms_forward(const Tensor& x, const Tensor& weight, const Tensor& residual, double eps, Tensor* rstd) {
   const Rows r(x);
-  Tensor y = at::empty(x.sizes(), x.options()), sum;
-  if (residual.defined()) sum = at::empty(x.sizes(), x.options());
-  if (rstd) *rstd = at::empty({r.rows}, x.options().dtype(at::kFloat));
+  Tensor y = fresh(x.sizes(), x), sum;
+  if (residual.defined()) sum = fresh(x.sizes(), x);
+  if (rstd) *rstd = fresh({r.rows}, x, at::kFloat);
   check_forward(ndvm_rms_norm_forward((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(weight, x), r.rows, r.cols, in(x), r.stride, in(residual),
                                       residual.defined() ? Rows(residual).stride : 0, in(weight), eps, out(y), r.cols, out(sum), r.cols,
                                       rstd ? static_cast<float*>(out(*rstd)) : nullptr, stream_of(x.get_device())));
@@ -373,16 +378,16 @@ struct RmsNormBackward : torch::autograd::Node {
     const bool want_x = task_should_compute_output(0), want_w = weighted && task_should_compute_output(1), want_r = residual && task_should_compute_output(2);
     const Tensor saved = s.unpack(residual ? getptr() : nullptr), w = weighted ? weight.unpack() : Tensor();
     Tensor dx, dw;
-    if (want_w) dw = at::empty({saved.size(-1)}, w.options());
+    if (want_w) dw = fresh({saved.size(-1)}, w);
     if (!grads[0].defined()) {  // (the sum alone has a cotangent, or nothing has)
       if (want_w) dw.zero_();
       dx = residual ? grads[1] : Tensor();
     } else {
       const Rows r(saved);
       const Tensor dy = rowed(grads[0]);
-      if (want_x || want_r) dx = at::empty(saved.sizes(), saved.options());
+      if (want_x || want_r) dx = fresh(saved.sizes(), saved);
       const size_t need = want_w ? ndvm_rms_norm_workspace_bytes(r.rows, r.cols) : 0;
-      Tensor ws = bytes(need, saved);
+      Tensor ws = need ? fresh({(int64_t)need}, saved, at::kByte) : Tensor();
       check_backward(ndvm_rms_norm_backward((ndvm_dtype)type_code(saved), (ndvm_dtype)weight_code(w, saved), r.rows, r.cols, in(dy), Rows(dy).stride,
                                             in(dsum), dsum.defined() ? Rows(dsum).stride : 0, in(saved), r.stride, in(w),
                                             static_cast<const float*>(in(rstd)), out(dx), r.cols, out(dw), out(ws), need,
@@ -419,17 +424,16 @@ struct Blocks {
   Tensor values, scales;  // values: of the given shape, rows of `stride` bytes
   int64_t rows, cols, stride;
   Blocks(const Tensor& like, at::IntArrayRef sizes, int64_t rows) : rows(rows), cols(sizes.back()), stride((cols + 15) / 16 * 16) {
-    const auto options = like.options().dtype(at::kFloat8_e4m3fn);
     if (stride == cols) {
-      values = at::empty(sizes, options);
+      values = fresh(sizes, like, at::kFloat8_e4m3fn);
     } else {
       auto strides = sizes.vec();
       int64_t step = stride;
       strides.back() = 1;
       for (int64_t d = (int64_t)sizes.size() - 2; d >= 0; d--) strides[d] = step, step *= std::max<int64_t>(sizes[d], 1);
-      values = at::empty({rows, stride}, options).as_strided(sizes, strides);
+      values = fresh({rows, stride}, like, at::kFloat8_e4m3fn).as_strided(sizes, strides);
     }
-    scales = at::empty({(rows + 127) / 128, (cols + 127) / 128, 32, 4, 4}, like.options().dtype(at::kByte));
+    scales = fresh({(rows + 127) / 128, (cols + 127) / 128, 32, 4, 4}, like, at::kByte);
   }
   uint8_t* v() const { return static_cast<uint8_t*>(out(values)); }
   uint8_t* s() const { return static_cast<uint8_t*>(out(scales)); }
@@ -467,7 +471,7 @@ std::optional<std::tuple<Tensor, Tensor, int64_t, int64_t, int64_t, Tensor>> rms
   if (recorded({&x, &weight, &residual})) raise_forward(NDVM_E_UNSUPPORTED, kNoGradient);
   const Rows rows(x);
   const Blocks b(x, x.sizes(), rows.rows);
-  if (residual.defined()) sum = at::empty(x.sizes(), x.options());
+  if (residual.defined()) sum = fresh(x.sizes(), x);
   check_forward(ndvm_rms_norm_quantized((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(weight, x), rows.rows, rows.cols, in(x), rows.stride, in(residual),
                                         residual.defined() ? Rows(residual).stride : 0, in(weight), eps, b.v(), b.stride, b.s(), out(sum), rows.cols,
                                         stream_of(x.get_device())));
@@ -494,9 +498,9 @@ Tensor linear_forward(const Tensor& x, const Tensor& w, const Tensor& bias, int6
   const int64_t n = w.size(0);
   auto shape = x.sizes().vec();
   shape.back() = n;
-  Tensor y = at::empty(shape, x.options());
+  Tensor y = fresh(shape, x);
   const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rx.rows, rx.cols, n, 0, ready(x, rx) && ready(w, rw), 0);
-  Tensor ws = bytes(need, x);
+  Tensor ws = need ? fresh({(int64_t)need}, x, at::kByte) : Tensor();
   check_forward(ndvm_linear_forward((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(bias, x), (ndvm_activation)act, rx.rows, rx.cols, n, in(x), rx.stride,
                                     in(w), rw.stride, in(bias), in(residual), residual.defined() ? Rows(residual).stride : 0, out(y), n,
                                     static_cast<float*>(out(z)), held ? held->v() : nullptr, held ? held->s() : nullptr, out(ws), need,
@@ -526,16 +530,16 @@ struct LinearBackward : torch::autograd::Node {
     const int64_t n = weight.size(0), k = weight.size(1);
     const Rows rd(dy), rw(weight);
     Tensor dx, dw, db;
-    if (task_should_compute_output(0)) dx = at::empty(sizes, dy.options());
-    if (task_should_compute_output(1)) dw = at::empty({n, k}, dy.options());
-    if (biased && task_should_compute_output(2)) db = at::empty({n}, dy.options().dtype(btype));
+    if (task_should_compute_output(0)) dx = fresh(sizes, dy);
+    if (task_should_compute_output(1)) dw = fresh({n, k}, dy);
+    if (biased && task_should_compute_output(2)) db = fresh({n}, dy, btype);
     if (dx.defined() || dw.defined() || db.defined()) {
       const bool held = eight && dw.defined();
       std::optional<Rows> rx;
       if (given.defined()) rx.emplace(given);
       const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rd.rows, k, n, 1,
                                                       (!rx || ready(given, *rx)) && ready(weight, rw) && ready(dy, rd), held);
-      Tensor ws = bytes(need, dy);
+      Tensor ws = need ? fresh({(int64_t)need}, dy, at::kByte) : Tensor();
       check_backward(ndvm_linear_backward(
           (ndvm_dtype)type_code(dy), db.defined() && btype == at::kFloat ? NDVM_F32 : (ndvm_dtype)type_code(dy), (ndvm_activation)act, rd.rows, k, n,
           in(dy), rd.stride, rx ? in(given) : nullptr, rx ? rx->stride : 0, held ? static_cast<const uint8_t*>(in(x_values)) : nullptr,
@@ -565,7 +569,7 @@ Tensor linear_recorded(const Tensor& x, const Tensor& w, const Tensor& bias, con
       blocks.emplace(x, at::IntArrayRef({rx.rows, n}), rx.rows);
       z = blocks->values, z_scales = blocks->scales;
     } else if (wants_z) {
-      z = at::empty({rx.rows, ndvm_linear_kept_stride(n)}, x.options().dtype(at::kFloat));
+      z = fresh({rx.rows, ndvm_linear_kept_stride(n)}, x, at::kFloat);
     }
     y = linear_forward(x, w, bias, act, residual, eight ? Tensor() : z, blocks ? &*blocks : nullptr);
   }
@@ -610,9 +614,9 @@ Maybe linear_quantized(const Tensor& xv, const Tensor& xs, int64_t rows, int64_t
   if (!linear_extras(device, b, r, n, shape, type, &bias, &residual)) return std::nullopt;
   check_inputs({&xv, &wv, &bias, &residual});
   if (recorded({&bias, &residual})) raise_forward(NDVM_E_UNSUPPORTED, kNoGradient);
-  Tensor y = at::empty(shape, xv.options().dtype(type));
+  Tensor y = fresh(shape, xv, type);
   const size_t need = ndvm_linear_quantized_workspace_bytes(rows, k, n);
-  Tensor room = bytes(need, xv);
+  Tensor room = need ? fresh({(int64_t)need}, xv, at::kByte) : Tensor();
   check_forward(ndvm_linear_quantized((ndvm_dtype)type_code(y), (ndvm_dtype)weight_code(bias, y), (ndvm_activation)act, rows, k, n,
                                       static_cast<const uint8_t*>(in(xv)), x_stride, static_cast<const uint8_t*>(in(xs)),
                                       static_cast<const uint8_t*>(in(wv)), w_stride, static_cast<const uint8_t*>(in(ws)), in(bias), in(residual),
