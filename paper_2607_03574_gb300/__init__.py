@@ -7,7 +7,8 @@ memory and streams.  The names follow the C ABI in ``include/ndvm.h``:
     tape = trace_build(program_text, frontend=FE_SCHEME)
     loss, grad = value_and_grad(tape, params, obs)     # params (B, P) CUDA tensor
     loss = loss_op(tape)(params, obs)                  # differentiable in params
-    y = layer_norm(x, w, b), gated(...), dropout(...)  # a parameter-proposing network's parts (network.py)
+    y = layer_norm(x, w, b), gated(...), dropout(...)  # a parameter-proposing network's parts (network.py):
+                                                       # also rms_norm, linear, quantize, linear_quantized
 
 There is no CPU fallback: if the library is missing or the device is not a CUDA
 GPU, the calls raise.
