@@ -721,8 +721,8 @@ cudaError_t product(const LinearArgs& a, const Cut& k, float* partial, cudaStrea
   return cudaGetLastError();
 }
 
-// The workspace: aligned copies of what TMA cannot read (or x out of its blocks), dz, split sums (dx's and dw's take
-// turns) and db's.
+// The workspace: aligned copies of what TMA cannot read (or x out of its blocks), dz, split sums (the forward product's or dx's,
+// and dw's) and db's.
 bool x_ready(const LinearArgs& a) { return a.x && tma_ready(a.x, a.x_stride, a.rows, a.k); }
 bool w_ready(const LinearArgs& a) { return tma_ready(a.w, a.w_stride, a.n, a.k); }
 bool dy_ready(const LinearArgs& a) { return tma_ready(a.dy, a.dy_stride, a.rows, a.n); }
@@ -733,7 +733,8 @@ int64_t slope_splits(int64_t rows, int64_t n) { return std::clamp<int64_t>(kSms 
 struct Layout {
   int64_t k_pitch, n_pitch;
   int parts;
-  size_t x, w, dz, partial, sums, total;
+  size_t x, w, dz, partial, partial_w, sums, total;
+  Cuts cuts;  // of the backward pass's products
   Layout(int64_t rows, int64_t k, int64_t n, bool activated, bool backward, bool x_copy, bool w_copy, bool dy_copy) {
     k_pitch = up(k, 8);
     n_pitch = up(n, 8);
@@ -747,16 +748,17 @@ struct Layout {
     x = take(x_copy ? rows * k_pitch * 2 : 0);
     w = take(w_copy ? n * k_pitch * 2 : 0);
     dz = take(backward && (activated || dy_copy) ? parts * rows * n_pitch * 2 : 0);
-    int64_t most = 0;
+    int64_t most = 0, most_w = 0;
     if (rows > 0 && backward) {
-      const Cut i = cut(kInput, rows * parts, k, n, 1, 1), o = cut(kWeight, n, k, rows, parts, 1);
-      if (i.splits > 1 || parts > 1) most = i.splits * parts * rows * up(k, 4);
-      if (o.splits > 1) most = std::max(most, o.splits * n * up(k, 4));
+      cuts = cut_both(rows, k, n, parts);
+      if (cuts.input.splits > 1 || parts > 1) most = cuts.input.splits * parts * rows * up(k, 4);
+      if (cuts.weight.splits > 1) most_w = cuts.weight.splits * n * up(k, 4);
     } else if (rows > 0) {
       const Cut f = cut(kInput, rows, n, k, 1, 1);
       if (f.splits > 1) most = f.splits * rows * up(n, 4);
     }
     partial = take(most * 4);
+    partial_w = take(most_w * 4);
     sums = take(backward && rows > 0 ? slope_splits(rows, n) * n * 4 : 0);
   }
   static Layout of(const LinearArgs& a, bool backward) {
@@ -854,28 +856,28 @@ cudaError_t backward(LinearArgs a, cudaStream_t s) {
     a.x_stride = l.k_pitch;
   }
   make_ready(a, l, a.dw != nullptr, a.dx != nullptr, s);
-  ProductArgs p{};
-  p.partial = reinterpret_cast<float*>(ws + l.partial);
-  p.matrices = 1;
+  // (one of the two alone is cut as if both were wanted: the same bits)
+  ProductArgs input{}, weight{};
   if (a.dx) {
     const int64_t m = a.rows * l.parts;
-    const Cut k = cut(kInput, m, a.k, a.n, 1, 1);
-    if (!map_matrix(&p.a[0], kType<T>, dz, m, a.n, dz_stride, a_box(m)) || !map_matrix(&p.b[0], kType<T>, a.w, a.n, a.k, a.w_stride, 64))
+    if (!map_matrix(&input.a[0], kType<T>, dz, m, a.n, dz_stride, a_box(m)) || !map_matrix(&input.b[0], kType<T>, a.w, a.n, a.k, a.w_stride, 64))
       return cudaErrorInvalidValue;
-    p.parts = 1;
-    p.m = (int)m; p.n = (int)a.k; p.c = (int)a.n; p.out[0] = a.dx; p.stride = a.dx_stride;
-    if ((e = launch_product(kInput, kType<T>, p, k, s, l.parts > 1)) != cudaSuccess) return e;
+    input.partial = reinterpret_cast<float*>(ws + l.partial);
+    input.matrices = input.parts = 1;
+    input.m = (int)m; input.n = (int)a.k; input.c = (int)a.n; input.out[0] = a.dx; input.stride = a.dx_stride;
   }
   if (a.dw) {
-    const Cut k = cut(kWeight, a.n, a.k, a.rows, l.parts, 1);
     for (int half = 0; half < l.parts; half++)
-      if (!map_matrix(&p.a[half], kType<T>, static_cast<const T*>(dz) + half * a.rows * dz_stride, a.rows, a.n, dz_stride, 64)) return cudaErrorInvalidValue;
-    if (!map_matrix(&p.b[0], kType<T>, a.x, a.rows, a.k, a.x_stride, 64)) return cudaErrorInvalidValue;
-    p.parts = l.parts;
-    p.m = (int)a.n; p.n = (int)a.k; p.c = (int)a.rows; p.out[0] = a.dw; p.stride = a.k;
-    if ((e = launch_product(kWeight, kType<T>, p, k, s)) != cudaSuccess) return e;
+      if (!map_matrix(&weight.a[half], kType<T>, static_cast<const T*>(dz) + half * a.rows * dz_stride, a.rows, a.n, dz_stride, 64)) return cudaErrorInvalidValue;
+    if (!map_matrix(&weight.b[0], kType<T>, a.x, a.rows, a.k, a.x_stride, 64)) return cudaErrorInvalidValue;
+    weight.partial = reinterpret_cast<float*>(ws + l.partial_w);
+    weight.matrices = 1;
+    weight.parts = l.parts;
+    weight.m = (int)a.n; weight.n = (int)a.k; weight.c = (int)a.rows; weight.out[0] = a.dw; weight.stride = a.k;
   }
-  return cudaGetLastError();
+  if (a.dx && a.dw) return launch_products(kType<T>, weight, input, l.cuts, s, l.parts > 1);
+  if (a.dx) return launch_product(kInput, kType<T>, input, l.cuts.input, s, l.parts > 1);
+  return launch_product(kWeight, kType<T>, weight, l.cuts.weight, s);
 }
 
 }  // namespace

@@ -4,9 +4,12 @@
 //   gradient  the same products; the epilogue reads dh and writes dG and dU to the workspace
 //   input     dx: A = dG, B = Wg^T, then A = dU, B = Wu^T into the same sums (a dense layer's: A = dz, B = w^T alone)
 //   weight    dW: A = dG^T (or dU^T, dz^T), B = x^T
+//   both      a dense layer's dw and dx in one launch
 // Transposes are read as they lie: the operand's rows are contiguous instead of its contraction.
 #include <atomic>
+#include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "activation.cuh"
 #include "product.h"
@@ -23,7 +26,7 @@ template <Mode kMode> constexpr int kReaders = kMode == kForward || kMode == kGr
 template <Mode kMode> constexpr int kThreads = 64 + 32 * kReaders<kMode>;  // and one that loads, one that multiplies
 
 __host__ __device__ constexpr bool a_rows(Mode m) { return m == kWeight; }
-__host__ __device__ constexpr bool b_rows(Mode m) { return m == kInput || m == kWeight; }
+__host__ __device__ constexpr bool b_rows(Mode m) { return m == kInput || m == kWeight || m == kBoth; }
 __host__ __device__ constexpr bool dual(Mode m) { return m == kForward || m == kGradient; }
 
 // A block's share: kN columns of sums for its 128 rows, of whose operand B a pair's blocks hold half each.
@@ -65,8 +68,15 @@ __device__ __forceinline__ void unstage(const char* buffer, int lane, T* out, in
     if (lane < cols) out[r * stride + lane] = *reinterpret_cast<const T*>(buffer + r * 64 + ((lane / 8 ^ (r >> 1 & 3)) << 4) + lane % 8 * 2);
 }
 
+// What a launch computes: one product, or (kBoth) two, the one with the longer items first.  Of two, each unit takes every
+// so-manieth of the first's items (full of them, the first `rest` units one more) and then of the second's: all units for `rounds`
+// rounds, from there on those that did not have one more of the first's.
+struct Single { ProductArgs of[1]; };
+struct Double { ProductArgs of[2]; int full, rest, rounds; };
+template <Mode kMode> using Launch = std::conditional_t<kMode == kBoth, Double, Single>;
+
 template <typename T, Mode kMode, int kN, int kCtas>
-__global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_constant__ ProductArgs p) {
+__global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_constant__ Launch<kMode> launch) {
   extern __shared__ char raw[];
   constexpr int S = kStages<kMode, kN, kCtas>, kStage = kStageBytes<kN, kCtas>, R = kReaders<kMode>, kNext = R / 4 * 32;
   constexpr uint32_t kABytes = kM * kC * 2;
@@ -103,13 +113,17 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
   tc::fence_after();
   const uint32_t tmem = s_tmem;
 
-  const int tiles = p.tiles_m * p.tiles_n, items = tiles * p.matrices * p.splits;
-  const int segment = (p.c + kC - 1) / kC;  // steps of one segment
-  struct Item { int m0, n0, matrix, split, from, to; };
+  const auto count = [&](const ProductArgs& p) { return p.tiles_m * p.tiles_n * p.matrices * p.splits; };
+  const int items0 = count(launch.of[0]), items = items0 + (kMode == kBoth ? count(launch.of[kMode == kBoth]) : 0);
+  struct Item { int which, m0, n0, matrix, split, from, to; };
   constexpr int kBand = 16 / kCtas;
   // tiles in bands of 2048 rows, down a band first: blocks that run together share operands in L2
   const auto item = [&](int i) {
     Item it;
+    it.which = kMode == kBoth && i >= items0;
+    i -= it.which * items0;
+    const ProductArgs& p = launch.of[it.which];
+    const int tiles = p.tiles_m * p.tiles_n;
     it.split = i / (tiles * p.matrices);
     i -= it.split * (tiles * p.matrices);
     it.matrix = i / tiles;
@@ -122,6 +136,19 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
     it.to = (int)((int64_t)p.steps * (it.split + 1) / p.splits);
     return it;
   };
+  const auto nth = [&](int r) {  // a unit's items; `items` and more: no more of them
+    if constexpr (kMode != kBoth) {
+      return r * units + unit;
+    } else {
+      const bool more = unit < launch.rest;
+      if (r < launch.full + more) return r * units + unit;
+      r -= launch.full + more;
+      if (r < launch.rounds) return items0 + r * units + unit;
+      return more ? items : items0 + launch.rounds * units + (r - launch.rounds) * (units - launch.rest) + unit - launch.rest;
+    }
+  };
+  // whether an item's A has its rows contiguous, and not its contraction
+  const auto rows_of = [&](const Item& it) { return kMode == kBoth ? launch.of[it.which].rows != 0 : a_rows(kMode); };
 
   // (the whole warp waits, and goes on or gives up)
   const auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(~0u, tc::barrier_wait(bar, parity, stop)) != 0; };
@@ -131,17 +158,20 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
     uint32_t phase = 0;
     int issued = 0;
     bool ok = true;
-    for (int i = unit; ok && i < items; i += units) {
+    for (int r = 0, i = nth(0); ok && i < items; i = nth(++r)) {
       const Item it = item(i);
+      const ProductArgs& p = launch.of[it.which];
+      const bool a_r = rows_of(it);
+      const int segment = (p.c + kC - 1) / kC;  // steps of one segment
       for (int s = it.from; s < it.to; s++) {
         if (!(ok = wait(empty(stage), phase ^ 1))) break;
-        const int bytes = a_rows(kMode) ? kStage : kStage - (int)kABytes + p.a_box * kC * 2;
-        const int part = kMode == kInput || kMode == kWeight ? s / segment : 0, seg = kMode == kWeight ? it.matrix * p.parts + part : part;
+        const int bytes = a_r ? kStage : kStage - (int)kABytes + p.a_box * kC * 2;
+        const int part = dual(kMode) ? 0 : s / segment, seg = a_r ? it.matrix * p.parts + part : part;
         const int c = (s - part * segment) * kC;
         if (tc::elect()) {
           const uint32_t a = base + stage * kStage, b = a + kABytes, bar = kCtas == 1 ? full(stage) : tc::in_first(full(stage));
           if (rank == 0) tc::barrier_expect(full(stage), kCtas * bytes);
-          if (a_rows(kMode)) {
+          if (a_r) {
             for (int q = 0; q < kM / 64; q++) tc::load_box<kCtas>(a + q * 8192, &p.a[seg], it.m0 + q * 64, c, bar);
           } else {
             tc::load_box<kCtas>(a, &p.a[seg], c, it.m0, bar);
@@ -153,7 +183,7 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
             tc::load_box<kCtas>(b + kN / 2 * kC * 2, &p.b[1], c, it.n0, bar);
           } else {
             for (int q = 0; q < kN / kCtas / 64; q++)
-              tc::load_box<kCtas>(b + q * 8192, &p.b[kMode == kInput ? seg : 0], it.n0 + rank * (kN / kCtas) + q * 64, c, bar);
+              tc::load_box<kCtas>(b + q * 8192, &p.b[a_r ? 0 : seg], it.n0 + rank * (kN / kCtas) + q * 64, c, bar);
           }
         }
         __syncwarp();
@@ -170,12 +200,13 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
     }
   } else if (warp == 1 && rank == 0) {
     // ---- products
-    constexpr uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, a_rows(kMode), b_rows(kMode), kM * kCtas, kN);
     int stage = 0, slot = 0;
     uint32_t phase = 0, slot_phase = 0;
     bool ok = true;
-    for (int i = unit; ok && i < items; i += units) {
+    for (int r = 0, i = nth(0); ok && i < items; i = nth(++r)) {
       const Item it = item(i);
+      const bool a_r = rows_of(it);
+      const uint32_t desc = tc::instruction(std::is_same<T, __nv_bfloat16>::value, a_r, b_rows(kMode), kM * kCtas, kN);
       if (!(ok = wait(taken(slot), slot_phase ^ 1))) break;
       tc::fence_after();
       for (int s = it.from; s < it.to; s++) {
@@ -183,10 +214,10 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
         tc::fence_after();
         if (tc::elect()) {
           const uint32_t at = base + stage * kStage;
-          const uint64_t a = tc::operand(at, a_rows(kMode)), b = tc::operand(at + kABytes, b_rows(kMode));
+          const uint64_t a = tc::operand(at, a_r), b = tc::operand(at + kABytes, b_rows(kMode));
 #pragma unroll
           for (int q = 0; q < kC / 16; q++)  // 16 of the contraction: 32 bytes along a line, or 16 lines
-            tc::mma<kCtas>(tmem + slot * kN, a + q * (a_rows(kMode) ? 2048 >> 4 : 32 >> 4), b + q * (b_rows(kMode) ? 2048 >> 4 : 32 >> 4),
+            tc::mma<kCtas>(tmem + slot * kN, a + q * (a_r ? 2048 >> 4 : 32 >> 4), b + q * (b_rows(kMode) ? 2048 >> 4 : 32 >> 4),
                            desc, s > it.from || q > 0);
           tc::commit<kCtas>(empty(stage));
           if (s + 1 == it.to) tc::commit<kCtas>(done(slot));
@@ -213,6 +244,7 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
     uint32_t slot_phase = 0;
     // kGradient: the pieces of dh that this warp needs, in the order it needs them, two of them asked for ahead
     const int reader = warp - 2;
+    const ProductArgs& p = launch.of[0];
     struct Place { int i, j; Item it; } ask{unit, first, {}};
     const auto settle = [&] {  // past the tiles that have no columns of this warp's
       while (ask.i < items && ask.it.n0 + first >= p.n) {
@@ -245,8 +277,9 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
       ask_next();
     }
     bool ok = true;
-    for (int i = unit; ok && i < items; i += units) {
+    for (int r = 0, i = nth(0); ok && i < items; i = nth(++r)) {
       const Item it = item(i);
+      const ProductArgs& p = launch.of[it.which];
       const int row0 = it.m0 + lanes;
       if (!wait(done(slot), slot_phase)) break;
       tc::fence_after();
@@ -334,12 +367,12 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
             tc::fence_async();
             __syncwarp();
             if (lane == 0 && row0 < p.m) {
-              tc::store_box(&p.o[kMode == kWeight ? it.matrix : 0], col, row0, to);
+              tc::store_box(&p.o[it.matrix], col, row0, to);
               if (kMode == kGradient) tc::store_box(&p.o[1], col, row0, to + 2048);
             }
           } else {
             __syncwarp();
-            T* out = static_cast<T*>(p.out[kMode == kWeight ? it.matrix : 0]) + row0 * p.stride + col;
+            T* out = static_cast<T*>(p.out[it.matrix]) + row0 * p.stride + col;
             unstage<T>(mine_ptr + (to - mine), lane, out, p.stride, min(32, p.m - row0), count);
           }
         }
@@ -370,30 +403,37 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
   if (warp == 1) tc::tmem_free<kCtas, kColumns>(tmem);
 }
 
-// the parts of split sums added up in order, and rounded: 4 columns a thread.  fold: each matrix's rows come
-// twice, and are added up too.
+// The parts of split sums added up in order, and rounded: 4 columns a thread; blockIdx.y says of which product.  fold: each
+// matrix's rows come twice, and are added up too.
+struct JoinArgs {
+  const float* partial; int64_t pitch;
+  int splits, matrices, fold;
+  int64_t m, n;
+  void* out[2]; int64_t stride;
+};
+struct Joins { JoinArgs of[2]; };
 template <typename T>
-__global__ void __launch_bounds__(256) k_join(const float* partial, int64_t pitch, int splits, int matrices, int fold, int64_t m,
-                                              int64_t n, T* out0, T* out1, int64_t stride) {
-  const int64_t quads = pitch / 4, total = matrices * m * quads, part = total << fold;
+__global__ void __launch_bounds__(256) k_join(const __grid_constant__ Joins joins) {
+  const JoinArgs& a = joins.of[blockIdx.y];
+  const int64_t quads = a.pitch / 4, total = a.matrices * a.m * quads, part = total << a.fold;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / quads, c = (i - row * quads) * 4;
-    const float* p = partial + (i + (fold && row >= m ? m * quads : 0)) * 4;
+    const float* p = a.partial + (i + (a.fold && row >= a.m ? a.m * quads : 0)) * 4;
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-    for (int k = 0; k < splits; k++) {
+    for (int k = 0; k < a.splits; k++) {
       const float4 v = *reinterpret_cast<const float4*>(p + k * part * 4);
       s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-      if (fold) {
-        const float4 l = *reinterpret_cast<const float4*>(p + (k * part + m * quads) * 4);
+      if (a.fold) {
+        const float4 l = *reinterpret_cast<const float4*>(p + (k * part + a.m * quads) * 4);
         s.x += l.x, s.y += l.y, s.z += l.z, s.w += l.w;
       }
     }
-    T* out = row >= m ? out1 + (row - m) * stride + c : out0 + row * stride + c;
+    T* out = row >= a.m ? static_cast<T*>(a.out[1]) + (row - a.m) * a.stride + c : static_cast<T*>(a.out[0]) + row * a.stride + c;
     const float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
     for (int e = 0; e < 4; e++)
-      if (c + e < n) out[e] = from_f32<T>(v[e]);
+      if (c + e < a.n) out[e] = from_f32<T>(v[e]);
   }
 }
 
@@ -410,8 +450,10 @@ __global__ void __launch_bounds__(256) k_pack(const __grid_constant__ PackArgs a
   }
 }
 
+int items_of(const ProductArgs& p) { return p.tiles_m * p.tiles_n * p.matrices * p.splits; }
+
 template <typename T, Mode kMode, int kN, int kCtas>
-cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
+cudaError_t launch_width(const Launch<kMode>& l, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may take its shared memory
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
@@ -421,7 +463,8 @@ cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (device < 64) allowed.fetch_or((uint64_t)1 << device, std::memory_order_relaxed);
   }
-  const int items = p.tiles_m * p.tiles_n * p.matrices * p.splits;
+  int items = 0;
+  for (const ProductArgs& p : l.of) items += items_of(p);
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)std::min(items, kSms / kCtas) * kCtas);
   c.blockDim = dim3(kThreads<kMode>);
@@ -433,39 +476,87 @@ cudaError_t launch_width(const ProductArgs& p, cudaStream_t s) {
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   c.attrs = &cluster;
   c.numAttrs = kCtas == 1 ? 0 : 1;
-  return cudaLaunchKernelEx(&c, k_product<T, kMode, kN, kCtas>, p);
+  return cudaLaunchKernelEx(&c, k_product<T, kMode, kN, kCtas>, l);
 }
 
+// what a product's size and cut say of its arguments
 template <typename T, Mode kMode>
-cudaError_t launch_mode(ProductArgs& p, const Cut& k, cudaStream_t s, bool fold) {
+bool settle(ProductArgs& p, const Cut& k, bool fold) {
   const int out = dual(kMode) ? k.width / 2 : k.width;
   p.tiles_m = (int)ceil_div(p.m, kM * k.ctas);
   p.tiles_n = (int)ceil_div(p.n, out);
   p.steps = (int)ceil_div(p.c, kC) * (dual(kMode) ? 1 : p.parts);
   p.splits = k.splits;
+  p.rows = a_rows(kMode);
   p.a_box = a_rows(kMode) ? kM : a_box(p.m);
   p.copies = 1;
   p.sums = p.splits > 1 || fold;
   if (p.sums) {
     p.partial_pitch = up(p.n, 4);
-    if (!map_partial(&p.o[0], p.partial, (int64_t)p.splits * p.matrices, p.m, p.n, p.partial_pitch)) return cudaErrorInvalidValue;
+    if (!map_partial(&p.o[0], p.partial, (int64_t)p.splits * p.matrices, p.m, p.n, p.partial_pitch)) return false;
   } else {
     for (int w = 0; w < 2; w++) {
       if (!p.out[w]) continue;
       p.copies &= tma_ready(p.out[w], p.stride, p.m, p.n);
-      if (p.copies && !map_matrix(&p.o[w], kType<T>, p.out[w], p.m, p.n, p.stride, 32, true)) return cudaErrorInvalidValue;
+      if (p.copies && !map_matrix(&p.o[w], kType<T>, p.out[w], p.m, p.n, p.stride, 32, true)) return false;
     }
   }
-  if ((int64_t)p.tiles_m * p.tiles_n * p.matrices * p.splits > 0x40000000) return cudaErrorInvalidConfiguration;
-  const cudaError_t e = k.ctas == 2      ? launch_width<T, kMode, 256, 2>(p, s)
-                        : k.width == 256 ? launch_width<T, kMode, 256, 1>(p, s)
-                        : k.width == 128 ? launch_width<T, kMode, 128, 1>(p, s)
-                                         : launch_width<T, kMode, 64, 1>(p, s);
-  if (e != cudaSuccess || !p.sums) return e;
-  const int64_t m = fold ? p.m / 2 : p.m, total = (int64_t)p.matrices * m * p.partial_pitch / 4;
-  k_join<T><<<(unsigned)std::min<int64_t>(ceil_div(total, 256), kSms * 8), 256, 0, s>>>(
-      p.partial, p.partial_pitch, p.splits, p.matrices, fold, m, p.n, static_cast<T*>(p.out[0]), static_cast<T*>(p.out[1]), p.stride);
+  return (int64_t)p.tiles_m * p.tiles_n * p.matrices * p.splits <= 0x20000000;
+}
+
+template <typename T, Mode kMode>
+cudaError_t run(const Launch<kMode>& l, const Cut& k, cudaStream_t s, std::initializer_list<int> folds) {
+  const cudaError_t e = k.ctas == 2      ? launch_width<T, kMode, 256, 2>(l, s)
+                        : k.width == 256 ? launch_width<T, kMode, 256, 1>(l, s)
+                        : k.width == 128 ? launch_width<T, kMode, 128, 1>(l, s)
+                                         : launch_width<T, kMode, 64, 1>(l, s);
+  if (e != cudaSuccess) return e;
+  Joins joins{};
+  int count = 0;
+  int64_t most = 0;
+  const int* fold = folds.begin();
+  for (const ProductArgs& p : l.of) {
+    const int f = *fold++;
+    if (!p.sums) continue;
+    JoinArgs& a = joins.of[count++];
+    a = JoinArgs{p.partial, p.partial_pitch, p.splits, p.matrices, f, f ? p.m / 2 : p.m, p.n, {p.out[0], p.out[1]}, p.stride};
+    most = std::max(most, a.matrices * a.m * a.pitch / 4);
+  }
+  if (!count) return e;
+  k_join<T><<<dim3((unsigned)std::min<int64_t>(ceil_div(most, 256), kSms * 8), (unsigned)count), 256, 0, s>>>(joins);
   return cudaGetLastError();
+}
+
+template <typename T, Mode kMode>
+cudaError_t launch_mode(ProductArgs& p, const Cut& k, cudaStream_t s, bool fold) {
+  if (!settle<T, kMode>(p, k, fold)) return cudaErrorInvalidValue;
+  return run<T, kMode>(Launch<kMode>{{p}}, k, s, {fold});
+}
+// the estimated time of an item (see cut)
+double item_time(const Cut& k, int steps) {
+  return (double)ceil_div(steps, k.splits) * (k.ctas == 2 ? 0.9 : k.width == 256 ? 1.0 : k.width == 128 ? 0.6 : 0.4) + 8;
+}
+template <typename T>
+cudaError_t launch_both(ProductArgs& weight, ProductArgs& input, const Cuts& k, cudaStream_t s, bool fold) {
+  if (!settle<T, kWeight>(weight, k.weight, false) || !settle<T, kInput>(input, k.input, fold)) return cudaErrorInvalidValue;
+  // in units of the shorter items' time: how many of each a unit has
+  const double item_w = item_time(k.weight, weight.steps), item_i = item_time(k.input, input.steps);
+  const bool first = item_w >= item_i;
+  Double l{first ? Double{{weight, input}} : Double{{input, weight}}};
+  const int units = kSms / k.weight.ctas, a = items_of(l.of[0]), b = items_of(l.of[1]);
+  const int longer = (int)std::lround(first ? item_w / item_i : item_i / item_w);
+  l.full = a / units;
+  l.rest = a % units;
+  if (a + b > units) {  // the least time `slots` in which all of the second's items find room
+    const auto room = [&](int64_t slots) {
+      const int64_t less = std::max<int64_t>(slots - (int64_t)longer * (l.full + 1), 0), most = std::max<int64_t>(slots - (int64_t)longer * l.full, 0);
+      return less * l.rest + most * (units - l.rest);
+    };
+    int64_t slots = ((int64_t)longer * a + b) / units;
+    while (room(slots) < b) slots++;
+    l.rounds = (int)std::max<int64_t>(slots - (int64_t)longer * (l.full + (l.rest > 0)), 0);
+  }
+  return run<T, kBoth>(l, k.weight, s, first ? std::initializer_list<int>{0, fold} : std::initializer_list<int>{fold, 0});
 }
 
 }  // namespace
@@ -523,6 +614,38 @@ Cut cut(Mode mode, int64_t m, int64_t n, int64_t c, int parts, int matrices) {
   return best;
 }
 
+// The same for a dense layer's two gradients, which share a launch: as the items are dealt out, the longer ones first, a unit
+// has its share of the work and up to one item more.
+Cuts cut_both(int64_t rows, int64_t k, int64_t n, int parts) {
+  // (a call asks three times: for its workspace, whether it fits, and for the launch)
+  thread_local struct { int64_t rows = -1, k, n; int parts; Cuts cuts; } last;
+  if (last.rows == rows && last.k == k && last.n == n && last.parts == parts) return last.cuts;
+  struct Shape { int width, ctas; double step; };
+  static constexpr Shape shapes[] = {{256, 2, 0.9}, {256, 1, 1.0}, {128, 1, 0.6}, {64, 1, 0.4}};
+  const int64_t steps_w = ceil_div(rows, kC) * parts, steps_i = ceil_div(n, kC);
+  const double sum_w = (double)(n * k) * 4e-6, sum_i = (double)(rows * parts * k) * 4e-6;  // steps' time of writing and reading one part
+  Cuts best{};
+  double least = 1e300;
+  for (const Shape& s : shapes) {
+    if (s.ctas == 2 && std::min(steps_w, steps_i) < 12) continue;
+    const double units = kSms / s.ctas;
+    const int64_t tiles_w = ceil_div(n, kM * s.ctas) * ceil_div(k, s.width), tiles_i = ceil_div(rows * parts, kM * s.ctas) * ceil_div(k, s.width);
+    for (const int w : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (w > 1 && w > steps_w / 8) break;
+      for (const int i : {1, 2, 4, 8}) {
+        if (i > 1 && i > steps_i / 8) break;
+        const double item_w = (double)ceil_div(steps_w, w) * s.step + 8, item_i = (double)ceil_div(steps_i, i) * s.step + 8;
+        const double count_w = (double)(tiles_w * w), count_i = (double)(tiles_i * i), work = (count_w * item_w + count_i * item_i) / units;
+        const double rounds = count_w + count_i > units ? work + 0.5 * std::min(item_w, item_i) : 0;
+        const double time = std::max({rounds, item_w, item_i}) + (w > 1 || i > 1 ? 13 : 0) + (w > 1 ? w * sum_w : 0) + (i > 1 ? i * sum_i : 0);
+        if (time < least) least = time, best = Cuts{{s.width, s.ctas, w}, {s.width, s.ctas, i}};
+      }
+    }
+  }
+  last = {rows, k, n, parts, best};
+  return best;
+}
+
 void launch_pack(const PackArgs& p, int count, int64_t most_rows, cudaStream_t s) {
   const int64_t blocks = std::min<int64_t>(ceil_div(most_rows, 8), kSms * 32);
   k_pack<<<dim3((unsigned)blocks, (unsigned)count), 256, 0, s>>>(p);
@@ -534,6 +657,10 @@ cudaError_t launch_product(Mode mode, ndvm_dtype t, ProductArgs& p, const Cut& k
   if (mode == kGradient) return half ? launch_mode<__half, kGradient>(p, k, s, fold) : launch_mode<__nv_bfloat16, kGradient>(p, k, s, fold);
   if (mode == kInput) return half ? launch_mode<__half, kInput>(p, k, s, fold) : launch_mode<__nv_bfloat16, kInput>(p, k, s, fold);
   return half ? launch_mode<__half, kWeight>(p, k, s, fold) : launch_mode<__nv_bfloat16, kWeight>(p, k, s, fold);
+}
+
+cudaError_t launch_products(ndvm_dtype t, ProductArgs& weight, ProductArgs& input, const Cuts& k, cudaStream_t s, bool fold) {
+  return t == NDVM_F16 ? launch_both<__half>(weight, input, k, s, fold) : launch_both<__nv_bfloat16>(weight, input, k, s, fold);
 }
 
 cudaError_t product_stopped(int* flag) {

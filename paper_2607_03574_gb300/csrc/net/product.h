@@ -11,7 +11,7 @@
 
 namespace ndvm {
 
-enum Mode { kForward, kGradient, kInput, kWeight };
+enum Mode { kForward, kGradient, kInput, kWeight, kBoth };
 
 constexpr int kM = 128, kC = 64;  // rows of a tile, contraction of a step (128 bytes)
 
@@ -27,6 +27,7 @@ struct ProductArgs {
   int steps, splits;             // contraction steps of a result, and how many parts they are cut into
   int act;
   int a_box;                     // rows of A that a tile loads (fewer than 128 where the result has fewer)
+  int rows;                      // A's rows are contiguous, and not its contraction
   int sums;                      // results are binary32 sums, which k_join finishes
   int copies;                    // results are stored by copies (their rows start on 16 bytes)
   void* out[2]; int64_t stride;  // kWeight: both matrices'; kGradient: dG and dU; else out[0]
@@ -36,8 +37,12 @@ struct ProductArgs {
 // how a product of the given size is cut up: columns and rows of a tile's sums (256 rows are a pair's), parts
 struct Cut { int width, ctas, splits; };
 Cut cut(Mode mode, int64_t m, int64_t n, int64_t c, int parts, int matrices);
+struct Cuts { Cut weight, input; };  // (of one width)
+Cuts cut_both(int64_t rows, int64_t k, int64_t n, int parts);
 // t: half or bfloat16.  fold: the result's rows come twice (two halves of A), and are added up.
 cudaError_t launch_product(Mode mode, ndvm_dtype t, ProductArgs& p, const Cut& k, cudaStream_t s, bool fold = false);
+// a dense layer's two gradients in one launch (fold: of the input's)
+cudaError_t launch_products(ndvm_dtype t, ProductArgs& weight, ProductArgs& input, const Cuts& k, cudaStream_t s, bool fold);
 
 inline int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
