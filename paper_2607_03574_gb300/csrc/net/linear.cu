@@ -367,11 +367,7 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
           if (lane == 0 && row0 < p.m) tc::store_box(&p.o, col, row0, to);
         } else {
           __syncwarp();
-          T* out = static_cast<T*>(p.out) + row0 * p.stride + col;
-          const char* from = mine_ptr + (to - mine);
-          const int rows = min(32, p.m - row0);
-          for (int r = 0; r < rows; r++)
-            if (lane < count) out[r * p.stride + lane] = *reinterpret_cast<const T*>(from + r * 64 + ((lane / 8 ^ (r >> 1 & 3)) << 4) + lane % 8 * 2);
+          tc::unstage<T>(mine_ptr + (to - mine), lane, static_cast<T*>(p.out) + row0 * p.stride + col, p.stride, min(32, p.m - row0), count);
         }
         if (lane == 0) tc::stores_commit();
       }

@@ -61,13 +61,6 @@ __device__ __forceinline__ void stage_row(uint32_t buffer, int lane, const float
                 make_uint4(__float_as_uint(v[q * 4]), __float_as_uint(v[q * 4 + 1]), __float_as_uint(v[q * 4 + 2]),
                            __float_as_uint(v[q * 4 + 3])));
 }
-// the buffer's rows to rows that start anywhere, a row at a time
-template <typename T>
-__device__ __forceinline__ void unstage(const char* buffer, int lane, T* out, int64_t stride, int rows, int cols) {
-  for (int r = 0; r < rows; r++)
-    if (lane < cols) out[r * stride + lane] = *reinterpret_cast<const T*>(buffer + r * 64 + ((lane / 8 ^ (r >> 1 & 3)) << 4) + lane % 8 * 2);
-}
-
 // What a launch computes: one product, or (kBoth) two, the one with the longer items first.  Of two, each unit takes every
 // so-manieth of the first's items (full of them, the first `rest` units one more) and then of the second's: all units for `rounds`
 // rounds, from there on those that did not have one more of the first's.
@@ -373,7 +366,7 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
           } else {
             __syncwarp();
             T* out = static_cast<T*>(p.out[it.matrix]) + row0 * p.stride + col;
-            unstage<T>(mine_ptr + (to - mine), lane, out, p.stride, min(32, p.m - row0), count);
+            tc::unstage<T>(mine_ptr + (to - mine), lane, out, p.stride, min(32, p.m - row0), count);
           }
         }
         if (lane == 0) tc::stores_commit();

@@ -126,6 +126,19 @@ __device__ __forceinline__ void store16(uint32_t to, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// 32 rows of 32 16-bit elements in the 64-byte swizzle to rows that start anywhere, a row a warp and store, eight read at once
+template <typename T>
+__device__ __forceinline__ void unstage(const char* buffer, int lane, T* out, int64_t stride, int rows, int cols) {
+  for (int r0 = 0; r0 < rows; r0 += 8) {
+    T v[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) v[u] = *reinterpret_cast<const T*>(buffer + (r0 + u) * 64 + ((lane / 8 ^ ((r0 + u) >> 1 & 3)) << 4) + lane % 8 * 2);
+#pragma unroll
+    for (int u = 0; u < 8; u++)
+      if (r0 + u < rows && lane < cols) out[(r0 + u) * stride + lane] = v[u];
+  }
+}
+
 template <int kCtas, int kColumns>
 __device__ __forceinline__ void tmem_alloc(uint32_t to) {
   if constexpr (kCtas == 1) {
