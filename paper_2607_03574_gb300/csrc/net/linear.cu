@@ -433,23 +433,30 @@ __global__ void __launch_bounds__(256) k_finish(const float* partial, int64_t pi
 
 // ------------------------------------------------------------------------------------ one row: vectors
 // w is read once and is nearly all the traffic, so what counts is how much of it is under way: kSplits warps share a row of w, 16
-// bytes a lane and four loads at once, against x (from L1); a block's sums are joined in shared memory.
+// bytes a lane and two loads at once past L1, against x (from L1); a block's sums are joined in shared memory.  Many warps of few
+// loads beat few of many (8192 -> 8192: 22.6 us at 64 warps an SM, 32.8 at 32 with four loads), and keeping w out of L1 helps
+// both (25.6 with it).
 template <typename T, int V, int kSplits>
-__global__ void __launch_bounds__(256, 4) k_linear_one(LinearArgs a) {
+__global__ void __launch_bounds__(256, 8) k_linear_one(LinearArgs a) {
   using P = Pairs<V>;
-  constexpr int H = kPairs<V>, kUnroll = 4, kPer = 8 / kSplits;  // rows of w a block
+  constexpr int H = kPairs<V>, kUnroll = 2, kPer = 8 / kSplits;  // rows of w a block
   __shared__ float part[8];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, split = warp % kSplits;
   const int64_t j = (int64_t)blockIdx.x * kPer + warp / kSplits;
   P s = both(0.0f, P());
+  float bias = 0.0f, residual = 0.0f;
   if (j < a.n) {
+    if (lane == 0) {  // (asked for first: what the end waits for)
+      bias = bias_at<T>(a.bias, a.bias_f32, j);
+      if (a.residual) residual = to_f32(static_cast<const T*>(a.residual)[j]);
+    }
     const T *w = static_cast<const T*>(a.w) + j * a.w_stride, *x = static_cast<const T*>(a.x);
     constexpr int kStep = kSplits * 32 * V;
     for (int64_t c0 = (split * 32 + lane) * V; c0 < a.k; c0 += kUnroll * kStep) {
       Pack<T, V> pw[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; u++)
-        if (c0 + u * kStep < a.k) pw[u] = load_pack<T, V>(w + c0 + u * kStep);
+        if (c0 + u * kStep < a.k) pw[u] = load_once<T, V>(w + c0 + u * kStep);
 #pragma unroll
       for (int u = 0; u < kUnroll; u++) {
         if (c0 + u * kStep >= a.k) break;
@@ -473,19 +480,18 @@ __global__ void __launch_bounds__(256, 4) k_linear_one(LinearArgs a) {
     for (int q = 1; q < kSplits; q++) z += part[warp + q];
   }
   if (lane || j >= a.n) return;
-  z += bias_at<T>(a.bias, a.bias_f32, j);
+  z += bias;
   if (a.z) a.z[j] = z;
   by_activation_or_none(a.act, [&](auto k) {
     const float2 act = activation<decltype(k)::value>(make_float2(z, z));
-    const float r = a.residual ? to_f32(static_cast<const T*>(a.residual)[j]) : 0.0f;
-    static_cast<T*>(a.y)[j] = from_f32<T>(act.x + r);
+    static_cast<T*>(a.y)[j] = from_f32<T>(act.x + residual);
   });
 }
 
 template <typename T, int V>
 void one_of(const LinearArgs& a, cudaStream_t s) {
-  // as many warps a row as 40 on each SM have room for, each with two batches of loads at least (8192 -> 1024 6.0 us, 10.0 with one)
-  const int64_t room = kSms * 40 / a.n, most = a.k / (8 * 32 * V);
+  // as many warps a row as 64 on each SM have room for, each with two batches of loads at least (4096 -> 4096 7.4 us; 8.4 with 40 and four)
+  const int64_t room = kSms * 64 / a.n, most = a.k / (4 * 32 * V);
   if (std::min(room, most) >= 8) k_linear_one<T, V, 8><<<(unsigned)a.n, 256, 0, s>>>(a);
   else if (std::min(room, most) >= 4) k_linear_one<T, V, 4><<<(unsigned)ceil_div(a.n, 2), 256, 0, s>>>(a);
   else if (std::min(room, most) >= 2) k_linear_one<T, V, 2><<<(unsigned)ceil_div(a.n, 4), 256, 0, s>>>(a);
@@ -530,7 +536,7 @@ __global__ void __launch_bounds__(256, 3) k_slope(SlopeArgs a) {
       if (row >= a.rows) continue;
       const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride + c;
       if (kVectors && all) {
-        d[u] = load_pack<T, 8>(dy);
+        d[u] = load_once<T, 8>(dy);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; e++) d[u].v[e] = c + e < a.n ? dy[e] : from_f32<T>(0.0f);

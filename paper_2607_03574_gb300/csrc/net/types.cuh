@@ -46,6 +46,17 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
     return *reinterpret_cast<const Pack<T, V>*>(p);
   }
 }
+// the same of what is read once: it takes no room in L1
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_once(const T* p) {
+  if constexpr (sizeof(T) * V == 16) {
+    union { uint4 u; Pack<T, V> p; } b;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(b.u.x), "=r"(b.u.y), "=r"(b.u.z), "=r"(b.u.w) : "l"(p) : "memory");
+    return b.p;
+  } else {
+    return load_pack<T, V>(p);
+  }
+}
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
   if constexpr (sizeof(T) * V == 16) {
