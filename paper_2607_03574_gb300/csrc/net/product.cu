@@ -226,9 +226,9 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
       tc::barrier_drain(drain, 0);
     }
   } else if (warp >= 2) {
-    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, 32
-    // columns, by way of staging that asynchronous copies empty.  (Two warps a scheduler: one alone left the
-    // latencies of the reads, the copies and dh in the open: backward of 4096 x 1024 -> 4096 174 and 159 us.)
+    // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, 32 columns at a time, by way of
+    // staging that asynchronous copies empty.  (Two warps a scheduler or four: one alone left the latencies of the reads, the
+    // copies and dh in the open.)
     const int lanes = (warp % 4) * 32;
     const uint32_t mine = staging + (warp - 2) * kStaging<kMode, kCtas>;
     const char* const mine_ptr = raw + (mine - tc::smem(raw));
@@ -587,7 +587,7 @@ bool map_partial(CUtensorMap* map, float* p, int64_t parts, int64_t m, int64_t n
 
 // The shape with the least estimated time, in steps of a tile 256 wide (0.27 us): a round of tiles takes its
 // steps and about 8 more to fill and empty; narrower tiles' steps are shorter, but not in proportion (more bytes an
-// operation), a pair's a little shorter (16384 x 2048 -> 8192 forward: 630 us alone, 576 in pairs) if there are 12 or
+// operation), a pair's a little shorter (16384 x 2048 -> 8192 forward: 612 us alone, 560 in pairs) if there are 12 or
 // more (pairs start and end together: 4096 x 256 -> 1024 takes 9.2 us alone, 10.6 in pairs).  Where tiles are fewer than
 // SMs, a contraction is cut into parts of 8 steps or more, which costs the launch that joins them.  (The gated
 // projection's weight gradients are cut as if both were wanted: one of them alone has the same bits.)

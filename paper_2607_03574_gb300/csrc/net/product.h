@@ -75,10 +75,10 @@ void launch_pack(const PackArgs& p, int count, int64_t most_rows, cudaStream_t s
 // Few elements: dG and dU are handed on in two halves of 16 bits, so that next to nothing is lost before the last
 // rounding.  (Over many elements the rounding of dG and dU adds to the results' own as squares add, 1.41 times in
 // all; over few it scatters, to more than twice: 4096 elements leave 1.2 to 1.55, 16384 1.37 to 1.49.)  dx has the halves' rows
-// one after the other in its tiles, the weights' gradients twice the steps, and G and U are made in binary32 first.  A step with
-// the products kept, bf16, with and without halves: 8 x 2048 -> 8192 63 / 56 us, 16 x 1024 -> 4096 32 / 30, 64 x 256 -> 512 20.3 /
-// 19.5, 4096 x 32 -> 64 23 / 20; the cost grows with the rows where n k is small (65536 x 32 -> 64 67 / 52, and 77 / 50 with
-// nothing kept) and with n where k is (1000 x 16 -> 8192 76 / 62).
+// one after the other in its tiles, the weights' gradients twice the steps, and G and U are made in binary32 first.  A gated step with
+// the products kept, bf16, with and without halves: 8 x 2048 -> 8192 66 / 55 us, 16 x 1024 -> 4096 32 / 27, 64 x 256 -> 512 20.0 /
+// 18.8, 4096 x 32 -> 64 25 / 21; the cost grows with the rows where n k is small (65536 x 32 -> 64 72 / 61, and 82 / 60 with
+// nothing kept) and with n where k is (1000 x 16 -> 8192 76 / 64).
 inline bool in_halves(int64_t rows, int64_t k, int64_t n) { return rows * std::min(n, k) <= 16384 || n * k <= 2048; }
 
 }  // namespace ndvm

@@ -265,9 +265,9 @@ struct Gated : torch::autograd::Function<Gated> {
   static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w_gate, const Tensor& w_up, int64_t act, int64_t keep) {
     // The two products are kept (8 bytes an element of h) if the caller says so (keep 1; 0: not), or by default (-1) where
     // that is the faster: a long contraction, or few elements.  Forward and backward, computed again / kept:
-    // 16384 x 2048 -> 8192 2660 / 2357 us, 4096 x 2048 -> 8192 648 / 596, 16 x 2048 -> 8192 67 / 57, 1501 x 333 -> 777 49 / 44;
-    // but 4096 x 1024 -> 4096 194 / 198, 4096 x 256 -> 1024 47 / 50, 16384 x 1024 -> 4096 687 / 725, 100000 x 256 -> 512
-    // 238 / 310.
+    // 16384 x 2048 -> 8192 2612 / 2270 us, 4096 x 2048 -> 8192 631 / 582, 16 x 2048 -> 8192 69 / 60, 1501 x 333 -> 777 47 / 41;
+    // but 4096 x 1024 -> 4096 183 / 192, 4096 x 256 -> 1024 47 / 50, 16384 x 1024 -> 4096 637 / 678, 100000 x 256 -> 512
+    // 235 / 307.
     const Rows r(x);
     const int64_t n = w_gate.size(0);
     Tensor kept;
@@ -346,7 +346,7 @@ variable_list rms_forward(const Tensor& x, const Tensor& weight, const Tensor& r
   return sum.defined() ? variable_list{y, sum} : variable_list{y};
 }
 // The nodes of the norm and of the dense layers are plain ones: a Function's context costs 10 us more a pass (forward and backward
-// on small inputs: norm 148 us, dense layer 167; a plain product of torch 121).  Each is made when its outputs are there;
+// on small inputs: norm 131 and 121 us, dense layer 149 and 136; torch's elementwise product 107).  Each is made when its outputs are there;
 // edges are those of its inputs in order, undefined ones among them.
 using torch::autograd::SavedVariable;
 template <typename N>
