@@ -343,3 +343,74 @@ def test_trained_block_together(ndvm, cuda):
         for i, (a, c) in enumerate(zip(torch.autograd.grad(y, leaves, dy), want)):
             assert float((a.double() - c).norm() / c.norm()) <= most, (keep, i)
     ndvm.check_operators()
+
+
+@pytest.mark.parametrize("act,keep", [("silu", None), ("gelu", "8bit"), (None, None)])
+def test_linear_past_32_bit_offsets(ndvm, cuda, act, keep):
+    """4.3e9 elements of the result: its last rows, and gradients that only they and the first ones make."""
+    import torch
+    rows, k, n = 131200, 16, 33000
+    some = torch.cat((torch.arange(40), torch.arange(rows - 60, rows))).cuda()
+    x, w, b, res, dy = _case(14, 100, k, n, "bf16", "f32")
+    d = [v.double() for v in (x, w, b, res, dy)]
+    big = torch.zeros(rows, k, device="cuda", dtype=torch.bfloat16)
+    big[some] = x
+    y = torch.zeros(rows, n, device="cuda", dtype=torch.bfloat16)
+    y[some] = res
+    kept = ndvm.linear_kept(big, w, keep) if act else None
+    ndvm.linear_forward(big, w, b, act, y, y=y, kept=kept)
+    want, err, z, ez = _forward64(*d[:4], act)
+    _inside(y[some], want, _rounded(want, err, "bf16"), "y")
+    held = ndvm.quantize_forward(big) if keep else big
+    if keep:
+        part = ndvm.linear_kept(x, w, keep)
+        ndvm.linear_forward(x, w, b, act, res, kept=part)
+        assert torch.equal(kept.values.view(torch.uint8)[some], part.values.view(torch.uint8))
+        z, ez, d[0] = _decode(part), 0 * z, _decode(ndvm.quantize_forward(x))
+    elif act:
+        _inside(kept[some][:, :n], z, ez, "kept")
+    y.zero_()
+    y[some] = dy
+    got = ndvm.linear_backward(y, held, w, act, kept=kept, btype=torch.float32)
+    want, err = _backward64(d[0], d[1], z, ez, d[4], act, "bf16")
+    for name, a, v, e, o in zip(("dx", "dw", "dbias"), (got[0][some], *got[1:]), want, err, ("bf16", "bf16", "f32")):
+        _inside(a, v, _rounded(v, e, o), name)
+    assert not got[0][40:rows - 60].any()
+    ndvm.check_operators()
+
+
+def test_linear_quantized_past_32_bit_offsets(ndvm, cuda):
+    import torch
+    rows, k, n = 131200, 40, 33000
+    x, w, b, res, _ = _case(15, 60, k, n, "bf16", "f32")
+    q = ndvm.quantize_forward(w)
+    big = torch.zeros(rows, k, device="cuda", dtype=torch.bfloat16)
+    big[-60:] = x
+    y = torch.zeros(rows, n, device="cuda", dtype=torch.bfloat16)
+    y[-60:] = res
+    ndvm.linear_quantized_forward(ndvm.quantize_forward(big), q, b, "relu", y, y=y)
+    assert torch.equal(y[-60:], ndvm.linear_quantized_forward(ndvm.quantize_forward(x), q, b, "relu", res))
+    assert torch.equal(y[70000], torch.relu(b).bfloat16())
+
+
+def test_inputs_whose_rows_are_one(ndvm, cuda):
+    """Rows of stride 0 (an expanded row) as x, residual and cotangent; blocks of such rows; a part of other blocks."""
+    import torch
+    x, w, b, res, dy = _case(16, 200, 136, 72, "bf16", "bf16")
+    for i, act in enumerate(ACTS):
+        one = [v[:1].expand(200, v.shape[1]) for v in (x, res, dy)]
+        full = [v.contiguous() for v in one]
+        keep = "8bit" if act and i % 2 else None
+        results = []
+        for xi, ri, di in (one, full):
+            kept = ndvm.linear_kept(xi, w, keep) if act else None
+            y = ndvm.linear_forward(xi, w, b, act, ri, kept=kept)
+            results.append((y, *ndvm.linear_backward(di, ndvm.quantize_forward(xi) if keep else xi, w, act, kept=kept)))
+        assert all(torch.equal(a, c) for a, c in zip(*results)), act
+    one, full = x[:1].expand(200, 136), x[:1].repeat(200, 1)
+    assert all(torch.equal(a, c) for a, c in zip(ndvm.rms_norm_forward(one, None, 1e-6, one), ndvm.rms_norm_forward(full, None, 1e-6, full)))
+    q = ndvm.quantize_forward(x.repeat(2, 1))
+    part = ndvm.Quantized(q.values[128:], q.scales[1:])
+    assert torch.equal(part.dequantize(), q.dequantize()[128:])
+    p = ndvm.quantize_forward(w)
+    assert torch.equal(ndvm.linear_quantized_forward(part, p, b), ndvm.linear_quantized_forward(q, p, b)[128:])
