@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(kLong) k_rms_forward_long(RmsArgs a, int w_f32
 
 // Backward: a group of kRow threads takes every so-manieth row.  Each thread asks for its part of the rows to come by asynchronous
 // copies, kDepth - 1 rows ahead, to shared memory that it alone reads: registers would hold one row ahead, which left the latency of
-// memory in the open (16384 x 1024 bf16 with a residual 37 us, 3.7 TB/s).  Rows off 16 bytes do take registers, one row ahead.
+// memory in the open (16384 x 1024 bf16 with a residual 37 us; 25 so, and 65536 x 2048 154 us, 7.0 TB/s).  Rows off 16 bytes do take
+// registers, one row ahead.
 // partial[block][c] = the block's sum of dy sh.
 template <int V, int N, int kRow, int kResident, int kBytes>
 constexpr int kDepth = V * kBytes != 16 ? 0 : std::min(4, 221184 / kResident / (3 * N * kBackBlock<kRow> * 16));
@@ -457,7 +458,9 @@ cudaError_t rms_backward(RmsArgs a, int w_f32, cudaStream_t s) {
   if (a.rows > 0 && (a.dx || a.dweight)) {
     const int width = load_width<T>(a.rows, a.cols, w_f32, {a.weight},
                                     {{a.x, a.x_stride}, {a.dy, a.dy_stride}, {a.dsum, a.dsum ? a.dsum_stride : 0}, {a.dx, a.dx ? a.dx_stride : 0}});
-    const bool held = backward_variant<T>(width, a.rows, a.cols, [&](auto v, auto n, auto r, auto b) {
+    // (rows: not the layer norm's rule for many of them, whose one load a thread leaves more barriers a row: with the rows ahead in
+    // shared memory two loads are the faster, 65536 x 2048 154 us against 190)
+    const bool held = backward_variant<T>(width, 0, a.cols, [&](auto v, auto n, auto r, auto b) {
       constexpr int kRow = decltype(r)::value, kThreads = kBackBlock<kRow>, kRows = kThreads / kRow;
       constexpr auto kernel = k_rms_backward<T, decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value>;
       constexpr int kRing = kDepth<decltype(v)::value, decltype(n)::value, kRow, decltype(b)::value, sizeof(T)> * decltype(n)::value * kThreads * 16;
