@@ -23,9 +23,9 @@ __device__ int g_linear_stopped;  // a wait in k_linear ran out (ndvm_check_oper
 
 // ---------------------------------------------------------------------------------- the product
 // Warps that read the sums: four (in 8 bits, whose tiles have at most 192 columns, three) for each quarter of a tile's rows, which
-// share its columns.
-template <bool kEight> constexpr int kReaders = kEight ? 12 : 16;
-template <bool kEight> constexpr int kThreads = 64 + 32 * kReaders<kEight>;  // and one that loads, one that multiplies
+// share its columns; a tile of 64 columns has work for two.
+template <bool kEight, int kN> constexpr int kReaders = kN == 64 ? 8 : kEight ? 12 : 16;
+template <bool kEight, int kN> constexpr int kThreads = 64 + 32 * kReaders<kEight, kN>;  // and one that loads, one that multiplies
 constexpr int kRoom = 4096;                   // bytes of each: what its stores are made from
 constexpr int kLine = 128;                    // bytes of a row in a step: 64 elements of the contraction, or 128 in 8 bits
 
@@ -34,9 +34,9 @@ template <int kN, int kCtas> constexpr int kTileBytes = (kM + kN / kCtas) * kLin
 template <int kN> constexpr int kScaleTiles = kN > 128 ? 2 : 1;
 template <bool kEight, int kN> constexpr int kScaleBytes = kEight ? 512 * (1 + kScaleTiles<kN>) : 0;
 template <bool kEight, int kN, int kCtas>
-constexpr int kSteps = std::min(8, (229376 - kReaders<kEight> * kRoom) / (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>));
+constexpr int kSteps = std::min(8, (229376 - kReaders<kEight, kN> * kRoom) / (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>));
 template <bool kEight, int kN, int kCtas>
-constexpr int kShared = kSteps<kEight, kN, kCtas> * (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>) + kReaders<kEight> * kRoom +
+constexpr int kShared = kSteps<kEight, kN, kCtas> * (kTileBytes<kN, kCtas> + kScaleBytes<kEight, kN>) + kReaders<kEight, kN> * kRoom +
                         1024 /* alignment */ + 256 /* barriers */;
 // of tensor memory: two tiles' sums, and two steps' scales
 template <bool kEight, int kN> constexpr int kColumns = !kEight ? 2 * kN : kN == 64 ? 256 : 512;
@@ -120,6 +120,11 @@ __device__ __forceinline__ void add32(float (&v)[32], const Pack<T, 8> (&a)[4]) 
     v[e] = s.x, v[e + 1] = s.y;
   }
 }
+template <typename T>
+__device__ __forceinline__ void prefetch_bias(const void* bias, int f32, int64_t c) {
+  const void* p = f32 ? static_cast<const void*>(static_cast<const float*>(bias) + c) : static_cast<const T*>(bias) + c;
+  asm volatile("prefetch.global.L1 [%0];" ::"l"(p));
+}
 // the same 32 values for every lane (a broadcast from L1)
 template <typename T>
 __device__ __forceinline__ void add_bias(float (&v)[32], const void* bias, int f32, int col, int count, bool wide) {
@@ -148,10 +153,10 @@ __device__ __forceinline__ void add_bias(float (&v)[32], const void* bias, int f
 // 16384 x 256 -> 8192 74 us and 127 with gelu.  In 8 bits two tiles' sums of 256 columns would leave no room for scales, and
 // 128 columns read more bytes an operation (360 us).
 template <typename T, bool kEight, int kN, int kCtas>
-__global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_constant__ ForwardArgs p) {
+__global__ void __launch_bounds__(kThreads<kEight, kN>, 1) k_linear(const __grid_constant__ ForwardArgs p) {
   extern __shared__ char raw[];
   constexpr int S = kSteps<kEight, kN, kCtas>, kTile = kTileBytes<kN, kCtas>, kScales = kScaleBytes<kEight, kN>;
-  constexpr int kABytes = kM * kLine, kElements = kEight ? 128 : 64, R = kReaders<kEight>;  // (of the contraction a step)
+  constexpr int kABytes = kM * kLine, kElements = kEight ? 128 : 64, R = kReaders<kEight, kN>;  // (of the contraction a step)
   __shared__ uint32_t s_tmem;
   __shared__ int s_stop;
   const uint32_t base = (tc::smem(raw) + 1023) & ~1023u;
@@ -308,11 +313,14 @@ __global__ void __launch_bounds__(kThreads<kEight>, 1) k_linear(const __grid_con
       const Item it = item(i);
       const int row0 = it.m0 + lanes, row = row0 + lane;
       ask(row, it.n0 + first);
+      if (p.bias && !sums)  // (so that L1 has it when the sums come)
+        for (int j = first; j < kN; j += kNext)
+          if (it.n0 + j + lane < p.n) prefetch_bias<T>(p.bias, p.bias_f32, it.n0 + j + lane);
       if (!wait(done(slot), slot_phase)) break;
       tc::fence_after();
       const uint32_t at = tmem + slot * kN + ((uint32_t)lanes << 16);
 #pragma unroll 1
-      for (int j = first; j < kN; j += kNext) {
+      for (int j = first; j < kN && row0 < p.m; j += kNext) {
         const int col = it.n0 + j, count = min(32, p.n - col);
         if (count <= 0) break;
         float v[32];
@@ -659,7 +667,7 @@ cudaError_t launch_shape(const ForwardArgs& p, cudaStream_t s) {
   }
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)std::min(p.tiles_m * p.tiles_n * p.splits, kSms / kCtas) * kCtas);
-  c.blockDim = dim3(kThreads<kEight>);
+  c.blockDim = dim3(kThreads<kEight, kN>);
   c.dynamicSmemBytes = kShared<kEight, kN, kCtas>;
   c.stream = s;
   cudaLaunchAttribute cluster{};
