@@ -217,3 +217,46 @@ def test_arguments_are_refused_with_their_reason(ndvm, cuda):
         with pytest.raises(ndvm.NdvmError, match=reason):
             call()
             pytest.fail(f"call {i} was not refused")
+
+
+def test_what_is_held_for_the_gradients(ndvm, cuda):
+    """Beside its result a dense layer holds z in binary32, or z and x in 33/32 bytes an element each; nothing without an activation;
+    and nothing of it outlives the graph."""
+    import torch
+    rows, k, n = 4096, 1024, 2048
+    g = _gen(11)
+    x, w, b = _randn(g, rows, k).bfloat16().requires_grad_(True), _randn(g, n, k).bfloat16().requires_grad_(True), _randn(g, n).requires_grad_(True)
+    dy = _randn(g, rows, n).bfloat16()
+    torch.autograd.grad(ndvm.linear(x, w, b, "silu", keep="8bit"), (x, w, b), dy)
+    base = torch.cuda.memory_allocated()
+    for act, keep, want in ((None, None, 0), ("silu", None, 4 * rows * n), (None, "8bit", rows * k * 33 // 32), ("gelu", "8bit", rows * (n + k) * 33 // 32)):
+        y = ndvm.linear(x, w, b, act, keep=keep)
+        assert 0 <= torch.cuda.memory_allocated() - base - 2 * rows * n - want <= 8192, (act, keep)
+        torch.autograd.grad(y, (x, w, b), dy)
+        assert torch.cuda.memory_allocated() - base <= 2 * rows * n + 8192
+        y = ndvm.linear(x, w, b, act, keep=keep)
+        del y
+        assert torch.cuda.memory_allocated() == base
+    y, s = ndvm.rms_norm(x, None, 1e-6, x)
+    assert torch.cuda.memory_allocated() - base <= 4 * rows * k + 4 * rows + 1024
+    del y, s
+    assert torch.cuda.memory_allocated() == base
+
+
+def test_gradients_of_some_inputs_alone(ndvm, cuda):
+    """Whichever inputs want gradients, they get those of all wanting them."""
+    import itertools
+
+    import torch
+    for name, call, args in _ops(ndvm):
+        every = [a.clone().requires_grad_(True) for a in args]
+        y = _first(call(*every))
+        d = torch.ones_like(y)
+        want = torch.autograd.grad(y, every, d)
+        for wanted in itertools.product((False, True), repeat=len(args)):
+            if not any(wanted):
+                assert not _first(call(*args)).requires_grad
+                continue
+            some = [a.clone().requires_grad_(w) for a, w in zip(args, wanted)]
+            got = torch.autograd.grad(_first(call(*some)), [a for a, w in zip(some, wanted) if w], d)
+            assert all(torch.equal(a, c) for a, c in zip(got, [c for c, w in zip(want, wanted) if w])), (name, wanted)
