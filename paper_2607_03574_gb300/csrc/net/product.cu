@@ -291,8 +291,7 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
           const char* from = raw + (asked_at - tc::smem(raw)) + reader * kAsked<kMode> + b * 2048 + lane * 64;
 #pragma unroll
           for (int q = 0; q < 4; q++) dh[q] = load_pack<T, 8>(reinterpret_cast<const T*>(from + ((q ^ (lane >> 1 & 3)) << 4)));
-          __syncwarp();
-          if (ok) had++, ask_next();
+          if (ok) had++;
         }
         tc::tmem_loaded(v);
         if (dual(kMode)) tc::tmem_loaded(u);
@@ -371,6 +370,12 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
         }
         if (lane == 0) tc::stores_commit();
         buffer = (buffer + 1) % kSmall;
+        // The next but one piece of dh takes this one's place: asked for behind the stores of what was made of it, which cannot be
+        // issued before its reads have come back.  (A read alone that is issued can still wait when a copy asked for behind it lands.)
+        if (kMode == kGradient && ok) {
+          __syncwarp();
+          ask_next();
+        }
       }
       tc::fence_before();
       __syncwarp();
