@@ -433,7 +433,7 @@ ndvm_status ndvm_rms_norm_quantized(ndvm_dtype dtype, ndvm_dtype wtype, int64_t 
  *   bias     : device, n values, or NULL;  residual : or NULL; y may be residual
  *   z        : receives z for the backward pass, which needs it if act is not NDVM_ACT_NONE: device, 16-byte aligned floats,
  *              rows rows of ndvm_linear_kept_stride(n); or z_values and z_scales: z as 8-bit blocks whose row stride is n
- *              up to a multiple of 16; or all NULL
+ *              up to a multiple of 16 (scales of no block are left as they are); or all NULL
  *   workspace : device, 256-byte aligned, ndvm_linear_workspace_bytes bytes (NULL if that is 0)
  */
 int64_t ndvm_linear_kept_stride(int64_t n);

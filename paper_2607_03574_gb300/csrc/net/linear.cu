@@ -295,7 +295,8 @@ __global__ void __launch_bounds__(kThreads<kEight, kN>, 1) k_linear(const __grid
     }
   } else if (warp >= 2) {
     // ---- sums to memory: a warp reads the 32 lanes (rows of the tile) that are its own, and 32 columns at a time: a block
-    // of one row a thread.  The residual is asked for a piece ahead.  (What these warps do for each other is hide the waits between
+    // of one row a thread.  The residual is asked for a piece ahead: by copies of neighbours to half of the staging, where z does not
+    // take that whole, or a thread its own row (16384 x 256 -> 8192 with a residual 116 us so, 134 by its own row).  (What these warps do for each other is hide the waits between
     // their instructions: 16384 x 256 -> 8192 takes 74 us, with eight of them, and the bias by way of shared memory, it took 147.)
     const int lanes = (warp % 4) * 32, reader = warp - 2, first = reader / 4 * 32;
     constexpr int kNext = R / 4 * 32;
@@ -305,9 +306,23 @@ __global__ void __launch_bounds__(kThreads<kEight, kN>, 1) k_linear(const __grid
     int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
     Pack<T, 8> next[4];
+    const bool by_copies = p.residual && p.wide && !sums && !floats;
+    const uint32_t residual_at = mine + 2048;
     const auto ask = [&](int row, int col) {
-      if (p.residual && !sums && col < p.n && row < p.m)
+      if (!p.residual || sums || col >= p.n) return;
+      if (by_copies) {  // four lanes a row of 64 bytes, in the 64-byte swizzle; nothing behind a row's end is read
+        const int c = col + lane % 4 * 8, bytes = min(16, max(0, p.n - c) * 2);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+          const int r = q * 8 + lane / 4, from = row - lane + r;
+          if (from < p.m && bytes > 0)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(residual_at + r * 64 + ((lane % 4 ^ (r >> 1 & 3)) << 4)),
+                         "l"(static_cast<const T*>(p.residual) + from * p.r_stride + c), "r"(bytes) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      } else if (row < p.m) {
         load32<T>(next, static_cast<const T*>(p.residual) + row * p.r_stride + col, p.n - col, p.wide);
+      }
     };
     for (int i = unit; i < items; i += units) {
       const Item it = item(i);
@@ -325,10 +340,10 @@ __global__ void __launch_bounds__(kThreads<kEight, kN>, 1) k_linear(const __grid
         if (count <= 0) break;
         float v[32];
         tc::tmem_load32(v, at + j);
-        // binary32 takes the staging whole, y half of it by turns
-        const uint32_t to = mine + (sums || floats ? 0 : (buffer++ & 1) * 2048);
+        // binary32 takes the staging whole, y half of it by turns, or one half beside the residual
+        const uint32_t to = mine + (sums || floats || by_copies ? 0 : (buffer++ & 1) * 2048);
         if (lane == 0) {
-          if (sums || floats) tc::stores_read<0>();
+          if (sums || floats || by_copies) tc::stores_read<0>();
           else tc::stores_read<1>();
         }
         __syncwarp();
@@ -364,10 +379,14 @@ __global__ void __launch_bounds__(kThreads<kEight, kN>, 1) k_linear(const __grid
             v[e] = a.x, v[e + 1] = a.y;
           }
         });
-        if (p.residual) {
-          add32<T>(v, next);
-          if (j + kNext < kN) ask(row, col + kNext);
+        if (by_copies) {
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          __syncwarp();
+          const char* from = mine_ptr + 2048 + lane * 64;
+#pragma unroll
+          for (int q = 0; q < 4; q++) next[q] = load_pack<T, 8>(reinterpret_cast<const T*>(from + ((q ^ (lane >> 1 & 3)) << 4)));
         }
+        if (p.residual) add32<T>(v, next);
         if (floats) {
           if (lane == 0) tc::stores_read<0>();
           __syncwarp();
@@ -382,6 +401,11 @@ __global__ void __launch_bounds__(kThreads<kEight, kN>, 1) k_linear(const __grid
           tc::unstage<T>(mine_ptr + (to - mine), lane, static_cast<T*>(p.out) + row0 * p.stride + col, p.stride, min(32, p.m - row0), count);
         }
         if (lane == 0) tc::stores_commit();
+        // (behind the stores of what the residual went into: its reads have come back, and copies may take its place)
+        if (p.residual && j + kNext < kN) {
+          __syncwarp();
+          ask(row, col + kNext);
+        }
       }
       tc::fence_before();
       __syncwarp();
@@ -392,6 +416,7 @@ __global__ void __launch_bounds__(kThreads<kEight, kN>, 1) k_linear(const __grid
       if (++slot == 2) slot = 0, slot_phase ^= 1;
     }
     if (lane == 0) tc::stores_read<0>();  // (what they write is there when the kernel ends)
+    asm volatile("cp.async.wait_all;" ::: "memory");  // (what a launch that gave up had asked for)
   }
   __syncwarp();
   __syncthreads();
