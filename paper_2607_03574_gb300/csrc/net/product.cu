@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
     const int first = (warp - 2) / 4 * 32;
     int slot = 0, buffer = 0;
     uint32_t slot_phase = 0;
+    bool was_large = false;  // (kBoth: of one product binary32 sums are staged, of the other results)
     // kGradient: the pieces of dh that this warp needs, in the order it needs them, two of them asked for ahead
     const int reader = warp - 2;
     const ProductArgs& p = launch.of[0];
@@ -337,12 +338,13 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
             }
           });
         // A piece takes 2048 bytes of 16-bit results, or 4096 for both of dG and dU or for binary32; while it is
-        // made, the copies of as many others as the staging holds may be under way (none where it held G and U).
+        // made, the copies of as many others as the staging holds may be under way (none where it held G and U, or where the
+        // last piece, of the launch's other product, took all of it).
         constexpr int kSmall = kStaging<kMode, kCtas> / 2048, kLarge = kStaging<kMode, kCtas> / 4096;
         const bool large = kMode == kGradient || (!dual(kMode) && p.sums), alone = kMode == kForward && p.keep;
         const uint32_t to = mine + (alone ? 0 : large ? buffer % kLarge * 4096 : buffer * 2048);
         if (lane == 0) {
-          if (alone) tc::stores_read<0>();
+          if (alone || (kMode == kBoth && was_large)) tc::stores_read<0>();
           else if (large) tc::stores_read<kLarge - 1>();
           else tc::stores_read<kSmall - 1>();
         }
@@ -370,6 +372,7 @@ __global__ void __launch_bounds__(kThreads<kMode>, 1) k_product(const __grid_con
         }
         if (lane == 0) tc::stores_commit();
         buffer = (buffer + 1) % kSmall;
+        was_large = large;
         // The next but one piece of dh takes this one's place: asked for behind the stores of what was made of it, which cannot be
         // issued before its reads have come back.  (A read alone that is issued can still wait when a copy asked for behind it lands.)
         if (kMode == kGradient && ok) {

@@ -2,7 +2,8 @@
 a few elements that differ once in some ten calls."""
 import pytest
 
-from test_network_gpu import _gated_case, _randn, _gen
+from test_network_gpu import _gated_case, _inside, _randn, _rounded, _gen
+from test_network_linear_gpu import _backward64
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,33 @@ def test_rms_norm_same_bits(ndvm, cuda, rows, cols):
         return (y, s, *ndvm.rms_norm_backward(dy, s, w, rstd, ds), ndvm.rms_norm_quantized_forward(x, w, 1e-6, res)[0].dequantize())
 
     _repeat(step, 100)
+
+
+# Sizes whose two gradients share units, one with binary32 sums that are split (dw, or of few rows dx) and, right after them, the
+# other's 16-bit results: the staging of the one must have been read when it takes the other.  By the rule that cuts them
+# (parts of dw, parts of dx; how many units go from sums to results): 16384 x 1024 -> 64 (8, 1; 32), 16384 x 3357 -> 264 (2, 1; 84),
+# 150 x 1001 -> 4096 (1, 8; 64), 3 x 2000 -> 4096 in halves (1, 4; 32).
+SHARED = [(16384, 1024, 64, None), (16384, 3357, 264, "silu"), (150, 1001, 4096, None), (3, 2000, 4096, "gelu")]
+
+
+@pytest.mark.parametrize("rows,k,n,act", SHARED)
+def test_linear_gradients_of_shared_units(ndvm, cuda, rows, k, n, act):
+    """Against 64 bits, against each gradient alone, and again and again; into rows off 16 bytes too, which are not stored by copies."""
+    import torch
+    g = _gen(rows + k + n)
+    x, w, dy = _randn(g, rows, k).bfloat16(), (_randn(g, n, k) * k ** -0.5).bfloat16(), _randn(g, rows, n).bfloat16()
+    kept = ndvm.linear_kept(x, w) if act else None
+    ndvm.linear_forward(x, w, None, act, kept=kept)
+    got = ndvm.linear_backward(dy, x, w, act, kept=kept)
+    z = kept[:, :n].double() if act else dy.double()
+    want, err = _backward64(x.double(), w.double(), z, 0 * z, dy.double(), act, "bf16")
+    for name, a, v, e in zip(("dx", "dw", "dbias"), got, want, err):
+        _inside(a, v, _rounded(v, e, "bf16"), name)
+    for i in range(3):
+        assert torch.equal(ndvm.linear_backward(dy, x, w, act, wants=[i == j for j in range(3)], kept=kept)[i], got[i])
+    wide = torch.full((rows, k + 3), 7.0, device="cuda").bfloat16()
+    again = ndvm.linear_backward(dy, x, w, act, dx=wide[:, 1:1 + k], kept=kept)
+    assert all(torch.equal(a, b) for a, b in zip(again, got)) and bool((wide[:, 0] == 7).all()) and bool((wide[:, 1 + k:] == 7).all())
+    _repeat(lambda: ndvm.linear_backward(dy, x, w, act, kept=kept), 100)
+    _repeat(lambda: ndvm.linear_backward(dy, x, w, act, dx=wide[:, 1:1 + k], kept=kept), 100)
+    ndvm.check_operators()
