@@ -7,6 +7,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/AutogradState.h>
+#include <c10/core/InferenceMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -132,8 +133,9 @@ void* out(const Tensor& t) { return t.defined() ? t.mutable_data_ptr() : nullptr
 Tensor bytes(size_t n, const Tensor& like) {
   return n ? at::empty({(int64_t)n}, like.options().dtype(at::kByte)) : Tensor();
 }
+// (in inference mode nothing is, whatever the gradient mode within it: what is made there cannot be held for a backward pass)
 bool recorded(std::initializer_list<const Tensor*> ts) {
-  if (!at::GradMode::is_enabled()) return false;
+  if (!at::GradMode::is_enabled() || c10::InferenceMode::is_enabled()) return false;
   for (const Tensor* t : ts)
     if (t->defined() && t->requires_grad()) return true;
   return false;

@@ -260,3 +260,23 @@ def test_gradients_of_some_inputs_alone(ndvm, cuda):
             some = [a.clone().requires_grad_(w) for a, w in zip(args, wanted)]
             got = torch.autograd.grad(_first(call(*some)), [a for a, w in zip(some, wanted) if w], d)
             assert all(torch.equal(a, c) for a, c in zip(got, [c for c, w in zip(want, wanted) if w])), (name, wanted)
+
+
+def test_inference_mode_records_nothing(ndvm, cuda):
+    """Whatever the gradient mode within it, as torch's own operations; also where the inputs want gradients."""
+    import torch
+    x = torch.ones(12, 24, device="cuda").bfloat16().requires_grad_(True)
+    m = torch.ones(40, 24, device="cuda").bfloat16().requires_grad_(True)
+    calls = [(name, lambda call=call, args=[a.clone().requires_grad_(True) for a in args]: call(*args)) for name, call, args in _ops(ndvm)]
+    calls += [("layer_norm", lambda: ndvm.layer_norm(x)), ("gated", lambda: ndvm.gated(x, m, m, keep=True)), ("dropout", lambda: ndvm.dropout(x, 0.5, 1)),
+              ("rms_norm", lambda: ndvm.rms_norm(x, None, 1e-6, x)), ("linear", lambda: ndvm.linear(x, m, None, "silu")),
+              ("linear, 8 bits", lambda: ndvm.linear(x, m, None, "silu", keep="8bit")), ("quantize", lambda: ndvm.quantize(x).dequantize()),
+              ("rms_norm_quantized", lambda: ndvm.rms_norm_quantized(x).dequantize())]
+    for name, call in calls:
+        with torch.no_grad():
+            want = _first(call())
+        with torch.inference_mode():
+            plain = _first(call())
+            with torch.enable_grad():
+                got = _first(call())
+        assert not got.requires_grad and got.grad_fn is None and torch.equal(got, want) and torch.equal(plain, want), name
