@@ -361,16 +361,28 @@ std::shared_ptr<N> new_node(std::initializer_list<const Tensor*> inputs) {
   return node;
 }
 
+// What they hold is saved where torch's hooks see it (checkpoints free it and make it again, save_on_cpu moves it away).  A hook
+// may give back other memory: here a tensor of the saved one's type and sizes, as the kernels read it (rows with one stride, or, `whole`,
+// contiguous from 16 bytes on).
+Tensor unpacked(const SavedVariable& v, at::IntArrayRef sizes, at::ScalarType type, at::Device device, bool whole,
+                std::shared_ptr<torch::autograd::Node> from = nullptr) {
+  const Tensor t = v.unpack(std::move(from));
+  if (!t.defined() || t.sizes() != sizes || t.scalar_type() != type || t.device() != device || t.layout() != at::kStrided)
+    raise_backward(NDVM_E_INVALID_ARG, "a saved-tensor hook gave back a tensor of another shape, dtype or device");
+  if (!whole) return rowed(t);
+  return t.is_contiguous() && !t.is_neg() && (uintptr_t)in(t) % 16 == 0 ? t : resolved(t).clone(at::MemoryFormat::Contiguous);
+}
+
 struct RmsNormBackward : torch::autograd::Node {
-  SavedVariable s, weight;
-  Tensor rstd;
+  SavedVariable s, weight, rstd;
+  std::vector<int64_t> sizes;  // s's
+  at::ScalarType type = at::kFloat, wtype = at::kFloat;
+  at::Device device = at::kCUDA;
   bool residual = false, weighted = false;
   std::string name() const override { return "RmsNormBackward"; }
   void release_variables() override {
     std::lock_guard<std::mutex> lock(mutex_);
-    s.reset_data();
-    weight.reset_data();
-    rstd.reset();
+    for (SavedVariable* v : {&s, &weight, &rstd}) v->reset_data();
   }
   variable_list apply(variable_list&& grads) override {
     std::lock_guard<std::mutex> lock(mutex_);
@@ -378,7 +390,8 @@ struct RmsNormBackward : torch::autograd::Node {
       if (g.defined()) first_order(g);
     const Tensor dsum = residual && grads[1].defined() ? rowed(grads[1]) : Tensor();
     const bool want_x = task_should_compute_output(0), want_w = weighted && task_should_compute_output(1), want_r = residual && task_should_compute_output(2);
-    const Tensor saved = s.unpack(residual ? getptr() : nullptr), w = weighted ? weight.unpack() : Tensor();
+    const Tensor saved = unpacked(s, sizes, type, device, false, residual ? getptr() : nullptr);
+    const Tensor w = weighted ? unpacked(weight, sizes.back(), wtype, device, true) : Tensor();
     Tensor dx, dw;
     if (want_w) dw = fresh({saved.size(-1)}, w);
     if (!grads[0].defined()) {  // (the sum alone has a cotangent, or nothing has)
@@ -386,13 +399,13 @@ struct RmsNormBackward : torch::autograd::Node {
       dx = residual ? grads[1] : Tensor();
     } else {
       const Rows r(saved);
-      const Tensor dy = rowed(grads[0]);
+      const Tensor dy = rowed(grads[0]), stats = unpacked(rstd, r.rows, at::kFloat, device, true);
       if (want_x || want_r) dx = fresh(saved.sizes(), saved);
       const size_t need = want_w ? ndvm_rms_norm_workspace_bytes(r.rows, r.cols) : 0;
       Tensor ws = need ? fresh({(int64_t)need}, saved, at::kByte) : Tensor();
       check_backward(ndvm_rms_norm_backward((ndvm_dtype)type_code(saved), (ndvm_dtype)weight_code(w, saved), r.rows, r.cols, in(dy), Rows(dy).stride,
                                             in(dsum), dsum.defined() ? Rows(dsum).stride : 0, in(saved), r.stride, in(w),
-                                            static_cast<const float*>(in(rstd)), out(dx), r.cols, out(dw), out(ws), need,
+                                            static_cast<const float*>(in(stats)), out(dx), r.cols, out(dw), out(ws), need,
                                             stream_of(saved.get_device())));
     }
     return {want_x ? dx : Tensor(), dw, want_r ? dx : Tensor()};
@@ -410,8 +423,11 @@ variable_list rms_recorded(const Tensor& x, const Tensor& weight, const Tensor& 
   node->weighted = weight.defined();
   for (Tensor& t : y) torch::autograd::set_history(t, node);
   node->s = residual.defined() ? SavedVariable(y[1], true) : SavedVariable(x, false);
-  if (weight.defined()) node->weight = SavedVariable(weight, false);
-  node->rstd = rstd;
+  node->sizes = x.sizes().vec();
+  node->type = x.scalar_type();
+  node->device = x.device();
+  if (weight.defined()) node->weight = SavedVariable(weight, false), node->wtype = weight.scalar_type();
+  node->rstd = SavedVariable(rstd, false);
   return y;
 }
 std::optional<variable_list> rms_norm(const Tensor& given, const Maybe& w, double eps, const Maybe& r) {
@@ -495,7 +511,9 @@ bool linear_extras(int device, const Maybe& b, const Maybe& r, int64_t n, at::In
   }
   return true;
 }
-Tensor linear_forward(const Tensor& x, const Tensor& w, const Tensor& bias, int64_t act, const Tensor& residual, const Tensor& z, const Blocks* held) {
+// z: where it is kept, as floats, or beside scales as the bytes of blocks
+Tensor linear_forward(const Tensor& x, const Tensor& w, const Tensor& bias, int64_t act, const Tensor& residual, const Tensor& z,
+                      const Tensor& z_scales) {
   const Rows rx(x), rw(w);
   const int64_t n = w.size(0);
   auto shape = x.sizes().vec();
@@ -505,49 +523,69 @@ Tensor linear_forward(const Tensor& x, const Tensor& w, const Tensor& bias, int6
   Tensor ws = need ? fresh({(int64_t)need}, x, at::kByte) : Tensor();
   check_forward(ndvm_linear_forward((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(bias, x), (ndvm_activation)act, rx.rows, rx.cols, n, in(x), rx.stride,
                                     in(w), rw.stride, in(bias), in(residual), residual.defined() ? Rows(residual).stride : 0, out(y), n,
-                                    static_cast<float*>(out(z)), held ? held->v() : nullptr, held ? held->s() : nullptr, out(ws), need,
-                                    stream_of(x.get_device())));
+                                    z_scales.defined() ? nullptr : static_cast<float*>(out(z)), z_scales.defined() ? static_cast<uint8_t*>(out(z)) : nullptr,
+                                    static_cast<uint8_t*>(out(z_scales)), out(ws), need, stream_of(x.get_device())));
   return y;
 }
+// 8-bit blocks as a node holds them: bytes, in rows of whole 16s
+struct HeldBlocks {
+  Tensor values, scales;
+  static int64_t pitch(int64_t cols) { return (cols + 15) / 16 * 16; }
+  static std::array<int64_t, 2> value_sizes(int64_t rows, int64_t cols) { return {rows, pitch(cols)}; }
+  static std::array<int64_t, 5> scale_sizes(int64_t rows, int64_t cols) { return {(rows + 127) / 128, (cols + 127) / 128, 32, 4, 4}; }
+  HeldBlocks(const Tensor& like, int64_t rows, int64_t cols)
+      : values(fresh(value_sizes(rows, cols), like, at::kByte)), scales(fresh(scale_sizes(rows, cols), like, at::kByte)) {}
+};
 struct LinearBackward : torch::autograd::Node {
-  SavedVariable x, w;  // (x: where it is held as it is)
-  Tensor x_values, x_scales, z, z_scales;
+  SavedVariable x, w, z;        // (x and z: as they are, or the bytes of their blocks)
+  SavedVariable x_scales, z_scales;
   std::vector<int64_t> sizes;  // x's
-  int64_t act = 0, pitch = 0;  // (of x's blocks)
+  int64_t act = 0;
   at::ScalarType btype = at::kFloat;
-  bool eight = false, biased = false, wants_w = false;
+  bool eight = false, biased = false, wants_z = false;
   std::string name() const override { return "LinearBackward"; }
   void release_variables() override {
     std::lock_guard<std::mutex> lock(mutex_);
-    x.reset_data();
-    w.reset_data();
-    for (Tensor* t : {&x_values, &x_scales, &z, &z_scales}) t->reset();
+    for (SavedVariable* v : {&x, &w, &z, &x_scales, &z_scales}) v->reset_data();
   }
   variable_list apply(variable_list&& grads) override {
     std::lock_guard<std::mutex> lock(mutex_);
     if (!grads[0].defined()) return {Tensor(), Tensor(), Tensor(), Tensor()};
     first_order(grads[0]);
-    const Tensor weight = w.unpack(), given = wants_w && !eight ? x.unpack() : Tensor();  // (which raise where they were released)
     const Tensor dy = rowed(grads[0]);
-    const int64_t n = weight.size(0), k = weight.size(1);
-    const Rows rd(dy), rw(weight);
+    const Rows rd(dy);
+    const int64_t rows = rd.rows, n = dy.size(-1), k = sizes.back();
+    const at::ScalarType type = dy.scalar_type();
+    const Tensor weight = unpacked(w, {n, k}, type, dy.device(), false);  // (raises where it was released)
     Tensor dx, dw, db;
     if (task_should_compute_output(0)) dx = fresh(sizes, dy);
     if (task_should_compute_output(1)) dw = fresh({n, k}, dy);
     if (biased && task_should_compute_output(2)) db = fresh({n}, dy, btype);
     if (dx.defined() || dw.defined() || db.defined()) {
-      const bool held = eight && dw.defined();
+      const Rows rw(weight);
+      Tensor given, values, scales, held_z, held_scales;  // x, or its blocks; z, or its blocks
+      if (dw.defined() && !eight) given = unpacked(x, sizes, type, dy.device(), false);
+      if (dw.defined() && eight) {
+        values = unpacked(x, HeldBlocks::value_sizes(rows, k), at::kByte, dy.device(), true);
+        scales = unpacked(x_scales, HeldBlocks::scale_sizes(rows, k), at::kByte, dy.device(), true);
+      }
+      if (wants_z && eight) {
+        held_z = unpacked(z, HeldBlocks::value_sizes(rows, n), at::kByte, dy.device(), true);
+        held_scales = unpacked(z_scales, HeldBlocks::scale_sizes(rows, n), at::kByte, dy.device(), true);
+      } else if (wants_z) {
+        held_z = unpacked(z, {rows, ndvm_linear_kept_stride(n)}, at::kFloat, dy.device(), true);
+      }
       std::optional<Rows> rx;
       if (given.defined()) rx.emplace(given);
-      const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rd.rows, k, n, 1,
-                                                      (!rx || ready(given, *rx)) && ready(weight, rw) && ready(dy, rd), held);
+      const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rows, k, n, 1,
+                                                      (!rx || ready(given, *rx)) && ready(weight, rw) && ready(dy, rd), values.defined());
       Tensor ws = need ? fresh({(int64_t)need}, dy, at::kByte) : Tensor();
       check_backward(ndvm_linear_backward(
-          (ndvm_dtype)type_code(dy), db.defined() && btype == at::kFloat ? NDVM_F32 : (ndvm_dtype)type_code(dy), (ndvm_activation)act, rd.rows, k, n,
-          in(dy), rd.stride, rx ? in(given) : nullptr, rx ? rx->stride : 0, held ? static_cast<const uint8_t*>(in(x_values)) : nullptr,
-          pitch, held ? static_cast<const uint8_t*>(in(x_scales)) : nullptr, in(weight), rw.stride,
-          eight ? nullptr : static_cast<const float*>(in(z)), eight ? static_cast<const uint8_t*>(in(z)) : nullptr,
-          eight ? static_cast<const uint8_t*>(in(z_scales)) : nullptr, out(dx), k, out(dw), out(db), out(ws), need, stream_of(dy.get_device())));
+          (ndvm_dtype)type_code(dy), db.defined() && btype == at::kFloat ? NDVM_F32 : (ndvm_dtype)type_code(dy), (ndvm_activation)act, rows, k, n,
+          in(dy), rd.stride, in(given), rx ? rx->stride : 0, static_cast<const uint8_t*>(in(values)), HeldBlocks::pitch(k),
+          static_cast<const uint8_t*>(in(scales)), in(weight), rw.stride, eight ? nullptr : static_cast<const float*>(in(held_z)),
+          eight ? static_cast<const uint8_t*>(in(held_z)) : nullptr, static_cast<const uint8_t*>(in(held_scales)), out(dx), k, out(dw), out(db), out(ws),
+          need, stream_of(dy.get_device())));
     }
     return {dx, dw, db, task_should_compute_output(3) ? grads[0] : Tensor()};
   }
@@ -558,36 +596,34 @@ Tensor linear_recorded(const Tensor& x, const Tensor& w, const Tensor& bias, con
   // what the gradients need: z of an activation, and x for w's
   const bool wants_w = w.requires_grad();
   const bool wants_z = act != NDVM_ACT_NONE && (wants_w || x.requires_grad() || (bias.defined() && bias.requires_grad()));
-  Tensor y, z, x_values, x_scales, z_scales;
-  int64_t pitch = 0;
+  Tensor y, z, z_scales;
+  std::optional<HeldBlocks> held;
   {
     at::AutoDispatchBelowADInplaceOrView below;
-    std::optional<Blocks> blocks;
     if (eight && wants_w) {
-      const Blocks held = to_blocks(x);
-      x_values = held.values, x_scales = held.scales, pitch = held.stride;
+      held.emplace(x, rx.rows, rx.cols);
+      check_forward(ndvm_quantize((ndvm_dtype)type_code(x), rx.rows, rx.cols, in(x), rx.stride, static_cast<uint8_t*>(out(held->values)),
+                                  HeldBlocks::pitch(rx.cols), static_cast<uint8_t*>(out(held->scales)), stream_of(x.get_device())));
     }
     if (eight && wants_z) {
-      blocks.emplace(x, at::IntArrayRef({rx.rows, n}), rx.rows);
-      z = blocks->values, z_scales = blocks->scales;
+      HeldBlocks blocks(x, rx.rows, n);
+      z = blocks.values, z_scales = blocks.scales;
     } else if (wants_z) {
       z = fresh({rx.rows, ndvm_linear_kept_stride(n)}, x, at::kFloat);
     }
-    y = linear_forward(x, w, bias, act, residual, eight ? Tensor() : z, blocks ? &*blocks : nullptr);
+    y = linear_forward(x, w, bias, act, residual, z, z_scales);
   }
   const auto node = new_node<LinearBackward>({&x, &w, &bias, &residual});
   torch::autograd::set_history(y, node);
   node->w = SavedVariable(w, false);
-  if (wants_w && !eight) node->x = SavedVariable(x, false);
-  node->x_values = x_values;
-  node->x_scales = x_scales;
-  node->pitch = pitch;
-  node->z = z;
-  node->z_scales = z_scales;
+  if (held) node->x = SavedVariable(held->values, false), node->x_scales = SavedVariable(held->scales, false);
+  else if (wants_w) node->x = SavedVariable(x, false);
+  if (wants_z) node->z = SavedVariable(z, false);
+  if (z_scales.defined()) node->z_scales = SavedVariable(z_scales, false);
   node->sizes = x.sizes().vec();
   node->act = act;
   node->eight = eight;
-  node->wants_w = wants_w;
+  node->wants_z = wants_z;
   if ((node->biased = bias.defined())) node->btype = bias.scalar_type();
   return y;
 }
@@ -603,7 +639,7 @@ Maybe linear(const Tensor& gx, const Tensor& gw, const Maybe& b, int64_t act, co
   const Tensor x = rowed(gx), w = rowed(gw);
   check_inputs({&x, &w, &bias, &residual});
   if (recorded({&x, &w, &bias, &residual})) return linear_recorded(x, w, bias, residual, act, eight);
-  return linear_forward(x, w, bias, act, residual, Tensor(), nullptr);
+  return linear_forward(x, w, bias, act, residual, Tensor(), Tensor());
 }
 Maybe linear_quantized(const Tensor& xv, const Tensor& xs, int64_t rows, int64_t k, int64_t x_stride, const Tensor& wv, const Tensor& ws, int64_t n,
                        int64_t wk, int64_t w_stride, const Maybe& b, int64_t act, const Maybe& r, int64_t code) {
