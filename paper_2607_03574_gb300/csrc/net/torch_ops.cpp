@@ -85,14 +85,15 @@ void first_order(const Tensor& grad) {
   if (traced()) raise_backward(NDVM_E_UNSUPPORTED, kNoTraces);
 }
 
-int type_code(const Tensor& t) {
-  switch (t.scalar_type()) {
+int type_code(at::ScalarType t) {
+  switch (t) {
     case at::kFloat: return NDVM_F32;
     case at::kHalf: return NDVM_F16;
     case at::kBFloat16: return NDVM_BF16;
     default: return -1;
   }
 }
+int type_code(const Tensor& t) { return type_code(t.scalar_type()); }
 bool here(const Tensor& t, int device) { return t.is_cuda() && t.get_device() == device; }
 
 // a tensor as rows of contiguous elements with one stride
@@ -391,19 +392,22 @@ struct RmsNormBackward : torch::autograd::Node {
     const Tensor dsum = residual && grads[1].defined() ? rowed(grads[1]) : Tensor();
     const bool want_x = task_should_compute_output(0), want_w = weighted && task_should_compute_output(1), want_r = residual && task_should_compute_output(2);
     const Tensor saved = unpacked(s, sizes, type, device, false, residual ? getptr() : nullptr);
-    const Tensor w = weighted ? unpacked(weight, sizes.back(), wtype, device, true) : Tensor();
     Tensor dx, dw;
-    if (want_w) dw = fresh({saved.size(-1)}, w);
+    if (want_w) dw = fresh({saved.size(-1)}, saved, wtype);
     if (!grads[0].defined()) {  // (the sum alone has a cotangent, or nothing has)
       if (want_w) dw.zero_();
       dx = residual ? grads[1] : Tensor();
     } else {
       const Rows r(saved);
       const Tensor dy = rowed(grads[0]), stats = unpacked(rstd, r.rows, at::kFloat, device, true);
-      if (want_x || want_r) dx = fresh(saved.sizes(), saved);
+      Tensor w;
+      if (want_x || want_r) {
+        dx = fresh(saved.sizes(), saved);
+        if (weighted) w = unpacked(weight, sizes.back(), wtype, device, true);
+      }
       const size_t need = want_w ? ndvm_rms_norm_workspace_bytes(r.rows, r.cols) : 0;
       Tensor ws = need ? fresh({(int64_t)need}, saved, at::kByte) : Tensor();
-      check_backward(ndvm_rms_norm_backward((ndvm_dtype)type_code(saved), (ndvm_dtype)weight_code(w, saved), r.rows, r.cols, in(dy), Rows(dy).stride,
+      check_backward(ndvm_rms_norm_backward((ndvm_dtype)type_code(saved), (ndvm_dtype)type_code(weighted ? wtype : type), r.rows, r.cols, in(dy), Rows(dy).stride,
                                             in(dsum), dsum.defined() ? Rows(dsum).stride : 0, in(saved), r.stride, in(w),
                                             static_cast<const float*>(in(stats)), out(dx), r.cols, out(dw), out(ws), need,
                                             stream_of(saved.get_device())));
@@ -426,7 +430,10 @@ variable_list rms_recorded(const Tensor& x, const Tensor& weight, const Tensor& 
   node->sizes = x.sizes().vec();
   node->type = x.scalar_type();
   node->device = x.device();
-  if (weight.defined()) node->weight = SavedVariable(weight, false), node->wtype = weight.scalar_type();
+  if (weight.defined()) {  // (its own gradient does not need it)
+    node->wtype = weight.scalar_type();
+    if (x.requires_grad() || (residual.defined() && residual.requires_grad())) node->weight = SavedVariable(weight, false);
+  }
   node->rstd = SavedVariable(rstd, false);
   return y;
 }
@@ -556,14 +563,13 @@ struct LinearBackward : torch::autograd::Node {
     const Rows rd(dy);
     const int64_t rows = rd.rows, n = dy.size(-1), k = sizes.back();
     const at::ScalarType type = dy.scalar_type();
-    const Tensor weight = unpacked(w, {n, k}, type, dy.device(), false);  // (raises where it was released)
     Tensor dx, dw, db;
     if (task_should_compute_output(0)) dx = fresh(sizes, dy);
     if (task_should_compute_output(1)) dw = fresh({n, k}, dy);
     if (biased && task_should_compute_output(2)) db = fresh({n}, dy, btype);
     if (dx.defined() || dw.defined() || db.defined()) {
-      const Rows rw(weight);
-      Tensor given, values, scales, held_z, held_scales;  // x, or its blocks; z, or its blocks
+      Tensor weight, given, values, scales, held_z, held_scales;  // w; x, or its blocks; z, or its blocks
+      if (dx.defined()) weight = unpacked(w, {n, k}, type, dy.device(), false);
       if (dw.defined() && !eight) given = unpacked(x, sizes, type, dy.device(), false);
       if (dw.defined() && eight) {
         values = unpacked(x, HeldBlocks::value_sizes(rows, k), at::kByte, dy.device(), true);
@@ -575,15 +581,16 @@ struct LinearBackward : torch::autograd::Node {
       } else if (wants_z) {
         held_z = unpacked(z, {rows, ndvm_linear_kept_stride(n)}, at::kFloat, dy.device(), true);
       }
-      std::optional<Rows> rx;
+      std::optional<Rows> rx, rw;
       if (given.defined()) rx.emplace(given);
+      if (weight.defined()) rw.emplace(weight);
       const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rows, k, n, 1,
-                                                      (!rx || ready(given, *rx)) && ready(weight, rw) && ready(dy, rd), values.defined());
+                                                      (!rx || ready(given, *rx)) && (!rw || ready(weight, *rw)) && ready(dy, rd), values.defined());
       Tensor ws = need ? fresh({(int64_t)need}, dy, at::kByte) : Tensor();
       check_backward(ndvm_linear_backward(
           (ndvm_dtype)type_code(dy), db.defined() && btype == at::kFloat ? NDVM_F32 : (ndvm_dtype)type_code(dy), (ndvm_activation)act, rows, k, n,
           in(dy), rd.stride, in(given), rx ? rx->stride : 0, static_cast<const uint8_t*>(in(values)), HeldBlocks::pitch(k),
-          static_cast<const uint8_t*>(in(scales)), in(weight), rw.stride, eight ? nullptr : static_cast<const float*>(in(held_z)),
+          static_cast<const uint8_t*>(in(scales)), in(weight), rw ? rw->stride : 0, eight ? nullptr : static_cast<const float*>(in(held_z)),
           eight ? static_cast<const uint8_t*>(in(held_z)) : nullptr, static_cast<const uint8_t*>(in(held_scales)), out(dx), k, out(dw), out(db), out(ws),
           need, stream_of(dy.get_device())));
     }
@@ -593,7 +600,7 @@ struct LinearBackward : torch::autograd::Node {
 Tensor linear_recorded(const Tensor& x, const Tensor& w, const Tensor& bias, const Tensor& residual, int64_t act, bool eight) {
   const Rows rx(x);
   const int64_t n = w.size(0);
-  // what the gradients need: z of an activation, and x for w's
+  // what the gradients need: z of an activation, x for w's, and w for x's
   const bool wants_w = w.requires_grad();
   const bool wants_z = act != NDVM_ACT_NONE && (wants_w || x.requires_grad() || (bias.defined() && bias.requires_grad()));
   Tensor y, z, z_scales;
@@ -615,7 +622,7 @@ Tensor linear_recorded(const Tensor& x, const Tensor& w, const Tensor& bias, con
   }
   const auto node = new_node<LinearBackward>({&x, &w, &bias, &residual});
   torch::autograd::set_history(y, node);
-  node->w = SavedVariable(w, false);
+  if (x.requires_grad()) node->w = SavedVariable(w, false);
   if (held) node->x = SavedVariable(held->values, false), node->x_scales = SavedVariable(held->scales, false);
   else if (wants_w) node->x = SavedVariable(x, false);
   if (wants_z) node->z = SavedVariable(z, false);

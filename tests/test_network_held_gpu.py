@@ -115,3 +115,39 @@ def test_no_cotangent_is_no_gradient(ndvm, cuda):
         y = call(*leaves)
         got = torch.autograd.grad(Nothing.apply(y[0], y[-1]), leaves, allow_unused=True)
         assert all(v is None or not v.any() for v in got), op
+
+
+def test_what_no_gradient_needs_is_not_held(ndvm, cuda):
+    """w is held for x's gradient alone, x for w's, the norm's weight for x's and the residual's: a leaf that none of the wanted
+    gradients needs may be written to between the passes."""
+    import itertools
+
+    import torch
+    needs = {"linear": {0: (1,), 1: (0,), 2: (), 3: ()}, "rms_norm": {0: (0, 1), 1: (0,), 2: (0, 1)}}  # (what x's, w's, ... gradients read)
+    for op, act, keep in CASES:
+        for wanted in itertools.product((False, True), repeat=3 if op == "linear" or act else 2):
+            if not any(wanted):
+                continue
+            call, leaves, ds = _case(ndvm, op, act, keep, 70, 136, 200)
+            leaves = [t.detach().clone().requires_grad_(w) for t, w in zip(leaves, wanted)]
+            inputs = [t for t in leaves if t.requires_grad]
+            want = _grads(lambda *ts: call(*leaves), inputs, ds)
+            read = set().union(*(needs[op][i] for i, w in enumerate(wanted) if w))
+            if op == "rms_norm" and act:  # (the stream is the call's own sum)
+                read.discard(0)
+            if keep:  # (x is held as blocks)
+                read.discard(0)
+            for i, t in enumerate(leaves):
+                y = call(*leaves)
+                before = t.detach().clone()
+                with torch.no_grad():
+                    t.mul_(2)
+                if i in read:
+                    with pytest.raises(RuntimeError, match="inplace"):
+                        torch.autograd.grad(y, inputs, ds)
+                else:
+                    got = torch.autograd.grad(y, inputs, ds)
+                    assert all(torch.equal(a, b) for a, b in zip(got, want)), (op, act, keep, wanted, i)
+                with torch.no_grad():
+                    t.copy_(before)
+    ndvm.check_operators()
