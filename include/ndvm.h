@@ -445,7 +445,8 @@ ndvm_status ndvm_linear_forward(ndvm_dtype dtype, ndvm_dtype btype, ndvm_activat
 /*
  * ndvm_linear_workspace_bytes -- device workspace of a forward (backward = 0) or backward (1) call.  aligned = 1: x, w (and
  * dy) start on 16 bytes and their row strides are multiples of 8 elements that hold a row; otherwise 0, which adds room
- * for copies that are.  held = 1: the backward call has x as 8-bit blocks.  0 on invalid sizes.
+ * for copies that are.  held = 1: the backward call has x as 8-bit blocks.  0 on invalid sizes.  A forward call of one row
+ * that keeps no z_values needs none, whatever this says for its sizes.
  */
 size_t ndvm_linear_workspace_bytes(ndvm_activation act, int64_t rows, int64_t k, int64_t n, int backward, int aligned, int held);
 

@@ -526,7 +526,9 @@ Tensor linear_forward(const Tensor& x, const Tensor& w, const Tensor& bias, int6
   auto shape = x.sizes().vec();
   shape.back() = n;
   Tensor y = fresh(shape, x);
-  const size_t need = ndvm_linear_workspace_bytes((ndvm_activation)act, rx.rows, rx.cols, n, 0, ready(x, rx) && ready(w, rw), 0);
+  // (one row without blocks takes no workspace, whatever its operands start on)
+  const size_t need = rx.rows == 1 && !z_scales.defined() ? 0
+                      : ndvm_linear_workspace_bytes((ndvm_activation)act, rx.rows, rx.cols, n, 0, ready(x, rx) && ready(w, rw), 0);
   Tensor ws = need ? fresh({(int64_t)need}, x, at::kByte) : Tensor();
   check_forward(ndvm_linear_forward((ndvm_dtype)type_code(x), (ndvm_dtype)weight_code(bias, x), (ndvm_activation)act, rx.rows, rx.cols, n, in(x), rx.stride,
                                     in(w), rw.stride, in(bias), in(residual), residual.defined() ? Rows(residual).stride : 0, out(y), n,

@@ -651,7 +651,10 @@ def linear_forward(x, w, bias=None, activation=None, residual=None, y=None, kept
         _given(y, "y", shape, x.dtype, device)
         ys = _rows(y, "y")[2]
     rp, rs = _like(residual, "residual", y, device)
-    need = lib.ndvm_linear_workspace_bytes(act, rows, k, n, 0, int(_ready(x.data_ptr(), xs, rows, k) and _ready(w.data_ptr(), ws_, n, k)), 0)
+    if rows == 1 and not isinstance(kept, Quantized):  # (vectors: no workspace, whatever the operands start on)
+        need = 0
+    else:
+        need = lib.ndvm_linear_workspace_bytes(act, rows, k, n, 0, int(_ready(x.data_ptr(), xs, rows, k) and _ready(w.data_ptr(), ws_, n, k)), 0)
     ws, wp, nbytes = _workspace(torch, workspace, need, device, stream)
     status = lib.ndvm_linear_forward(code, _weight_type(code, None, bias), act, rows, k, n, x.data_ptr(), xs, w.data_ptr(), ws_,
                                      _vector(bias, "bias", n, device), rp, rs, y.data_ptr(), ys,

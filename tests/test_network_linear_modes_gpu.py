@@ -280,3 +280,25 @@ def test_inference_mode_records_nothing(ndvm, cuda):
             with torch.enable_grad():
                 got = _first(call())
         assert not got.requires_grad and got.grad_fn is None and torch.equal(got, want) and torch.equal(plain, want), name
+
+
+@pytest.mark.parametrize("k,shift", [(2049, 0), (2048, 1)])
+def test_one_row_allocates_its_result_alone(ndvm, cuda, k, shift):
+    """Rows off 16 bytes too: no room for copies of the weights that nothing makes."""
+    import torch
+    g = _gen(31)
+    n = 4096
+    w = torch.empty(n * k + shift, device="cuda", dtype=torch.bfloat16)[shift:].view(n, k)
+    w.copy_(_randn(g, n, k))
+    x, b = _randn(g, 1, k).bfloat16(), _randn(g, n)
+    want = ndvm.linear(x, w.clone(), b, "silu")
+    xg = x.clone().requires_grad_(True)
+    ndvm.linear(xg, w, b, "silu")
+    for call, most in ((lambda: ndvm.linear(x, w, b, "silu"), 2 * n), (lambda: ndvm.linear_forward(x, w, b, "silu"), 2 * n),
+                       (lambda: ndvm.linear(xg, w, b, "silu"), 6 * n)):
+        base = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        y = call()
+        assert torch.cuda.max_memory_allocated() - base <= most + 1024
+        assert torch.equal(y, want) or k % 8 == 0  # (vectors of eight sum in another order than single elements)
+        del y
