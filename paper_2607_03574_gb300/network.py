@@ -459,7 +459,8 @@ class Quantized:
     with which none is over 448 in size; an element is the nearest e4m3 value to v / 2^e.  A block with an infinity or a
     NaN is NaN.
 
-    values: float8_e4m3fn of the tensor's shape, rows with one stride that is a multiple of 16 and starts on 16 bytes.
+    values: float8_e4m3fn of the tensor's shape, rows with one stride that is a multiple of 16 and starts on 16 bytes.  A row's
+    bytes go up to a multiple of 16: those behind its last element are written as 0 where the blocks are.
     scales: uint8 [rows / 128, columns / 128, 32, 4, 4] (both rounded up), e + 127 at [row / 128, column / 128, row % 32,
     row / 32 % 4, column / 32 % 4].  quantize() and rms_norm_quantized() make them."""
 
