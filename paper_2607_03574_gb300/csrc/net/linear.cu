@@ -149,7 +149,8 @@ __device__ __forceinline__ void add_bias(float (&v)[32], const void* bias, int f
 // One warp loads, one issues the products, the others read the sums of a tile while the next one's are made.  A block has
 // kN columns of sums for its 128 rows; a pair's blocks (kCtas = 2) hold half of those rows of B each.  Bound by the tensor
 // cores where the contraction is long, by the epilogue's instructions where it is short: 16384 x 2048 -> 8192 bf16 295 us (1.86 PFLOP/s), 302
-// with gelu, 347 with z kept in binary32 too; in 8 bits 177 us (3.1 PFLOP/s) and 204, by what feeds them (without the scales' copies 177);
+// with gelu, 347 with z kept in binary32 too; in 8 bits 177 us (3.1 PFLOP/s) and 204, which no counter explains (it is not the scales'
+// copies: 177 without them);
 // 16384 x 256 -> 8192 74 us and 127 with gelu.  In 8 bits two tiles' sums of 256 columns would leave no room for scales, and
 // 128 columns read more bytes an operation (360 us).
 template <typename T, bool kEight, int kN, int kCtas>
@@ -662,7 +663,11 @@ bool map_scales(CUtensorMap* map, const uint8_t* p, int64_t rows, int64_t cols, 
                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a product of 8-bit operands is cut up, as cut() for 16-bit ones (in the same units: 0.27 us).
+// How a product of 8-bit operands is cut up, as cut() for 16-bit ones (in the same units: 0.27 us).  Pairs of 192 columns, 192 alone, 128
+// and 64, us: 16384 x 2048 -> 8192 178, 236, 239, 401; 16384 x 256 -> 8192 (2 steps: no pairs) 88, 62, 83, 92; 4096 x 4096 -> 1024 22,
+// 25, 21, 32; 64 x 1024 -> 4096 8.1, 7.3, 6.7, 6.0; 64 x 8192 -> 1024 whole 21, 24, 19, 18 and in 8 parts 12.0, 11.3, 10.5, 10.1.
+// What the rule takes is the best of them, but for 1000 x 2000 -> 500 (10.0 in two parts, 8.7 whole) and 16384 x 1024 -> 1024 (22.7 in
+// pairs, 21.5 alone).
 Cut cut_blocks(int64_t m, int64_t n, int64_t c) {
   struct Shape { int width, ctas; double step; };
   static constexpr Shape shapes[] = {{192, 2, 0.68}, {192, 1, 0.75}, {128, 1, 0.55}, {64, 1, 0.4}};

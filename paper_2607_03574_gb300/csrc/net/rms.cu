@@ -99,8 +99,9 @@ __global__ void __launch_bounds__(kBlock<kRow>, kResident) k_rms_forward(RmsArgs
   if (!kBlocks && t == 0 && a.rstd) a.rstd[row] = rstd;
 }
 
-// Rows longer than the registers of a block hold: two passes over the row, the later one from L2.  (The sum's rounded
-// values are made again where they are not stored.)
+// Rows longer than the registers of a block hold: two passes over the row, the later one from L2, one element a load.  (The sum's
+// rounded values are made again where they are not stored.)  With a residual, 2048 rows: 20000 columns of bf16 148 us (2.2 TB/s; 16384, which
+// are held, 43), 12288 of f32 108.
 template <typename T, bool kBlocks>
 __global__ void __launch_bounds__(kLong) k_rms_forward_long(RmsArgs a, int w_f32) {
   __shared__ float part[32];
@@ -295,6 +296,8 @@ __global__ void __launch_bounds__(kBackBlock<kRow>, kResident) k_rms_backward(Rm
   }
 }
 
+// (one element a load, and dw by a kernel of its own: 2048 rows with a residual, 12288 columns of bf16 129 us, 1.6 TB/s, against 29 for 8192, which
+// k_rms_backward holds; of f32 149)
 template <typename T>
 __global__ void __launch_bounds__(kLong) k_rms_backward_long(RmsArgs a, int w_f32) {
   __shared__ float part[32];
@@ -442,8 +445,9 @@ cudaError_t rms_forward(const RmsArgs& a, int w_f32, cudaStream_t s) {
   const bool held = forward_variant<T>(width, a.cols, [&](auto v, auto n, auto r, auto b) {
     constexpr int V = decltype(v)::value, R = decltype(r)::value, N = decltype(n)::value;
     // 8-bit blocks want 32 consecutive elements in one turn of a row's threads, and two warps rather than one for a row of eight
-    // loads a thread: the blocks' instructions are what a row waits for (16384 x 2048 bf16 with a residual 45 and 38 us, 64 rows
-    // 6.1 and 4.0)
+    // loads a thread: the blocks' instructions are what a row waits for (one warp and two, with a residual, us: bf16 16384 x 2048 45
+    // and 39, x 1536 37 and 31, x 1280 33 and 28, x 1032 31 and 28; 64 rows 4.8 to 6.3 and 3.1 to 3.8; f32 16384 x 1024 45 and
+    // 36, x 516 29 and 23)
     constexpr bool kTwo = kBlocks && R == 32 && N == 8 && V > 1;
     constexpr int kRow = kTwo ? 64 : kBlocks && R * V < 32 ? 32 : R, kRows = kBlock<kRow> / kRow;
     k_rms_forward<T, V, kTwo ? 4 : N, kRow, kTwo ? 8 : decltype(b)::value, kBlocks>
