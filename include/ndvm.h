@@ -427,7 +427,9 @@ ndvm_status ndvm_rms_norm_quantized(ndvm_dtype dtype, ndvm_dtype wtype, int64_t 
 /*
  * ndvm_linear_forward -- y = act(z) + residual with z = x w^T + bias, in one kernel (two where a long contraction is
  * split): x is rows x k, w is n x k, y and residual are rows x n.
- *   dtype    : every matrix (F16, BF16; sums in binary32);  btype : bias, dtype or F32
+ *   dtype    : every matrix (F16, BF16; sums in binary32, which tensor cores cut off where others round: z is off towards 0 by
+ *              some 1e-9 k of its size, so one that close to relu's 0 or to an 8-bit step may fall on its other side);
+ *              btype : bias, dtype or F32
  *   act      : as the gated projection's, or NDVM_ACT_NONE
  *   rows     : 0 is allowed and does nothing;  k, n : at least 1; rows, k and n at most 2^28
  *   bias     : device, n values, or NULL;  residual : or NULL; y may be residual
